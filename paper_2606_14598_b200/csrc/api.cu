@@ -47,24 +47,6 @@ struct Range {
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// The kernels are built for sm_100a only: tcgen05.mma.kind::i8 exists on compute capability 10.0 and not, for
-// instance, on 10.3.
-int check_arch() {
-    static thread_local int cached_dev = -1;
-    static thread_local int cached_ok = 0;
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) return W8A8_ERR_CUDA;
-    if (dev != cached_dev) {
-        int major = 0, minor = 0;
-        if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-            return W8A8_ERR_CUDA;
-        cached_dev = dev;
-        cached_ok = (major == 10 && minor == 0);
-    }
-    return cached_ok ? W8A8_OK : W8A8_ERR_ARCH;
-}
-
 int check_dims(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || N <= 0 || K <= 0) return W8A8_ERR_INVALID_ARG;
     if (M > INT32_MAX || N > INT32_MAX) return W8A8_ERR_INVALID_ARG;
@@ -82,6 +64,24 @@ void offsets(int64_t M, size_t* s_tok_off, size_t* qa_off) {
 } // namespace
 
 namespace w8a8 {
+
+// The kernels are built for sm_100a only: tcgen05.mma.kind::i8 exists on compute capability 10.0 and not, for
+// instance, on 10.3.
+int check_arch() {
+    static thread_local int cached_dev = -1;
+    static thread_local int cached_ok = 0;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return W8A8_ERR_CUDA;
+    if (dev != cached_dev) {
+        int major = 0, minor = 0;
+        if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+            return W8A8_ERR_CUDA;
+        cached_dev = dev;
+        cached_ok = (major == 10 && minor == 0);
+    }
+    return cached_ok ? W8A8_OK : W8A8_ERR_ARCH;
+}
 
 uint64_t wait_limit_ns() { return g_wait_limit_ns.load(); }
 int starve_mode() { return g_starve.load(); }

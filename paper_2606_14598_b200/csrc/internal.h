@@ -59,6 +59,8 @@ uint64_t wait_limit_ns();
 // the consumers' bounded waits run out, the kernel unwinds and returns, and the status word says which wait gave up.
 constexpr int kStarveGemm = 1, kStarveQuant = 2;
 int starve_mode();
+// W8A8_OK on a device of compute capability 10.0, else the status to return.
+int check_arch();
 // Device address, on the current device, of the word that keeps the first time-out of any call until the host
 // reads and clears it (int8_sticky_status); nullptr if it cannot be resolved.
 int* sticky_status_word();
@@ -126,5 +128,27 @@ TcPlan tc_plan(int M, int N, int K, int forced, size_t scratch_bytes);
 size_t tc_max_scratch_bytes(int M, int N, int K);
 // Launches the plan. Returns a w8a8_status.
 int launch_gemm_tc(const GemmArgs& a, const TcPlan& plan, cudaStream_t st);
+
+// ---- mxfp4_quantize.cu
+// early: let the kernel behind this one be set up while this one runs (never for what may be used as a weight).
+cudaError_t launch_mx_quantize(const void* x, bool fp32, int64_t ldx, int M, int K, uint8_t* codes, uint8_t* scales, int* status_to_clear,
+                               bool early, cudaStream_t st);
+cudaError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, bool fp32, int64_t ldo, cudaStream_t st);
+
+// ---- mxfp4_simt.cu
+struct MxLinearArgs {
+    const uint8_t* qa;     // codes of the activations [M, K/2], row stride ldqa bytes
+    const uint8_t* sa;     // their scale tiles
+    int64_t ldqa;
+    const uint8_t* qw;     // codes of the weights [N, K/2], dense
+    const uint8_t* sw;     // their scale tiles
+    const float* bias;     // [N] or nullptr
+    void* out;             // bf16 [M,N], row stride ldo
+    int64_t ldo;
+    int M, N, K;
+    int* status;           // workspace status word
+    bool after_quantizer;  // launched behind the quantizer, which has cleared the status word
+};
+cudaError_t launch_mx_linear_simt(const MxLinearArgs& a, cudaStream_t st);
 
 } // namespace w8a8

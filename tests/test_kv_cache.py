@@ -1,0 +1,241 @@
+"""The quantized paged cache: refusals without a GPU, contents and values read back against plain 64-bit forms on one."""
+import ctypes
+
+import pytest
+import torch
+
+import lowbit_reference as ref
+import paper_2606_14598_b200 as w8
+from paper_2606_14598_b200 import kv_cache
+
+INVALID, ALIGNMENT = 1, 2
+P = ctypes.c_void_p
+
+
+def test_write_refusals():
+    f = kv_cache._lib.kv_cache_write
+    names = ["fmt", "k", "kt", "kh", "v", "vt", "vh", "slots", "tokens", "heads", "dim", "kc", "ks", "vc", "vs", "num_slots", "stream"]
+    ok = dict(zip(names, [0, P(4096), 128, 64, P(4096), 128, 64, P(4096), 3, 2, 64, P(4096), P(4096), P(4096), P(4096), 32, None]))
+
+    def status(**change):
+        return f(*{**ok, **change}.values())
+
+    for name in ("k", "slots", "kc", "ks", "vc", "vs"):
+        assert status(**{name: None}) == INVALID, name
+    assert status(fmt=2) == INVALID and status(heads=0) == INVALID and status(dim=0) == INVALID and status(dim=264) == INVALID
+    assert status(tokens=-1) == INVALID and status(num_slots=-1) == INVALID
+    assert status(dim=12) == ALIGNMENT and status(kt=129) == ALIGNMENT and status(kh=60) == ALIGNMENT and status(vt=4) == ALIGNMENT
+    for name in ("k", "v", "kc", "vc"):
+        assert status(**{name: P(4104)}) == ALIGNMENT, name
+    assert status(slots=P(4100)) == ALIGNMENT and status(ks=P(4098)) == ALIGNMENT
+
+
+def test_read_refusals():
+    f = kv_cache._lib.kv_cache_read
+    names = ["fmt", "kc", "ks", "vc", "vs", "num_pages", "page", "heads", "dim", "table", "stride", "max_pages", "cu", "starts", "seqs", "total",
+             "ko", "kt", "kh", "vo", "vt", "vh", "stream"]
+    ok = dict(zip(names, [1, P(4096), P(4096), P(4096), P(4096), 4, 16, 2, 64, P(4096), 3, 3, P(4096), None, 2, 10,
+                          P(4096), 128, 64, P(4096), 128, 64, None]))
+
+    def status(**change):
+        return f(*{**ok, **change}.values())
+
+    for name in ("kc", "ks", "vc", "vs", "table", "cu", "ko"):
+        assert status(**{name: None}) == INVALID, name
+    assert status(page=0) == INVALID and status(num_pages=-1) == INVALID and status(stride=2) == INVALID and status(total=-1) == INVALID
+    assert status(total=1 << 31) == INVALID and status(seqs=-1) == INVALID and status(fmt=-1) == INVALID
+    assert status(dim=20) == ALIGNMENT and status(kt=100) == ALIGNMENT and status(vh=2) == ALIGNMENT
+    for name in ("kc", "vc", "ko", "vo"):
+        assert status(**{name: P(4104)}) == ALIGNMENT, name
+    assert status(table=P(4097)) == ALIGNMENT and status(cu=P(4098)) == ALIGNMENT and status(starts=P(4098)) == ALIGNMENT
+
+
+def test_python_refusals():
+    c = w8.QuantKVCache.empty(2, 4, 3, 16, "int8", device="cpu")
+    k = torch.zeros(5, 3, 16, dtype=torch.bfloat16)
+    slots = torch.arange(5)
+    with pytest.raises(TypeError):
+        w8.kv_cache_write(c, k.float(), k, slots)
+    with pytest.raises(TypeError):
+        w8.kv_cache_write(c, k, k, slots.int())
+    with pytest.raises(ValueError):
+        w8.kv_cache_write(c, k[:4], k, slots)
+    with pytest.raises(ValueError):
+        w8.kv_cache_write(c, k, None, slots)
+    with pytest.raises(ValueError):
+        w8.kv_cache_write(c, k, k, slots)                        # no CPU fallback
+    with pytest.raises(ValueError):
+        w8.QuantKVCache.empty(2, 4, 3, 16, "int4", device="cpu")
+    with pytest.raises(ValueError):
+        w8.QuantKVCache(c.k_codes, c.k_scales, c.v_codes)
+    with pytest.raises(ValueError):
+        w8.QuantKVCache(c.k_codes, c.k_scales[:, :2])
+    table, cu = torch.zeros(2, 1, dtype=torch.int32), torch.tensor([0, 1, 3], dtype=torch.int32)
+    with pytest.raises(TypeError):
+        w8.kv_cache_read(c, table.long(), cu, 3)
+    with pytest.raises(TypeError):
+        w8.kv_cache_read(c, table, cu[:2], 3)
+    with pytest.raises(TypeError):
+        w8.kv_cache_read(c, table, cu, 3, starts=cu)
+    with pytest.raises(ValueError):
+        w8.kv_cache_read(c, table, cu, 3, k_out=torch.zeros(2, 3, 16, dtype=torch.bfloat16))
+
+
+# ------------------------------------------------------------------------------------------ on the GPU
+
+def random_cache(fmt, pages, page, heads, dim, values=True):
+    c = w8.QuantKVCache.empty(pages, page, heads, dim, fmt, values=values)
+    for codes, scales in ((c.k_codes, c.k_scales), (c.v_codes, c.v_scales)):
+        if codes is None:
+            continue
+        if fmt == "int8":
+            codes.copy_(torch.randint(-127, 128, codes.shape, device="cuda"))
+            scales.copy_(torch.rand(scales.shape, device="cuda") + 0.01)
+        else:
+            codes.copy_(torch.randint(0, 256, codes.shape, device="cuda"))
+            scales.copy_(torch.randint(100, 150, scales.shape, device="cuda"))
+    return c
+
+
+def expected_write(fmt, codes, scales, x, slots):
+    codes, scales = codes.clone().flatten(0, 1), scales.clone().flatten(0, 1)
+    keep = (slots >= 0) & (slots < codes.shape[0])
+    if fmt == "int8":
+        q, s = ref.int8_quantize(x)
+        q, s = q.to(torch.int8), s.float()
+    else:
+        q, s = ref.mx_quantize(x)
+        q, s = ref.pack(q), s.to(torch.uint8)
+    codes[slots[keep]], scales[slots[keep]] = q[keep], s[keep]
+    return codes, scales
+
+
+def same(a, b):
+    return torch.equal(a, b) if a.dtype != torch.float32 else ref.same_values(a, b)
+
+
+def expected_read(fmt, codes, scales, table, lens, starts, page):
+    codes, scales, out = codes.flatten(0, 1), scales.flatten(0, 1), []
+    dim = codes.shape[2] * (1 if fmt == "int8" else 2)
+    for b, n in enumerate(lens):
+        for p in range(starts[b], starts[b] + n):
+            at = p // page
+            id = int(table[b, at]) if 0 <= p and at < table.shape[1] else -1
+            if 0 <= id < codes.shape[0] // page:
+                row = id * page + p % page
+                if fmt == "int8":
+                    out.append((codes[row].float() * scales[row][:, None]).double())     # fp32 product, as defined
+                else:
+                    out.append(ref.mx_values(ref.unpack(codes[row]), scales[row].long()))
+            else:
+                out.append(torch.zeros(codes.shape[1], dim, dtype=torch.float64, device=codes.device))
+    return torch.stack(out) if out else torch.zeros(0, codes.shape[1], dim, dtype=torch.float64, device=codes.device)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("tokens,heads,dim,page", [(1, 1, 8, 1), (1, 8, 128, 16), (5, 3, 16, 4), (33, 2, 24, 7), (64, 5, 64, 16), (70, 4, 72, 100),
+                                                   (129, 3, 80, 32), (17, 2, 96, 16), (257, 36, 128, 16), (40, 3, 200, 8), (31, 7, 256, 64)])
+def test_write(fmt, tokens, heads, dim, page):
+    pages = tokens // page + 3
+    c = random_cache(fmt, pages, page, heads, dim)
+    slots = torch.randperm(pages * page, device="cuda")[:tokens]
+    slots[0] = -1 if tokens > 1 else slots[0]
+    if tokens > 4:
+        slots[2], slots[4] = pages * page, 1 << 40                  # outside: skipped
+    qkv = torch.randn(tokens, 3, heads, dim, device="cuda").bfloat16()
+    qkv[tokens // 2, 1:] = 0
+    if tokens > 8:
+        qkv[7, 1, 0, dim - 1], qkv[7, 2, heads - 1, 0] = float("nan"), float("-inf")
+        qkv[8, 1:] *= 2.0 ** -125
+        qkv[6, 1:] *= 2.0 ** 120
+    k, v = qkv[:, 1], qkv[:, 2]                                      # strided: slices of a fused projection
+    want = [expected_write(fmt, *side, x, slots) for side, x in (((c.k_codes, c.k_scales), k), ((c.v_codes, c.v_scales), v))]
+    w8.kv_cache_write(c, k, v, slots)
+    got = [(c.k_codes, c.k_scales), (c.v_codes, c.v_scales)]
+    for (gc, gs), (wc, ws) in zip(got, want):
+        assert same(gc.flatten(0, 1), wc) and same(gs.flatten(0, 1), ws)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("lens,heads,dim,page", [([1], 1, 8, 1), ([0, 1, 0, 17, 33, 0], 2, 64, 16), ([100], 5, 72, 16), ([5, 250, 3], 3, 128, 32),
+                                                 ([64, 64], 8, 128, 64), ([7, 0, 130], 4, 80, 100), ([40, 1, 1, 1, 60], 2, 256, 7), ([35], 36, 96, 16),
+                                                 ([90, 20], 3, 24, 5)])
+@pytest.mark.parametrize("window", [False, True])
+def test_read(fmt, lens, heads, dim, page, window):
+    starts = [(3 * i + 2) % 11 if window else 0 for i in range(len(lens))]
+    most = max((n + s + page - 1) // page for n, s in zip(lens, starts)) + 1
+    pages = len(lens) * most
+    c = random_cache(fmt, pages, page, heads, dim)
+    table = torch.randperm(pages, device="cuda").int().view(len(lens), most)
+    if page > 1 and len(lens) > 1:
+        table[1, 0], table[0, most - 1] = -1, pages                  # missing pages read as zeros
+    wide = torch.full((len(lens), most + 2), 1 << 30, dtype=torch.int32, device="cuda")
+    wide[:, :most] = table
+    cu = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
+    first = torch.tensor(starts, dtype=torch.int32, device="cuda") if window else None
+    total = sum(lens)
+    k, v = w8.kv_cache_read(c, wide[:, :most], cu, total, starts=first)
+    assert k.shape == v.shape == (total, heads, dim)
+    assert ref.same_values(k, expected_read(fmt, c.k_codes, c.k_scales, table, lens, starts, page))
+    assert ref.same_values(v, expected_read(fmt, c.v_codes, c.v_scales, table, lens, starts, page))
+    # into strided outputs with rows past the last sequence: only the tokens' heads are written
+    buf = torch.full((total + 3, 3, heads, dim), 5.0, device="cuda", dtype=torch.bfloat16)
+    w8.kv_cache_read(c, wide[:, :most], cu, total + 3, starts=first, k_out=buf[:, 0], v_out=buf[:, 2])
+    assert torch.equal(buf[:total, 0], k) and torch.equal(buf[:total, 2], v)
+    assert (buf[total:] == 5).all() and (buf[:, 1] == 5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_read_past_the_table_and_negative_starts(fmt):
+    c = random_cache(fmt, 4, 16, 2, 64)
+    table = torch.tensor([[2, 0]], dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 50], dtype=torch.int32, device="cuda")
+    k, _ = w8.kv_cache_read(c, table, cu, 50, starts=torch.tensor([-5], dtype=torch.int32, device="cuda"))
+    assert (k[:5] == 0).all() and (k[37:] == 0).all()
+    assert ref.same_values(k[5:37], expected_read(fmt, c.k_codes, c.k_scales, table, [32], [0], 16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_one_sided_cache_empty_calls_and_graph(fmt):
+    c = w8.QuantKVCache.empty(3, 16, 2, 128, fmt, values=False)
+    assert (w8.kv_cache_read(c, torch.zeros(1, 3, dtype=torch.int32, device="cuda"), torch.tensor([0, 4], dtype=torch.int32, device="cuda"), 4)[0] == 0).all()
+    x = torch.randn(20, 2, 128, device="cuda").bfloat16()
+    slots = torch.arange(5, 25, device="cuda")
+    w8.kv_cache_write(c, x[:0], None, slots[:0])
+    table, cu = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), torch.tensor([0, 20], dtype=torch.int32, device="cuda")
+    first = torch.tensor([5], dtype=torch.int32, device="cuda")
+    empty, none = w8.kv_cache_read(c, table, cu, 0)
+    assert empty.shape == (0, 2, 128) and none is None
+    out = torch.zeros_like(x)
+    w8.kv_cache_write(c, x, None, slots)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w8.kv_cache_write(c, x, None, slots)
+        w8.kv_cache_read(c, table, cu, 20, starts=first, k_out=out)
+    x.copy_(torch.randn(20, 2, 128, device="cuda"))
+    graph.replay()
+    codes, scales = ref.int8_quantize(x) if fmt == "int8" else ref.mx_quantize(x)
+    want = (codes.float() * scales.float()[..., None]).double() if fmt == "int8" else ref.mx_values(codes, scales)
+    assert ref.same_values(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_offsets_past_32_bits(fmt):
+    heads, dim, page = 64, 256, 64
+    pages = ((1 << 32) // (heads * dim * page // (1 if fmt == "int8" else 2))) + 3        # the codes pass 2^32 bytes
+    c = w8.QuantKVCache.empty(pages, page, heads, dim, fmt, values=False)
+    x = torch.randn(page, heads, dim, device="cuda").bfloat16()
+    slots = torch.arange((pages - 1) * page, pages * page, device="cuda")
+    w8.kv_cache_write(c, x, None, slots)
+    table, cu = torch.tensor([[pages - 1]], dtype=torch.int32, device="cuda"), torch.tensor([0, page], dtype=torch.int32, device="cuda")
+    k, _ = w8.kv_cache_read(c, table, cu, page)
+    codes, scales = ref.int8_quantize(x) if fmt == "int8" else ref.mx_quantize(x)
+    want = (codes.float() * scales.float()[..., None]).double() if fmt == "int8" else ref.mx_values(codes, scales)
+    assert ref.same_values(k, want)
+    assert not c.k_codes[: pages - 1].any()

@@ -1,0 +1,325 @@
+"""The MXFP4 linear, its quantizer and its inverse: refusals without a GPU, values against plain 64-bit forms on one."""
+import ctypes
+
+import pytest
+import torch
+
+import lowbit_reference as ref
+import paper_2606_14598_b200 as w8
+from paper_2606_14598_b200 import mxfp4
+
+OK, INVALID, ALIGNMENT, WORKSPACE = 0, 1, 2, 4
+P = ctypes.c_void_p
+
+
+# ------------------------------------------------------------------------------------------ without a GPU
+
+def test_sizes():
+    assert mxfp4._lib.mxfp4_scale_bytes(1, 32) == 512
+    assert mxfp4._lib.mxfp4_scale_bytes(128, 128) == 512
+    assert mxfp4._lib.mxfp4_scale_bytes(129, 160) == 4 * 512
+    assert mxfp4._lib.mxfp4_scale_bytes(0, 32) == 0 and mxfp4._lib.mxfp4_scale_bytes(4, 48) == 0
+    assert w8.mxfp4_linear_workspace_bytes(77, 2048, 1056) >= 256 + 9 * 512 + 77 * 528
+    assert w8.mxfp4_linear_workspace_bytes(77, 0, 1056) == 0 and w8.mxfp4_linear_workspace_bytes(77, 8, 1050) == 0
+
+
+def test_quantize_refusals():
+    q = mxfp4._lib.mxfp4_quantize
+    ok = [P(4096), 0, 4, 64, 64, P(8192), P(16384), None]
+
+    def status(**change):
+        a = list(ok)
+        for i, v in change.items():
+            a[int(i[1:])] = v
+        return q(*a)
+
+    assert status(_0=None) == INVALID and status(_5=None) == INVALID and status(_6=None) == INVALID
+    assert status(_1=2) == INVALID and status(_1=-1) == INVALID
+    assert status(_2=0) == INVALID and status(_2=(1 << 30) + 1) == INVALID and status(_3=0) == INVALID and status(_3=(1 << 24) + 32) == INVALID
+    assert status(_4=32) == INVALID
+    assert status(_3=48) == ALIGNMENT and status(_4=68) == ALIGNMENT
+    assert status(_0=P(4104)) == ALIGNMENT and status(_5=P(8196)) == ALIGNMENT and status(_6=P(16388)) == ALIGNMENT
+    d = mxfp4._lib.mxfp4_dequantize
+    assert d(P(4096), P(8192), 4, 64, None, 0, 64, None) == INVALID
+    assert d(P(4096), P(8192), 4, 64, P(16384), 3, 64, None) == INVALID
+    assert d(P(4096), P(8192), 4, 64, P(16384), 0, 60, None) == INVALID
+    assert d(P(4096), P(8192), 4, 64, P(16384), 0, 68, None) == ALIGNMENT
+    assert d(P(4096), P(8192), 4, 64, P(16392), 0, 64, None) == ALIGNMENT
+
+
+def test_linear_refusals():
+    f = mxfp4._lib.mxfp4_linear_fused
+    names = ["A", "a_dtype", "lda", "a_scales", "qw", "sw", "bias", "out", "ldo", "M", "N", "K", "ws", "ws_bytes", "stream"]
+    ok = dict(zip(names, [P(4096), 0, 64, None, P(8192), P(8192), None, P(4096), 16, 4, 16, 64, P(4096), 1 << 20, None]))
+
+    def status(**change):
+        return f(*{**ok, **change}.values())
+
+    for name in ("A", "qw", "sw", "out"):
+        assert status(**{name: None}) == INVALID, name
+    assert status(a_dtype=1) == INVALID and status(a_dtype=7) == INVALID
+    assert status(a_scales=P(4096)) == INVALID and status(a_dtype=2) == INVALID          # scales go with codes, codes with scales
+    for name in ("M", "N", "K"):
+        assert status(**{name: 0}) == INVALID and status(**{name: -8}) == INVALID
+    assert status(M=(1 << 30) + 1) == INVALID
+    assert status(lda=56) == INVALID and status(ldo=8) == INVALID
+    assert status(K=48) == ALIGNMENT and status(N=12) == ALIGNMENT and status(lda=68) == ALIGNMENT and status(ldo=20) == ALIGNMENT
+    for name in ("A", "qw", "sw", "out"):
+        assert status(**{name: P(4104)}) == ALIGNMENT, name
+    assert status(bias=P(4098)) == ALIGNMENT
+    assert status(ws=None) == WORKSPACE and status(ws=P(4096 + 128)) == WORKSPACE and status(ws_bytes=256) == WORKSPACE
+
+
+def test_python_refusals():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        w8.mxfp4_quantize(x.half())
+    with pytest.raises(TypeError):
+        w8.mxfp4_quantize(x.t())
+    with pytest.raises(ValueError):
+        w8.mxfp4_quantize(x, scales=torch.zeros(1, 2, 512, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        w8.mxfp4_quantize(x)                                     # no CPU fallback
+    codes, scales = torch.zeros(16, 32, dtype=torch.uint8), torch.zeros(1, 1, 512, dtype=torch.uint8)
+    with pytest.raises(TypeError):
+        w8.mxfp4_dequantize(codes, scales, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        w8.mxfp4_linear_fused(torch.zeros(4, 96, dtype=torch.bfloat16), codes, scales)
+    with pytest.raises(TypeError):
+        w8.mxfp4_linear_fused(x.float(), codes, scales)
+    with pytest.raises(TypeError):
+        w8.mxfp4_linear_fused(x, codes, scales, torch.zeros(8))
+    with pytest.raises(TypeError):
+        w8.mxfp4_linear_fused(x, codes, scales, out=torch.zeros(4, 16))
+    with pytest.raises(ValueError):
+        w8.mxfp4_linear_fused(x, codes, scales)
+
+
+def test_reference_grid():
+    """The reference's own rounding on hand-made values: every tie goes to the even code, 7 saturates."""
+    x = torch.zeros(1, 32, dtype=torch.float64)
+    x[0, :14] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, -0.25, -0.75, 5.001, 0.2501, 4.0], dtype=torch.float64)
+    codes, scale = ref.mx_quantize(x)
+    assert scale.item() == 127 and codes[0, :14].tolist() == [0, 2, 2, 4, 4, 6, 6, 7, 7, 8, 10, 7, 1, 6]
+
+
+# ------------------------------------------------------------------------------------------ quantizer
+
+def check_quantized(x):
+    codes, scales = w8.mxfp4_quantize(x)
+    want_codes, want_bytes = ref.mx_quantize(x)
+    assert torch.equal(scales, ref.tile(want_bytes))                 # zero bytes past the end included
+    assert torch.equal(codes, ref.pack(want_codes))
+    for dtype in (torch.bfloat16, torch.float32):
+        out = w8.mxfp4_dequantize(codes, scales, dtype=dtype)
+        assert out.dtype == dtype and ref.same_values(out, ref.mx_values(want_codes, want_bytes))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m,k", [(1, 32), (1, 4608), (3, 64), (127, 96), (128, 128), (129, 160), (7, 1056), (300, 992), (33, 12288), (1000, 224)])
+def test_quantizer(m, k, dtype):
+    g = torch.Generator("cuda").manual_seed(m * 1000 + k)
+    x = torch.randn(m, k, generator=g, device="cuda") * torch.exp2(torch.randint(-20, 20, (m, 1), generator=g, device="cuda").float())
+    check_quantized(x.to(dtype))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantizer_strides(dtype):
+    x = torch.randn(70, 3, 352, device="cuda").to(dtype)
+    check_quantized(x[:, 1])                                         # a slice of a fused buffer
+    check_quantized(x.view(70, 1056)[:, 32:32 + 320])
+    wide = torch.full((40, 512), 7.0, device="cuda", dtype=dtype)
+    codes, scales = w8.mxfp4_quantize(x.view(70, 1056)[:40, :256])
+    w8.mxfp4_dequantize(codes, scales, out=wide[:, 128:384])
+    assert (wide[:, :128] == 7).all() and (wide[:, 384:] == 7).all()
+    assert torch.equal(wide[:, 128:384], w8.mxfp4_dequantize(codes, scales, dtype=dtype))
+
+
+@pytest.mark.gpu
+def test_quantizer_special_values():
+    x = torch.zeros(12, 64, device="cuda")
+    x[1] = -0.0
+    x[2, 0] = 2.0 ** -133                      # bf16 subnormal: the scale clamps at 2^-127
+    x[2, 1] = 2.0 ** -128
+    x[2, 40] = 2.0 ** -126
+    x[3, 5] = float("inf")                     # first block bad, second untouched
+    x[3, 40] = 3.0
+    x[4, 33] = float("nan")
+    x[4, 0] = -5.0
+    x[5, 63] = float("-inf")
+    x[6] = torch.finfo(torch.bfloat16).max
+    x[7, ::2] = -torch.finfo(torch.bfloat16).max
+    x[8, :9] = torch.tensor([4.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0])
+    x[9] = -x[8] * 2.0 ** 100
+    x[10, 0], x[10, 1] = 1.0, 2.0 ** -120      # far below the block's largest
+    x[11, :2] = torch.tensor([7.96875, 6.96875])
+    check_quantized(x.bfloat16())
+    x[2, 2] = 2.0 ** -149                      # fp32 subnormals
+    x[6] = torch.finfo(torch.float32).max
+    check_quantized(x)
+
+
+@pytest.mark.gpu
+def test_quantizer_every_finite_bf16_value():
+    """Every finite bf16 value in blocks led by a value 0 to 9 powers of two above it."""
+    bits = torch.arange(1 << 16, device="cuda", dtype=torch.int32)
+    v = bits.to(torch.int16).view(torch.bfloat16)
+    v = v[torch.isfinite(v)]
+    for up in range(10):
+        x = torch.zeros(v.numel() // 31 + 1, 32, device="cuda", dtype=torch.bfloat16)
+        x[:, 1:].reshape(-1)
+        flat = torch.zeros(x.shape[0] * 31, device="cuda", dtype=torch.bfloat16)
+        flat[: v.numel()] = v
+        x[:, 1:] = flat.view(-1, 31)
+        lead = x.float().abs().amax(1) * 2.0 ** up
+        x[:, 0] = torch.where(torch.isfinite(lead.bfloat16()), lead, torch.zeros_like(lead)).bfloat16()
+        check_quantized(x)
+
+
+@pytest.mark.gpu
+def test_dequantize_all_codes_and_scales():
+    codes = torch.arange(16, device="cuda").repeat(256, 2)
+    rows = torch.arange(256, device="cuda")[:, None]
+    got = w8.mxfp4_dequantize(ref.pack(codes), ref.tile(rows), dtype=torch.float32)
+    want = ref.mx_values(codes, rows)
+    want[254][want[254].abs() > torch.finfo(torch.bfloat16).max] *= float("inf")     # 2^127 * 2 and above: past bf16 and fp32
+    want[253][want[253].abs() > torch.finfo(torch.bfloat16).max] *= float("inf")
+    assert ref.same_values(got, want)
+
+
+# ------------------------------------------------------------------------------------------ linear
+
+def operands(m, n, k, seed=0, loud=True):
+    g = torch.Generator("cuda").manual_seed(seed + 7 * m + 11 * n + 13 * k)
+    a = torch.randn(m, k, generator=g, device="cuda")
+    if loud:
+        a[:, torch.randperm(k, generator=g, device="cuda")[: max(1, k // 100)]] *= 20
+    w = torch.randn(n, k, generator=g, device="cuda") * 0.02
+    bias = torch.randn(n, generator=g, device="cuda") * 0.01
+    return a.bfloat16(), w, bias
+
+
+def check_linear(out, a, w, bias):
+    """out against the 64-bit product of the quantized values. Tolerance: half an ulp of bf16 (8 significant bits: at most 2^-8 of the result), and for the
+    fp32 accumulation at most 2^-22 of the sum of the products' magnitudes for each step of 32 along K."""
+    av, wv = ref.mx_values(*ref.mx_quantize(a)), ref.mx_values(*ref.mx_quantize(w))
+    want = av @ wv.t() + (0 if bias is None else bias.double())
+    size = av.abs() @ wv.abs().t() + (0 if bias is None else bias.double().abs())
+    tol = want.abs() * 2.0 ** -8 + (a.shape[1] // 32 + 2) * 2.0 ** -22 * size + 2.0 ** -133
+    assert out.dtype == torch.bfloat16 and out.shape == want.shape
+    worst = ((out.double() - want).abs() / tol).max().item()
+    assert worst <= 1.0, worst
+
+
+SHAPES = [(1, 8, 32), (1, 4608, 4608), (1, 136, 96), (2, 27648, 1056), (3, 1000, 160), (4, 256, 12288), (7, 264, 64), (8, 128, 256), (9, 2048, 1056),
+          (15, 24, 544), (16, 512, 512), (17, 120, 2048), (31, 264, 288), (32, 128, 4128), (33, 136, 1024), (64, 1160, 768), (65, 384, 96),
+          (77, 2048, 1056), (100, 4616, 4608), (127, 128, 128), (128, 256, 256), (129, 264, 320), (200, 16, 3008), (255, 520, 1088),
+          (257, 248, 224), (300, 328, 384), (513, 1032, 1184), (1000, 2056, 736), (1200, 4608, 2336), (2305, 1000, 512)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", SHAPES)
+def test_linear(m, n, k):
+    a, w, bias = operands(m, n, k)
+    qw, sw = w8.mxfp4_quantize(w)
+    ws = w8.mxfp4_alloc_workspace(m, n, k)
+    ws.fill_(255)
+    out = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    assert w8.int8_check_status(ws) == 0
+    check_linear(out, a, w, bias)
+    plain = w8.mxfp4_linear_fused(a, qw, sw)
+    check_linear(plain, a, w, None)
+    codes, scales = w8.mxfp4_quantize(a)
+    again = w8.mxfp4_linear_fused(codes, qw, sw, bias, a_scales=scales, workspace=ws)
+    assert torch.equal(again, out)                                   # the same kernel on the same codes: the same bits
+    for _ in range(3):
+        assert torch.equal(w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws), out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [1, 5, 40, 150, 700])
+def test_linear_strides_and_guards(m):
+    n, k = 264, 416
+    a, w, bias = operands(m, n, k)
+    qw, sw = w8.mxfp4_quantize(w)
+    want = w8.mxfp4_linear_fused(a, qw, sw, bias)
+    wide = torch.full((m + 2, 3 * k), float("nan"), device="cuda", dtype=torch.bfloat16)      # neighbours must not be read
+    wide[1:-1, k:2 * k] = a
+    buf = torch.full((m + 2, n + 32), 9.0, device="cuda", dtype=torch.bfloat16)
+    w8.mxfp4_linear_fused(wide[1:-1, k:2 * k], qw, sw, bias, out=buf[1:-1, 16:16 + n])
+    assert torch.equal(buf[1:-1, 16:16 + n], want)
+    buf[1:-1, 16:16 + n] = 9.0
+    assert (buf == 9.0).all()
+    codes, scales = w8.mxfp4_quantize(a)
+    padded = torch.full((m, k // 2 + 48), 255, device="cuda", dtype=torch.uint8)
+    padded[:, 16:16 + k // 2] = codes
+    assert torch.equal(w8.mxfp4_linear_fused(padded[:, 16:16 + k // 2], qw, sw, bias, a_scales=scales), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [2, 20, 130, 300])
+def test_linear_non_finite_rows_stay_apart(m):
+    n, k = 144, 352
+    a, w, bias = operands(m, n, k)
+    qw, sw = w8.mxfp4_quantize(w)
+    want = w8.mxfp4_linear_fused(a, qw, sw, bias)
+    a[1, k - 1] = float("nan")
+    out = w8.mxfp4_linear_fused(a, qw, sw, bias)
+    assert torch.isnan(out[1]).all()
+    keep = [i for i in range(m) if i != 1]
+    assert torch.equal(out[keep], want[keep])
+    w[7, 3] = float("inf")
+    qw, sw = w8.mxfp4_quantize(w)
+    out = w8.mxfp4_linear_fused(a, qw, sw, bias)
+    assert torch.isnan(out[:, 7]).all() and torch.equal(out[keep][:, :7], want[keep][:, :7]) and torch.equal(out[keep][:, 8:], want[keep][:, 8:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(1, 128, 256), (24, 128, 512), (200, 256, 256)])
+def test_linear_scale_range(m, n, k):
+    """Scales from the smallest to ones whose products nearly overflow fp32; zero rows and columns."""
+    g = torch.Generator("cuda").manual_seed(5)
+    a = torch.randn(m, k, generator=g, device="cuda") * torch.exp2(torch.randint(-60, 50, (m, 1), generator=g, device="cuda").float())
+    w = torch.randn(n, k, generator=g, device="cuda") * torch.exp2(torch.randint(-60, 50, (n, 1), generator=g, device="cuda").float())
+    a[0], w[3], w[5] = a[0] if m == 1 else 0, 0, torch.zeros(k, device="cuda")
+    a = a.bfloat16()
+    qw, sw = w8.mxfp4_quantize(w)
+    check_linear(w8.mxfp4_linear_fused(a, qw, sw), a, w, None)
+
+
+@pytest.mark.gpu
+def test_linear_on_another_stream_and_in_a_graph():
+    n, k = 520, 1056
+    for m in (1, 12, 300):
+        a, w, bias = operands(m, n, k)
+        qw, sw = w8.mxfp4_quantize(w)
+        want = w8.mxfp4_linear_fused(a, qw, sw, bias)
+        ws, out = w8.mxfp4_alloc_workspace(m, n, k), torch.zeros_like(want)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            w8.mxfp4_linear_fused(a, qw, sw, bias, out=out, workspace=ws)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(out, want)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            w8.mxfp4_linear_fused(a, qw, sw, bias, out=out, workspace=ws)
+            w8.mxfp4_linear_fused(a, qw, sw, bias, out=out, workspace=ws)
+        a2 = operands(m, n, k, seed=99)[0]
+        a.copy_(a2)
+        graph.replay()
+        assert torch.equal(out, w8.mxfp4_linear_fused(a2, qw, sw, bias))
+
+
+@pytest.mark.gpu
+def test_linear_random_shapes():
+    import random
+    r = random.Random(3)
+    for _ in range(60):
+        m, n, k = r.choice([r.randint(1, 40), r.randint(1, 300), r.randint(1, 1200)]), 8 * r.randint(1, 160), 32 * r.randint(1, 60)
+        a, w, bias = operands(m, n, k, seed=r.randint(0, 999))
+        qw, sw = w8.mxfp4_quantize(w)
+        check_linear(w8.mxfp4_linear_fused(a, qw, sw, bias), a, w, bias)
