@@ -21,7 +21,7 @@
  * of row r, block c is byte 16 * (r % 32) + 4 * (r / 32) + c. Bytes for rows or blocks past the end are 0.
  *
  * Sizes: K % 32 == 0, N % 8 == 0, 1 <= M, N <= 2^30, 1 <= K <= MXFP4_K_MAX. Pointers 16-byte aligned, row strides
- * multiples of 16 bytes (scales: 16-byte aligned; bias: 4-byte aligned).
+ * multiples of 16 bytes.
  */
 #ifndef MXFP4_LINEAR_H_
 #define MXFP4_LINEAR_H_
@@ -64,6 +64,12 @@ size_t mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
  */
 int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a_scales, const uint8_t* qw, const uint8_t* sw, const float* bias,
                        void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * For sweeps and tests: the kernel configuration of the following linears of this process. -1 (default) chooses from the
+ * sizes; an id outside the list makes mxfp4_linear_fused return W8A8_ERR_INVALID_ARG. Returns the previous value.
+ */
+int mxfp4_linear_force_config(int config_id);
 
 #ifdef __cplusplus
 }

@@ -26,7 +26,7 @@ _BINDING_NAMES = (
 )
 # entry points of the modules next to ``binding``, by module
 _MODULE_NAMES = {
-    "mxfp4": ("MXFP4_BF16", "MXFP4_CODES", "MXFP4_FP32", "MXFP4_K_MAX", "mxfp4_alloc_workspace", "mxfp4_dequantize",
+    "mxfp4": ("MXFP4_BF16", "MXFP4_CODES", "MXFP4_FP32", "MXFP4_K_MAX", "MXFP4_NUM_CONFIGS", "mxfp4_alloc_workspace", "mxfp4_dequantize", "mxfp4_force_config",
               "mxfp4_linear_fused", "mxfp4_linear_workspace_bytes", "mxfp4_quantize"),
     "kv_cache": ("KV_CACHE_INT8", "KV_CACHE_MAX_DIM", "KV_CACHE_MXFP4", "QuantKVCache", "kv_cache_read", "kv_cache_write"),
 }

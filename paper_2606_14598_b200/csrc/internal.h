@@ -135,7 +135,7 @@ cudaError_t launch_mx_quantize(const void* x, bool fp32, int64_t ldx, int M, int
                                bool early, cudaStream_t st);
 cudaError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, bool fp32, int64_t ldo, cudaStream_t st);
 
-// ---- mxfp4_simt.cu
+// ---- mxfp4_gemm.cu
 struct MxLinearArgs {
     const uint8_t* qa;     // codes of the activations [M, K/2], row stride ldqa bytes
     const uint8_t* sa;     // their scale tiles
@@ -149,6 +149,8 @@ struct MxLinearArgs {
     int* status;           // workspace status word
     bool after_quantizer;  // launched behind the quantizer, which has cleared the status word
 };
-cudaError_t launch_mx_linear_simt(const MxLinearArgs& a, cudaStream_t st);
+// The configuration for these sizes, and its launch. Return a configuration id / a w8a8_status.
+int choose_mx_config(int M, int N, int K);
+int launch_mx_gemm(const MxLinearArgs& a, int config, cudaStream_t st);
 
 } // namespace w8a8

@@ -5,11 +5,14 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include <atomic>
+
 namespace {
 
 using namespace w8a8;
 
 constexpr size_t kStatusBlock = 256;
+std::atomic<int> g_forced_config{-1};
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 
 struct Range {
@@ -19,7 +22,6 @@ struct Range {
 
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int check_matrix(int64_t rows, int64_t K) {
     if (rows <= 0 || K <= 0 || rows > kMaxRows || K > MXFP4_K_MAX) return W8A8_ERR_INVALID_ARG;
@@ -60,6 +62,8 @@ int mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int
                                 static_cast<cudaStream_t>(stream)) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }
 
+int mxfp4_linear_force_config(int config_id) { return g_forced_config.exchange(config_id); }
+
 size_t mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (check_matrix(M, K) != W8A8_OK || N <= 0 || N > kMaxRows) return 0;
     return kStatusBlock + mxfp4_scale_bytes(M, K) + round_up(static_cast<size_t>(M) * static_cast<size_t>(K / 2), 256);
@@ -74,7 +78,7 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     if (int e = check_matrix(M, K)) return e;
     if (N <= 0 || N > kMaxRows || lda < (a_dtype == MXFP4_BF16 ? K : K / 2) || ldo < N) return W8A8_ERR_INVALID_ARG;
     if (N % 8 != 0 || ldo % 8 != 0 || lda % (a_dtype == MXFP4_BF16 ? 8 : 16) != 0) return W8A8_ERR_ALIGNMENT;
-    if (!aligned16(A) || !aligned16(a_scales) || !aligned16(qw) || !aligned16(sw) || !aligned16(out) || !aligned4(bias)) return W8A8_ERR_ALIGNMENT;
+    if (!aligned16(A) || !aligned16(a_scales) || !aligned16(qw) || !aligned16(sw) || !aligned16(out) || !aligned16(bias)) return W8A8_ERR_ALIGNMENT;
     const size_t need = a_dtype == MXFP4_BF16 ? mxfp4_linear_workspace_bytes(M, N, K) : kStatusBlock;
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < need) return W8A8_ERR_WORKSPACE;
     if (int e = check_arch()) return e;
@@ -93,7 +97,8 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     } else {
         g.qa = static_cast<const uint8_t*>(A); g.sa = a_scales; g.ldqa = lda; g.after_quantizer = false;
     }
-    return launch_mx_linear_simt(g, st) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
+    const int forced = g_forced_config.load();
+    return launch_mx_gemm(g, forced >= 0 ? forced : choose_mx_config(g.M, g.N, g.K), st);
 }
 
 } // extern "C"

@@ -194,6 +194,32 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&v)
         : "r"(taddr) : "memory");
 }
 
+// Block-scaled MXFP4: D[tmem] (+)= (A * scale_A)(B * scale_B)^T, E2M1 operands packed two to a byte in shared memory, K = 64
+// per instruction, one E8M0 scale for 32 elements read from tensor memory; fp32 accumulators. CG = 1: one CTA; 2: a CTA pair.
+template <int CG>
+__device__ __forceinline__ void mma_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa_tmem, uint32_t sfb_tmem,
+                                            uint32_t accumulate) {
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa_tmem), "r"(sfb_tmem) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa_tmem), "r"(sfb_tmem) : "memory");
+}
+// One scale tile (128 rows x 4 blocks, 512 bytes of shared memory) into 4 columns of tensor memory, repeated in the four lane
+// groups; ordered before the MMAs this thread issues afterwards. CG = 2: in both CTAs of the pair, each from its own tile.
+template <int CG>
+__device__ __forceinline__ void tc_cp_scales(uint32_t taddr, uint64_t s_desc) {
+    if (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(s_desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(s_desc) : "memory");
+}
+
 // ------------------------------------------------------------------ clusters / CTA pairs (cta_group::2)
 __device__ __forceinline__ uint32_t cluster_ctarank() {
     uint32_t r;
@@ -267,6 +293,29 @@ __host__ __device__ constexpr uint32_t make_i8_idesc(int mma_m, int mma_n) {
          | (1u << 10)                             // B format: signed 8-bit
          | (static_cast<uint32_t>(mma_n >> 3) << 17)
          | (static_cast<uint32_t>(mma_m >> 4) << 24);
+}
+
+
+// Shared-memory descriptor of a scale tile for tcgen05.cp.32x128b: 32 rows of 16 bytes, dense, no swizzle (groups of 8 rows
+// are 128 bytes apart).
+__device__ __forceinline__ uint64_t make_scale_desc(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3ffffu) >> 4);
+    d |= static_cast<uint64_t>(128 >> 4) << 16;                // leading byte offset (one 16-byte column: not used)
+    d |= static_cast<uint64_t>(128 >> 4) << 32;                // stride byte offset
+    d |= static_cast<uint64_t>(1) << 46;                       // descriptor version (sm_100)
+    return d;
+}
+// Instruction descriptor of tcgen05.mma.kind::mxf4: E2M1 A and B (both K-major), E8M0 scales, fp32 D. sf: which half (0 or 2)
+// of the four scale bytes of a tensor-memory cell the instruction's two blocks of 32 take.
+__host__ __device__ constexpr uint32_t make_mxf4_idesc(int mma_m, int mma_n, int sf) {
+    return (static_cast<uint32_t>(sf) << 4)       // scale bytes of B
+         | (1u << 7)                              // A format: E2M1
+         | (1u << 10)                             // B format: E2M1
+         | (static_cast<uint32_t>(mma_n >> 3) << 17)
+         | (1u << 23)                             // scale format: E8M0
+         | (static_cast<uint32_t>(mma_m >> 7) << 27)
+         | (static_cast<uint32_t>(sf) << 29);     // scale bytes of A
 }
 
 } // namespace w8a8

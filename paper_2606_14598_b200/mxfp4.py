@@ -12,6 +12,7 @@ from .binding import W8A8Error, _i64, _int, _lib, _sz, _vp
 
 MXFP4_BF16, MXFP4_FP32, MXFP4_CODES = 0, 1, 2
 MXFP4_K_MAX = 1 << 24
+MXFP4_NUM_CONFIGS = 3
 _DTYPES = {torch.bfloat16: MXFP4_BF16, torch.float32: MXFP4_FP32}
 
 _lib.mxfp4_scale_bytes.argtypes = [_i64, _i64]
@@ -24,6 +25,8 @@ _lib.mxfp4_linear_workspace_bytes.argtypes = [_i64, _i64, _i64]
 _lib.mxfp4_linear_workspace_bytes.restype = _sz
 _lib.mxfp4_linear_fused.argtypes = [_vp, _int, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _sz, _vp]
 _lib.mxfp4_linear_fused.restype = _int
+_lib.mxfp4_linear_force_config.argtypes = [_int]
+_lib.mxfp4_linear_force_config.restype = _int
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -96,6 +99,11 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tenso
     same_device("mxfp4_dequantize", codes, scales, out)
     call(_lib.mxfp4_dequantize, "mxfp4_dequantize", codes, codes.data_ptr(), scales.data_ptr(), M, K, out.data_ptr(), kind, out.stride(0))
     return out
+
+
+def mxfp4_force_config(config_id: int) -> int:
+    """For sweeps and tests: the kernel configuration of the following linears (-1: chosen from the sizes). Returns the old one."""
+    return int(_lib.mxfp4_linear_force_config(int(config_id)))
 
 
 def mxfp4_linear_workspace_bytes(M: int, N: int, K: int) -> int:

@@ -66,7 +66,7 @@ def test_linear_refusals():
     assert status(K=48) == ALIGNMENT and status(N=12) == ALIGNMENT and status(lda=68) == ALIGNMENT and status(ldo=20) == ALIGNMENT
     for name in ("A", "qw", "sw", "out"):
         assert status(**{name: P(4104)}) == ALIGNMENT, name
-    assert status(bias=P(4098)) == ALIGNMENT
+    assert status(bias=P(4104)) == ALIGNMENT
     assert status(ws=None) == WORKSPACE and status(ws=P(4096 + 128)) == WORKSPACE and status(ws_bytes=256) == WORKSPACE
 
 
@@ -312,6 +312,49 @@ def test_linear_on_another_stream_and_in_a_graph():
         a.copy_(a2)
         graph.replay()
         assert torch.equal(out, w8.mxfp4_linear_fused(a2, qw, sw, bias))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("config", range(w8.MXFP4_NUM_CONFIGS))
+def test_linear_every_configuration(config):
+    """Shapes of several tiles for a CTA, odd numbers of k-blocks, ragged edges, on each kernel configuration."""
+    try:
+        for m, n, k in [(1, 8, 32), (130, 264, 96), (129, 136, 288), (300, 520, 1056), (700, 1000, 800), (2305, 4104, 544), (1500, 9224, 3104)]:
+            a, w, bias = operands(m, n, k)
+            qw, sw = w8.mxfp4_quantize(w)
+            w8.mxfp4_force_config(config)
+            ws = w8.mxfp4_alloc_workspace(m, n, k)
+            out = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+            assert w8.int8_check_status(ws) == 0
+            check_linear(out, a, w, bias)
+            for _ in range(3):
+                assert torch.equal(w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws), out)
+    finally:
+        w8.mxfp4_force_config(-1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("config", range(w8.MXFP4_NUM_CONFIGS))
+def test_linear_wait_runs_out_and_the_kernel_returns(config):
+    a, w, bias = operands(600, 1032, 2080)
+    qw, sw = w8.mxfp4_quantize(w)
+    ws = w8.mxfp4_alloc_workspace(600, 1032, 2080)
+    want = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    try:
+        w8.mxfp4_force_config(config)
+        want = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+        w8.debug_set_wait_limit_ns(3_000_000)
+        w8.debug_set_starve(1)
+        w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+        assert w8.int8_check_status(ws) == 7 and w8.int8_sticky_status() == 7
+    finally:
+        w8.debug_set_starve(0)
+        w8.debug_set_wait_limit_ns(0)
+    try:
+        again = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    finally:
+        w8.mxfp4_force_config(-1)
+    assert w8.int8_check_status(ws) == 0 and w8.int8_sticky_status() == 0 and torch.equal(again, want)
 
 
 @pytest.mark.gpu
