@@ -152,5 +152,11 @@ struct MxLinearArgs {
 // The configuration for these sizes, and its launch. Return a configuration id / a w8a8_status.
 int choose_mx_config(int M, int N, int K);
 int launch_mx_gemm(const MxLinearArgs& a, int config, cudaStream_t st);
+constexpr int kMxGemmConfigs = 3;
+
+// ---- mxfp4_skinny.cu : at most 16 tokens, one launch. A: bf16 (lda in elements) or, codes, packed codes (lda in bytes) with scale
+// tiles sa; the activations' fields of g are not used. Returns a w8a8_status.
+bool mx_skinny_fits(int M, int N, int K);
+int launch_mx_skinny(const MxLinearArgs& g, const void* A, bool codes, int64_t lda, const uint8_t* sa, cudaStream_t st);
 
 } // namespace w8a8

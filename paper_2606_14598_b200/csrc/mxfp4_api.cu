@@ -89,6 +89,10 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     g.qw = qw; g.sw = sw; g.bias = bias; g.out = out; g.ldo = ldo;
     g.M = static_cast<int>(M); g.N = static_cast<int>(N); g.K = static_cast<int>(K);
     g.status = reinterpret_cast<int*>(ws);
+    const int forced = g_forced_config.load();
+    if (forced > kMxGemmConfigs || (forced == kMxGemmConfigs && !mx_skinny_fits(g.M, g.N, g.K))) return W8A8_ERR_INVALID_ARG;
+    if (forced == kMxGemmConfigs || (forced < 0 && mx_skinny_fits(g.M, g.N, g.K)))
+        return launch_mx_skinny(g, A, a_dtype == MXFP4_CODES, lda, a_scales, st);
     if (a_dtype == MXFP4_BF16) {
         uint8_t* sa = ws + kStatusBlock;
         uint8_t* qa = sa + mxfp4_scale_bytes(M, K);
@@ -97,7 +101,6 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     } else {
         g.qa = static_cast<const uint8_t*>(A); g.sa = a_scales; g.ldqa = lda; g.after_quantizer = false;
     }
-    const int forced = g_forced_config.load();
     return launch_mx_gemm(g, forced >= 0 ? forced : choose_mx_config(g.M, g.N, g.K), st);
 }
 

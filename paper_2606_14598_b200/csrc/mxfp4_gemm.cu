@@ -22,8 +22,7 @@
 #include "internal.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"
-
-#include <cuda.h>
+#include "tensor_map.h"
 
 namespace w8a8 {
 namespace {
@@ -93,7 +92,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                const __grid_constant__ CUtensorMap tm_sb, const __grid_constant__ CUtensorMap tm_out, const float* bias, int M, int N, int K,
                const RunCtl rc) {
     using L = Layout<CG, BN, STAGES, KBS>;
-    grid_dep_launch_dependents();
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -140,6 +138,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     if (CG == 2) cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_holder;
+    // Only now: a kernel behind this one that allocates tensor memory and then waits for this one must not get there first.
+    grid_dep_launch_dependents();
 
     constexpr int TILE_M = BM * CG;
     const int num_nb = (N + BN - 1) / BN;
@@ -384,39 +384,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
 
 // ---------------------------------------------------------------------------- host side
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn get_encode() {
-    static EncodeFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    return fn;
-}
-
-bool encode_2d(CUtensorMap* tm, CUtensorMapDataType dt, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld_bytes, uint32_t box_rows,
-               uint32_t box_cols, CUtensorMapSwizzle swizzle) {
-    EncodeFn enc = get_encode();
-    if (enc == nullptr) return false;
-    cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {ld_bytes};
-    cuuint32_t box[2] = {box_cols, box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    return enc(tm, dt, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Scale tiles as rows of 128 words: a box of two rows is what 128 matrix rows need for one k-block. The second row of the
-// last box of an odd number of tiles belongs to the next 128 rows (or is past the end, and reads as zeros): it is not used.
-bool encode_scales(CUtensorMap* tm, const uint8_t* s, int rows, int K) {
-    const uint64_t tiles = static_cast<uint64_t>((rows + kScaleTileRows - 1) / kScaleTileRows) *
-                           ((K + kScaleTileBlocks * kMxBlock - 1) / (kScaleTileBlocks * kMxBlock));
-    return encode_2d(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, s, tiles, kScaleTileBytes / 4, kScaleTileBytes, 2, kScaleTileBytes / 4, CU_TENSOR_MAP_SWIZZLE_NONE);
-}
-
 template <int CG, int BN, int STAGES, int KBS>
 int launch_cfg(const MxLinearArgs& a, cudaStream_t st) {
     using L = Layout<CG, BN, STAGES, KBS>;
@@ -425,10 +392,9 @@ int launch_cfg(const MxLinearArgs& a, cudaStream_t st) {
     if (smem_opt_in.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::DYN_BYTES); }) != cudaSuccess)
         return W8A8_ERR_CUDA;
     CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_out;
-    if (!encode_2d(&tm_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.qa, a.M, a.K / 2, a.ldqa, BM, BKB, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_2d(&tm_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.qw, a.N, a.K / 2, a.K / 2, L::B_ROWS, BKB, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_scales(&tm_sa, a.sa, a.M, a.K) || !encode_scales(&tm_sb, a.sw, a.N, a.K) ||
-        !encode_2d(&tm_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.out, a.M, a.N, a.ldo * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+    if (!encode_mx_codes(&tm_a, a.qa, a.M, a.K, a.ldqa, BM) || !encode_mx_codes(&tm_b, a.qw, a.N, a.K, a.K / 2, L::B_ROWS) ||
+        !encode_mx_scales(&tm_sa, a.sa, a.M, a.K) || !encode_mx_scales(&tm_sb, a.sw, a.N, a.K) ||
+        !encode_map_2d(&tm_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.out, a.M, a.N, a.ldo * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return W8A8_ERR_CUDA;
     const int64_t tiles = static_cast<int64_t>((a.M + BM * CG - 1) / (BM * CG)) * ((a.N + BN - 1) / BN);
     if (tiles > INT32_MAX / 2) return W8A8_ERR_INVALID_ARG;

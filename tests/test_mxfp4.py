@@ -357,6 +357,43 @@ def test_linear_wait_runs_out_and_the_kernel_returns(config):
     assert w8.int8_check_status(ws) == 0 and w8.int8_sticky_status() == 0 and torch.equal(again, want)
 
 
+SKINNY = [(1, 8, 32), (2, 136, 96), (3, 4608, 1024), (16, 128, 2048), (5, 264, 4352), (7, 1000, 6176), (13, 40, 12288), (1, 20000, 544), (16, 256, 24608), (4, 24, 49152)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", SKINNY)
+def test_linear_few_tokens(m, n, k):
+    """Every way the few-token kernel cuts K (1 to 8 parts), odd numbers of k-blocks, ragged edges; bf16 and codes agree."""
+    a, w, bias = operands(m, n, k)
+    qw, sw = w8.mxfp4_quantize(w)
+    ws = w8.mxfp4_alloc_workspace(m, n, k)
+    out = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    assert w8.int8_check_status(ws) == 0
+    check_linear(out, a, w, bias)
+    codes, scales = w8.mxfp4_quantize(a)
+    for _ in range(5):
+        assert torch.equal(w8.mxfp4_linear_fused(codes, qw, sw, bias, a_scales=scales, workspace=ws), out)
+        assert torch.equal(w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws), out)
+
+
+@pytest.mark.gpu
+def test_linear_few_tokens_wait_runs_out():
+    a, w, bias = operands(3, 1032, 4128)
+    qw, sw = w8.mxfp4_quantize(w)
+    ws = w8.mxfp4_alloc_workspace(3, 1032, 4128)
+    want = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    try:
+        w8.debug_set_wait_limit_ns(3_000_000)
+        w8.debug_set_starve(1)
+        w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+        assert w8.int8_check_status(ws) == 7 and w8.int8_sticky_status() == 7
+    finally:
+        w8.debug_set_starve(0)
+        w8.debug_set_wait_limit_ns(0)
+    again = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+    assert w8.int8_check_status(ws) == 0 and w8.int8_sticky_status() == 0 and torch.equal(again, want)
+
+
 @pytest.mark.gpu
 def test_linear_random_shapes():
     import random
