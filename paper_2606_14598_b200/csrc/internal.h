@@ -156,7 +156,8 @@ constexpr int kMxGemmConfigs = 3;
 
 // ---- mxfp4_skinny.cu : at most 16 tokens, one launch. A: bf16 (lda in elements) or, codes, packed codes (lda in bytes) with scale
 // tiles sa; the activations' fields of g are not used. Returns a w8a8_status.
-bool mx_skinny_fits(int M, int N, int K);
+bool mx_skinny_fits(int M);              // what the kernel can run
+bool mx_skinny_preferred(int M);         // where it is chosen when nothing is forced
 int launch_mx_skinny(const MxLinearArgs& g, const void* A, bool codes, int64_t lda, const uint8_t* sa, cudaStream_t st);
 
 } // namespace w8a8

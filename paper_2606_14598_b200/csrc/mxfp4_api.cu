@@ -90,8 +90,8 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     g.M = static_cast<int>(M); g.N = static_cast<int>(N); g.K = static_cast<int>(K);
     g.status = reinterpret_cast<int*>(ws);
     const int forced = g_forced_config.load();
-    if (forced > kMxGemmConfigs || (forced == kMxGemmConfigs && !mx_skinny_fits(g.M, g.N, g.K))) return W8A8_ERR_INVALID_ARG;
-    if (forced == kMxGemmConfigs || (forced < 0 && mx_skinny_fits(g.M, g.N, g.K)))
+    if (forced > kMxGemmConfigs || (forced == kMxGemmConfigs && !mx_skinny_fits(g.M))) return W8A8_ERR_INVALID_ARG;
+    if (forced == kMxGemmConfigs || (forced < 0 && mx_skinny_preferred(g.M)))
         return launch_mx_skinny(g, A, a_dtype == MXFP4_CODES, lda, a_scales, st);
     if (a_dtype == MXFP4_BF16) {
         uint8_t* sa = ws + kStatusBlock;

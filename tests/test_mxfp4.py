@@ -357,7 +357,8 @@ def test_linear_wait_runs_out_and_the_kernel_returns(config):
     assert w8.int8_check_status(ws) == 0 and w8.int8_sticky_status() == 0 and torch.equal(again, want)
 
 
-SKINNY = [(1, 8, 32), (2, 136, 96), (3, 4608, 1024), (16, 128, 2048), (5, 264, 4352), (7, 1000, 6176), (13, 40, 12288), (1, 20000, 544), (16, 256, 24608), (4, 24, 49152)]
+SKINNY = [(1, 8, 32), (2, 136, 96), (3, 4608, 1024), (16, 128, 2048), (5, 264, 4352), (7, 1000, 6176), (13, 40, 12288), (1, 20000, 544), (16, 256, 24608), (4, 24, 49152),
+          (1, 20000, 4608), (2, 28000, 9216), (3, 19008, 3488), (9, 30000, 2560), (16, 27656, 4384), (11, 8, 65536)]
 
 
 @pytest.mark.gpu
@@ -366,14 +367,30 @@ def test_linear_few_tokens(m, n, k):
     """Every way the few-token kernel cuts K (1 to 8 parts), odd numbers of k-blocks, ragged edges; bf16 and codes agree."""
     a, w, bias = operands(m, n, k)
     qw, sw = w8.mxfp4_quantize(w)
-    ws = w8.mxfp4_alloc_workspace(m, n, k)
-    out = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
-    assert w8.int8_check_status(ws) == 0
-    check_linear(out, a, w, bias)
     codes, scales = w8.mxfp4_quantize(a)
-    for _ in range(5):
-        assert torch.equal(w8.mxfp4_linear_fused(codes, qw, sw, bias, a_scales=scales, workspace=ws), out)
-        assert torch.equal(w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws), out)
+    ws = w8.mxfp4_alloc_workspace(m, n, k)
+    w8.mxfp4_force_config(w8.MXFP4_NUM_CONFIGS)
+    try:
+        out = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
+        assert w8.int8_check_status(ws) == 0
+        check_linear(out, a, w, bias)
+        for _ in range(5):
+            assert torch.equal(w8.mxfp4_linear_fused(codes, qw, sw, bias, a_scales=scales, workspace=ws), out)
+            assert torch.equal(w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws), out)
+    finally:
+        w8.mxfp4_force_config(-1)
+
+
+@pytest.mark.gpu
+def test_linear_few_tokens_refuses_many():
+    a, w, bias = operands(17, 64, 64)
+    qw, sw = w8.mxfp4_quantize(w)
+    w8.mxfp4_force_config(w8.MXFP4_NUM_CONFIGS)
+    try:
+        with pytest.raises(w8.W8A8Error):
+            w8.mxfp4_linear_fused(a, qw, sw, bias)
+    finally:
+        w8.mxfp4_force_config(-1)
 
 
 @pytest.mark.gpu
