@@ -10,7 +10,7 @@
  *     KV_CACHE_MXFP4  codes uint8 [slots, heads, dim / 2]  scales uint8 [slots, heads, ceil(dim / 32)]
  *                     the MXFP4 format of mxfp4_linear.h in blocks of 32 along dim (the last may be shorter)
  * A head vector (int8) or block (MXFP4) that holds an Inf or a NaN gets a NaN scale and codes 0 and reads back as NaN.
- * dim % 8 == 0, dim <= KV_CACHE_MAX_DIM. Codes, inputs and outputs 16-byte aligned; token and head strides in elements,
+ * dim % 8 == 0, dim <= KV_CACHE_MAX_DIM, heads * dim <= KV_CACHE_MAX_WIDTH. Codes, inputs and outputs 16-byte aligned; token and head strides in elements,
  * multiples of 8 (inputs may be slices of a fused projection); a head's elements are contiguous. A NULL v (write) or
  * v_out (read) leaves the value side out, for caches that keep one vector a head.
  */
@@ -25,6 +25,7 @@ extern "C" {
 
 enum { KV_CACHE_INT8 = 0, KV_CACHE_MXFP4 = 1 };
 #define KV_CACHE_MAX_DIM 256
+#define KV_CACHE_MAX_WIDTH 65536 /* heads * dim */
 
 /*
  * Quantizes `tokens` tokens into their slots. slots: int64 [tokens], device; one outside [0, num_slots) is skipped (-1 for

@@ -32,6 +32,22 @@ private:
     cudaError_t err_[kMaxDevices] = {};
 };
 
+// A launch with programmatic dependent launch: the kernel may be set up while the one ahead of it on the stream is finishing
+// (it waits for that kernel before it touches what that kernel may write).
+template <typename... P, typename... A>
+cudaError_t launch_pdl(void (*kern)(P...), dim3 grid, int threads, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, P(args)...);
+}
+
 // SM count of the current device (148 if no device can be queried, so that host-only planning still works).
 inline int sm_count() {
     static std::mutex mutex;

@@ -2,9 +2,10 @@
 // Both move bytes and compute next to nothing (a conversion and a multiply an element): HBM is the bound, 2.53 bytes an
 // element for bf16, 4.53 for fp32.
 //
-// A lane holds 8 consecutive elements of a row (16 bytes of bf16), four neighbouring lanes one block of 32, a warp one
-// segment of 256 elements: loads and stores are contiguous across the warp, the block's maximum takes two shuffles, and
-// a segment's eight scale bytes leave as two 4-byte words (one for each tile of four blocks that the segment crosses).
+// A lane holds 16 consecutive elements of a row, two neighbouring lanes one block of 32, a warp one segment of 512: codes
+// leave as 8 bytes a lane, the block's maximum takes one shuffle, and a segment's 16 scale bytes leave as four 4-byte
+// words (one for each tile of four blocks that the segment crosses). Where the rows allow it a lane moves 32 bytes at
+// a time, so that every memory sector is touched by one instruction.
 #include "internal.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"
@@ -13,151 +14,210 @@ namespace w8a8 {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kSegment = 256;        // elements of a row a warp takes at a time
-constexpr int kUnroll = 4;           // segments whose loads are in flight together
+constexpr int kLane = 16;            // elements a lane takes at a time
+constexpr int kSegment = 32 * kLane;
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8], uint32_t& amax) {
-    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p));
-    amax = absmax_bits8(v);
-    unpack_bf16x8(v, x);
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8], uint32_t& amax) {
-    const float4 a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    amax = 0;
+// N 16-byte words at p: WIDE = p is 32-byte aligned. Coherent loads past L1: the kernel may be resident while the one ahead writes.
+template <int N, bool WIDE>
+__device__ __forceinline__ void load_words(const void* p, uint32_t (&r)[4 * N]) {
+    if (WIDE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
+        for (int i = 0; i < N / 2; ++i) ldcg_32(static_cast<const uint8_t*>(p) + 32 * i, r + 8 * i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint4 v = __ldcg(static_cast<const uint4*>(p) + i);
+            r[4 * i] = v.x; r[4 * i + 1] = v.y; r[4 * i + 2] = v.z; r[4 * i + 3] = v.w;
+        }
+    }
+}
+template <int N, bool WIDE>
+__device__ __forceinline__ void store_words(void* p, const uint32_t (&r)[4 * N]) {
+    if (WIDE) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) st_32(static_cast<uint8_t*>(p) + 32 * i, r + 8 * i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) static_cast<uint4*>(p)[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+    }
 }
 
-// Work: tasks of kUnroll segments of one row, row by row; rows up to the end of the last scale tile (rows past M get
-// zero scales, so that a scale tensor's contents depend on nothing but x).
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32)
-mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                   int tasks_per_row, int64_t num_tasks, int* status_to_clear, int early) {
+// bit pattern of the largest magnitude of 16 elements, as binary32
+__device__ __forceinline__ uint32_t absmax_bits(const uint32_t (&r)[8]) {
+    uint32_t m = r[0] & 0x7fff7fffu;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = __vmaxu2(m, r[i] & 0x7fff7fffu);
+    return max(m >> 16, m & 0xffffu) << 16;
+}
+__device__ __forceinline__ uint32_t absmax_bits(const uint32_t (&r)[16]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, r[i] & 0x7fffffffu);
+    return m;
+}
+__device__ __forceinline__ float element(const uint32_t (&r)[8], int i) { return __uint_as_float((i & 1) ? r[i / 2] & 0xffff0000u : r[i / 2] << 16); }
+__device__ __forceinline__ float element(const uint32_t (&r)[16], int i) { return __uint_as_float(r[i]); }
+
+// Segment number to row and segment of the row; 32-bit division wherever the numbers allow it.
+__device__ __forceinline__ void split_segment(int64_t seg, int per_row, int& row, int& s) {
+    if (seg <= 0xffffffffll) {
+        row = static_cast<int>(static_cast<uint32_t>(seg) / static_cast<uint32_t>(per_row));
+    } else {
+        row = static_cast<int>(seg / per_row);
+    }
+    s = static_cast<int>(seg - static_cast<int64_t>(row) * per_row);
+}
+
+// A warp takes U consecutive segments at a time (rows one after another). Rows go up to the end of the last scale tile: rows past
+// M get zero scales, so that a scale tensor's contents depend on nothing but x.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kWarps * 32, 4)
+mx_quantize_kernel(const T* x, int64_t ldx, int M, int K, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int per_row, int64_t num_segs,
+                   int* status_to_clear, int early) {
+    constexpr int WORDS = kLane * sizeof(T) / 4, U = sizeof(T) == 2 ? 4 : 2;
     if (early) grid_dep_launch_dependents();
     grid_dep_wait();
     if (status_to_clear != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *status_to_clear = 0;
     const int lane = threadIdx.x & 31;
     const int ktiles = (K + kScaleTileBlocks * kMxBlock - 1) / (kScaleTileBlocks * kMxBlock);
-    for (int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); task < num_tasks;
-         task += static_cast<int64_t>(gridDim.x) * kWarps) {
-        const int row = static_cast<int>(task / tasks_per_row);
-        const int k0 = static_cast<int>(task - static_cast<int64_t>(row) * tasks_per_row) * (kUnroll * kSegment) + lane * 8;
-        float v[kUnroll][8];
-        uint32_t amax[kUnroll];
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * U;
+    for (int64_t seg = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * U; seg < num_segs; seg += step) {
+        uint32_t r[U][WORDS];
+        int row[U], k[U];
+        int rw, s;
+        split_segment(seg, per_row, rw, s);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int k = k0 + u * kSegment;
-            if (row < M && k < K) {
-                load8(x + row * ldx + k, v[u], amax[u]);
+        for (int u = 0; u < U; ++u) {
+            row[u] = rw;
+            k[u] = s * kSegment + lane * kLane;
+            if (seg + u < num_segs && rw < M && k[u] < K) {
+                load_words<WORDS / 4, WIDE>(x + rw * ldx + k[u], r[u]);
             } else {
-                amax[u] = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+                for (int i = 0; i < WORDS; ++i) r[u][i] = 0;
             }
+            if (++s == per_row) { s = 0; ++rw; }
         }
-        uint8_t* tile_row = scales + static_cast<int64_t>(row / kScaleTileRows) * ktiles * kScaleTileBytes + scale_in_tile(row % kScaleTileRows, 0);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int k = k0 + u * kSegment;
-            uint32_t m = amax[u];
+        for (int u = 0; u < U; ++u) {
+            uint32_t m = absmax_bits(r[u]);
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
             const uint32_t byte = mx_scale_byte(m);
-            if (row < M && k < K) *reinterpret_cast<uint32_t*>(codes + static_cast<int64_t>(row) * (K / 2) + k / 2) = mx_codes8(v[u], byte);
-            // the four blocks of a tile sit in 16 lanes: two shuffles bring their bytes into one word
-            uint32_t word = byte << (((lane >> 2) & 3) * 8);
+            const float inv = byte == 255u ? 0.f : mx_inverse_scale(byte);
+            uint2 c = make_uint2(0, 0);
+            if (byte != 255u) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = element(r[u], i) * inv;
+                c.x = e2m1x8(y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = element(r[u], 8 + i) * inv;
+                c.y = e2m1x8(y);
+            }
+            // the four blocks of a tile sit in 8 lanes: two shuffles bring their bytes into one word
+            uint32_t word = byte << (((lane >> 1) & 3) * 8);
+            word |= __shfl_xor_sync(0xffffffffu, word, 2);
             word |= __shfl_xor_sync(0xffffffffu, word, 4);
-            word |= __shfl_xor_sync(0xffffffffu, word, 8);
-            const int kt = k / (kScaleTileBlocks * kMxBlock);
-            if ((lane & 15) == 0 && kt < ktiles) *reinterpret_cast<uint32_t*>(tile_row + static_cast<int64_t>(kt) * kScaleTileBytes) = word;
+            if (seg + u < num_segs) {
+                if (row[u] < M && k[u] < K) *reinterpret_cast<uint2*>(codes + static_cast<int64_t>(row[u]) * (K / 2) + k[u] / 2) = c;
+                const int kt = k[u] / (kScaleTileBlocks * kMxBlock);
+                if ((lane & 7) == 0 && kt < ktiles)
+                    *reinterpret_cast<uint32_t*>(scales + (static_cast<int64_t>(row[u] / kScaleTileRows) * ktiles + kt) * kScaleTileBytes +
+                                                 scale_in_tile(row[u] % kScaleTileRows, 0)) = word;
+            }
         }
     }
 }
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const uint4& v) { *reinterpret_cast<uint4*>(p) = v; }
-__device__ __forceinline__ void store8(float* p, const uint4& v) {
-    float f[8];
-    unpack_bf16x8(v, f);
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32)
-mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int M, int K, T* __restrict__ out, int64_t ldo,
-                     int tasks_per_row, int64_t num_tasks) {
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kWarps * 32, 4)
+mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int M, int K, T* __restrict__ out, int64_t ldo, int per_row, int64_t num_segs) {
+    constexpr int U = 4;
     grid_dep_wait();
     const int lane = threadIdx.x & 31;
     const int ktiles = (K + kScaleTileBlocks * kMxBlock - 1) / (kScaleTileBlocks * kMxBlock);
-    for (int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); task < num_tasks;
-         task += static_cast<int64_t>(gridDim.x) * kWarps) {
-        const int row = static_cast<int>(task / tasks_per_row);
-        const int k0 = static_cast<int>(task - static_cast<int64_t>(row) * tasks_per_row) * (kUnroll * kSegment) + lane * 8;
-        const uint8_t* tile_row = scales + static_cast<int64_t>(row / kScaleTileRows) * ktiles * kScaleTileBytes + scale_in_tile(row % kScaleTileRows, 0);
-        uint32_t c[kUnroll], s[kUnroll];
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * U;
+    for (int64_t seg = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * U; seg < num_segs; seg += step) {
+        uint2 c[U];
+        uint32_t b[U];
+        int row[U], k[U];
+        int rw, s;
+        split_segment(seg, per_row, rw, s);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int k = k0 + u * kSegment, b = k / kMxBlock;
-            c[u] = s[u] = 0;
-            if (k < K) {
-                c[u] = __ldcg(reinterpret_cast<const uint32_t*>(codes + static_cast<int64_t>(row) * (K / 2) + k / 2));
-                s[u] = __ldcg(tile_row + static_cast<int64_t>(b / kScaleTileBlocks) * kScaleTileBytes + b % kScaleTileBlocks);
+        for (int u = 0; u < U; ++u) {
+            row[u] = rw;
+            k[u] = s * kSegment + lane * kLane;
+            c[u] = make_uint2(0, 0);
+            b[u] = 0;
+            if (rw < M && k[u] < K) {
+                const int block = k[u] / kMxBlock;
+                c[u] = __ldcg(reinterpret_cast<const uint2*>(codes + static_cast<int64_t>(rw) * (K / 2) + k[u] / 2));
+                b[u] = __ldcg(scales + (static_cast<int64_t>(rw / kScaleTileRows) * ktiles + block / kScaleTileBlocks) * kScaleTileBytes +
+                              scale_in_tile(rw % kScaleTileRows, block % kScaleTileBlocks));
             }
+            if (++s == per_row) { s = 0; ++rw; }
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int k = k0 + u * kSegment;
-            if (k < K) store8(out + row * ldo + k, mx_values8(c[u], s[u]));
+        for (int u = 0; u < U; ++u) {
+            if (row[u] < M && k[u] < K) {
+                const uint4 lo = mx_values8(c[u].x, b[u]), hi = mx_values8(c[u].y, b[u]);
+                const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                T* p = out + row[u] * ldo + k[u];
+                if (sizeof(T) == 2) {
+                    store_words<2, WIDE>(p, v);
+                } else {
+                    uint32_t f[16];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        f[2 * i] = v[i] << 16;
+                        f[2 * i + 1] = v[i] & 0xffff0000u;
+                    }
+                    store_words<4, WIDE>(p, f);
+                }
+            }
         }
     }
 }
 
-// Launched so that it may be set up while the kernel ahead of it on the stream is finishing; it waits for that kernel
-// before it touches global memory.
-template <typename... P, typename... A>
-cudaError_t launch_pdl(void (*kern)(P...), int grid, int threads, cudaStream_t st, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, P(args)...);
+int grid_for(int64_t num_segs, int per_warp) {
+    const int64_t ctas = (num_segs + kWarps * per_warp - 1) / (kWarps * per_warp), most = static_cast<int64_t>(sm_count()) * 8;
+    return static_cast<int>(ctas < most ? ctas : most);
 }
 
-int grid_for(int64_t num_tasks) {
-    const int64_t ctas = (num_tasks + kWarps - 1) / kWarps, most = static_cast<int64_t>(sm_count()) * 8;
-    return static_cast<int>(ctas < most ? ctas : most);
+bool aligned32(const void* p, int64_t row_bytes) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(row_bytes)) & 31u) == 0; }
+
+template <typename T, bool WIDE>
+cudaError_t quantize(const void* x, int64_t ldx, int M, int K, uint8_t* codes, uint8_t* scales, int* status_to_clear, bool early, cudaStream_t st) {
+    const int per_row = (K + kSegment - 1) / kSegment;
+    const int64_t rows = (static_cast<int64_t>(M) + kScaleTileRows - 1) / kScaleTileRows * kScaleTileRows, segs = rows * per_row;
+    return launch_pdl(mx_quantize_kernel<T, WIDE>, dim3(grid_for(segs, sizeof(T) == 2 ? 4 : 2)), kWarps * 32, st, static_cast<const T*>(x), ldx, M, K,
+                      codes, scales, per_row, segs, status_to_clear, early ? 1 : 0);
+}
+template <typename T, bool WIDE>
+cudaError_t dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, int64_t ldo, cudaStream_t st) {
+    const int per_row = (K + kSegment - 1) / kSegment;
+    const int64_t segs = static_cast<int64_t>(M) * per_row;
+    return launch_pdl(mx_dequantize_kernel<T, WIDE>, dim3(grid_for(segs, 4)), kWarps * 32, st, codes, scales, M, K, static_cast<T*>(out), ldo, per_row, segs);
 }
 
 } // namespace
 
 cudaError_t launch_mx_quantize(const void* x, bool fp32, int64_t ldx, int M, int K, uint8_t* codes, uint8_t* scales, int* status_to_clear,
                                bool early, cudaStream_t st) {
-    const int tasks_per_row = (K + kUnroll * kSegment - 1) / (kUnroll * kSegment);
-    const int64_t rows = (static_cast<int64_t>(M) + kScaleTileRows - 1) / kScaleTileRows * kScaleTileRows;
-    const int64_t tasks = rows * tasks_per_row;
+    const bool wide = aligned32(x, ldx * (fp32 ? 4 : 2));
     if (fp32)
-        return launch_pdl(mx_quantize_kernel<float>, grid_for(tasks), kWarps * 32, st, static_cast<const float*>(x), ldx, M, K, codes, scales,
-                          tasks_per_row, tasks, status_to_clear, early ? 1 : 0);
-    return launch_pdl(mx_quantize_kernel<__nv_bfloat16>, grid_for(tasks), kWarps * 32, st, static_cast<const __nv_bfloat16*>(x), ldx, M, K, codes,
-                      scales, tasks_per_row, tasks, status_to_clear, early ? 1 : 0);
+        return wide ? quantize<float, true>(x, ldx, M, K, codes, scales, status_to_clear, early, st)
+                    : quantize<float, false>(x, ldx, M, K, codes, scales, status_to_clear, early, st);
+    return wide ? quantize<__nv_bfloat16, true>(x, ldx, M, K, codes, scales, status_to_clear, early, st)
+                : quantize<__nv_bfloat16, false>(x, ldx, M, K, codes, scales, status_to_clear, early, st);
 }
 
 cudaError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, bool fp32, int64_t ldo, cudaStream_t st) {
-    const int tasks_per_row = (K + kUnroll * kSegment - 1) / (kUnroll * kSegment);
-    const int64_t tasks = static_cast<int64_t>(M) * tasks_per_row;
+    const bool wide = aligned32(out, ldo * (fp32 ? 4 : 2));
     if (fp32)
-        return launch_pdl(mx_dequantize_kernel<float>, grid_for(tasks), kWarps * 32, st, codes, scales, M, K, static_cast<float*>(out), ldo,
-                          tasks_per_row, tasks);
-    return launch_pdl(mx_dequantize_kernel<__nv_bfloat16>, grid_for(tasks), kWarps * 32, st, codes, scales, M, K,
-                      static_cast<__nv_bfloat16*>(out), ldo, tasks_per_row, tasks);
+        return wide ? dequantize<float, true>(codes, scales, M, K, out, ldo, st) : dequantize<float, false>(codes, scales, M, K, out, ldo, st);
+    return wide ? dequantize<__nv_bfloat16, true>(codes, scales, M, K, out, ldo, st)
+                : dequantize<__nv_bfloat16, false>(codes, scales, M, K, out, ldo, st);
 }
 
 } // namespace w8a8

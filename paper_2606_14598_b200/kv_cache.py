@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from .binding import _i64, _int, _lib, _vp
-from .mxfp4 import call, same_device
+from .mxfp4 import call, different_devices
 
 KV_CACHE_INT8, KV_CACHE_MXFP4 = 0, 1
 KV_CACHE_MAX_DIM = 256
@@ -45,8 +45,16 @@ class QuantKVCache:
                 raise ValueError(f"{name}_codes: dense {k_codes.dtype} {tuple(k_codes.shape)} expected")
             if scales.dtype != dtype or tuple(scales.shape) != shape or not scales.is_contiguous():
                 raise ValueError(f"{name}_scales: dense {dtype} {shape} expected")
-        same_device("QuantKVCache", k_codes, k_scales, v_codes, v_scales)
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.device, self.device_index = k_codes.device, k_codes.get_device()
+        if any(t is not None and t.get_device() != self.device_index for t in (k_scales, v_codes, v_scales)):
+            raise different_devices("QuantKVCache")
+        self._tensors = (k_codes, k_scales, v_codes, v_scales)           # held for as long as the cache is, and not replaced
+        self._places = tuple(None if t is None else t.data_ptr() for t in self._tensors)
+
+    k_codes = property(lambda self: self._tensors[0])
+    k_scales = property(lambda self: self._tensors[1])
+    v_codes = property(lambda self: self._tensors[2])
+    v_scales = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, num_pages: int, page_size: int, heads: int, dim: int, fmt: str = "int8", device="cuda", values: bool = True) -> "QuantKVCache":
@@ -64,64 +72,75 @@ class QuantKVCache:
         return cls(*side(), *(side() if values else (None, None)))
 
 
-def _need_vectors(cache: QuantKVCache, t: torch.Tensor, name: str, rows: int) -> None:
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1:
-        raise TypeError(f"{name}: bf16 [tokens, heads, dim] with contiguous heads expected, got {t.dtype} {tuple(t.shape)}")
-    if t.shape[0] != rows or t.shape[1] != cache.heads or t.shape[2] != cache.dim:
+def _vectors(cache: QuantKVCache, t: torch.Tensor, name: str, rows: int) -> tuple[int, int, int]:
+    """Checks bf16 [rows, heads, dim] with contiguous heads on the cache's device; returns (pointer, token stride, head stride)."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 3:
+        raise TypeError(f"{name}: bf16 [tokens, heads, dim] expected, got {t.dtype} {tuple(t.shape)}")
+    if t.shape != (rows, cache.heads, cache.dim):
         raise ValueError(f"{name}: [{rows}, {cache.heads}, {cache.dim}] expected, got {tuple(t.shape)}")
+    st, sh, one = t.stride()
+    if one != 1:
+        raise TypeError(f"{name}: heads must be contiguous")
+    if t.get_device() != cache.device_index:
+        raise different_devices(name)
+    return t.data_ptr(), st if rows > 1 else 0, sh if cache.heads > 1 else 0
 
 
 def kv_cache_write(cache: QuantKVCache, k: torch.Tensor, v: torch.Tensor | None, slots: torch.Tensor) -> None:
     """Quantizes k (and v) bf16 [T, heads, dim] into the cache at slots int64 [T]; slots outside the cache are skipped."""
-    if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
+    c = cache
+    if slots.dtype is not torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
         raise TypeError("slots: dense int64 [tokens] expected")
     tokens = slots.shape[0]
-    _need_vectors(cache, k, "k", tokens)
-    if (v is None) != (cache.v_codes is None):
+    kp, kt, kh = _vectors(c, k, "k", tokens)
+    kc, ks, vc, vs = c._places
+    if (v is None) != (vc is None):
         raise ValueError("v goes with a cache that keeps values, and only with one")
-    if v is not None:
-        _need_vectors(cache, v, "v", tokens)
-    same_device("kv_cache_write", cache.k_codes, k, v, slots)
+    vp, vt, vh = (None, 0, 0) if v is None else _vectors(c, v, "v", tokens)
+    if slots.get_device() != c.device_index:
+        raise different_devices("kv_cache_write")
     if tokens == 0:
         return
-    c = cache
-    call(_lib.kv_cache_write, "kv_cache_write", k, c.fmt, k.data_ptr(), k.stride(0), k.stride(1),
-         None if v is None else v.data_ptr(), 0 if v is None else v.stride(0), 0 if v is None else v.stride(1), slots.data_ptr(), tokens,
-         c.heads, c.dim, c.k_codes.data_ptr(), c.k_scales.data_ptr(), None if v is None else c.v_codes.data_ptr(),
-         None if v is None else c.v_scales.data_ptr(), c.num_pages * c.page_size)
+    call(_lib.kv_cache_write, "kv_cache_write", c.device_index, c.fmt, kp, kt, kh, vp, vt, vh, slots.data_ptr(), tokens, c.heads, c.dim, kc, ks, vc, vs,
+         c.num_pages * c.page_size)
 
 
 def kv_cache_read(cache: QuantKVCache, table: torch.Tensor, cu_seqlens: torch.Tensor, total: int, starts: torch.Tensor | None = None,
                   k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
     """The sequences' tokens as bf16 [total, heads, dim], one sequence after another: (k, v), or (k, None) without values.
     table int32 [B, max_pages], cu_seqlens int32 [B + 1], starts int32 [B] (first token to read of each) or None."""
-    if table.dtype != torch.int32 or table.dim() != 2 or (table.numel() > 0 and table.stride(1) != 1):
-        raise TypeError("table: int32 [sequences, max_pages] with contiguous rows expected")
+    if table.dtype is not torch.int32 or table.dim() != 2:
+        raise TypeError("table: int32 [sequences, max_pages] expected")
     seqs, max_pages = table.shape
-    if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] != seqs + 1 or not cu_seqlens.is_contiguous():
+    row, one = table.stride()
+    if one != 1 and max_pages > 1:
+        raise TypeError("table: rows must be contiguous")
+    if cu_seqlens.dtype is not torch.int32 or cu_seqlens.shape != (seqs + 1,) or not cu_seqlens.is_contiguous():
         raise TypeError("cu_seqlens: dense int32 [sequences + 1] expected")
-    if starts is not None and (starts.dtype != torch.int32 or starts.dim() != 1 or starts.shape[0] != seqs or not starts.is_contiguous()):
+    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (seqs,) or not starts.is_contiguous()):
         raise TypeError("starts: dense int32 [sequences] expected")
     c = cache
-    values = c.v_codes is not None
-    if v_out is not None and not values:
+    kc, ks, vc, vs = c._places
+    dev = c.device_index
+    if v_out is not None and vc is None:
         raise ValueError("v_out goes with a cache that keeps values")
-    shape = (total, c.heads, c.dim)
+    dense = c.heads * c.dim
     if k_out is None:
-        k_out = torch.empty(shape, dtype=torch.bfloat16, device=c.k_codes.device)
+        k_out = torch.empty((total, c.heads, c.dim), dtype=torch.bfloat16, device=c.device)
+        kp, kt, kh = k_out.data_ptr(), dense, c.dim
     else:
-        _need_vectors(c, k_out, "k_out", total)
-    if values:
-        if v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=c.k_codes.device)
-        else:
-            _need_vectors(c, v_out, "v_out", total)
-    same_device("kv_cache_read", c.k_codes, table, cu_seqlens, starts, k_out, v_out)
+        kp, kt, kh = _vectors(c, k_out, "k_out", total)
+    if vc is None:
+        vp, vt, vh = None, 0, 0
+    elif v_out is None:
+        v_out = torch.empty((total, c.heads, c.dim), dtype=torch.bfloat16, device=c.device)
+        vp, vt, vh = v_out.data_ptr(), dense, c.dim
+    else:
+        vp, vt, vh = _vectors(c, v_out, "v_out", total)
+    if table.get_device() != dev or cu_seqlens.get_device() != dev or (starts is not None and starts.get_device() != dev):
+        raise different_devices("kv_cache_read")
     if total == 0 or seqs == 0:
         return k_out, v_out
-    call(_lib.kv_cache_read, "kv_cache_read", k_out, c.fmt, c.k_codes.data_ptr(), c.k_scales.data_ptr(),
-         c.v_codes.data_ptr() if values else None, c.v_scales.data_ptr() if values else None, c.num_pages, c.page_size, c.heads, c.dim,
-         table.data_ptr(), table.stride(0) if seqs > 1 else max_pages, max_pages, cu_seqlens.data_ptr(), None if starts is None else starts.data_ptr(),
-         seqs, total, k_out.data_ptr(), k_out.stride(0), k_out.stride(1),
-         v_out.data_ptr() if values else None, v_out.stride(0) if values else 0, v_out.stride(1) if values else 0)
+    call(_lib.kv_cache_read, "kv_cache_read", dev, c.fmt, kc, ks, vc, vs, c.num_pages, c.page_size, c.heads, c.dim, table.data_ptr(),
+         row if seqs > 1 else max_pages, max_pages, cu_seqlens.data_ptr(), None if starts is None else starts.data_ptr(), seqs, total, kp, kt, kh, vp, vt, vh)
     return k_out, v_out

@@ -23,6 +23,7 @@ def test_write_refusals():
     for name in ("k", "slots", "kc", "ks", "vc", "vs"):
         assert status(**{name: None}) == INVALID, name
     assert status(fmt=2) == INVALID and status(heads=0) == INVALID and status(dim=0) == INVALID and status(dim=264) == INVALID
+    assert status(heads=1025) == INVALID and status(heads=1 << 40) == INVALID
     assert status(tokens=-1) == INVALID and status(num_slots=-1) == INVALID
     assert status(dim=12) == ALIGNMENT and status(kt=129) == ALIGNMENT and status(kh=60) == ALIGNMENT and status(vt=4) == ALIGNMENT
     for name in ("k", "v", "kc", "vc"):
