@@ -71,10 +71,10 @@ __device__ __forceinline__ void split_segment(int64_t seg, int per_row, int& row
 // A warp takes U consecutive segments at a time (rows one after another). Rows go up to the end of the last scale tile: rows past
 // M get zero scales, so that a scale tensor's contents depend on nothing but x.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kWarps * 32, 4)
+__global__ void __launch_bounds__(kWarps * 32, 6)
 mx_quantize_kernel(const T* x, int64_t ldx, int M, int K, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int per_row, int64_t num_segs,
                    int* status_to_clear, int early) {
-    constexpr int WORDS = kLane * sizeof(T) / 4, U = sizeof(T) == 2 ? 4 : 2;
+    constexpr int WORDS = kLane * sizeof(T) / 4, U = sizeof(T) == 2 ? 2 : 1;
     if (early) grid_dep_launch_dependents();
     grid_dep_wait();
     if (status_to_clear != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *status_to_clear = 0;
@@ -130,9 +130,9 @@ mx_quantize_kernel(const T* x, int64_t ldx, int M, int K, uint8_t* __restrict__ 
 }
 
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kWarps * 32, 4)
+__global__ void __launch_bounds__(kWarps * 32, 6)
 mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int M, int K, T* __restrict__ out, int64_t ldo, int per_row, int64_t num_segs) {
-    constexpr int U = 4;
+    constexpr int U = 2;
     grid_dep_wait();
     const int lane = threadIdx.x & 31;
     const int ktiles = (K + kScaleTileBlocks * kMxBlock - 1) / (kScaleTileBlocks * kMxBlock);
@@ -179,8 +179,10 @@ mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int M, int K, 
     }
 }
 
+// One task a warp up to 64 CTAs an SM. (With twice the bytes a warp and CTAs that walk over the rest, 8 an SM: 25.1 against 24.2 us to
+// quantize 4110 x 12288 bf16, 47.9 against 42.3 us for 13824 x 4608 fp32, 2.5 against 1.9 us for 77 x 4608.)
 int grid_for(int64_t num_segs, int per_warp) {
-    const int64_t ctas = (num_segs + kWarps * per_warp - 1) / (kWarps * per_warp), most = static_cast<int64_t>(sm_count()) * 8;
+    const int64_t ctas = (num_segs + kWarps * per_warp - 1) / (kWarps * per_warp), most = static_cast<int64_t>(sm_count()) * 64;
     return static_cast<int>(ctas < most ? ctas : most);
 }
 
@@ -190,14 +192,14 @@ template <typename T, bool WIDE>
 cudaError_t quantize(const void* x, int64_t ldx, int M, int K, uint8_t* codes, uint8_t* scales, int* status_to_clear, bool early, cudaStream_t st) {
     const int per_row = (K + kSegment - 1) / kSegment;
     const int64_t rows = (static_cast<int64_t>(M) + kScaleTileRows - 1) / kScaleTileRows * kScaleTileRows, segs = rows * per_row;
-    return launch_pdl(mx_quantize_kernel<T, WIDE>, dim3(grid_for(segs, sizeof(T) == 2 ? 4 : 2)), kWarps * 32, st, static_cast<const T*>(x), ldx, M, K,
+    return launch_pdl(mx_quantize_kernel<T, WIDE>, dim3(grid_for(segs, sizeof(T) == 2 ? 2 : 1)), kWarps * 32, st, static_cast<const T*>(x), ldx, M, K,
                       codes, scales, per_row, segs, status_to_clear, early ? 1 : 0);
 }
 template <typename T, bool WIDE>
 cudaError_t dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, int64_t ldo, cudaStream_t st) {
     const int per_row = (K + kSegment - 1) / kSegment;
     const int64_t segs = static_cast<int64_t>(M) * per_row;
-    return launch_pdl(mx_dequantize_kernel<T, WIDE>, dim3(grid_for(segs, 4)), kWarps * 32, st, codes, scales, M, K, static_cast<T*>(out), ldo, per_row, segs);
+    return launch_pdl(mx_dequantize_kernel<T, WIDE>, dim3(grid_for(segs, 2)), kWarps * 32, st, codes, scales, M, K, static_cast<T*>(out), ldo, per_row, segs);
 }
 
 } // namespace

@@ -14,9 +14,9 @@ from __future__ import annotations
 
 import torch
 
-from . import binding
+from . import binding, mxfp4
 
-__all__ = ["linear_fused", "W8A8Linear"]
+__all__ = ["linear_fused", "W8A8Linear", "mxfp4_linear", "MXFP4Linear"]
 
 
 @torch.library.custom_op("w8a8_b200::linear_fused", mutates_args=())
@@ -61,3 +61,42 @@ class W8A8Linear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         return linear_fused(x, self.qw, self.s_ch, self.bias)
+
+
+@torch.library.custom_op("w8a8_b200::mxfp4_linear", mutates_args=())
+def mxfp4_linear(A: torch.Tensor, qw: torch.Tensor, sw: torch.Tensor, bias: torch.Tensor | None) -> torch.Tensor:
+    """bf16 [..., K] activations x MXFP4 weights (codes [N, K/2], scale tiles) -> bf16 [..., N]."""
+    lead = A.shape[:-1]
+    A2 = A.reshape(-1, A.shape[-1])
+    if A2.stride(-1) != 1:
+        A2 = A2.contiguous()
+    if A2.shape[0] == 0:
+        return A.new_empty((*lead, qw.shape[0]), dtype=torch.bfloat16)
+    return mxfp4.mxfp4_linear_fused(A2, qw, sw, bias).reshape(*lead, qw.shape[0])
+
+
+@mxfp4_linear.register_fake
+def _mxfp4_linear_fake(A, qw, sw, bias):
+    torch._check(A.dtype == torch.bfloat16, lambda: "activations must be bf16")
+    torch._check(qw.dtype == torch.uint8 and qw.dim() == 2, lambda: "weights must be uint8 codes [N, K/2]")
+    torch._check(A.shape[-1] == 2 * qw.shape[1], lambda: "K mismatch")
+    return A.new_empty((*A.shape[:-1], qw.shape[0]), dtype=torch.bfloat16)
+
+
+class MXFP4Linear(torch.nn.Module):
+    """The 4-bit counterpart of W8A8Linear: weights are quantized to MXFP4 once, activations on every call."""
+
+    def __init__(self, qw: torch.Tensor, sw: torch.Tensor, bias: torch.Tensor | None = None):
+        super().__init__()
+        self.register_buffer("qw", qw)
+        self.register_buffer("sw", sw)
+        self.register_buffer("bias", bias)
+
+    @classmethod
+    def from_float(cls, weight: torch.Tensor, bias: torch.Tensor | None = None) -> "MXFP4Linear":
+        """weight: [N, K] on the CUDA device; bias: [N] or None."""
+        qw, sw = mxfp4.mxfp4_quantize(weight.detach().float().contiguous())
+        return cls(qw, sw, None if bias is None else bias.detach().float().contiguous())
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return mxfp4_linear(x, self.qw, self.sw, self.bias)

@@ -420,3 +420,44 @@ def test_linear_random_shapes():
         a, w, bias = operands(m, n, k, seed=r.randint(0, 999))
         qw, sw = w8.mxfp4_quantize(w)
         check_linear(w8.mxfp4_linear_fused(a, qw, sw, bias), a, w, bias)
+
+
+# ------------------------------------------------------------------------------------------ operator, module, example
+
+def test_operator_traces_without_a_gpu():
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    from paper_2606_14598_b200 import torch_op
+    with FakeTensorMode():
+        out = torch_op.mxfp4_linear(torch.empty(2, 5, 64, dtype=torch.bfloat16), torch.empty(24, 32, dtype=torch.uint8),
+                                    torch.empty(1, 1, 512, dtype=torch.uint8), None)
+    assert out.shape == (2, 5, 24) and out.dtype == torch.bfloat16
+
+
+@pytest.mark.gpu
+def test_module():
+    from paper_2606_14598_b200.torch_op import MXFP4Linear
+    a, w, bias = operands(70, 136, 96)
+    layer = MXFP4Linear.from_float(w, bias)
+    x = a.view(2, 35, 96)
+    want = w8.mxfp4_linear_fused(a, *w8.mxfp4_quantize(w), bias)
+    assert torch.equal(layer(x).view(70, 136), want)
+    assert torch.equal(layer(x.transpose(0, 1)).transpose(0, 1).reshape(70, 136), want)      # rows in another order, copied
+    assert layer(x[:, :0]).shape == (2, 0, 136)
+    assert torch.equal(torch.compile(layer, fullgraph=True, backend="eager")(x).view(70, 136), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_example_block(fmt):
+    """The example's block stays near its fp32 form. Each MXFP4 matrix is off by about a tenth of its norm (a step of 0.5 to 2 in 6,
+    uniform within a step), a linear by about 0.14 of its output; the residual stream, as large as what the three linears of a step
+    add to it, keeps the result of three steps within a cosine of 0.9."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "mxfp4_block.py")
+    spec = importlib.util.spec_from_file_location("mxfp4_block", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    four, full = module.run(fmt)
+    assert four.shape == full.shape and torch.isfinite(four).all()
+    assert torch.nn.functional.cosine_similarity(four.flatten(), full.flatten(), dim=0) > 0.9
