@@ -366,6 +366,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                         tma_store_2d_hint(&tm_out, base + off, n, m0 + lg * 32, stream_out);
                         bulk_commit_group();
                     }
+                    __syncwarp();                              // (what follows may be a warp-wide load of tensor memory)
                 }
             }
         }
