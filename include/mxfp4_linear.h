@@ -50,7 +50,7 @@ int mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int
 
 /*
  * Device workspace of mxfp4_linear_fused (256-byte aligned, no initialisation; 0 on invalid sizes): a 256-byte status
- * block, then the scale tiles and the codes of the activations. With a_dtype MXFP4_CODES 256 bytes are enough.
+ * block, then scratch for the scale tiles and the codes of the activations. With a_dtype MXFP4_CODES 256 bytes are enough.
  */
 size_t mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
@@ -67,7 +67,9 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
 
 /*
  * For sweeps and tests: the kernel configuration of the following linears of this process. -1 (default) chooses from the
- * sizes; an id outside the list makes mxfp4_linear_fused return W8A8_ERR_INVALID_ARG. Returns the previous value.
+ * sizes; 0, 1, 2 are the tiled GEMM with 256 x 256 and 256 x 192 tiles on CTA pairs and 128 x 128 tiles on single CTAs, 3 the
+ * kernel for at most 64 tokens. Another id, or 3 with more tokens, makes mxfp4_linear_fused return W8A8_ERR_INVALID_ARG.
+ * Returns the previous value.
  */
 int mxfp4_linear_force_config(int config_id);
 

@@ -170,10 +170,12 @@ int choose_mx_config(int M, int N, int K);
 int launch_mx_gemm(const MxLinearArgs& a, int config, cudaStream_t st);
 constexpr int kMxGemmConfigs = 3;
 
-// ---- mxfp4_skinny.cu : at most 16 tokens, one launch. A: bf16 (lda in elements) or, codes, packed codes (lda in bytes) with scale
-// tiles sa; the activations' fields of g are not used. Returns a w8a8_status.
-bool mx_skinny_fits(int M);              // what the kernel can run
-bool mx_skinny_preferred(int M);         // where it is chosen when nothing is forced
-int launch_mx_skinny(const MxLinearArgs& g, const void* A, bool codes, int64_t lda, const uint8_t* sa, cudaStream_t st);
+// ---- mxfp4_skinny.cu : few tokens. Either bf16 activations, quantized in the kernel (lda in elements; the activations' fields of g are
+// not used), or their codes. Return a w8a8_status.
+constexpr int kMxSkinnyMost = 64;         // tokens the kernel takes (up to 16 if it is to quantize them)
+bool mx_skinny_fits(int M);                  // what the kernel can run
+bool mx_skinny_preferred(int M, int K);     // where it is chosen when nothing is forced
+int launch_mx_skinny_bf16(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream_t st);
+int launch_mx_skinny_codes(const MxLinearArgs& g, cudaStream_t st);
 
 } // namespace w8a8

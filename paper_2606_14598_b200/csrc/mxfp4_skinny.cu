@@ -1,14 +1,14 @@
-// MXFP4 linear for a handful of tokens (at most 16), in one launch: activations are quantized where they are used, the
-// weights are streamed once.
+// MXFP4 linear for few tokens (at most 64): the weights are streamed once, K is cut over clusters of CTAs. Up to 8 tokens in one
+// launch, activations quantized where they are used; above that their codes come from a quantizer ahead.
 //
 // The work is reading the weights (N * K * 0.53 bytes); everything is laid out for that stream. The tensor cores take the weights
-// as their first operand (128 output channels = the rows of tcgen05.mma, M = 128) and the tokens as the second (N = 16),
+// as their first operand (128 output channels = the rows of tcgen05.mma, M = 128) and the tokens as the second (N = 16 to 64),
 // so that a CTA streams 128 rows of W through a TMA ring whose first stages are requested before the kernel ahead has
 // finished (weights do not depend on it). K is cut over the CTAs of a cluster until the grid fills two CTAs an SM; the partial
-// sums meet in the first CTA's shared memory and are added in the order of the ranks (the result does not depend on
-// timing). While the weights are on their way the other warps quantize the tokens' k-blocks straight into the swizzled
-// operand tile of the same ring stage. Accumulators are transposed (lane = output channel, column = token): a warp stores 64
-// contiguous bytes a token.
+// sums stay in the shared memory of their CTAs; each CTA reads the others' for its share of the tokens and adds them in the order of
+// the ranks (the result does not depend on timing). While the weights are on their way the other warps quantize the tokens'
+// k-blocks straight into the swizzled operand tile of the same ring stage. Accumulators are transposed (lane = output channel, column = token): they
+// go through shared memory, so that a warp stores 256 contiguous bytes a token.
 #include "../../include/mxfp4_linear.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"
@@ -18,36 +18,41 @@
 namespace w8a8 {
 namespace {
 
-constexpr int NT = 16;                    // tokens
 constexpr int ROWS = 128;                 // output channels of a CTA
 constexpr int BKB = 128;                  // bytes of K per k-block
 constexpr int BK = 2 * BKB;               // elements of K per k-block
 constexpr int MMA_K = 64;
-// Warps: 0 TMA producer, 1 MMA issuer, 2 scale copies, 3 and up quantize (4..7 epilogue). Up to 4 tokens 5 warps quantize, and
-// three CTAs fit an SM; more tokens need 10 (8 x 4608 -> 4608: 9.4 against 10.0 us; 1 x 12288 -> 4608 in 8 parts: 15 against 9.8 us).
-constexpr int kFewTokens = 4;
-template <bool FEW> constexpr int QUANT_WARPS = FEW ? 5 : 10;
-template <bool FEW> constexpr int THREADS = 32 * (3 + QUANT_WARPS<FEW>);
-constexpr int kMaxStages = 5;             // 5 x 20 KB: two CTAs an SM
+constexpr int kMaxStages = 5;
 constexpr int kMaxCluster = 8;
+constexpr int kCrowdTokens = 4;           // up to here three CTAs fit an SM
 constexpr int W_BYTES = ROWS * BKB;
 constexpr int SF_BYTES = 2 * kScaleTileBytes;
-constexpr int ACT_BYTES = NT * BKB;       // codes of 16 tokens, one k-block
-constexpr int OFF_ACT = W_BYTES + SF_BYTES, OFF_ACT_SF = OFF_ACT + ACT_BYTES;      // the tokens' scales in tile layout (rows 0..15 are used)
-constexpr int STAGE_BYTES = OFF_ACT_SF + SF_BYTES;
-constexpr int TMEM_COLS = 128;            // the accumulator, then per stage 8 columns of weight and 8 of token scales
-constexpr int SF_COL = 32;
-// At least this much shared memory keeps a fourth CTA off the SM: three (of this kernel or of the one behind it) always find
-// tensor memory, so no CTA of a cluster waits for columns that another cluster's CTA holds, and a quarter of it stays free.
-constexpr int kLeastSmem = 60 * 1024;
-static_assert(SF_COL + kMaxStages * 16 <= TMEM_COLS, "tensor memory");
+
+// The kernel's variants. NT: tokens the MMA takes. WARPS that quantize bf16 tokens (0: the tokens come as codes, through TMA).
+// CTAS an SM: shared memory of at least a CTA's share keeps further ones off it, so that all CTAs on an SM (of this kernel or of
+// the one behind it) find tensor memory: no CTA of a cluster waits for columns that another cluster's CTA holds, and a
+// quarter of it stays free.
+template <int NT_, int QUANT_WARPS_, int CTAS_>
+struct Variant {
+    static constexpr int NT = NT_, QUANT_WARPS = QUANT_WARPS_, CTAS = CTAS_;
+    static constexpr bool QUANT = QUANT_WARPS > 0;
+    // warps: 0 TMA producer, 1 MMA issuer, 2 scale copies, 3 and up quantize; 4..7 epilogue (one for each quarter of tensor memory)
+    static constexpr int THREADS = 32 * (3 + (QUANT_WARPS > 5 ? QUANT_WARPS : 5));
+    static constexpr int TOKEN_BYTES = NT * BKB;                           // codes of the tokens, one k-block
+    static constexpr int OFF_TOKENS = W_BYTES + SF_BYTES, OFF_TOKEN_SF = OFF_TOKENS + TOKEN_BYTES;       // scales in tile layout
+    static constexpr int STAGE_BYTES = OFF_TOKEN_SF + SF_BYTES;
+    static constexpr int SF_COL = NT < 32 ? 32 : NT;                       // accumulator, then per stage 8 columns of weight and 8 of token scales
+    static constexpr int STAGES = NT <= 32 ? kMaxStages : 4;
+    static constexpr int TMEM_COLS = 128;
+    static constexpr int LEAST_SMEM = (CTAS == 3 ? 60 : 80) * 1024;
+    static_assert(SF_COL + STAGES * 16 <= TMEM_COLS, "tensor memory");
+};
 
 enum Where { W_EMPTY = 1, W_FULL = 2, W_ACTS = 3, W_DONE = 4 };
 
 struct Args {
-    const void* A;                        // bf16 [M,K] (CODES = false) or codes
-    int64_t lda;                          // elements / bytes
-    const uint8_t* sa;                    // scale tiles of codes
+    const void* A;                        // bf16 [M,K] (variants that quantize)
+    int64_t lda;
     const float* bias;
     __nv_bfloat16* out;
     int64_t ldo;
@@ -59,10 +64,11 @@ struct Args {
     int starve;
 };
 
-template <bool CODES, bool FEW>
-__global__ void __launch_bounds__(THREADS<FEW>, FEW ? 3 : 2)
-mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_sw, const Args a) {
-    constexpr int kQuantWarps = QUANT_WARPS<FEW>;
+template <typename V>
+__global__ void __launch_bounds__(V::THREADS, V::CTAS)
+mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_sw, const __grid_constant__ CUtensorMap tm_a,
+                 const __grid_constant__ CUtensorMap tm_sa, const Args a) {
+    constexpr int NT = V::NT;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 1];
     __shared__ uint32_t tmem_holder;
@@ -91,15 +97,16 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
             mbar_init(full_bar(s), 1);
             mbar_init(empty_bar(s), 1);
             mbar_init(scale_bar(s), 1);
-            mbar_init(acts_bar(s), a.M);       // one arrival a token
+            mbar_init(acts_bar(s), a.M);       // (variants that quantize) one arrival a token
         }
         mbar_init(done_bar, 1);
         abort_word = 0;
         fence_mbar_init();
         prefetch_tensormap(&tm_w);
         prefetch_tensormap(&tm_sw);
+        if (!V::QUANT) { prefetch_tensormap(&tm_a); prefetch_tensormap(&tm_sa); }
     }
-    if (warp == 1) { tmem_alloc(smem_u32(&tmem_holder), TMEM_COLS); tmem_relinquish(); }
+    if (warp == 1) { tmem_alloc(smem_u32(&tmem_holder), V::TMEM_COLS); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -110,18 +117,37 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     if (warp == 0) {
         if (lane == 0) {
             const uint64_t once = l2_policy_evict_first();
+            constexpr int BYTES = W_BYTES + SF_BYTES + (V::QUANT ? 0 : V::TOKEN_BYTES + SF_BYTES);
+            auto load_weights = [&](int kb, int stage) {
+                const uint32_t s = base + stage * V::STAGE_BYTES;
+                mbar_arrive_expect_tx(full_bar(stage), BYTES);
+                tma_load_2d_hint(s, &tm_w, full_bar(stage), kb * BKB, n0, once);
+                tma_load_2d_hint(s + W_BYTES, &tm_sw, full_bar(stage), 0, n0 / kScaleTileRows * ktiles + 2 * kb, once);
+            };
+            auto load_tokens = [&](int kb, int stage) {
+                const uint32_t s = base + stage * V::STAGE_BYTES;
+                tma_load_2d(s + V::OFF_TOKENS, &tm_a, full_bar(stage), kb * BKB, 0);
+                tma_load_2d(s + V::OFF_TOKEN_SF, &tm_sa, full_bar(stage), 0, 2 * kb);
+            };
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             bool withhold = a.starve != 0;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (kb - kb0 >= a.stages && !mbar_wait(empty_bar(stage), phase ^ 1u, ctl, W_EMPTY, kStatusTimeout)) break;
+            const int pre = withhold ? 0 : min(a.stages, kb1 - kb0);       // weights that do not wait for the kernel ahead
+            for (int i = 0; i < pre; ++i) load_weights(kb0 + i, i);
+            if (!V::QUANT) {
+                grid_dep_wait();
+                for (int i = 0; i < pre; ++i) load_tokens(kb0 + i, i);
+            }
+            issued = pre;
+            if (pre == a.stages) phase = 1;
+            else stage = pre;
+            for (int kb = kb0 + pre; kb < kb1; ++kb) {
+                if (issued >= a.stages && !mbar_wait(empty_bar(stage), phase ^ 1u, ctl, W_EMPTY, kStatusTimeout)) break;
                 if (withhold) {
                     withhold = false;          // test hook: this stage never arrives; the bounded waits run out
                 } else {
-                    const uint32_t s = base + stage * STAGE_BYTES;
-                    mbar_arrive_expect_tx(full_bar(stage), W_BYTES + SF_BYTES);
-                    tma_load_2d_hint(s, &tm_w, full_bar(stage), kb * BKB, n0, once);
-                    tma_load_2d_hint(s + W_BYTES, &tm_sw, full_bar(stage), 0, n0 / kScaleTileRows * ktiles + 2 * kb, once);
+                    load_weights(kb, stage);
+                    if (!V::QUANT) load_tokens(kb, stage);
                 }
                 if (++stage == a.stages) { stage = 0; phase ^= 1u; }
                 ++issued;
@@ -144,18 +170,18 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
             uint32_t phase = 0;
             for (int kb = kb0; kb < kb1 && ok; ++kb) {
                 // (the stage's columns are free: its bytes were requested after the MMAs that used them had completed)
-                if (!mbar_wait(full_bar(stage), phase, ctl, W_FULL, kStatusTimeout) || !mbar_wait(acts_bar(stage), phase, ctl, W_ACTS, kStatusTimeout)) {
+                if (!mbar_wait(full_bar(stage), phase, ctl, W_FULL, kStatusTimeout) ||
+                    (V::QUANT && !mbar_wait(acts_bar(stage), phase, ctl, W_ACTS, kStatusTimeout))) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t s = base + stage * STAGE_BYTES + W_BYTES, act_sf = base + stage * STAGE_BYTES + OFF_ACT_SF;
-                const uint32_t sf = tmem + SF_COL + stage * 16;
+                const uint32_t s = base + stage * V::STAGE_BYTES, sf = tmem + V::SF_COL + stage * 16;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (h * 2 * MMA_K < a.K - kb * BK) {
-                        tc_cp_scales<1>(sf + 4 * h, make_scale_desc(s + h * kScaleTileBytes));
-                        tc_cp_scales<1>(sf + 8 + 4 * h, make_scale_desc(act_sf + h * kScaleTileBytes));
+                        tc_cp_scales<1>(sf + 4 * h, make_scale_desc(s + W_BYTES + h * kScaleTileBytes));
+                        tc_cp_scales<1>(sf + 8 + 4 * h, make_scale_desc(s + V::OFF_TOKEN_SF + h * kScaleTileBytes));
                     }
                 }
                 tc_commit(scale_bar(stage));
@@ -170,14 +196,16 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
             int stage = 0;
             uint32_t phase = 0;
             for (int kb = kb0; kb < kb1 && ok; ++kb) {
-                if (!mbar_wait(full_bar(stage), phase, ctl, W_FULL, kStatusTimeout) || !mbar_wait(acts_bar(stage), phase, ctl, W_ACTS, kStatusTimeout) ||
+                if (!mbar_wait(full_bar(stage), phase, ctl, W_FULL, kStatusTimeout) ||
+                    (V::QUANT && !mbar_wait(acts_bar(stage), phase, ctl, W_ACTS, kStatusTimeout)) ||
                     !mbar_wait(scale_bar(stage), phase, ctl, W_FULL, kStatusTimeout)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint64_t dw = make_kmajor_sw128_desc(base + stage * STAGE_BYTES), dt = make_kmajor_sw128_desc(base + stage * STAGE_BYTES + OFF_ACT);
-                const uint32_t sf = tmem + SF_COL + stage * 16;
+                const uint32_t s = base + stage * V::STAGE_BYTES;
+                const uint64_t dw = make_kmajor_sw128_desc(s), dt = make_kmajor_sw128_desc(s + V::OFF_TOKENS);
+                const uint32_t sf = tmem + V::SF_COL + stage * 16;
                 const int left = a.K - kb * BK;
 #pragma unroll
                 for (int k = 0; k < BK / MMA_K; ++k) {
@@ -192,165 +220,171 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         }
         __syncwarp();
     } else {
-        // Tokens: a warp takes 256 elements (one k-block) of one token at a time, a lane 8 of them. A warp serves one ring stage,
-        // so that it waits for every use of the stage in turn (an mbarrier's parity cannot tell a use from the one after the
-        // next), and some of the tokens.
+        // every warp that may write global memory waits for the kernel ahead
         grid_dep_wait();
         if (blockIdx.x == 0 && warp == 3 && lane == 0) *a.status = 0;
-        const int stage = (warp - 3) % a.stages, sub = (warp - 3) / a.stages;
-        const int subs = (kQuantWarps - stage + a.stages - 1) / a.stages;       // warps of this stage
-        const int mine = sub < a.M ? (a.M - sub + subs - 1) / subs : 0;         // tokens sub, sub + subs, ...
-        const int blocks = (kb1 - kb0 - stage + a.stages - 1) / a.stages;       // k-blocks of this stage (stages <= k-blocks)
-        const int units = mine * blocks, div = mine > 0 ? mine : 1;
-        auto token_of = [&](int u) { return sub + u % div * subs; };
         bool ok = true;
-        constexpr int U = 4;                               // units whose loads are in flight together
-        for (int u0 = 0; u0 < units && ok; u0 += U) {
-            uint4 x[U];
-            uint32_t word[U];
+        if (V::QUANT && warp < 3 + V::QUANT_WARPS) {
+            // Tokens: a warp takes 256 elements (one k-block) of one token at a time, a lane 8 of them. A warp serves one ring stage,
+            // so that it waits for every use of the stage in turn (an mbarrier's parity cannot tell a use from the one after the
+            // next), and some of the tokens.
+            const int stage = (warp - 3) % a.stages, sub = (warp - 3) / a.stages;
+            const int subs = (V::QUANT_WARPS - stage + a.stages - 1) / a.stages;    // warps of this stage
+            const int mine = sub < a.M ? (a.M - sub + subs - 1) / subs : 0;         // tokens sub, sub + subs, ...
+            const int blocks = (kb1 - kb0 - stage + a.stages - 1) / a.stages;       // k-blocks of this stage (stages <= k-blocks)
+            const int units = mine * blocks, div = mine > 0 ? mine : 1;
+            auto token_of = [&](int u) { return sub + u % div * subs; };
+            constexpr int U = 4;                               // units whose loads are in flight together
+            for (int u0 = 0; u0 < units && ok; u0 += U) {
+                uint4 x[U];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int u = u0 + j, m = token_of(u), kb = kb0 + stage + u / div * a.stages, k = kb * BK + lane * 8;
-                x[j] = make_uint4(0, 0, 0, 0);
-                word[j] = 0;
-                if (u < units && k < a.K) {
-                    if (CODES) {
-                        const int t = kb * 2 + (lane >> 4);
-                        x[j].x = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.A) + m * a.lda + k / 2));
-                        word[j] = __ldcg(reinterpret_cast<const uint32_t*>(a.sa + static_cast<int64_t>(t) * kScaleTileBytes + scale_in_tile(m, 0)));
-                    } else {
-                        x[j] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.A) + m * a.lda + k));
-                    }
+                for (int j = 0; j < U; ++j) {
+                    const int u = u0 + j, m = token_of(u), kb = kb0 + stage + u / div * a.stages, k = kb * BK + lane * 8;
+                    x[j] = make_uint4(0, 0, 0, 0);
+                    if (u < units && k < a.K) x[j] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.A) + m * a.lda + k));
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int u = u0 + j;
-                if (u >= units) break;                     // uniform over the warp
-                const int m = token_of(u), use = u / div;
-                uint32_t codes = x[j].x;
-                if (!CODES) {
+                for (int j = 0; j < U; ++j) {
+                    const int u = u0 + j;
+                    if (u >= units) break;                     // uniform over the warp
+                    const int m = token_of(u), use = u / div;
                     float f[8];
                     unpack_bf16x8(x[j], f);
                     uint32_t top = absmax_bits8(x[j]);
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     const uint32_t byte = mx_scale_byte(top);
-                    codes = mx_codes8(f, byte);
-                    word[j] = byte << (((lane >> 2) & 3) * 8);
-                    word[j] |= __shfl_xor_sync(0xffffffffu, word[j], 4);
-                    word[j] |= __shfl_xor_sync(0xffffffffu, word[j], 8);
+                    const uint32_t codes = mx_codes8(f, byte);
+                    uint32_t word = byte << (((lane >> 2) & 3) * 8);
+                    word |= __shfl_xor_sync(0xffffffffu, word, 4);
+                    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+                    // the stage's previous k-block has been multiplied
+                    if (ok && use > 0 && !mbar_wait(empty_bar(stage), (use - 1) & 1, ctl, W_EMPTY, kStatusTimeout)) ok = false;
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    uint8_t* st = base_ptr + stage * V::STAGE_BYTES;
+                    // row m of the 128-byte-swizzled tile; scales of half of the k-block at row m of their tile
+                    *reinterpret_cast<uint32_t*>(st + V::OFF_TOKENS + m * BKB + (((lane >> 2) ^ (m & 7)) << 4) + (lane & 3) * 4) = codes;
+                    if ((lane & 15) == 0)
+                        *reinterpret_cast<uint32_t*>(st + V::OFF_TOKEN_SF + (lane >> 4) * kScaleTileBytes + scale_in_tile(m, 0)) = word;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acts_bar(stage));
                 }
-                // the stage's previous k-block has been multiplied
-                if (ok && use > 0 && !mbar_wait(empty_bar(stage), (use - 1) & 1, ctl, W_EMPTY, kStatusTimeout)) ok = false;
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                uint8_t* st = base_ptr + stage * STAGE_BYTES;
-                // row m of the 128-byte-swizzled tile; scales of half of the k-block at row m of their tile
-                *reinterpret_cast<uint32_t*>(st + OFF_ACT + m * BKB + (((lane >> 2) ^ (m & 7)) << 4) + (lane & 3) * 4) = codes;
-                if ((lane & 15) == 0)
-                    *reinterpret_cast<uint32_t*>(st + OFF_ACT_SF + (lane >> 4) * kScaleTileBytes + scale_in_tile(m, 0)) = word[j];
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(acts_bar(stage));
             }
+            __syncwarp();
         }
-        // ------------------------------------------------------------ partial sums and epilogue (warps 4..7: all TMEM lanes)
-        float v[NT];
+        // ------------------------------------------------------------ sums to shared memory (warps 4..7: all TMEM lanes)
+        // The CTA's MMAs are done and its copies have landed and been used: the ring is free. [token][channel], fp32.
         if (warp >= 4 && warp < 8) {
             if (ok && !mbar_wait(done_bar, 0, ctl, W_DONE, kStatusTimeout)) ok = false;
             ok = __all_sync(0xffffffffu, ok) != 0;
             if (ok) {
                 tc_fence_after();
                 const uint32_t t_row = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-                uint32_t r[NT];
-                tmem_ld_32x32b_x16(t_row, r);
-                tmem_wait_ld();
+                float* mine = reinterpret_cast<float*>(base_ptr) + (warp & 3) * 32 + lane;
+#pragma unroll 1
+                for (int c = 0; c * 16 < a.M; ++c) {
+                    uint32_t r[16];
+                    tmem_ld_32x32b_x16(t_row + c * 16, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) mine[(c * 16 + j) * ROWS] = __uint_as_float(r[j]);
+                }
                 tc_fence_before();
-#pragma unroll
-                for (int j = 0; j < NT; ++j) v[j] = __uint_as_float(r[j]);
             }
         }
-        // Every CTA of the cluster has done its MMAs, and its copies have landed: the rings are free. The partial sums go into
-        // the first CTA's, and are there after the second barrier.
-        if (split > 1) {
-            __syncwarp();
-            cluster_sync_all();
-            if (warp >= 4 && warp < 8 && ok) {
-                if (rank != 0) {
-                    // into the first CTA's slot for this rank: [token][channel]
-                    const uint32_t dst = mapa_shared(base + (rank - 1) * a.M * ROWS * 4 + ((warp & 3) * 32 + lane) * 4, 0);
-                    for (int j = 0; j < NT; ++j)
-                        if (j < a.M) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + j * ROWS * 4), "f"(v[j]) : "memory");
-                }
-            }
-            __syncwarp();
-            cluster_sync_all();
-        }
-        if (warp >= 4 && warp < 8 && ok && rank == 0) {
-            const int ch = (warp & 3) * 32 + lane, n = n0 + ch;
-            const float* part = reinterpret_cast<const float*>(base_ptr) + ch;
-            const float b = a.bias != nullptr && n < a.N ? __ldcg(a.bias + n) : 0.f;
+        __syncwarp();
+    }
+    if (split > 1) cluster_sync_all();
+    else __syncthreads();
+    // ---------------------------------------------------------------- the cluster's sums added up, bias, bf16
+    // A CTA finishes its share of the tokens: four channels a thread, a token's 128 channels (256 bytes) a warp. (All threads may
+    // write: the warps that have waited for the kernel ahead were at the barrier too.)
+    {
+        const int m_lo = a.M * static_cast<int>(rank) / static_cast<int>(split), m_hi = a.M * static_cast<int>(rank + 1) / static_cast<int>(split);
+        for (int i = threadIdx.x; i < (m_hi - m_lo) * (ROWS / 4); i += V::THREADS) {
+            const int m = m_lo + i / (ROWS / 4), ch = i % (ROWS / 4) * 4, n = n0 + ch;
+            const uint32_t at = base + (m * ROWS + ch) * 4;
+            float4 v[kMaxCluster];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (j < a.M) {
-                    float s = v[j];
-                    for (uint32_t q = 1; q < split; ++q) s += part[((q - 1) * a.M + j) * ROWS];
-                    if (n < a.N) a.out[static_cast<int64_t>(j) * a.ldo + n] = __float2bfloat16_rn(s + b);
+            for (uint32_t q = 0; q < kMaxCluster; ++q)
+                if (q < split) v[q] = ld_cluster_f32x4(mapa_shared(at, q));
+            float4 s = v[0];
+#pragma unroll
+            for (uint32_t q = 1; q < kMaxCluster; ++q)
+                if (q < split) { s.x += v[q].x; s.y += v[q].y; s.z += v[q].z; s.w += v[q].w; }
+            if (n < a.N) {
+                if (a.bias != nullptr) {
+                    const float4 b = __ldcg(reinterpret_cast<const float4*>(a.bias + n));
+                    s.x += b.x; s.y += b.y; s.z += b.z; s.w += b.w;
                 }
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+                *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(m) * a.ldo + n) =
+                    make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
             }
         }
     }
-    if (warp < 3 && split > 1) {
-        cluster_sync_all();
-        cluster_sync_all();
-    }
+    __syncwarp();
+    if (split > 1) cluster_sync_all();          // nobody leaves while its sums may still be read
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
+    if (warp == 1) tmem_dealloc(tmem, V::TMEM_COLS);
 }
 
-// K is cut as long as the grid stays within two CTAs an SM and a part keeps two and a half k-blocks. Clusters of 8 that fill the
-// GPU can only all be placed with three CTAs an SM. (Measured with parts of 1 / 2 / 4 / 8: 1 x 4608 -> 13824, 108 tiles,
-// 12.2 / 9.9 / 14.0 / 18.2 us; 1 x 12288 -> 4608, 36 tiles, 23.2 / 14.3 / 11.0 / 9.8 us.)
-int split_for(int N, int K, bool few) {
-    const int64_t tiles = (static_cast<int64_t>(N) + ROWS - 1) / ROWS, num_kb = (K + BK - 1) / BK;
-    int split = 1;
-    while (split < kMaxCluster && tiles * split * 2 <= (split * 2 == kMaxCluster && !few ? 1 : 2) * sm_count() && num_kb >= 5 * split) split *= 2;
-    return split;
+// K is cut as long as the grid stays within two CTAs an SM and a part keeps two and a half k-blocks. Clusters of 4 and more that fill
+// the GPU beyond one CTA an SM can only all be placed with three CTAs an SM (up to 4 tokens, a ring of three stages).
+// (Measured with parts of 1 / 2 / 4 / 8: 1 x 4608 -> 13824, 108 tiles, 12.2 / 9.9 / 14.0 / 18.2 us; 1 x 12288 -> 4608, 36 tiles,
+// 23.2 / 14.3 / 11.0 / 9.8 us; 50 x 4608 -> 9216, 72 tiles in 4 parts, two CTAs an SM, 15.9 us, the tiled GEMM 13.9.)
+// It goes by the sizes alone, so that tokens that come as codes give the same bits.
+struct Split {
+    int parts;
+    bool crowded;      // needs three CTAs an SM
+};
+Split split_for(int M, int N, int K) {
+    const int64_t tiles = (static_cast<int64_t>(N) + ROWS - 1) / ROWS, num_kb = (K + BK - 1) / BK, sms = sm_count();
+    Split s{1, false};
+    while (s.parts < kMaxCluster && num_kb >= 5 * s.parts) {
+        const int64_t ctas = tiles * s.parts * 2;
+        const bool crowded = s.parts >= 2 && ctas > sms;
+        if (ctas > 2 * sms || (crowded && M > kCrowdTokens)) break;
+        s.parts *= 2;
+        s.crowded = crowded;
+    }
+    return s;
 }
 
-} // namespace
-
-bool mx_skinny_fits(int M) { return M <= NT; }
-// (16 x 4608 -> 13824: 17.4 us here, 16.0 us quantized by a kernel of its own in front of the tiled GEMM; 8 x 4608 -> 4608: 9.4 and 12.9 us)
-bool mx_skinny_preferred(int M) { return M <= 12; }
-
-int launch_mx_skinny(const MxLinearArgs& g, const void* A, bool codes, int64_t lda, const uint8_t* sa, cudaStream_t st) {
-    const bool few = g.M <= kFewTokens;
-    const int split = split_for(g.N, g.K, few), kb_most = ((g.K + BK - 1) / BK + split - 1) / split;
-    const int ring_most = split == kMaxCluster ? 3 : kMaxStages;         // 60 KB: three CTAs an SM
-    const int stages = kb_most < ring_most ? kb_most : ring_most;
-    const int ring = stages * STAGE_BYTES, part = (split - 1) * g.M * ROWS * 4;      // (partial sums come into the ring when it is done)
-    const int most = ring > part ? ring : part, smem = (most > kLeastSmem ? most : kLeastSmem) + 1024;
-    const auto kern = few ? (codes ? mx_skinny_kernel<true, true> : mx_skinny_kernel<false, true>)
-                          : (codes ? mx_skinny_kernel<true, false> : mx_skinny_kernel<false, false>);
-    static PerDeviceOnce opt_in[2][2];
-    constexpr int kMostSmem = kMaxStages * STAGE_BYTES + 1024;
-    static_assert((kMaxCluster - 1) * NT * ROWS * 4 <= kMaxStages * STAGE_BYTES, "the partial sums fit in the largest ring");
-    if (opt_in[few][codes].run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem); }) != cudaSuccess)
-        return W8A8_ERR_CUDA;
-    CUtensorMap tm_w, tm_sw;
+template <typename V>
+int launch_variant(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream_t st) {
+    const Split cut = split_for(g.M, g.N, g.K);
+    const int split = cut.parts, kb_most = ((g.K + BK - 1) / BK + split - 1) / split;
+    int stages = cut.crowded ? 3 : V::STAGES;
+    static_assert(2 * (V::STAGES * V::STAGE_BYTES + 4096) <= 228 * 1024, "two CTAs an SM");
+    if (stages > kb_most) stages = kb_most;
+    int most = stages * V::STAGE_BYTES;                       // (the sums come into the ring when it is done)
+    static_assert(V::NT * ROWS * 4 <= V::LEAST_SMEM, "the sums fit");
+    if (most < V::LEAST_SMEM) most = V::LEAST_SMEM;
+    const auto kern = mx_skinny_kernel<V>;
+    static PerDeviceOnce opt_in;
+    constexpr int MOST_SMEM = (V::STAGES * V::STAGE_BYTES > V::LEAST_SMEM ? V::STAGES * V::STAGE_BYTES : V::LEAST_SMEM) + 1024;
+    if (opt_in.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM); }) != cudaSuccess) return W8A8_ERR_CUDA;
+    CUtensorMap tm_w, tm_sw, tm_a, tm_sa;
     if (!encode_mx_codes(&tm_w, g.qw, g.N, g.K, g.K / 2, ROWS) || !encode_mx_scales(&tm_sw, g.sw, g.N, g.K)) return W8A8_ERR_CUDA;
+    if (V::QUANT) {
+        tm_a = tm_w;      // unused
+        tm_sa = tm_sw;
+    } else if (!encode_mx_codes(&tm_a, g.qa, g.M, g.K, g.ldqa, V::NT) || !encode_mx_scales(&tm_sa, g.sa, g.M, g.K)) {
+        return W8A8_ERR_CUDA;
+    }
     Args a{};
-    a.A = A; a.lda = lda; a.sa = sa; a.bias = g.bias; a.out = static_cast<__nv_bfloat16*>(g.out); a.ldo = g.ldo;
+    a.A = A; a.lda = lda; a.bias = g.bias; a.out = static_cast<__nv_bfloat16*>(g.out); a.ldo = g.ldo;
     a.M = g.M; a.N = g.N; a.K = g.K; a.stages = stages;
     a.status = g.status; a.sticky = sticky_status_word(); a.wait_limit_ns = wait_limit_ns();
     a.starve = starve_mode() == kStarveGemm ? 1 : 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((g.N + ROWS - 1) / ROWS * split);
-    cfg.blockDim = dim3(few ? THREADS<true> : THREADS<false>);
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(V::THREADS);
+    cfg.dynamicSmemBytes = most + 1024;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -361,7 +395,25 @@ int launch_mx_skinny(const MxLinearArgs& g, const void* A, bool codes, int64_t l
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kern, tm_w, tm_sw, a) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kern, tm_w, tm_sw, tm_a, tm_sa, a) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
+}
+
+} // namespace
+
+bool mx_skinny_fits(int M) { return M <= kMxSkinnyMost; }
+// (64 x 4608 -> 4608: 9.7 us against 13.2 in the tiled GEMM, 48 x 1056 -> 2048 7.3 against 7.9, 64 x 512 -> 512 7.7 against 6.2)
+bool mx_skinny_preferred(int M, int K) { return M <= 16 || (M <= kMxSkinnyMost && K > 2 * BK); }
+
+// Up to 4 tokens 5 warps quantize and three CTAs fit an SM; more tokens need 10 warps.
+int launch_mx_skinny_bf16(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream_t st) {
+    return g.M <= kCrowdTokens ? launch_variant<Variant<16, 5, 3>>(g, A, lda, st) : launch_variant<Variant<16, 10, 2>>(g, A, lda, st);
+}
+
+int launch_mx_skinny_codes(const MxLinearArgs& g, cudaStream_t st) {
+    if (g.M <= 16) return launch_variant<Variant<16, 0, 3>>(g, nullptr, 0, st);
+    if (g.M <= 32) return launch_variant<Variant<32, 0, 2>>(g, nullptr, 0, st);
+    if (g.M <= 48) return launch_variant<Variant<48, 0, 2>>(g, nullptr, 0, st);
+    return launch_variant<Variant<64, 0, 2>>(g, nullptr, 0, st);
 }
 
 } // namespace w8a8

@@ -358,7 +358,9 @@ def test_linear_wait_runs_out_and_the_kernel_returns(config):
 
 
 SKINNY = [(1, 8, 32), (2, 136, 96), (3, 4608, 1024), (16, 128, 2048), (5, 264, 4352), (7, 1000, 6176), (13, 40, 12288), (1, 20000, 544), (16, 256, 24608), (4, 24, 49152),
-          (1, 20000, 4608), (2, 28000, 9216), (3, 19008, 3488), (9, 30000, 2560), (16, 27656, 4384), (11, 8, 65536)]
+          (1, 20000, 4608), (2, 28000, 9216), (3, 19008, 3488), (9, 30000, 2560), (16, 27656, 4384), (11, 8, 65536),
+          (17, 264, 2080), (32, 1024, 4608), (33, 136, 12288), (48, 2056, 1312), (49, 4608, 4608), (60, 136, 8224), (64, 1032, 4640), (64, 24, 544),
+          (63, 20000, 800)]
 
 
 @pytest.mark.gpu
@@ -383,7 +385,7 @@ def test_linear_few_tokens(m, n, k):
 
 @pytest.mark.gpu
 def test_linear_few_tokens_refuses_many():
-    a, w, bias = operands(17, 64, 64)
+    a, w, bias = operands(65, 64, 64)
     qw, sw = w8.mxfp4_quantize(w)
     w8.mxfp4_force_config(w8.MXFP4_NUM_CONFIGS)
     try:
@@ -394,10 +396,11 @@ def test_linear_few_tokens_refuses_many():
 
 
 @pytest.mark.gpu
-def test_linear_few_tokens_wait_runs_out():
-    a, w, bias = operands(3, 1032, 4128)
+@pytest.mark.parametrize("m", [3, 9, 30, 60])
+def test_linear_few_tokens_wait_runs_out(m):
+    a, w, bias = operands(m, 1032, 4128)
     qw, sw = w8.mxfp4_quantize(w)
-    ws = w8.mxfp4_alloc_workspace(3, 1032, 4128)
+    ws = w8.mxfp4_alloc_workspace(m, 1032, 4128)
     want = w8.mxfp4_linear_fused(a, qw, sw, bias, workspace=ws)
     try:
         w8.debug_set_wait_limit_ns(3_000_000)
