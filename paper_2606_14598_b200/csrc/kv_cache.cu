@@ -116,10 +116,8 @@ kv_write_kernel(const Side k, const Side v, const int64_t* slots, int64_t num_sl
                         m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                         m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
                         const uint32_t byte = mx_scale_byte(m);
-                        float f[8];
-                        unpack_bf16x8(x[j][q], f);
                         if (store) {
-                            *reinterpret_cast<uint32_t*>(s.codes + slot[j] * token_codes + code_off) = mx_codes8(f, byte);
+                            *reinterpret_cast<uint32_t*>(s.codes + slot[j] * token_codes + code_off) = mx_codes8(x[j][q], byte);
                             if (gl == 0) static_cast<uint8_t*>(s.scales)[slot[j] * token_scales + unit] = static_cast<uint8_t>(byte);
                         }
                     }

@@ -49,27 +49,26 @@ __device__ __forceinline__ uint32_t e2m1x8(const float (&y)[8]) {
     return r;
 }
 
-// Four E2M1 codes (the low 16 bits of c) to four bf16 values: the magnitudes' high and low bytes come from two
-// eight-entry byte tables (a byte permute takes three index bits a nibble), the sign moves from bit 3 of the nibble.
-__device__ __forceinline__ uint2 e2m1x4_to_bf16(uint32_t c) {
-    const uint32_t idx = c & 0x7777u;
-    const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, idx);     // 0 .5 1 1.5 2 3 4 6 as bf16, upper byte
-    const uint32_t lo = __byte_perm(0xc0800000u, 0xc0804000u, idx);     // lower byte
-    uint2 v = make_uint2(__byte_perm(lo, hi, 0x5140), __byte_perm(lo, hi, 0x7362));
-    v.x |= ((c << 12) & 0x8000u) | ((c << 24) & 0x80000000u);
-    v.y |= ((c << 4) & 0x8000u) | ((c << 16) & 0x80000000u);
-    return v;
-}
-// Two bf16 products, each rounded once (exact for a power of two unless it overflows, which no value of the format does)
+// Two bf16 products, each rounded once
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-// Eight codes times 2^e as eight bf16 values
+// Eight codes times 2^e as eight bf16 values. The magnitudes' upper and lower bytes come from two eight-entry byte tables (a byte
+// permute takes three index bits a nibble), the signs from a table of two; the product with a power of two is exact.
 __device__ __forceinline__ uint4 mx_values8(uint32_t codes, uint32_t byte) {
     const uint32_t s1 = mx_scale_bf16(byte), s = s1 | (s1 << 16);
-    const uint2 a = e2m1x4_to_bf16(codes), b = e2m1x4_to_bf16(codes >> 16);
-    return make_uint4(mul_bf16x2(a.x, s), mul_bf16x2(a.y, s), mul_bf16x2(b.x, s), mul_bf16x2(b.y, s));
+    const uint32_t idx = codes & 0x77777777u, sign = (codes >> 3) & 0x11111111u;
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t c = idx >> (16 * i);
+        const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, c) | __byte_perm(0x00008000u, 0u, sign >> (16 * i));     // 0 .5 1 1.5 2 3 4 6
+        const uint32_t lo = __byte_perm(0xc0800000u, 0xc0804000u, c);
+        v[2 * i] = mul_bf16x2(__byte_perm(lo, hi, 0x5140), s);
+        v[2 * i + 1] = mul_bf16x2(__byte_perm(lo, hi, 0x7362), s);
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // Largest |bf16| bit pattern of eight packed values, as an integer: patterns of magnitudes order like the magnitudes,
@@ -87,13 +86,13 @@ __device__ __forceinline__ void unpack_bf16x8(const uint4& v, float (&f)[8]) {
         f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
-// Codes of eight values whose block has this scale byte
-__device__ __forceinline__ uint32_t mx_codes8(const float (&x)[8], uint32_t byte) {
+// Codes of eight bf16 values whose block has this scale byte. The scaling is done in bf16: exact, but for values that land
+// below 2^-126, which round to code 0 all the same.
+__device__ __forceinline__ uint32_t mx_codes8(const uint4& x, uint32_t byte) {
     if (byte == 255u) return 0u;
-    const float inv = mx_inverse_scale(byte);
+    const uint32_t i1 = (254u - byte) << 7, inv = i1 | (i1 << 16);
     float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
+    unpack_bf16x8(make_uint4(mul_bf16x2(x.x, inv), mul_bf16x2(x.y, inv), mul_bf16x2(x.z, inv), mul_bf16x2(x.w, inv)), y);
     return e2m1x8(y);
 }
 

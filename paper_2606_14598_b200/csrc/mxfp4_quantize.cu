@@ -55,8 +55,21 @@ __device__ __forceinline__ uint32_t absmax_bits(const uint32_t (&r)[16]) {
     for (int i = 0; i < 16; ++i) m = max(m, r[i] & 0x7fffffffu);
     return m;
 }
-__device__ __forceinline__ float element(const uint32_t (&r)[8], int i) { return __uint_as_float((i & 1) ? r[i / 2] & 0xffff0000u : r[i / 2] << 16); }
-__device__ __forceinline__ float element(const uint32_t (&r)[16], int i) { return __uint_as_float(r[i]); }
+// codes of 16 elements whose block has this scale byte
+__device__ __forceinline__ uint2 codes_of(const uint32_t (&r)[8], uint32_t byte) {
+    return make_uint2(mx_codes8(make_uint4(r[0], r[1], r[2], r[3]), byte), mx_codes8(make_uint4(r[4], r[5], r[6], r[7]), byte));
+}
+__device__ __forceinline__ uint2 codes_of(const uint32_t (&r)[16], uint32_t byte) {
+    if (byte == 255u) return make_uint2(0, 0);
+    const float inv = mx_inverse_scale(byte);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(r[i]) * inv;
+    const uint32_t lo = e2m1x8(y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(r[8 + i]) * inv;
+    return make_uint2(lo, e2m1x8(y));
+}
 
 // Segment number to row and segment of the row; 32-bit division wherever the numbers allow it.
 __device__ __forceinline__ void split_segment(int64_t seg, int per_row, int& row, int& s) {
@@ -103,17 +116,7 @@ mx_quantize_kernel(const T* x, int64_t ldx, int M, int K, uint8_t* __restrict__ 
             uint32_t m = absmax_bits(r[u]);
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
             const uint32_t byte = mx_scale_byte(m);
-            const float inv = byte == 255u ? 0.f : mx_inverse_scale(byte);
-            uint2 c = make_uint2(0, 0);
-            if (byte != 255u) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = element(r[u], i) * inv;
-                c.x = e2m1x8(y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = element(r[u], 8 + i) * inv;
-                c.y = e2m1x8(y);
-            }
+            const uint2 c = codes_of(r[u], byte);
             // the four blocks of a tile sit in 8 lanes: two shuffles bring their bytes into one word
             uint32_t word = byte << (((lane >> 1) & 3) * 8);
             word |= __shfl_xor_sync(0xffffffffu, word, 2);

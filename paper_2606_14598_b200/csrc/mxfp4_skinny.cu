@@ -248,13 +248,11 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
                     const int u = u0 + j;
                     if (u >= units) break;                     // uniform over the warp
                     const int m = token_of(u), use = u / div;
-                    float f[8];
-                    unpack_bf16x8(x[j], f);
                     uint32_t top = absmax_bits8(x[j]);
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     const uint32_t byte = mx_scale_byte(top);
-                    const uint32_t codes = mx_codes8(f, byte);
+                    const uint32_t codes = mx_codes8(x[j], byte);
                     uint32_t word = byte << (((lane >> 2) & 3) * 8);
                     word |= __shfl_xor_sync(0xffffffffu, word, 4);
                     word |= __shfl_xor_sync(0xffffffffu, word, 8);
