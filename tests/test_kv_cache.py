@@ -159,6 +159,22 @@ def test_write(fmt, tokens, heads, dim, page):
 
 
 @pytest.mark.gpu
+def test_int8_codes_over_many_scales():
+    """16 million elements under 65536 scales from 2^-130 to 2^120, ties of the quotient among them: the codes and scales are those
+    of the fp32 division and quotient, whatever way the kernel takes to them."""
+    g = torch.Generator("cuda").manual_seed(11)
+    x = torch.randn(8192, 8, 256, generator=g, device="cuda") * torch.exp2(torch.randint(-130, 118, (8192, 8, 1), generator=g, device="cuda").float())
+    steps = torch.randint(-254, 255, (512, 8, 256), generator=g, device="cuda") / 2.0       # halves of a step of 1: amax 127, every tie
+    steps[:, :, 0] = 127.0
+    x[:512] = steps * torch.exp2(torch.randint(-100, 100, (512, 8, 1), generator=g, device="cuda").float())
+    x = x.bfloat16()
+    c = w8.QuantKVCache.empty(128, 64, 8, 256, "int8", values=False)
+    w8.kv_cache_write(c, x, None, torch.arange(8192, device="cuda"))
+    q, s = ref.int8_quantize(x)
+    assert torch.equal(c.k_codes.flatten(0, 1), q.to(torch.int8)) and torch.equal(c.k_scales.flatten(0, 1), s.float())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
 @pytest.mark.parametrize("lens,heads,dim,page", [([1], 1, 8, 1), ([0, 1, 0, 17, 33, 0], 2, 64, 16), ([100], 5, 72, 16), ([5, 250, 3], 3, 128, 32),
                                                  ([64, 64], 8, 128, 64), ([7, 0, 130], 4, 80, 100), ([40, 1, 1, 1, 60], 2, 256, 7), ([35], 36, 96, 16),
