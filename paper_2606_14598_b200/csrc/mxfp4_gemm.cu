@@ -32,8 +32,9 @@ constexpr int BKB = 128;            // bytes of K per k-block: one 128-byte swiz
 constexpr int BK = 2 * BKB;         // elements of K per k-block
 constexpr int MMA_K = 64;           // elements of K per instruction
 constexpr int EPI_THREADS = 128;
-constexpr int SCALE_WARP = 6;
-constexpr int NUM_THREADS = 64 + EPI_THREADS + 32;
+constexpr int SCALE_WARP = 6, SCALE_LOAD_WARP = 7;
+constexpr int NUM_THREADS = 64 + EPI_THREADS + 64;
+constexpr int SCALE_STAGES = 3;                        // stages of the scales' own ring, where they have one
 constexpr int SMEM_MAX = 232448;
 constexpr int SF_TILE_BYTES = 2 * kScaleTileBytes;     // 128 rows of scales for one k-block
 constexpr int SF_BUFS = 4;                             // k-blocks whose scales tensor memory holds
@@ -46,16 +47,20 @@ struct Layout {
     static constexpr int B_ROWS = BN / CG;
     static constexpr int B_BYTES = B_ROWS * BKB;
     static constexpr int SFB_TILES = (BN + 127) / 128;
-    static constexpr int SFA_OFF = A_BYTES + B_BYTES;
-    static constexpr int SFB_OFF = SFA_OFF + SF_TILE_BYTES;
-    static constexpr int KB_BYTES = SFB_OFF + SFB_TILES * SF_TILE_BYTES;      // one k-block
+    static constexpr int SF_KB_BYTES = (1 + SFB_TILES) * SF_TILE_BYTES;       // scales of one k-block: A, then W
+    // Scales in a ring of their own, fetched and copied ahead of the operands (see the scale warp), or in the operands' stages.
+    static constexpr bool OWN_RING = BN < 256;
+    static constexpr int KB_BYTES = A_BYTES + B_BYTES + (OWN_RING ? 0 : SF_KB_BYTES);       // one k-block of a stage
     static constexpr int STAGE_BYTES = KBS * KB_BYTES;
+    static constexpr int SF_STAGE_BYTES = KBS * SF_KB_BYTES;
+    static constexpr int OFF_SF = STAGES * STAGE_BYTES;
     static constexpr int BOX_BYTES = 32 * 64;                   // one 32-row x 32-column bf16 box
     static constexpr int BOXES = 2;                             // boxes that alternate per epilogue warp
-    static constexpr int OFF_STAGING = STAGES * STAGE_BYTES;
+    static constexpr int OFF_STAGING = OFF_SF + (OWN_RING ? SCALE_STAGES * SF_STAGE_BYTES : 0);
     static constexpr int OFF_BARS = OFF_STAGING + 4 * BOXES * BOX_BYTES;
     static constexpr int NUM_FULL = STAGES * KBS;               // a barrier per k-block
-    static constexpr int NUM_BARS = NUM_FULL + STAGES + 2 + 2 + SF_BUFS;     // full, empty, tfull[2], tempty[2], scales
+    static constexpr int NUM_SCALE_BARS = OWN_RING ? 2 * SCALE_STAGES : SF_BUFS;
+    static constexpr int NUM_BARS = NUM_FULL + STAGES + 2 + 2 + NUM_SCALE_BARS;     // full, empty, tfull[2], tempty[2], scales
     static constexpr int OFF_TMEM = OFF_BARS + NUM_BARS * 8;
     static constexpr int OFF_ABORT = OFF_TMEM + 4;
     static constexpr int USED = OFF_ABORT + 4;
@@ -109,7 +114,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     auto empty_bar = [&](int s) { return bars + 8u * (L::NUM_FULL + s); };                              // one per CTA
     auto tfull_bar = [&](int b) { return bars + 8u * (L::NUM_FULL + STAGES + b); };                     // one per CTA
     auto tempty_bar = [&](int b) { return bars + 8u * (L::NUM_FULL + STAGES + 2 + b); };                // used in the leader
-    auto scale_bar = [&](int b) { return bars + 8u * (L::NUM_FULL + STAGES + 4 + b); };                 // used in the leader
+    // scales in tensor memory: one barrier a buffer, used in the leader; with a ring of their own one a stage and CTA
+    auto scale_bar = [&](int b) { return bars + 8u * (L::NUM_FULL + STAGES + 4 + b); };
+    auto sfull_bar = [&](int s) { return bars + 8u * (L::NUM_FULL + STAGES + 4 + SCALE_STAGES + s); };  // (ring) scales landed: used in the leader
     volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + L::OFF_TMEM);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + L::OFF_ABORT);
     const WaitCtl ctl{abort_flag, rc.status, rc.sticky, rc.wait_limit_ns};
@@ -119,7 +126,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
             for (int sub = 0; sub < KBS; ++sub) mbar_init(full_bar(s, sub), 1);
             mbar_init(empty_bar(s), 1);
         }
-        for (int b = 0; b < SF_BUFS; ++b) mbar_init(scale_bar(b), 1);
+        for (int b = 0; b < L::NUM_SCALE_BARS; ++b) mbar_init(scale_bar(b), 1);
         for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4 * CG); }
         *abort_flag = 0;
         fence_mbar_init();
@@ -174,11 +181,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                         load(&tm_b, s + L::A_BYTES, bar, kb * BKB, n0 + rank * L::B_ROWS);
 #pragma unroll
                         for (int i = 0; i < L::SFB_TILES; ++i)
-                            load(&tm_sb, s + L::SFB_OFF + i * SF_TILE_BYTES, bar, 0, (n0 / kScaleTileRows + i) * ktiles + 2 * kb);
+                            if (!L::OWN_RING)
+                                load(&tm_sb, s + L::A_BYTES + L::B_BYTES + (1 + i) * SF_TILE_BYTES, bar, 0, (n0 / kScaleTileRows + i) * ktiles + 2 * kb);
                     }
                     if (acts) {
                         load(&tm_a, s, bar, kb * BKB, m0);
-                        load(&tm_sa, s + L::SFA_OFF, bar, 0, m0 / kScaleTileRows * ktiles + 2 * kb);
+                        if (!L::OWN_RING) load(&tm_sa, s + L::A_BYTES + L::B_BYTES, bar, 0, m0 / kScaleTileRows * ktiles + 2 * kb);
                     }
                 }
             };
@@ -218,10 +226,84 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
             }
         }
         __syncwarp();
+    } else if (warp == SCALE_LOAD_WARP) {
+        // ------------------------------------------------------------ TMA producer of the scales (both CTAs of a pair)
+        // A ring of its own: its stages come free as soon as they have been copied to tensor memory, so scales are fetched and
+        // copied well ahead of the operands that they go with.
+        if (L::OWN_RING && lane == 0) {
+            const uint64_t keep = l2_policy_evict_last();
+            grid_dep_wait();                                   // the activations' scales come from the kernel ahead
+            int st = 0, issued = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first_tile; t < num_tiles && ok; t += tile_step) {
+                const int mt = ((t / num_nb) * TILE_M + static_cast<int>(rank) * BM) / kScaleTileRows, nt = (t % num_nb) * BN / kScaleTileRows;
+                for (int ks = 0; ks < num_ks; ++ks) {
+                    if (issued >= SCALE_STAGES && !mbar_wait(scale_bar(st), phase ^ 1u, ctl, W_PRODUCER_EMPTY, kStatusTimeout)) { ok = false; break; }
+                    const uint32_t bar = CG == 2 ? mapa_shared(sfull_bar(st), 0) : sfull_bar(st);
+                    if (leader) mbar_arrive_expect_tx(sfull_bar(st), CG * L::SF_STAGE_BYTES);
+#pragma unroll
+                    for (int sub = 0; sub < KBS; ++sub) {
+                        const uint32_t dst = base + L::OFF_SF + st * L::SF_STAGE_BYTES + sub * L::SF_KB_BYTES;
+                        const int x = 2 * (ks * KBS + sub);
+#pragma unroll
+                        for (int i = 0; i <= L::SFB_TILES; ++i) {
+                            const CUtensorMap* tm = i == 0 ? &tm_sa : &tm_sb;
+                            const int y = (i == 0 ? mt : nt + i - 1) * ktiles + x;
+                            if (CG == 2) tma_load_2d_pair_hint(dst + i * SF_TILE_BYTES, tm, bar, 0, y, keep);
+                            else tma_load_2d_hint(dst + i * SF_TILE_BYTES, tm, bar, 0, y, keep);
+                        }
+                    }
+                    ++issued;
+                    if (++st == SCALE_STAGES) { st = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok && leader) {
+                for (int i = 0; i < SCALE_STAGES && i < issued; ++i) {      // let copies in flight land
+                    if (st == 0) { st = SCALE_STAGES; phase ^= 1u; }
+                    --st;
+                    const uint64_t t0 = globaltimer_ns();
+                    while (!mbar_try_wait(sfull_bar(st), phase) && globaltimer_ns() - t0 < 10000000ull) {}
+                }
+            }
+        }
+        __syncwarp();
     } else if (warp == SCALE_WARP) {
         // ------------------------------------------------------------ scales: shared -> tensor memory (leader CTA only)
-        // A thread of its own: in front of the MMAs, in their thread, every copy would hold the tensor pipe up.
-        if (lane == 0 && leader) {
+        // A thread of its own: in front of the MMAs, in their thread, every copy would hold the tensor pipe up. Tensor memory
+        // holds the scales of two stages. With a ring of their own the scales of a stage are copied before its operands have landed
+        // (4110 x 4608 -> 13824 at 256 x 192 118 against 132 us, 512 x 12288 -> 4608 at 128 x 128 18.8 against 20.8 us); the
+        // 256 x 256 tile, whose copies take a third longer, does better with copies and hand-over k-block by k-block (111 against
+        // 124 us on 4110 x 12288 -> 4608).
+        if (L::OWN_RING) {
+            if (lane == 0 && leader) {
+                int st = 0, n = 0;                                 // n: stages so far; buffers of stage n: n % BACK
+                uint32_t phase = 0;
+                bool ok = true;
+                constexpr int BACK = SF_BUFS / KBS;                // stages whose scales tensor memory holds
+                for (int t = first_tile; t < num_tiles && ok; t += tile_step) {
+                    for (int ks = 0; ks < num_ks; ++ks, ++n) {
+                        if (!mbar_wait(sfull_bar(st), phase, ctl, W_SCALES, kStatusTimeout)) { ok = false; break; }
+                        // the MMAs that used these buffers are done
+                        if (n >= BACK && !mbar_wait(empty_bar((n - BACK) % STAGES), ((n - BACK) / STAGES) & 1, ctl, W_SCALES, kStatusTimeout)) { ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int sub = 0; sub < KBS; ++sub) {
+                            const uint32_t s = base + L::OFF_SF + st * L::SF_STAGE_BYTES + sub * L::SF_KB_BYTES;
+                            const uint32_t sf = tmem_base + L::SF_COL + (n % BACK * KBS + sub) * 2 * L::SF_HALF;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)            // halves of 128 elements: one scale tile each
+#pragma unroll
+                                for (int q = 0; q <= L::SFB_TILES; ++q)
+                                    tc_cp_scales<CG>(sf + h * L::SF_HALF + 4 * q, make_scale_desc(s + q * SF_TILE_BYTES + h * kScaleTileBytes));
+                        }
+                        if (CG == 2) { tc_commit_pair(scale_bar(st)); tc_commit_pair(mapa_shared(scale_bar(st), 1)); }
+                        else tc_commit(scale_bar(st));
+                        if (++st == SCALE_STAGES) { st = 0; phase ^= 1u; }
+                    }
+                }
+            }
+        } else if (lane == 0 && leader) {
             int stage = 0, i = 0;                              // i: k-blocks so far, buffer i % SF_BUFS
             uint32_t phase = 0;
             bool ok = true;
@@ -238,15 +320,15 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                     for (int sub = 0; sub < KBS; ++sub, ++i) {
                         if (!mbar_wait(full_bar(stage, sub), phase, ctl, W_SCALES, kStatusTimeout)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t s = base + stage * L::STAGE_BYTES + sub * L::KB_BYTES;
+                        const uint32_t s = base + stage * L::STAGE_BYTES + sub * L::KB_BYTES + L::A_BYTES + L::B_BYTES;
                         const uint32_t sf = tmem_base + L::SF_COL + (i % SF_BUFS) * 2 * L::SF_HALF;
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {          // halves of 128 elements: one scale tile each
-                            tc_cp_scales<CG>(sf + h * L::SF_HALF, make_scale_desc(s + L::SFA_OFF + h * kScaleTileBytes));
+                            tc_cp_scales<CG>(sf + h * L::SF_HALF, make_scale_desc(s + h * kScaleTileBytes));
 #pragma unroll
                             for (int q = 0; q < L::SFB_TILES; ++q)
                                 tc_cp_scales<CG>(sf + h * L::SF_HALF + 4 + 4 * q,
-                                                 make_scale_desc(s + L::SFB_OFF + q * SF_TILE_BYTES + h * kScaleTileBytes));
+                                                 make_scale_desc(s + (1 + q) * SF_TILE_BYTES + h * kScaleTileBytes));
                         }
                         if (CG == 2) tc_commit_pair(scale_bar(i % SF_BUFS));
                         else tc_commit(scale_bar(i % SF_BUFS));
@@ -260,7 +342,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         // ------------------------------------------------------------ MMA issuer (leader CTA only)
         if (lane == 0 && leader) {
             constexpr uint32_t idesc_lo = make_mxf4_idesc(TILE_M, BN, 0), idesc_hi = make_mxf4_idesc(TILE_M, BN, 2);
-            int stage = 0, c = 0, i = 0;
+            int stage = 0, c = 0, n = 0;                      // n: stages so far
             uint32_t phase = 0;
             bool ok = true;
             for (int t = first_tile; t < num_tiles && ok; t += tile_step, ++c) {
@@ -274,16 +356,18 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                 const uint32_t d = tmem_base + (c & 1) * L::SLOT1;
                 // the tile's first column within its first scale tile, in tensor-memory columns of 32 rows
                 const uint32_t sfb_shift = ((t % num_nb) * BN % kScaleTileRows) / 32;
-                for (int ks = 0; ks < num_ks && ok; ++ks) {
+                for (int ks = 0; ks < num_ks && ok; ++ks, ++n) {
+                    if (L::OWN_RING && !mbar_wait(scale_bar(n % SCALE_STAGES), (n / SCALE_STAGES) & 1, ctl, W_MMA_FULL, kStatusTimeout)) { ok = false; break; }
 #pragma unroll
-                    for (int sub = 0; sub < KBS; ++sub, ++i) {
+                    for (int sub = 0; sub < KBS; ++sub) {
+                        const int buf = n % (SF_BUFS / KBS) * KBS + sub;           // of the k-block's scales
                         if (!mbar_wait(full_bar(stage, sub), phase, ctl, W_MMA_FULL, kStatusTimeout) ||
-                            !mbar_wait(scale_bar(i % SF_BUFS), (i / SF_BUFS) & 1, ctl, W_MMA_FULL, kStatusTimeout)) { ok = false; break; }
+                            (!L::OWN_RING && !mbar_wait(scale_bar(buf), (n / (SF_BUFS / KBS)) & 1, ctl, W_MMA_FULL, kStatusTimeout))) { ok = false; break; }
                         tc_fence_after();
                         const int kb = ks * KBS + sub;
                         const uint32_t s = base + stage * L::STAGE_BYTES + sub * L::KB_BYTES;
                         const uint64_t da = make_kmajor_sw128_desc(s), db = make_kmajor_sw128_desc(s + L::A_BYTES);
-                        const uint32_t sf = tmem_base + L::SF_COL + (i % SF_BUFS) * 2 * L::SF_HALF;
+                        const uint32_t sf = tmem_base + L::SF_COL + buf * 2 * L::SF_HALF;
                         const int left = K - kb * BK;                      // elements of K this k-block holds (none past the end)
 #pragma unroll
                         for (int k = 0; k < BK / MMA_K; ++k) {             // 64 elements = 32 bytes: +2 in 16-byte units
@@ -435,11 +519,11 @@ int launch_cfg(const MxLinearArgs& a, cudaStream_t st) {
 
 // The configuration with the lowest estimated time. Fitted on 20 shapes from (128, 256, 256) to (8192, 8192, 8192): launch,
 // fill and last epilogue, then for every wave of tiles its k-blocks and what the hand-over between tiles leaves exposed
-// (microseconds). The pair of 256 x 256 has the best rate (512 x 13824 x 4608 ... 4110 x 13824 x 4608: 120 against 133 us at
-// 256 x 192), 256 x 192 wins where it saves a wave (4110 x 4608 x 4608: 52 us both; 1536 x 4608 x 4608: 22.3 against 24.5 us),
-// single CTAs where pairs would leave SMs without a tile (512 x 4608 x 12288: 22.3 against 29.5 us).
+// (microseconds). Measured, 256 x 256 pairs / 256 x 192 pairs / 128 x 128: 8192 cubed 214 / 228 / 327 us, 4110 x 4608 -> 4608
+// 50.0 / 46.3 / 57.9, 2048 x 4608 -> 12288 57.4 / 54.0 / 75.8, 1024 x 4608 -> 4608 14.5 / 18.0 / 15.5, 512 x 12288 -> 4608
+// 25.7 / 22.3 / 18.8.
 int choose_mx_config(int M, int N, int K) {
-    struct { int cg, bn; double fixed, per_kb, per_tile; } const c[] = {{2, 256, 4.0, 0.47, 0.8}, {2, 192, 4.0, 0.44, 0.1}, {1, 128, 3.0, 0.395, 0.0}};
+    struct { int cg, bn; double fixed, per_kb, per_tile; } const c[] = {{2, 256, 4.5, 0.455, 0.8}, {2, 192, 4.0, 0.39, 0.1}, {1, 128, 2.8, 0.345, 0.0}};
     int best = 0;
     double best_us = 0.0;
     for (int i = 0; i < 3; ++i) {
