@@ -9,13 +9,20 @@
 // twice the arithmetic; on top of it come the scales: 1 KB for 128 rows and 256 elements, copied from shared into tensor
 // memory (tcgen05.cp) in front of the MMAs that read them.
 //
-// Tensor memory: 512 columns hold two accumulators of BN columns and the scales of one k-block (8 columns for A, 8 for each
-// 128 columns of the tile). Two accumulators of 256 columns would leave no room for scales, so at BN = 256 they
-// overlap by 32 columns ([0,256) and [224,480)): the epilogue takes the shared columns first and hands them on, and the
-// next tile's MMAs run under the rest of the epilogue.
+// Tensor memory: 512 columns hold two accumulators of BN columns and the scales of four k-blocks (for each half of a k-block 4
+// columns for A and 4 for every 128 columns of the tile). Two accumulators of 256 columns would leave no room for scales, so at
+// BN = 256 they overlap by 128 columns ([0,256) and [128,384)): the epilogue takes the shared columns into registers first and
+// hands them on, and the next tile's MMAs run under the rest of the epilogue.
 //
 // Warp roles: 0 TMA producer, 1 MMA issuer (and TMEM allocation), 2-5 epilogue (tcgen05.ld 32x32b, thread = row; bias; bf16;
-// swizzled staging; TMA store of 32 x 64 boxes, which clips ragged edges).
+// swizzled staging; TMA store of 32 x 32 boxes, which clips ragged edges), 6 copies scales into tensor memory, 7 loads them.
+//
+// What bounds it: the tensor queue and the way operands take to it, not HBM (the operands of a 4110 x 4608 -> 13824 product come
+// out of L2). There 120 us = 4.35 PFLOP/s, 0.66 of four times the measured bf16 rate (8192 cubed 5.1 PFLOP/s, 0.78). With parts
+// left out: MMAs alone 86 us (162 cycles an MMA of 256 x 256 x 64 where 128 would be the pipe's), with scale copies 94 (a copy or
+// commit holds the queue 35-45 cycles; in the MMA thread they made it 159), with operand loads 110, with the hand-over of the
+// shared columns 120 (0.5 us a tile from the accumulator's completion to the peer's answer). Tried without gain: bands in the
+// tile order, L2 hints, one commit for both CTAs, stages of one k-block (258 against 217 us on 8192 cubed), stores straight from registers.
 //
 // Every wait is bounded as in the int8 GEMM: on expiry the status word is set, all roles unwind, TMEM is freed.
 #include "../../include/mxfp4_linear.h"

