@@ -62,39 +62,51 @@ __device__ __forceinline__ RowScale2 head_scale2(const RowScale& rs) {
     return RowScale2{pack2(-rs.s, -rs.s), pack2(rs.inv, rs.inv), pack2(MAGIC, MAGIC), pack2(inv_hi, inv_hi), pack2(inv_lo, inv_lo)};
 }
 
-// A unit is what shares a scale: a head of a token (int8; 2^lane_shift lanes, at least dim / 8) or a block of 32 of it (MXFP4; 4
-// lanes). Keys and values of UNROLL tokens are in flight at once.
-template <int FMT, bool VALUES>
+// A unit is what shares a scale: a head of a token (int8) or a block of 32 of it (MXFP4); 2^lane_shift lanes, E elements each. 16
+// elements a lane, loaded as 32 bytes, where sizes, strides and addresses allow it: what a unit costs beside its elements (its
+// maximum, scale and places) is then shared by twice as many; else 8. Keys and values of UNROLL tokens are in flight at once.
+template <int FMT, bool VALUES, int E>
 __global__ void __launch_bounds__(kThreads, FMT == KV_CACHE_INT8 ? 3 : 4)
 kv_write_kernel(const Side k, const Side v, const int64_t* slots, int64_t num_slots, int64_t tokens, int heads, int dim, int lane_shift, int tile,
                 const Cover cover) {
-    constexpr int UNROLL = 4, SIDES = VALUES ? 2 : 1;
+    constexpr int UNROLL = E == 16 ? 2 : 4, SIDES = VALUES ? 2 : 1, WORDS = E / 2;
     grid_dep_wait();
     const int sub = static_cast<int>(threadIdx.x) / cover.width;
     const int lane = blockIdx.y * cover.width + static_cast<int>(threadIdx.x) - sub * cover.width;
     const int unit = lane >> lane_shift, gl = lane & ((1 << lane_shift) - 1);
     const int blocks = FMT == KV_CACHE_INT8 ? 1 : (dim + kMxBlock - 1) / kMxBlock;       // units of a head
-    const int head = unit / blocks, d = (unit - head * blocks) * kMxBlock + gl * 8;
+    const int head = unit / blocks, d = (unit - head * blocks) * kMxBlock + gl * E;
     const bool mine = sub < cover.subs && head < heads && d < dim;
     const int64_t k_off = head * k.sh + d, v_off = VALUES ? head * v.sh + d : 0;
     const int code_off = FMT == KV_CACHE_INT8 ? head * dim + d : (head * dim + d) / 2;
     const int64_t token_codes = static_cast<int64_t>(heads) * dim / (FMT == KV_CACHE_INT8 ? 1 : 2), token_scales = static_cast<int64_t>(heads) * blocks;
+    auto load = [](const __nv_bfloat16* p, uint32_t (&r)[WORDS]) {
+        if (E == 16) {
+            ldcg_32(p, r);
+        } else {
+            const uint4 q = __ldcg(reinterpret_cast<const uint4*>(p));
+            r[0] = q.x; r[1] = q.y; r[2] = q.z; r[3] = q.w;
+        }
+    };
     for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * tile; t0 < tokens; t0 += static_cast<int64_t>(gridDim.x) * tile) {
         const int count = static_cast<int>(tokens - t0 < tile ? tokens - t0 : tile);
         for (int base = 0; base < count; base += UNROLL * cover.subs) {          // (uniform: every lane takes part in the shuffles)
-            uint4 x[UNROLL][SIDES];
+            uint32_t x[UNROLL][SIDES][WORDS];
             int64_t slot[UNROLL];
 #pragma unroll
             for (int j = 0; j < UNROLL; ++j) {
                 const int tt = base + j * cover.subs + sub;
                 slot[j] = -1;
-#pragma unroll
-                for (int q = 0; q < SIDES; ++q) x[j][q] = make_uint4(0, 0, 0, 0);
                 if (mine && tt < count) {
                     const int64_t t = t0 + tt;
                     slot[j] = __ldcg(slots + t);
-                    x[j][0] = __ldcg(reinterpret_cast<const uint4*>(k.x + t * k.st + k_off));
-                    if (VALUES) x[j][SIDES - 1] = __ldcg(reinterpret_cast<const uint4*>(v.x + t * v.st + v_off));
+                    load(k.x + t * k.st + k_off, x[j][0]);
+                    if (VALUES) load(v.x + t * v.st + v_off, x[j][SIDES - 1]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < SIDES; ++q)
+#pragma unroll
+                        for (int i = 0; i < WORDS; ++i) x[j][q][i] = 0;
                 }
             }
 #pragma unroll
@@ -104,25 +116,36 @@ kv_write_kernel(const Side k, const Side v, const int64_t* slots, int64_t num_sl
 #pragma unroll
                 for (int q = 0; q < SIDES; ++q) {
                     const Side& s = q == 0 ? k : v;
-                    uint32_t m = absmax_bits8(x[j][q]);
+                    uint4 part[E / 8];
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int i = 0; i < E / 8; ++i) {
+                        part[i] = make_uint4(x[j][q][4 * i], x[j][q][4 * i + 1], x[j][q][4 * i + 2], x[j][q][4 * i + 3]);
+                        m = max(m, absmax_bits8(part[i]));
+                    }
                     if (FMT == KV_CACHE_INT8) {
                         for (int o = 1; o < 1 << lane_shift; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                        // (every lane of a head works the scale out: sharing them out over the lanes, one each, and passing them
-                        // on by shuffles was slower, 206 against 198 us on 120000 tokens of 8 x 128 and 3.8 against 2.2 us on 48)
+                        // (every lane of a head works the scale out: sharing the scales of several tokens out over the lanes and passing
+                        // them on by shuffles was slower, 206 against 198 us on 120000 tokens of 8 x 128 and 3.8 against 2.2 us on 48)
                         const bool finite = m < 0x7f800000u;
                         const RowScale rs = head_scale(finite ? __uint_as_float(m) : 0.f);
-                        uint2 c = make_uint2(0, 0);
-                        if (finite) c = quant8(x[j][q], rs, head_scale2(rs));
+                        const RowScale2 r2 = head_scale2(rs);
+                        uint2 c[E / 8];
+#pragma unroll
+                        for (int i = 0; i < E / 8; ++i) c[i] = finite ? quant8(part[i], rs, r2) : make_uint2(0, 0);
                         if (store) {
-                            *reinterpret_cast<uint2*>(s.codes + slot[j] * token_codes + code_off) = c;
+                            uint8_t* p = s.codes + slot[j] * token_codes + code_off;
+                            if (E == 16) *reinterpret_cast<uint4*>(p) = make_uint4(c[0].x, c[0].y, c[E / 8 - 1].x, c[E / 8 - 1].y);
+                            else *reinterpret_cast<uint2*>(p) = c[0];
                             if (gl == 0) static_cast<float*>(s.scales)[slot[j] * token_scales + unit] = finite ? rs.s : __uint_as_float(0x7fc00000u);
                         }
                     } else {
-                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                        for (int o = 1; o < kMxBlock / E; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
                         const uint32_t byte = mx_scale_byte(m);
                         if (store) {
-                            *reinterpret_cast<uint32_t*>(s.codes + slot[j] * token_codes + code_off) = mx_codes8(x[j][q], byte);
+                            uint8_t* p = s.codes + slot[j] * token_codes + code_off;
+                            if (E == 16) *reinterpret_cast<uint2*>(p) = make_uint2(mx_codes8(part[0], byte), mx_codes8(part[E / 8 - 1], byte));
+                            else *reinterpret_cast<uint32_t*>(p) = mx_codes8(part[0], byte);
                             if (gl == 0) static_cast<uint8_t*>(s.scales)[slot[j] * token_scales + unit] = static_cast<uint8_t>(byte);
                         }
                     }
@@ -131,6 +154,9 @@ kv_write_kernel(const Side k, const Side v, const int64_t* slots, int64_t num_sl
         }
     }
 }
+
+template <int FMT, bool VALUES>
+auto write_kernel(bool wide) { return wide ? kv_write_kernel<FMT, VALUES, 16> : kv_write_kernel<FMT, VALUES, 8>; }
 
 constexpr int kMaxTile = 32;       // tokens whose places a CTA looks up at a time, at most
 
@@ -298,9 +324,11 @@ int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_hea
     }
     if (int e = check_arch()) return e;
     if (tokens == 0 || num_slots == 0) return W8A8_OK;
-    int lane_shift = 2;                                            // a block's four lanes
-    if (fmt == KV_CACHE_INT8)
-        for (lane_shift = 0; (8 << lane_shift) < dim;) ++lane_shift;
+    auto wide_side = [](const void* p, int64_t token_stride, int64_t head_stride) { return aligned(p, 32) && token_stride % 16 == 0 && head_stride % 16 == 0; };
+    const bool wide = dim % 16 == 0 && wide_side(k, k_token_stride, k_head_stride) && (v == nullptr || wide_side(v, v_token_stride, v_head_stride));
+    const int each = wide ? 16 : 8;                                // elements a lane
+    int lane_shift = 0;
+    while ((each << lane_shift) < (fmt == KV_CACHE_INT8 ? dim : kMxBlock)) ++lane_shift;
     const int blocks = fmt == KV_CACHE_INT8 ? 1 : static_cast<int>((dim + kMxBlock - 1) / kMxBlock);
     Side ks{}, vs{};
     ks.x = static_cast<const __nv_bfloat16*>(k);
@@ -315,8 +343,8 @@ int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_hea
     vs.scales = v_scales;
     const Cover cover = make_cover(static_cast<int>(heads) * blocks << lane_shift);
     const int tile = tile_for(tokens, cover.slices);
-    const auto kern = fmt == KV_CACHE_INT8 ? (v != nullptr ? kv_write_kernel<KV_CACHE_INT8, true> : kv_write_kernel<KV_CACHE_INT8, false>)
-                                           : (v != nullptr ? kv_write_kernel<KV_CACHE_MXFP4, true> : kv_write_kernel<KV_CACHE_MXFP4, false>);
+    const auto kern = fmt == KV_CACHE_INT8 ? (v != nullptr ? write_kernel<KV_CACHE_INT8, true>(wide) : write_kernel<KV_CACHE_INT8, false>(wide))
+                                           : (v != nullptr ? write_kernel<KV_CACHE_MXFP4, true>(wide) : write_kernel<KV_CACHE_MXFP4, false>(wide));
     const cudaError_t e = launch_pdl(kern, grid_for(tokens, tile, cover), cover.threads, static_cast<cudaStream_t>(stream), ks, vs, slots, num_slots, tokens,
                                      static_cast<int>(heads), static_cast<int>(dim), lane_shift, tile, cover);
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;

@@ -156,6 +156,15 @@ def test_write(fmt, tokens, heads, dim, page):
     got = [(c.k_codes, c.k_scales), (c.v_codes, c.v_scales)]
     for (gc, gs), (wc, ws) in zip(got, want):
         assert same(gc.flatten(0, 1), wc) and same(gs.flatten(0, 1), ws)
+    # the same vectors 16 bytes off a 32-byte boundary, and heads 8 elements apart from a multiple of 16: the same contents
+    for t in (c.k_codes, c.k_scales, c.v_codes, c.v_scales):
+        t.zero_()
+    off = torch.empty(8 + tokens * 3 * heads * (dim + 8), device="cuda", dtype=torch.bfloat16)[8:].view(tokens, 3, heads, dim + 8)[..., :dim]
+    off.copy_(qkv)
+    w8.kv_cache_write(c, off[:, 1], off[:, 2], slots)
+    keep = slots[(slots >= 0) & (slots < pages * page)]
+    for (gc, gs), (wc, ws) in zip(got, want):
+        assert same(gc.flatten(0, 1)[keep], wc[keep]) and same(gs.flatten(0, 1)[keep], ws[keep])
 
 
 @pytest.mark.gpu
