@@ -6,10 +6,10 @@
 // Both directions move bytes: a write reads 2 and stores 1 (or 0.53) bytes an element, a read loads 1 (0.53) and stores
 // 2. A lane handles 8 elements. All offsets into the cache are 64-bit.
 //
-// What bounds them, keys and values of 8 x 128 a token: reads HBM (120000 int8 tokens 121 us = 6.2 TB/s, 230000 MXFP4 tokens 203 us
-// = 5.9 TB/s; the copy bandwidth is 6.5), small ones the chain sequence - page - codes (512 tokens of 36 x 128 5.5 us). MXFP4
-// writes HBM (230000 tokens 221 us = 5.4 TB/s), int8 writes the instructions of the exact quotient (120000 tokens 189 us =
-// 3.9 TB/s, 2.5 of 4 instructions a cycle).
+// What bounds them, keys and values of 8 x 128 a token: HBM, at 6.5 TB/s of copy bandwidth. Reads: 120000 int8 tokens 121 us =
+// 6.2 TB/s, 230000 MXFP4 tokens 202 us = 5.9 TB/s (16 elements a lane and 32-byte stores: 120 and 201 us, not kept); small ones
+// the chain sequence - page - codes (512 tokens of 36 x 128 5.5 us). Writes: 230000 MXFP4 tokens 184 us = 6.5 TB/s; int8 the
+// instructions of the exact quotient, 120000 tokens 137 us = 5.4 TB/s (189 us with 8 elements a lane).
 #include "../../include/kv_cache.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"

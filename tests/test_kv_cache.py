@@ -211,6 +211,10 @@ def test_read(fmt, lens, heads, dim, page, window):
     w8.kv_cache_read(c, wide[:, :most], cu, total + 3, starts=first, k_out=buf[:, 0], v_out=buf[:, 2])
     assert torch.equal(buf[:total, 0], k) and torch.equal(buf[:total, 2], v)
     assert (buf[total:] == 5).all() and (buf[:, 1] == 5).all()
+    # 16 bytes off a 32-byte boundary
+    off = torch.empty(8 + total * heads * dim, device="cuda", dtype=torch.bfloat16)[8:].view(total, heads, dim)
+    w8.kv_cache_read(c, wide[:, :most], cu, total, starts=first, k_out=off, v_out=buf[:total, 1])
+    assert torch.equal(off, k) and torch.equal(buf[:total, 1], v)
 
 
 @pytest.mark.gpu
