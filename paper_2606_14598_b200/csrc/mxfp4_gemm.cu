@@ -427,7 +427,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
-                        if (CG == 2) mbar_arrive_cluster(mapa_shared(tempty_bar(slot), 0));
+                        if (!leader) mbar_arrive_cluster(mapa_shared(tempty_bar(slot), 0));
                         else mbar_arrive(tempty_bar(slot));
                     }
                 }
@@ -537,7 +537,7 @@ int choose_mx_config(int M, int N, int K) {
         const int64_t tiles = static_cast<int64_t>((M + BM * c[i].cg - 1) / (BM * c[i].cg)) * ((N + c[i].bn - 1) / c[i].bn);
         const int64_t groups = sm_count() / c[i].cg, waves = (tiles + groups - 1) / groups;
         const double us = c[i].fixed + waves * ((K + BK - 1) / BK * c[i].per_kb + c[i].per_tile);
-        if (i == 0 || us < best_us) { best = i; best_us = us; }
+        if (i == 0 || us < 0.97 * best_us) { best = i; best_us = us; }       // on near ties the earlier one
     }
     return best;
 }

@@ -464,3 +464,48 @@ def test_example_block(fmt):
     four, full = module.run(fmt)
     assert four.shape == full.shape and torch.isfinite(four).all()
     assert torch.nn.functional.cosine_similarity(four.flatten(), full.flatten(), dim=0) > 0.9
+
+
+@pytest.mark.gpu
+def test_chained_with_the_int8_kernels():
+    """Launches that follow one another closely (programmatic dependent launch, shared tensor memory): int8 linears of one, a few dozen and
+    many tokens between 4-bit ones of every kind and cache calls, eagerly and as a graph, against each one run by itself."""
+    g = torch.Generator("cuda").manual_seed(21)
+    calls, alone = [], []
+    for m, n, k in [(1, 1024, 512), (6, 2048, 768), (40, 512, 1024), (30, 256, 512), (200, 384, 768), (700, 1032, 1056)]:
+        a, w, bias = operands(m, n, k, seed=m)
+        qw4, sw4 = w8.mxfp4_quantize(w)
+        qw8, s8 = w8.int8_quantize_weight_per_channel(w)
+        ws4, ws8 = w8.mxfp4_alloc_workspace(m, n, k), w8.alloc_workspace(m, n, k)
+        out4, out8 = (torch.empty(m, n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        calls.append((lambda a=a, q=qw8, s=s8, b=bias, o=out8, ws=ws8: w8.int8_linear_fused(a, q, s, b, out=o, workspace=ws), out8))
+        calls.append((lambda a=a, q=qw4, s=sw4, b=bias, o=out4, ws=ws4: w8.mxfp4_linear_fused(a, q, s, b, out=o, workspace=ws), out4))
+    x = torch.randn(200, 4, 64, generator=g, device="cuda").bfloat16()
+    cache = w8.QuantKVCache.empty(13, 16, 4, 64, "mxfp4")
+    table, cu = torch.arange(13, dtype=torch.int32, device="cuda")[None], torch.tensor([0, 200], dtype=torch.int32, device="cuda")
+    k_out, v_out, slots = torch.empty_like(x), torch.empty_like(x), torch.arange(200, device="cuda")
+
+    def cached():
+        w8.kv_cache_write(cache, x, x, slots)
+        w8.kv_cache_read(cache, table, cu, 200, k_out=k_out, v_out=v_out)
+
+    calls.insert(5, (cached, k_out))
+    for call, out in calls:
+        call()
+        torch.cuda.synchronize()
+        alone.append(out.clone())
+    order = list(range(len(calls))) * 3 + list(range(len(calls)))[::-1] * 2 + [0, 3, 0, 3, 1, 1, 3, 3, 5, 4, 5, 4, 7, 6, 7, 12, 3, 12, 0]
+    for _ in range(10):
+        for i in order:
+            calls[i][0]()
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for (_, out), want in zip(calls, alone))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for i in order:
+            calls[i][0]()
+    for _, out in calls:
+        out.zero_()
+    for _ in range(10):
+        graph.replay()
+    assert all(torch.equal(out, want) for (_, out), want in zip(calls, alone)) and w8.int8_sticky_status() == 0
