@@ -2,8 +2,8 @@
  * mxfp4_linear.h -- C ABI of the B200 (sm_100a) 4-bit linear layer: MXFP4 weights, activations quantized to MXFP4
  * inside the call, fp32 accumulation on the block-scaled tensor cores, bias added in the epilogue, bf16 out. The
  * 4-bit counterpart of w8a8_linear.h; its conventions on pointers, streams, chaining, capture and status codes hold
- * here too (weights must be complete before a linear is enqueued: it may request weight tiles before it waits for the
- * kernel ahead of it on the stream).
+ * here too. Every operand, the weights among them, is read after the work ahead of the call on its stream is complete: a
+ * quantizer, a copy or any other kernel may write them directly before the call.
  *
  * The format (OCP Microscaling v1.0, MXFP4): 32 consecutive elements of a row share a power-of-two scale.
  *     amax  = max |x| of the block

@@ -146,7 +146,8 @@ size_t tc_max_scratch_bytes(int M, int N, int K);
 int launch_gemm_tc(const GemmArgs& a, const TcPlan& plan, cudaStream_t st);
 
 // ---- mxfp4_quantize.cu
-// early: let the kernel behind this one be set up while this one runs (never for what may be used as a weight).
+// early: let the kernel behind this one be set up while this one runs (only where that kernel is the library's own: it waits before it
+// reads anything).
 cudaError_t launch_mx_quantize(const void* x, bool fp32, int64_t ldx, int M, int K, uint8_t* codes, uint8_t* scales, int* status_to_clear,
                                bool early, cudaStream_t st);
 cudaError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, void* out, bool fp32, int64_t ldo, cudaStream_t st);

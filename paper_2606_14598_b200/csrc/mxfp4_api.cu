@@ -49,7 +49,6 @@ int mxfp4_quantize(const void* x, int dtype, int64_t M, int64_t K, int64_t ldx, 
     if (ldx < K) return W8A8_ERR_INVALID_ARG;
     if (ldx % (dtype == MXFP4_BF16 ? 8 : 4) != 0 || !aligned16(x) || !aligned16(codes) || !aligned16(scales)) return W8A8_ERR_ALIGNMENT;
     if (int e = check_arch()) return e;
-    // the result may be a weight, which a linear behind this call reads before it waits: nothing is released early
     return launch_mx_quantize(x, dtype == MXFP4_FP32, ldx, static_cast<int>(M), static_cast<int>(K), codes, scales, nullptr, false,
                               static_cast<cudaStream_t>(stream)) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }

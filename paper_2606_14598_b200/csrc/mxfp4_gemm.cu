@@ -174,45 +174,45 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                 if (CG == 2) tma_load_2d_pair_hint(dst, tm, bar, x, y, keep);
                 else tma_load_2d_hint(dst, tm, bar, x, y, keep);
             };
-            // The loads of stage ks of a tile into ring slot st: the weights' part (which arms the barriers) and the activations'
-            // part. A stage always receives all its k-blocks: what lies past the end of K arrives as zeros and is not used.
-            auto load_stage = [&](int t, int ks, int st, bool weights, bool acts) {
+            // The loads of stage ks of a tile into ring slot st. A stage always receives all its k-blocks: what lies past the end
+            // of K arrives as zeros and is not used.
+            auto load_stage = [&](int t, int ks, int st) {
                 const int m0 = (t / num_nb) * TILE_M + rank * BM, n0 = (t % num_nb) * BN;
 #pragma unroll
                 for (int sub = 0; sub < KBS; ++sub) {
                     const int kb = ks * KBS + sub;
                     const uint32_t s = base + st * L::STAGE_BYTES + sub * L::KB_BYTES;
                     const uint32_t bar = CG == 2 ? mapa_shared(full_bar(st, sub), 0) : full_bar(st, sub);
-                    if (weights) {
-                        if (leader) mbar_arrive_expect_tx(full_bar(st, sub), CG * L::KB_BYTES);
-                        load(&tm_b, s + L::A_BYTES, bar, kb * BKB, n0 + rank * L::B_ROWS);
+                    if (leader) mbar_arrive_expect_tx(full_bar(st, sub), CG * L::KB_BYTES);
+                    load(&tm_b, s + L::A_BYTES, bar, kb * BKB, n0 + rank * L::B_ROWS);
+                    load(&tm_a, s, bar, kb * BKB, m0);
+                    if (!L::OWN_RING) {
 #pragma unroll
                         for (int i = 0; i < L::SFB_TILES; ++i)
-                            if (!L::OWN_RING)
-                                load(&tm_sb, s + L::A_BYTES + L::B_BYTES + (1 + i) * SF_TILE_BYTES, bar, 0, (n0 / kScaleTileRows + i) * ktiles + 2 * kb);
-                    }
-                    if (acts) {
-                        load(&tm_a, s, bar, kb * BKB, m0);
-                        if (!L::OWN_RING) load(&tm_sa, s + L::A_BYTES + L::B_BYTES, bar, 0, m0 / kScaleTileRows * ktiles + 2 * kb);
+                            load(&tm_sb, s + L::A_BYTES + L::B_BYTES + (1 + i) * SF_TILE_BYTES, bar, 0, (n0 / kScaleTileRows + i) * ktiles + 2 * kb);
+                        load(&tm_sa, s + L::A_BYTES + L::B_BYTES, bar, 0, m0 / kScaleTileRows * ktiles + 2 * kb);
                     }
                 }
             };
-            // weights do not depend on the kernel ahead: those of the first ring of stages are requested before the wait
-            const int pre = first_tile < num_tiles && !withhold ? min(STAGES, num_ks) : 0;
-            for (int i = 0; i < pre; ++i) load_stage(first_tile, i, i, true, false);
+            // The weights of the first ring of stages are on their way to L2 while the kernel ahead finishes. They are read after
+            // it is complete, like everything else: it may be the one that writes them.
+            if (first_tile < num_tiles) {
+                const int n0 = (first_tile % num_nb) * BN;
+                for (int kb = 0; kb < min(STAGES * KBS, num_kb); ++kb) {
+                    tma_prefetch_2d_hint(&tm_b, kb * BKB, n0 + rank * L::B_ROWS, keep);
+#pragma unroll
+                    for (int i = 0; i < L::SFB_TILES; ++i) tma_prefetch_2d_hint(&tm_sb, 0, (n0 / kScaleTileRows + i) * ktiles + 2 * kb, keep);
+                }
+            }
             grid_dep_wait();
             if (!rc.after_quantizer && blockIdx.x == 0) *rc.status = 0;
-            for (int i = 0; i < pre; ++i) load_stage(first_tile, i, i, false, true);
-            issued = pre;
-            if (pre == STAGES) phase = 1;
-            else stage = pre;
             for (int t = first_tile; t < num_tiles && ok; t += tile_step) {
-                for (int ks = t == first_tile ? pre : 0; ks < num_ks; ++ks) {
+                for (int ks = 0; ks < num_ks; ++ks) {
                     if (!mbar_wait(empty_bar(stage), phase ^ 1u, ctl, W_PRODUCER_EMPTY, kStatusTimeout)) { ok = false; break; }
                     if (withhold) {
                         withhold = false;      // test hook: this stage never arrives; the bounded waits run out
                     } else {
-                        load_stage(t, ks, stage, true, true);
+                        load_stage(t, ks, stage);
                         ++issued;
                     }
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }

@@ -3,8 +3,8 @@
 //
 // The work is reading the weights (N * K * 0.53 bytes); everything is laid out for that stream. The tensor cores take the weights
 // as their first operand (128 output channels = the rows of tcgen05.mma, M = 128) and the tokens as the second (N = 16 to 64),
-// so that a CTA streams 128 rows of W through a TMA ring whose first stages are requested before the kernel ahead has
-// finished (weights do not depend on it). K is cut over the CTAs of a cluster until the grid fills two CTAs an SM; the partial
+// so that a CTA streams 128 rows of W through a TMA ring whose first stages are prefetched into L2 before the kernel ahead has
+// finished (and read after it, since it may have written them). K is cut over the CTAs of a cluster until the grid fills two CTAs an SM; the partial
 // sums stay in the shared memory of their CTAs; each CTA reads the others' for its share of the tokens and adds them in the order of
 // the ranks (the result does not depend on timing). While the weights are on their way the other warps quantize the tokens'
 // k-blocks straight into the swizzled operand tile of the same ring stage. Accumulators are transposed (lane = output channel, column = token): they
@@ -124,37 +124,30 @@ mx_skinny_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         if (lane == 0) {
             const uint64_t once = l2_policy_evict_first();
             constexpr int BYTES = W_BYTES + SF_BYTES + (V::QUANT ? 0 : V::TOKEN_BYTES + SF_BYTES);
-            auto load_weights = [&](int kb, int stage) {
+            auto load = [&](int kb, int stage) {
                 const uint32_t s = base + stage * V::STAGE_BYTES;
                 mbar_arrive_expect_tx(full_bar(stage), BYTES);
                 tma_load_2d_hint(s, &tm_w, full_bar(stage), kb * BKB, n0, once);
                 tma_load_2d_hint(s + W_BYTES, &tm_sw, full_bar(stage), 0, n0 / kScaleTileRows * ktiles + 2 * kb, once);
-            };
-            auto load_tokens = [&](int kb, int stage) {
-                const uint32_t s = base + stage * V::STAGE_BYTES;
-                tma_load_2d(s + V::OFF_TOKENS, &tm_a, full_bar(stage), kb * BKB, 0);
-                tma_load_2d(s + V::OFF_TOKEN_SF, &tm_sa, full_bar(stage), 0, 2 * kb);
+                if (!V::QUANT) {
+                    tma_load_2d(s + V::OFF_TOKENS, &tm_a, full_bar(stage), kb * BKB, 0);
+                    tma_load_2d(s + V::OFF_TOKEN_SF, &tm_sa, full_bar(stage), 0, 2 * kb);
+                }
             };
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             bool withhold = a.starve != 0;
-            const int pre = withhold ? 0 : min(a.stages, kb1 - kb0);       // weights that do not wait for the kernel ahead
-            for (int i = 0; i < pre; ++i) load_weights(kb0 + i, i);
-            if (!V::QUANT) {
-                grid_dep_wait();
-                for (int i = 0; i < pre; ++i) load_tokens(kb0 + i, i);
+            // The weights of the first ring of stages are on their way to L2 while the kernel ahead finishes. They are read after
+            // it is complete, like everything else: it may be the one that writes them.
+            for (int kb = kb0; kb < min(kb1, kb0 + a.stages); ++kb) {
+                tma_prefetch_2d_hint(&tm_w, kb * BKB, n0, once);
+                tma_prefetch_2d_hint(&tm_sw, 0, n0 / kScaleTileRows * ktiles + 2 * kb, once);
             }
-            issued = pre;
-            if (pre == a.stages) phase = 1;
-            else stage = pre;
-            for (int kb = kb0 + pre; kb < kb1; ++kb) {
+            grid_dep_wait();
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (issued >= a.stages && !mbar_wait(empty_bar(stage), phase ^ 1u, ctl, W_EMPTY, kStatusTimeout)) break;
-                if (withhold) {
-                    withhold = false;          // test hook: this stage never arrives; the bounded waits run out
-                } else {
-                    load_weights(kb, stage);
-                    if (!V::QUANT) load_tokens(kb, stage);
-                }
+                if (withhold) withhold = false;          // test hook: this stage never arrives; the bounded waits run out
+                else load(kb, stage);
                 if (++stage == a.stages) { stage = 0; phase ^= 1u; }
                 ++issued;
             }

@@ -106,6 +106,12 @@ __device__ __forceinline__ void tma_store_2d_hint(const void* tmap, uint32_t sme
         "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%2, %3}], [%1], %4;"
         ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_src), "r"(x), "r"(y), "l"(policy) : "memory");
 }
+// Brings the box a load would read into L2. Not a read: L2 is where every writer's stores arrive, so a line fetched too early is
+// still updated by them, and it may be issued before the kernel ahead is complete.
+__device__ __forceinline__ void tma_prefetch_2d_hint(const void* tmap, int x, int y, uint64_t policy) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.L2::cache_hint [%0, {%1, %2}], %3;"
+                 ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "l"(policy) : "memory");
+}
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void bulk_wait_group_read() {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");

@@ -415,6 +415,54 @@ def test_linear_few_tokens_wait_runs_out(m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("writer", ["quantize", "kernel"])
+@pytest.mark.parametrize("m,config", [(1, -1), (6, -1), (14, -1), (40, -1), (300, 0), (300, 1), (300, 2)])
+def test_linear_reads_weights_written_just_ahead(m, config, writer):
+    """Weights rewritten by the kernel directly ahead of every call, through the quantizer or another kernel, bf16 tokens and codes: each call
+    sees its own weights, eagerly and in a graph."""
+    n, k = 4608, 2080
+    a, w, bias = operands(m, n, k)
+    both = [w, w.flip(0).contiguous()]
+    made = [w8.mxfp4_quantize(x) for x in both]
+    codes, scales = w8.mxfp4_quantize(a)
+    ws = w8.mxfp4_alloc_workspace(m, n, k)
+    qw, sw = (torch.zeros_like(t) for t in made[0])
+    mask = torch.zeros_like(qw), torch.zeros_like(sw)
+    w8.mxfp4_force_config(config)
+    try:
+        want = [w8.mxfp4_linear_fused(a, *made[i], bias, workspace=ws) for i in range(2)]
+        torch.cuda.synchronize()
+        outs = torch.zeros(24, m, n, dtype=torch.bfloat16, device="cuda")
+
+        def calls():
+            for i, out in enumerate(outs):
+                if writer == "quantize":
+                    w8.mxfp4_quantize(both[i % 2], codes=qw, scales=sw)
+                else:
+                    torch.bitwise_xor(made[i % 2][1], mask[1], out=sw)
+                    torch.bitwise_xor(made[i % 2][0], mask[0], out=qw)
+                if i % 4 < 2:
+                    w8.mxfp4_linear_fused(a, qw, sw, bias, out=out, workspace=ws)
+                else:
+                    w8.mxfp4_linear_fused(codes, qw, sw, bias, a_scales=scales, out=out, workspace=ws)
+
+        for _ in range(4):
+            outs.zero_()
+            calls()
+            assert all(torch.equal(out, want[i % 2]) for i, out in enumerate(outs))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+        for _ in range(4):
+            outs.zero_()
+            graph.replay()
+            assert all(torch.equal(out, want[i % 2]) for i, out in enumerate(outs))
+        assert w8.int8_check_status(ws) == 0
+    finally:
+        w8.mxfp4_force_config(-1)
+
+
+@pytest.mark.gpu
 def test_linear_random_shapes():
     import random
     r = random.Random(3)
