@@ -130,6 +130,8 @@ __device__ __forceinline__ void red_add_s32(int32_t* gdst, int32_t v) {
     asm volatile("red.relaxed.gpu.global.add.s32 [%0], %1;" ::"l"(gdst), "r"(v) : "memory");
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
+
 // 32 bytes of global memory at a time (32-byte aligned), past L1
 __device__ __forceinline__ void ldcg_32(const void* p, uint32_t* r) {
     asm volatile("ld.global.cg.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"

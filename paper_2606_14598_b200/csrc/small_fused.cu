@@ -5,9 +5,9 @@
 // scales are computed online, ahead of the GEMM). For a problem of one or a few tiles that second launch, and the
 // trip of the codes through global memory, are most of the time. Here every CTA owns 32 output channels, and the
 // CTAs of a cluster (up to 4) share the quantizer's work through distributed shared memory:
-//   1. a CTA requests its 32 x K slice of the int8 weights (plain 16-byte loads; the weights do not depend on the
-//      kernel ahead, so they are requested before the dependency wait) and, after the wait, its share of the rows
-//      of A (row r belongs to the CTA of rank r mod cluster size): both fetches are in flight together;
+//   1. a CTA prefetches its 32 x K slice of the int8 weights into L2 and, after the dependency wait, requests it (plain
+//      16-byte loads) and its share of the rows of A (row r belongs to the CTA of rank r mod cluster size): both fetches
+//      are in flight together;
 //   2. the weights go to shared memory in the 128-byte-swizzled K-major layout tcgen05.mma reads; every row of A is
 //      quantized by one warp, which writes the codes in the same layout into the operand tile of EVERY CTA of the
 //      cluster (st.shared::cluster), and the row's scale likewise; the first cluster also writes codes and scales
@@ -105,31 +105,37 @@ small_fused_kernel(const SmallArgs p) {
         dummy_status = 0;
         fence_mbar_init();
     }
-    // ---- request the CTA's weights: 32 rows x K bytes in 16-byte chunks (at most four per thread), zero beyond N and
-    // beyond K (which is what makes the bytes of A past K harmless). Weights are complete before the call is
-    // enqueued: no need to wait for the kernel ahead.
+    // ---- the CTA's weights: 32 rows x K bytes in 16-byte chunks (at most four per thread), brought into L2 while the kernel
+    // ahead finishes
     const int chunks_per_row = num_kb * 8;
     const int w_chunks = active ? SF_BN * chunks_per_row : 0;
-    uint4 wv[4];
+    const uint8_t* w_src[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const int i = threadIdx.x + t * SF_THREADS;
-        wv[t] = make_uint4(0, 0, 0, 0);
+        w_src[t] = nullptr;
         if (i < w_chunks) {
             const int n = i / chunks_per_row, ck = i - n * chunks_per_row;
-            if (n0 + n < N && ck * 16 < K)
-                wv[t] = __ldg(reinterpret_cast<const uint4*>(p.qw + static_cast<int64_t>(n0 + n) * K + ck * 16));
+            if (n0 + n < N && ck * 16 < K) w_src[t] = reinterpret_cast<const uint8_t*>(p.qw) + static_cast<int64_t>(n0 + n) * K + ck * 16;
         }
+        if (w_src[t] != nullptr) prefetch_l2(w_src[t]);
+    }
+    // This kernel may have been launched while the kernel ahead of it was still running (programmatic dependent
+    // launch): operands (the weights too, which it may write) are read only after that kernel is complete.
+    grid_dep_wait();
+    // weights beyond N and beyond K are zeros (which is what makes the bytes of A past K harmless)
+    uint4 wv[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        wv[t] = make_uint4(0, 0, 0, 0);
+        if (w_src[t] != nullptr) wv[t] = __ldcg(reinterpret_cast<const uint4*>(w_src[t]));
     }
     float my_sch = 0.f, my_bias = 0.f;
     if (threadIdx.x < SF_BN && active) {
         const int n = min(n0 + static_cast<int>(threadIdx.x), N - 1);
-        my_sch = __ldg(p.s_ch + n);
-        my_bias = p.bias != nullptr ? __ldg(p.bias + n) : 0.f;
+        my_sch = __ldcg(p.s_ch + n);
+        my_bias = p.bias != nullptr ? __ldcg(p.bias + n) : 0.f;
     }
-    // This kernel may have been launched while the kernel ahead of it was still running (programmatic dependent
-    // launch): the activations (and a handed-in absmax) are read only after that kernel is complete.
-    grid_dep_wait();
     if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
 
     // ---- quantize this CTA's share of the rows of A into the operand tile of every CTA of the cluster.
