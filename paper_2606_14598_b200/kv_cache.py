@@ -26,6 +26,12 @@ class QuantKVCache:
     [.., dim / 2] uint8 with scales uint8 [.., heads, ceil(dim / 32)]. The value side may be left out (None)."""
 
     def __init__(self, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor | None = None, v_scales: torch.Tensor | None = None):
+        self._tensors = (k_codes, k_scales, v_codes, v_scales)           # held for as long as the cache is, and not replaced
+        self._look_over()
+
+    def _look_over(self) -> None:
+        """Checks the tensors and notes what the calls need of them."""
+        k_codes, k_scales, v_codes, v_scales = self._tensors
         if k_codes.dim() != 4 or k_codes.dtype not in (torch.int8, torch.uint8):
             raise TypeError("codes: int8 or uint8 [num_pages, page_size, heads, ...] expected")
         self.fmt = KV_CACHE_INT8 if k_codes.dtype == torch.int8 else KV_CACHE_MXFP4
@@ -45,11 +51,19 @@ class QuantKVCache:
                 raise ValueError(f"{name}_codes: dense {k_codes.dtype} {tuple(k_codes.shape)} expected")
             if scales.dtype != dtype or tuple(scales.shape) != shape or not scales.is_contiguous():
                 raise ValueError(f"{name}_scales: dense {dtype} {shape} expected")
+            for what, t in (("codes", codes), ("scales", scales)):
+                if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
+                    raise ValueError(f"{name}_{what}: the tensor's memory has been given back")
         self.device, self.device_index = k_codes.device, k_codes.get_device()
         if any(t is not None and t.get_device() != self.device_index for t in (k_scales, v_codes, v_scales)):
             raise different_devices("QuantKVCache")
-        self._tensors = (k_codes, k_scales, v_codes, v_scales)           # held for as long as the cache is, and not replaced
         self._places = tuple(None if t is None else t.data_ptr() for t in self._tensors)
+
+    def places(self) -> tuple:
+        """The tensors' addresses now: a caller may have moved their storage (offloaded it, given a tensor other data)."""
+        if tuple(None if t is None else t.data_ptr() for t in self._tensors) != self._places:
+            self._look_over()
+        return self._places
 
     k_codes = property(lambda self: self._tensors[0])
     k_scales = property(lambda self: self._tensors[1])
@@ -89,11 +103,11 @@ def _vectors(cache: QuantKVCache, t: torch.Tensor, name: str, rows: int) -> tupl
 def kv_cache_write(cache: QuantKVCache, k: torch.Tensor, v: torch.Tensor | None, slots: torch.Tensor) -> None:
     """Quantizes k (and v) bf16 [T, heads, dim] into the cache at slots int64 [T]; slots outside the cache are skipped."""
     c = cache
+    kc, ks, vc, vs = c.places()
     if slots.dtype is not torch.int64 or slots.dim() != 1 or not slots.is_contiguous():
         raise TypeError("slots: dense int64 [tokens] expected")
     tokens = slots.shape[0]
     kp, kt, kh = _vectors(c, k, "k", tokens)
-    kc, ks, vc, vs = c._places
     if (v is None) != (vc is None):
         raise ValueError("v goes with a cache that keeps values, and only with one")
     vp, vt, vh = (None, 0, 0) if v is None else _vectors(c, v, "v", tokens)
@@ -120,7 +134,7 @@ def kv_cache_read(cache: QuantKVCache, table: torch.Tensor, cu_seqlens: torch.Te
     if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (seqs,) or not starts.is_contiguous()):
         raise TypeError("starts: dense int32 [sequences] expected")
     c = cache
-    kc, ks, vc, vs = c._places
+    kc, ks, vc, vs = c.places()
     dev = c.device_index
     if v_out is not None and vc is None:
         raise ValueError("v_out goes with a cache that keeps values")

@@ -82,6 +82,47 @@ def test_python_refusals():
         w8.kv_cache_read(c, table, cu, 3, k_out=torch.zeros(2, 3, 16, dtype=torch.bfloat16))
 
 
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_storage_moved_after_the_cache_was_made(monkeypatch, fmt):
+    """The calls get the addresses that the tensors have at the time of the call, and sizes that go with them; memory that has been given
+    back is refused. (The calls themselves are recorded: no GPU.)"""
+    seen = []
+    monkeypatch.setattr(kv_cache, "call", lambda fn, where, dev, *args: seen.append((where, args)))
+    c = w8.QuantKVCache.empty(2, 4, 3, 16, fmt, device="cpu")
+    k, slots = torch.zeros(5, 3, 16, dtype=torch.bfloat16), torch.arange(5)
+    table, cu = torch.zeros(1, 2, dtype=torch.int32), torch.tensor([0, 5], dtype=torch.int32)
+
+    def places():
+        seen.clear()
+        w8.kv_cache_write(c, k, k, slots)
+        w8.kv_cache_read(c, table, cu, 5)
+        (_, write), (_, read) = seen
+        assert write[11:15] == read[1:5] and write[15] == read[5] * read[6] == c.num_pages * c.page_size
+        return write[11:15]
+
+    def now():
+        return tuple(t.data_ptr() for t in (c.k_codes, c.k_scales, c.v_codes, c.v_scales))
+
+    assert places() == now()
+    old = c.k_codes.data
+    c.k_codes.data = old.clone()
+    assert c.k_codes.data_ptr() != old.data_ptr() and places() == now()
+    keep = c.v_scales.clone()
+    size = c.v_scales.untyped_storage().nbytes()
+    c.v_scales.untyped_storage().resize_(0)
+    with pytest.raises(ValueError):
+        places()
+    c.v_scales.untyped_storage().resize_(size)
+    c.v_scales.copy_(keep)
+    assert places() == now()
+    for t in (c.k_codes, c.k_scales, c.v_codes, c.v_scales):                # grown by a page
+        t.data = torch.cat([t, t[:1]])
+    assert places() == now() and c.num_pages == 3
+    c.k_scales.data = c.k_scales[:2].clone()
+    with pytest.raises(ValueError):
+        places()
+
+
 # ------------------------------------------------------------------------------------------ on the GPU
 
 def random_cache(fmt, pages, page, heads, dim, values=True):
