@@ -24,6 +24,7 @@ extern "C" {
 #endif
 
 enum { KV_CACHE_INT8 = 0, KV_CACHE_MXFP4 = 1 };
+enum { KV_CACHE_ZERO_REST = 0x100 }; /* or'd into the fmt of a read */
 #define KV_CACHE_MAX_DIM 256
 #define KV_CACHE_MAX_WIDTH 65536 /* heads * dim */
 
@@ -42,7 +43,8 @@ int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_hea
  *   table       int32 [seqs, max_pages]; a page outside [0, num_pages), or a token past max_pages, reads as zeros
  *   cu_seqlens  int32 [seqs + 1], not decreasing; empty sequences are fine
  *   starts      int32 [seqs] or NULL: the first token to read of each sequence (a window's)
- *   total       rows of the outputs (<= 2^31 - 1); rows past cu_seqlens[seqs] are left as they are
+ *   total       rows of the outputs (<= 2^31 - 1); rows that belong to no sequence (before cu_seqlens[0], from cu_seqlens[seqs]
+ *               on) are left as they are, or written as zeros with KV_CACHE_ZERO_REST
  *   k_out, v_out  bf16 [total, heads, dim] with their strides
  */
 int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int64_t num_pages, int64_t page_size,

@@ -179,7 +179,7 @@ __device__ __forceinline__ uint4 int8_values8(uint2 c, float s) {
 template <int FMT, bool VALUES>
 __global__ void __launch_bounds__(kThreads, 4)
 kv_read_kernel(const Side k, const Side v, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* cu, const int32_t* starts, int seqs,
-               int64_t total, int64_t num_pages, int page, int heads, int dim, int tile, const Cover cover) {
+               int64_t total, int64_t num_pages, int page, int heads, int dim, int zero_rest, int tile, const Cover cover) {
     constexpr int UNROLL = 4, SIDES = VALUES ? 2 : 1;
     grid_dep_wait();
     __shared__ int64_t slots[kMaxTile];                           // cache row of each token of the tile, -1: reads as zeros, -2: left alone
@@ -216,7 +216,7 @@ kv_read_kernel(const Side k, const Side v, const int32_t* table, int64_t table_s
                 begin = end;
                 if (++b < seqs) end = __ldcg(cu + b + 1);
             }
-            int64_t row = -2;
+            int64_t row = zero_rest ? -1 : -2;                    // of no sequence
             if (b < seqs) {
                 if (t >= begin) {
                     const int64_t at = t - begin + (starts != nullptr ? __ldcg(starts + b) : 0);
@@ -354,6 +354,8 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
                   int64_t heads, int64_t dim, const int32_t* table, int64_t table_stride, int64_t max_pages, const int32_t* cu_seqlens,
                   const int32_t* starts, int64_t seqs, int64_t total, void* k_out, int64_t k_token_stride, int64_t k_head_stride, void* v_out,
                   int64_t v_token_stride, int64_t v_head_stride, void* stream) {
+    const bool zero_rest = (fmt & KV_CACHE_ZERO_REST) != 0;
+    fmt &= ~KV_CACHE_ZERO_REST;
     if (int e = check_shape(fmt, heads, dim)) return e;
     if (num_pages < 0 || page_size <= 0 || page_size > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || table_stride < max_pages || seqs < 0 ||
         seqs > INT32_MAX - 1 || total < 0 || total > INT32_MAX || k_out == nullptr || (seqs > 0 && cu_seqlens == nullptr) ||
@@ -367,7 +369,7 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
         if (!aligned(v_out, 16) || v_token_stride % 8 != 0 || v_head_stride % 8 != 0) return W8A8_ERR_ALIGNMENT;
     }
     if (int e = check_arch()) return e;
-    if (total == 0 || seqs == 0) return W8A8_OK;
+    if (total == 0 || (seqs == 0 && !zero_rest)) return W8A8_OK;
     Side ks{}, vs{};
     ks.codes = static_cast<uint8_t*>(const_cast<void*>(k_codes));
     ks.scales = const_cast<void*>(k_scales);
@@ -385,7 +387,7 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
                                            : (v_out != nullptr ? kv_read_kernel<KV_CACHE_MXFP4, true> : kv_read_kernel<KV_CACHE_MXFP4, false>);
     const cudaError_t e = launch_pdl(kern, grid_for(total, tile, cover), cover.threads, static_cast<cudaStream_t>(stream), ks, vs, table, table_stride,
                                      static_cast<int>(max_pages), cu_seqlens, starts, static_cast<int>(seqs), total, num_pages, static_cast<int>(page_size),
-                                     static_cast<int>(heads), static_cast<int>(dim), tile, cover);
+                                     static_cast<int>(heads), static_cast<int>(dim), zero_rest ? 1 : 0, tile, cover);
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }
 

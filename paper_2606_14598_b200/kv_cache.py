@@ -13,6 +13,7 @@ from .mxfp4 import call, different_devices
 
 KV_CACHE_INT8, KV_CACHE_MXFP4 = 0, 1
 KV_CACHE_MAX_DIM = 256
+KV_CACHE_ZERO_REST = 0x100
 
 _lib.kv_cache_write.argtypes = [_int, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp]
 _lib.kv_cache_write.restype = _int
@@ -122,7 +123,8 @@ def kv_cache_write(cache: QuantKVCache, k: torch.Tensor, v: torch.Tensor | None,
 def kv_cache_read(cache: QuantKVCache, table: torch.Tensor, cu_seqlens: torch.Tensor, total: int, starts: torch.Tensor | None = None,
                   k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
     """The sequences' tokens as bf16 [total, heads, dim], one sequence after another: (k, v), or (k, None) without values.
-    table int32 [B, max_pages], cu_seqlens int32 [B + 1], starts int32 [B] (first token to read of each) or None."""
+    table int32 [B, max_pages], cu_seqlens int32 [B + 1], starts int32 [B] (first token to read of each) or None. Rows that belong to
+    no sequence (total may be more than cu_seqlens[-1]) are zeros, in k_out and v_out they are left as they are."""
     if table.dtype is not torch.int32 or table.dim() != 2:
         raise TypeError("table: int32 [sequences, max_pages] expected")
     seqs, max_pages = table.shape
@@ -139,22 +141,25 @@ def kv_cache_read(cache: QuantKVCache, table: torch.Tensor, cu_seqlens: torch.Te
     if v_out is not None and vc is None:
         raise ValueError("v_out goes with a cache that keeps values")
     dense = c.heads * c.dim
+    # where both sides are allocated here the kernel writes the rows of no sequence too
+    fill = k_out is None and (vc is None or v_out is None)
+    new = torch.empty if fill else torch.zeros
     if k_out is None:
-        k_out = torch.empty(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
+        k_out = new(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
         kp, kt, kh = k_out.data_ptr(), dense, c.dim
     else:
         kp, kt, kh = _vectors(c, k_out, "k_out", total)
     if vc is None:
         vp, vt, vh = None, 0, 0
     elif v_out is None:
-        v_out = torch.empty(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
+        v_out = new(total, c.heads, c.dim, dtype=torch.bfloat16, device=c.device)
         vp, vt, vh = v_out.data_ptr(), dense, c.dim
     else:
         vp, vt, vh = _vectors(c, v_out, "v_out", total)
     if table.get_device() != dev or cu_seqlens.get_device() != dev or (starts is not None and starts.get_device() != dev):
         raise different_devices("kv_cache_read")
-    if total == 0 or seqs == 0:
+    if total == 0 or (seqs == 0 and not fill):
         return k_out, v_out
-    call(_lib.kv_cache_read, "kv_cache_read", dev, c.fmt, kc, ks, vc, vs, c.num_pages, c.page_size, c.heads, c.dim, table.data_ptr(),
+    call(_lib.kv_cache_read, "kv_cache_read", dev, c.fmt | (KV_CACHE_ZERO_REST if fill else 0), kc, ks, vc, vs, c.num_pages, c.page_size, c.heads, c.dim, table.data_ptr(),
          row if seqs > 1 else max_pages, max_pages, cu_seqlens.data_ptr(), None if starts is None else starts.data_ptr(), seqs, total, kp, kt, kh, vp, vt, vh)
     return k_out, v_out

@@ -297,6 +297,43 @@ def test_one_sided_cache_empty_calls_and_graph(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("values", [True, False])
+def test_rows_of_no_sequence(fmt, values):
+    """A total beyond the sequences, sequences that begin behind row 0, no sequences at all: the other rows are zeros in outputs that the
+    call allocates, and stay as they are in the caller's."""
+    heads, dim, total = 3, 72, 300
+    c = random_cache(fmt, 20, 16, heads, dim, values=values)
+    table = torch.randperm(20, device="cuda").int().view(2, 10)
+
+    def soil():                                                      # blocks that the allocations below get hold NaN
+        for _ in range(4):
+            torch.full((total, heads, dim), float("nan"), device="cuda", dtype=torch.bfloat16)
+
+    for begin, lens in ((0, [30, 150]), (17, [100, 1]), (5, [0, 0])):
+        cu = torch.tensor([begin, begin + lens[0], begin + sum(lens)], dtype=torch.int32, device="cuda")
+        end = begin + sum(lens)
+        soil()
+        got = w8.kv_cache_read(c, table, cu, total)
+        for out, codes, scales in ((got[0], c.k_codes, c.k_scales), (got[1], c.v_codes, c.v_scales)):
+            if codes is None:
+                assert out is None
+                continue
+            assert (out[:begin] == 0).all() and (out[end:] == 0).all()
+            assert ref.same_values(out[begin:end], expected_read(fmt, codes, scales, table, lens, [0, 0], 16))
+        soil()
+        mine = torch.full((total, heads, dim), 5.0, device="cuda", dtype=torch.bfloat16)
+        again = w8.kv_cache_read(c, table, cu, total, k_out=mine)
+        assert again[0] is mine and torch.equal(mine[begin:end], got[0][begin:end]) and (mine[:begin] == 5).all() and (mine[end:] == 5).all()
+        assert not values or torch.equal(again[1], got[1])
+    soil()
+    none = w8.kv_cache_read(c, table[:0], cu[:1], total)
+    assert (none[0] == 0).all() and (none[1] is None if not values else (none[1] == 0).all())
+    w8.kv_cache_read(c, table[:0], cu[:1], total, k_out=mine.fill_(5.0))
+    assert (mine == 5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
 def test_offsets_past_32_bits(fmt):
     heads, dim, page = 64, 256, 64
     pages = ((1 << 32) // (heads * dim * page // (1 if fmt == "int8" else 2))) + 3        # the codes pass 2^32 bytes
