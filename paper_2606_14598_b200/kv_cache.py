@@ -58,11 +58,15 @@ class QuantKVCache:
         self.device, self.device_index = k_codes.device, k_codes.get_device()
         if any(t is not None and t.get_device() != self.device_index for t in (k_scales, v_codes, v_scales)):
             raise different_devices("QuantKVCache")
-        self._places = tuple(None if t is None else t.data_ptr() for t in self._tensors)
+        self._places = self._now()
+
+    def _now(self) -> tuple:
+        k_codes, k_scales, v_codes, v_scales = self._tensors
+        return k_codes.data_ptr(), k_scales.data_ptr(), None if v_codes is None else v_codes.data_ptr(), None if v_scales is None else v_scales.data_ptr()
 
     def places(self) -> tuple:
         """The tensors' addresses now: a caller may have moved their storage (offloaded it, given a tensor other data)."""
-        if tuple(None if t is None else t.data_ptr() for t in self._tensors) != self._places:
+        if self._now() != self._places:
             self._look_over()
         return self._places
 
