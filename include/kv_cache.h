@@ -30,7 +30,7 @@ enum { KV_CACHE_ZERO_REST = 0x100 }; /* or'd into the fmt of a read */
 
 /*
  * Quantizes `tokens` tokens into their slots. slots: int64 [tokens], device; one outside [0, num_slots) is skipped (-1 for
- * padding tokens). Slots of one call must be distinct. No tokens is a valid call.
+ * padding tokens). Slots of one call must be distinct. No tokens and a cache of no slots are valid calls; their pointers may be NULL.
  */
 int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
                    int64_t v_head_stride, const int64_t* slots, int64_t tokens, int64_t heads, int64_t dim, void* k_codes, void* k_scales,
@@ -46,6 +46,7 @@ int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_hea
  *   total       rows of the outputs (<= 2^31 - 1); rows that belong to no sequence (before cu_seqlens[0], from cu_seqlens[seqs]
  *               on) are left as they are, or written as zeros with KV_CACHE_ZERO_REST
  *   k_out, v_out  bf16 [total, heads, dim] with their strides
+ * No rows, no sequences and a cache of no pages are valid calls; pointers to what has no elements may be NULL.
  */
 int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int64_t num_pages, int64_t page_size,
                   int64_t heads, int64_t dim, const int32_t* table, int64_t table_stride, int64_t max_pages, const int32_t* cu_seqlens,

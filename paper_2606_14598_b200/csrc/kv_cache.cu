@@ -298,8 +298,8 @@ int check_shape(int fmt, int64_t heads, int64_t dim) {
     return dim % 8 == 0 ? W8A8_OK : W8A8_ERR_ALIGNMENT;
 }
 
-int check_store(int fmt, const void* codes, const void* scales) {
-    if (codes == nullptr || scales == nullptr) return W8A8_ERR_INVALID_ARG;
+int check_store(int fmt, const void* codes, const void* scales, int64_t places) {
+    if (places > 0 && (codes == nullptr || scales == nullptr)) return W8A8_ERR_INVALID_ARG;
     if (!aligned(codes, 16) || !aligned(scales, fmt == KV_CACHE_INT8 ? 4 : 1)) return W8A8_ERR_ALIGNMENT;
     return W8A8_OK;
 }
@@ -315,11 +315,11 @@ int kv_cache_write(int fmt, const void* k, int64_t k_token_stride, int64_t k_hea
                    int64_t v_head_stride, const int64_t* slots, int64_t tokens, int64_t heads, int64_t dim, void* k_codes, void* k_scales,
                    void* v_codes, void* v_scales, int64_t num_slots, void* stream) {
     if (int e = check_shape(fmt, heads, dim)) return e;
-    if (tokens < 0 || num_slots < 0 || k == nullptr || (tokens > 0 && slots == nullptr)) return W8A8_ERR_INVALID_ARG;
-    if (int e = check_store(fmt, k_codes, k_scales)) return e;
+    if (tokens < 0 || num_slots < 0 || (tokens > 0 && (k == nullptr || slots == nullptr))) return W8A8_ERR_INVALID_ARG;
+    if (int e = check_store(fmt, k_codes, k_scales, num_slots)) return e;
     if (!aligned(k, 16) || k_token_stride % 8 != 0 || k_head_stride % 8 != 0 || !aligned(slots, 8)) return W8A8_ERR_ALIGNMENT;
     if (v != nullptr) {
-        if (int e = check_store(fmt, v_codes, v_scales)) return e;
+        if (int e = check_store(fmt, v_codes, v_scales, num_slots)) return e;
         if (!aligned(v, 16) || v_token_stride % 8 != 0 || v_head_stride % 8 != 0) return W8A8_ERR_ALIGNMENT;
     }
     if (int e = check_arch()) return e;
@@ -358,14 +358,14 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
     fmt &= ~KV_CACHE_ZERO_REST;
     if (int e = check_shape(fmt, heads, dim)) return e;
     if (num_pages < 0 || page_size <= 0 || page_size > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || table_stride < max_pages || seqs < 0 ||
-        seqs > INT32_MAX - 1 || total < 0 || total > INT32_MAX || k_out == nullptr || (seqs > 0 && cu_seqlens == nullptr) ||
+        seqs > INT32_MAX - 1 || total < 0 || total > INT32_MAX || (total > 0 && k_out == nullptr) || (seqs > 0 && cu_seqlens == nullptr) ||
         (seqs > 0 && max_pages > 0 && table == nullptr))
         return W8A8_ERR_INVALID_ARG;
-    if (int e = check_store(fmt, k_codes, k_scales)) return e;
+    if (int e = check_store(fmt, k_codes, k_scales, num_pages)) return e;
     if (!aligned(k_out, 16) || k_token_stride % 8 != 0 || k_head_stride % 8 != 0 || !aligned(table, 4) || !aligned(cu_seqlens, 4) || !aligned(starts, 4))
         return W8A8_ERR_ALIGNMENT;
     if (v_out != nullptr) {
-        if (int e = check_store(fmt, v_codes, v_scales)) return e;
+        if (int e = check_store(fmt, v_codes, v_scales, num_pages)) return e;
         if (!aligned(v_out, 16) || v_token_stride % 8 != 0 || v_head_stride % 8 != 0) return W8A8_ERR_ALIGNMENT;
     }
     if (int e = check_arch()) return e;

@@ -82,6 +82,22 @@ def test_python_refusals():
         w8.kv_cache_read(c, table, cu, 3, k_out=torch.zeros(2, 3, 16, dtype=torch.bfloat16))
 
 
+def test_calls_on_nothing_are_not_refused():
+    """No tokens, no slots, no rows, no pages: whatever has no elements may be NULL (a tensor without elements has no address). None of
+    these calls launches anything; without a GPU they end at the check of the device."""
+    write, read = kv_cache._lib.kv_cache_write, kv_cache._lib.kv_cache_read
+    p = P(4096)
+    assert write(0, None, 0, 0, None, 0, 0, None, 0, 2, 64, p, p, None, None, 32, None) not in (INVALID, ALIGNMENT)
+    assert write(1, p, 128, 64, p, 128, 64, p, 3, 2, 64, None, None, None, None, 0, None) not in (INVALID, ALIGNMENT)
+    assert write(1, None, 0, 0, None, 0, 0, None, 0, 2, 64, None, None, None, None, 0, None) not in (INVALID, ALIGNMENT)
+    assert read(0, p, p, p, p, 4, 16, 2, 64, p, 3, 3, p, None, 2, 0, None, 0, 0, None, 0, 0, None) not in (INVALID, ALIGNMENT)
+    assert read(1, None, None, None, None, 0, 16, 2, 64, p, 3, 3, p, None, 2, 0, None, 0, 0, None, 0, 0, None) not in (INVALID, ALIGNMENT)
+    # what has elements is still needed
+    assert write(0, None, 0, 0, None, 0, 0, p, 1, 2, 64, p, p, None, None, 32, None) == INVALID
+    assert write(0, None, 0, 0, None, 0, 0, None, 0, 2, 64, None, p, None, None, 32, None) == INVALID
+    assert read(0, None, p, None, None, 4, 16, 2, 64, p, 3, 3, p, None, 2, 0, None, 0, 0, None, 0, 0, None) == INVALID
+
+
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
 def test_storage_moved_after_the_cache_was_made(monkeypatch, fmt):
     """The calls get the addresses that the tensors have at the time of the call, and sizes that go with them; memory that has been given
@@ -330,6 +346,18 @@ def test_rows_of_no_sequence(fmt, values):
     assert (none[0] == 0).all() and (none[1] is None if not values else (none[1] == 0).all())
     w8.kv_cache_read(c, table[:0], cu[:1], total, k_out=mine.fill_(5.0))
     assert (mine == 5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_cache_without_pages(fmt):
+    c = w8.QuantKVCache.empty(0, 16, 2, 64, fmt)
+    x = torch.randn(5, 2, 64, device="cuda").bfloat16()
+    w8.kv_cache_write(c, x, x, torch.arange(5, device="cuda"))                 # no slot is inside
+    cu = torch.tensor([0, 5], dtype=torch.int32, device="cuda")
+    for table in (torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, 0, dtype=torch.int32, device="cuda")):
+        k, v = w8.kv_cache_read(c, table, cu, 5)
+        assert (k == 0).all() and (v == 0).all()
 
 
 @pytest.mark.gpu
