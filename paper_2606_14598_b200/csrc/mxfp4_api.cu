@@ -83,6 +83,8 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     if (!aligned16(A) || !aligned16(a_scales) || !aligned16(qw) || !aligned16(sw) || !aligned16(out) || !aligned16(bias)) return W8A8_ERR_ALIGNMENT;
     const size_t need = a_dtype == MXFP4_BF16 ? mxfp4_linear_workspace_bytes(M, N, K) : kStatusBlock;
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < need) return W8A8_ERR_WORKSPACE;
+    const int forced = g_forced_config.load();
+    if (forced < -1 || forced > kMxGemmConfigs || (forced == kMxGemmConfigs && !mx_skinny_fits(static_cast<int>(M)))) return W8A8_ERR_INVALID_ARG;
     if (int e = check_arch()) return e;
 
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -91,8 +93,6 @@ int mxfp4_linear_fused(const void* A, int a_dtype, int64_t lda, const uint8_t* a
     g.qw = qw; g.sw = sw; g.bias = bias; g.out = out; g.ldo = ldo;
     g.M = static_cast<int>(M); g.N = static_cast<int>(N); g.K = static_cast<int>(K);
     g.status = reinterpret_cast<int*>(ws);
-    const int forced = g_forced_config.load();
-    if (forced > kMxGemmConfigs || (forced == kMxGemmConfigs && !mx_skinny_fits(g.M))) return W8A8_ERR_INVALID_ARG;
     const bool skinny = forced == kMxGemmConfigs || (forced < 0 && mx_skinny_preferred(g.M, g.K));
     if (skinny && a_dtype == MXFP4_BF16 && g.M <= kQuantizeInside) return launch_mx_skinny_bf16(g, A, lda, st);
     if (a_dtype == MXFP4_BF16) {

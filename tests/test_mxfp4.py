@@ -70,6 +70,22 @@ def test_linear_refusals():
     assert status(ws=None) == WORKSPACE and status(ws=P(4096 + 128)) == WORKSPACE and status(ws_bytes=256) == WORKSPACE
 
 
+def test_unknown_configurations_are_refused():
+    """Ids other than -1 (automatic) and those of the kernels; the few-token kernel with too many tokens. Refused before the device is looked at."""
+    f = mxfp4._lib.mxfp4_linear_fused
+
+    def status(config, m):
+        old = w8.mxfp4_force_config(config)
+        try:
+            return f(P(4096), 0, 64, None, P(8192), P(8192), None, P(4096), 16, m, 16, 64, P(4096), 1 << 20, None)
+        finally:
+            assert w8.mxfp4_force_config(old) == config
+
+    for config in (-2, -1000, w8.MXFP4_NUM_CONFIGS + 1, 1000):
+        assert status(config, 4) == INVALID, config
+    assert status(w8.MXFP4_NUM_CONFIGS, 65) == INVALID
+
+
 def test_python_refusals():
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
     with pytest.raises(TypeError):
