@@ -185,6 +185,8 @@ def mxfp4_linear_fused(A: torch.Tensor, qw: torch.Tensor, sw: torch.Tensor, bias
             raise different_devices("mxfp4_linear_fused")
     if workspace is None:
         workspace = mxfp4_alloc_workspace(M, N, K, A.device)
+    elif not workspace.is_contiguous():
+        raise TypeError("workspace: dense tensor expected")          # (its size is what the kernels may write)
     elif workspace.get_device() != dev:
         raise different_devices("mxfp4_linear_fused")
     if qw.get_device() != dev or sw.get_device() != dev:

@@ -86,6 +86,20 @@ def test_unknown_configurations_are_refused():
     assert status(w8.MXFP4_NUM_CONFIGS, 65) == INVALID
 
 
+def test_workspace_whose_memory_is_smaller_than_its_shape_is_refused(monkeypatch):
+    """An expanded or strided tensor counts more bytes than it owns in one piece. (The call is recorded: no GPU.)"""
+    seen = []
+    monkeypatch.setattr(mxfp4, "call", lambda fn, where, dev, *args: seen.append(args))
+    x, codes, scales = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(16, 32, dtype=torch.uint8), torch.zeros(1, 1, 512, dtype=torch.uint8)
+    need = w8.mxfp4_linear_workspace_bytes(4, 16, 64)
+    for workspace in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2], torch.zeros(4, need, dtype=torch.uint8).t()):
+        with pytest.raises(TypeError):
+            w8.mxfp4_linear_fused(x, codes, scales, workspace=workspace)
+    assert not seen
+    w8.mxfp4_linear_fused(x, codes, scales, workspace=torch.zeros(need + 64, dtype=torch.uint8))
+    assert seen[0][-1] == need + 64
+
+
 def test_python_refusals():
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
     with pytest.raises(TypeError):
