@@ -112,8 +112,12 @@ def _ptr(t: torch.Tensor | None):
     return None if t is None else t.data_ptr()
 
 
+# The handle of a device's current stream; torch's own short way to it where it has one.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _stream(t: torch.Tensor):
-    return torch.cuda.current_stream(t.device).cuda_stream if t.is_cuda else None
+    return _raw_stream(t.get_device()) if t.is_cuda else None
 
 
 def _need(t: torch.Tensor, dtype, name: str, ndim: int):
@@ -123,6 +127,28 @@ def _need(t: torch.Tensor, dtype, name: str, ndim: int):
         raise TypeError(f"{name}: rows must be contiguous")
     if ndim == 1 and t.numel() > 1 and t.stride(0) != 1:
         raise TypeError(f"{name}: must be contiguous")
+
+
+def _shaped(t: torch.Tensor, dtype, name: str, *shape: int):
+    """_need, and this shape: the kernels go by the sizes of A and qw."""
+    _need(t, dtype, name, len(shape))
+    if t.shape != shape:
+        raise ValueError(f"{name}: {list(shape)} expected, got {list(t.shape)}")
+
+
+def _dense(t: torch.Tensor, name: str):
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be dense")
+
+
+def _together(where: str, first: torch.Tensor, *others: torch.Tensor | None):
+    """All on the CUDA device of the first: the kernels take the addresses as they are."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError(f"{where}: tensors must be on a CUDA device")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{where}: tensors are on different devices")
 
 
 def status_string(status: int) -> str:
@@ -148,6 +174,7 @@ def int8_quantize_weight_per_channel(W: torch.Tensor):
     N, K = W.shape
     qw = torch.empty((N, K), dtype=torch.int8, device=W.device)
     s_ch = torch.empty((N,), dtype=torch.float32, device=W.device)
+    _together("int8_quantize_weight_per_channel", W)
     _check(_lib.int8_quantize_weight_per_channel(_ptr(W), N, K, W.stride(0), _ptr(qw), _ptr(s_ch), _stream(W)),
            "int8_quantize_weight_per_channel")
     return qw, s_ch
@@ -161,6 +188,10 @@ def int8_quantize_act_per_token(A: torch.Tensor, qa: torch.Tensor | None = None,
         qa = torch.empty((M, K), dtype=torch.int8, device=A.device)
     if s_tok is None:
         s_tok = torch.empty((M,), dtype=torch.float32, device=A.device)
+    _shaped(qa, torch.int8, "qa", M, K)
+    _dense(qa, "qa")
+    _shaped(s_tok, torch.float32, "s_tok", M)
+    _together("int8_quantize_act_per_token", A, qa, s_tok)
     _check(_lib.int8_quantize_act_per_token(_ptr(A), M, K, A.stride(0), _ptr(qa), _ptr(s_tok), _stream(A)),
            "int8_quantize_act_per_token")
     return qa, s_tok
@@ -175,6 +206,7 @@ def int8_quantize_weight_per_channel_smooth(W: torch.Tensor, w_mult: torch.Tenso
         raise ValueError("w_mult must have K entries")
     qw = torch.empty((N, K), dtype=torch.int8, device=W.device)
     s_ch = torch.empty((N,), dtype=torch.float32, device=W.device)
+    _together("int8_quantize_weight_per_channel_smooth", W, w_mult)
     _check(_lib.int8_quantize_weight_per_channel_smooth(_ptr(W), N, K, W.stride(0), _ptr(w_mult), _ptr(qw), _ptr(s_ch),
                                                         _stream(W)), "int8_quantize_weight_per_channel_smooth")
     return qw, s_ch
@@ -189,6 +221,7 @@ def int8_quantize_act_per_token_smooth(A: torch.Tensor, a_mult: torch.Tensor):
         raise ValueError("a_mult must have K entries")
     qa = torch.empty((M, K), dtype=torch.int8, device=A.device)
     s_tok = torch.empty((M,), dtype=torch.float32, device=A.device)
+    _together("int8_quantize_act_per_token_smooth", A, a_mult)
     _check(_lib.int8_quantize_act_per_token_smooth(_ptr(A), M, K, A.stride(0), _ptr(a_mult), _ptr(qa), _ptr(s_tok),
                                                    _stream(A)), "int8_quantize_act_per_token_smooth")
     return qa, s_tok
@@ -207,11 +240,14 @@ def int8_linear_fused_smooth(A: torch.Tensor, a_mult: torch.Tensor, qw: torch.Te
     if qw.shape[1] != K or s_ch.shape[0] != N or a_mult.shape[0] != K or not qw.is_contiguous():
         raise ValueError("shape mismatch")
     if bias is not None:
-        _need(bias, torch.float32, "bias", 1)
+        _shaped(bias, torch.float32, "bias", N)
     if out is None:
         out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = alloc_workspace(M, N, K, ACT_BF16, A.device)
+    _shaped(out, torch.bfloat16, "out", M, N)
+    _dense(workspace, "workspace")
+    _together("int8_linear_fused_smooth", A, a_mult, qw, s_ch, bias, out, workspace)
     _check(_lib.int8_linear_fused_smooth(_ptr(A), A.stride(0), _ptr(a_mult), _ptr(qw), _ptr(s_ch), _ptr(bias), _ptr(out),
                                          out.stride(0), M, N, K, _ptr(workspace), workspace.numel(), _stream(A)),
            "int8_linear_fused_smooth")
@@ -227,6 +263,7 @@ def int8_quantize_act_per_token_given_absmax(A: torch.Tensor, rowmax: torch.Tens
         raise ValueError("rowmax must have M entries")
     qa = torch.empty((M, K), dtype=torch.int8, device=A.device)
     s_tok = torch.empty((M,), dtype=torch.float32, device=A.device)
+    _together("int8_quantize_act_per_token_given_absmax", A, rowmax)
     _check(_lib.int8_quantize_act_per_token_given_absmax(_ptr(A), M, K, A.stride(0), _ptr(rowmax), _ptr(qa), _ptr(s_tok),
                                                          _stream(A)), "int8_quantize_act_per_token_given_absmax")
     return qa, s_tok
@@ -246,11 +283,16 @@ def int8_linear_fused_rowmax(A: torch.Tensor, qw: torch.Tensor, s_ch: torch.Tens
     if qw.shape[1] != K or s_ch.shape[0] != N or not qw.is_contiguous():
         raise ValueError("shape mismatch")
     if bias is not None:
-        _need(bias, torch.float32, "bias", 1)
+        _shaped(bias, torch.float32, "bias", N)
     if out is None:
         out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = alloc_workspace(M, N, K, a_dtype, A.device)
+    if s_tok is not None:
+        _shaped(s_tok, torch.float32, "s_tok", M)
+    _shaped(out, torch.bfloat16, "out", M, N)
+    _dense(workspace, "workspace")
+    _together("int8_linear_fused_rowmax", A, qw, s_ch, bias, s_tok, out, workspace, rowmax_in)
     rowmax = torch.empty((M,), dtype=torch.float32, device=A.device)
     if rowmax_in is None:
         _check(_lib.int8_linear_fused_rowmax(_ptr(A), a_dtype, A.stride(0), _ptr(s_tok), _ptr(qw), _ptr(s_ch), _ptr(bias),
@@ -316,14 +358,16 @@ def int8_linear_fused(A: torch.Tensor, qw: torch.Tensor, s_ch: torch.Tensor, bia
     if qw.shape[1] != K or s_ch.shape[0] != N:
         raise ValueError("shape mismatch")
     if bias is not None:
-        _need(bias, torch.float32, "bias", 1)
+        _shaped(bias, torch.float32, "bias", N)
     if s_tok is not None:
-        _need(s_tok, torch.float32, "s_tok", 1)
+        _shaped(s_tok, torch.float32, "s_tok", M)
     if out is None:
         out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
-    _need(out, torch.bfloat16, "out", 2)
+    _shaped(out, torch.bfloat16, "out", M, N)
     if workspace is None:
         workspace = alloc_workspace(M, N, K, a_dtype, A.device)
+    _dense(workspace, "workspace")
+    _together("int8_linear_fused", A, qw, s_ch, bias, s_tok, out, workspace)
     _check(_lib.int8_linear_fused(_ptr(A), a_dtype, A.stride(0), _ptr(s_tok), _ptr(qw), _ptr(s_ch), _ptr(bias),
                                   _ptr(out), out.stride(0), M, N, K, _ptr(workspace), workspace.numel(), _stream(A)),
            "int8_linear_fused")
@@ -336,6 +380,15 @@ def int8_linear_fused_host(A_host: torch.Tensor, d_A: torch.Tensor, qw: torch.Te
     """Host-buffer variant: A_host/out_host are (pinned) CPU bf16 tensors, the rest device tensors."""
     M, K = A_host.shape
     N = qw.shape[0]
+    _shaped(qw, torch.int8, "qw", N, K)
+    _dense(qw, "qw")
+    _shaped(s_ch, torch.float32, "s_ch", N)
+    if bias is not None:
+        _shaped(bias, torch.float32, "bias", N)
+    for name, t, width in (("A_host", A_host, K), ("d_A", d_A, K), ("d_out", d_out, N), ("out_host", out_host, N)):
+        _shaped(t, torch.bfloat16, name, M, width)
+    _dense(workspace, "workspace")
+    _together("int8_linear_fused_host", d_A, qw, s_ch, bias, d_out, workspace)
     assert not A_host.is_cuda and not out_host.is_cuda and d_A.is_cuda and d_out.is_cuda
     assert A_host.is_contiguous() and out_host.is_contiguous() and d_A.is_contiguous() and d_out.is_contiguous()
     _check(_lib.int8_linear_fused_host(_ptr(A_host), _ptr(d_A), _ptr(qw), _ptr(s_ch), _ptr(bias), _ptr(d_out),
@@ -360,10 +413,11 @@ def int8_linear_fused_static(A: torch.Tensor, qw: torch.Tensor, s_ch: torch.Tens
     if qw.shape[1] != K or s_ch.shape[0] != N or not qw.is_contiguous():
         raise ValueError("shape mismatch")
     if bias is not None:
-        _need(bias, torch.float32, "bias", 1)
+        _shaped(bias, torch.float32, "bias", N)
     if out is None:
         out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)   # the caller's output, not scratch
-    _need(out, torch.bfloat16, "out", 2)
+    _shaped(out, torch.bfloat16, "out", M, N)
+    _together("int8_linear_fused_static", A, qw, s_ch, bias, out)
     _check(_lib.int8_linear_fused_static(_ptr(A), A.stride(0), _ptr(qw), _ptr(s_ch), _ptr(bias), _ptr(out),
                                          out.stride(0), M, N, K, 1 if sync_and_check else 0, _stream(A)),
            "int8_linear_fused_static")
@@ -376,9 +430,13 @@ def int8_gemm_i32_debug(qa: torch.Tensor, qw: torch.Tensor, workspace: torch.Ten
     _need(qw, torch.int8, "qw", 2)
     M, K = qa.shape
     N = qw.shape[0]
+    if qw.shape[1] != K:
+        raise ValueError("shape mismatch")
     acc = torch.empty((M, N), dtype=torch.int32, device=qa.device)
     if workspace is None:
         workspace = alloc_workspace(M, N, K, ACT_INT8, qa.device)
+    _dense(workspace, "workspace")
+    _together("int8_gemm_i32_debug", qa, qw, workspace)
     _check(_lib.int8_gemm_i32_debug(_ptr(qa.contiguous()), _ptr(qw.contiguous()), _ptr(acc), M, N, K,
                                     _ptr(workspace), workspace.numel(), _stream(qa)), "int8_gemm_i32_debug")
     return acc
