@@ -8,7 +8,7 @@ from __future__ import annotations
 import torch
 
 from . import binding
-from .binding import W8A8Error, _i64, _int, _lib, _sz, _vp
+from .binding import W8A8Error, _i64, _int, _lib, _raw_stream, _sz, _vp
 
 MXFP4_BF16, MXFP4_FP32, MXFP4_CODES = 0, 1, 2
 MXFP4_K_MAX = 1 << 24
@@ -28,8 +28,8 @@ _lib.mxfp4_linear_fused.restype = _int
 _lib.mxfp4_linear_force_config.argtypes = [_int]
 _lib.mxfp4_linear_force_config.restype = _int
 
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
-_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+# torch's own short way to the current device, where it has one
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def call(fn, where: str, dev: int, *args) -> None:

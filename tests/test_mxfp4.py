@@ -100,6 +100,30 @@ def test_workspace_whose_memory_is_smaller_than_its_shape_is_refused(monkeypatch
     assert seen[0][-1] == need + 64
 
 
+def test_stream_and_device_without_the_short_ways_to_them():
+    """A torch without the two private functions: calls go through its public ones. In a process of its own, with a stand-in for the library's call."""
+    import os
+    import subprocess
+    import sys
+    code = """if True:
+        import torch
+        for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+            if hasattr(torch._C, name):
+                delattr(torch._C, name)
+        from types import SimpleNamespace
+        torch.cuda.current_device = lambda: 3
+        torch.cuda.current_stream = lambda device: SimpleNamespace(cuda_stream=1000 + device)
+        from paper_2606_14598_b200 import mxfp4
+        seen = []
+        mxfp4.call(lambda *args: seen.append(args) or 0, "here", 3, 7, 8)
+        assert seen == [(7, 8, 1003)], seen
+        print("called")
+    """
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "called" in r.stdout, r.stdout + r.stderr
+
+
 def test_python_refusals():
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
     with pytest.raises(TypeError):
