@@ -19,13 +19,21 @@ from . import binding, mxfp4
 __all__ = ["linear_fused", "W8A8Linear", "mxfp4_linear", "MXFP4Linear"]
 
 
+def _rows(A: torch.Tensor) -> torch.Tensor:
+    """[..., K] as the [M, K] that the kernels read: elements of a row side by side, rows apart by at least a row and by whole 16
+    bytes, from a 16-byte boundary. Anything else (expanded rows, odd slices) is copied."""
+    K = A.shape[-1]
+    A2 = A.reshape(-1, K)
+    if A2.stride(1) != 1 or A2.stride(0) < K or A2.stride(0) % 8 != 0 or A2.data_ptr() % 16 != 0:
+        A2 = A2.clone(memory_format=torch.contiguous_format)
+    return A2
+
+
 @torch.library.custom_op("w8a8_b200::linear_fused", mutates_args=())
 def linear_fused(A: torch.Tensor, qw: torch.Tensor, s_ch: torch.Tensor, bias: torch.Tensor | None) -> torch.Tensor:
     """bf16 [..., K] activations x int8 [N, K] per-channel weights -> bf16 [..., N] (quantize, int8 GEMM, dequantize)."""
     lead = A.shape[:-1]
-    A2 = A.reshape(-1, A.shape[-1])
-    if A2.stride(-1) != 1:
-        A2 = A2.contiguous()
+    A2 = _rows(A)
     M, K = A2.shape
     N = qw.shape[0]
     out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
@@ -67,9 +75,7 @@ class W8A8Linear(torch.nn.Module):
 def mxfp4_linear(A: torch.Tensor, qw: torch.Tensor, sw: torch.Tensor, bias: torch.Tensor | None) -> torch.Tensor:
     """bf16 [..., K] activations x MXFP4 weights (codes [N, K/2], scale tiles) -> bf16 [..., N]."""
     lead = A.shape[:-1]
-    A2 = A.reshape(-1, A.shape[-1])
-    if A2.stride(-1) != 1:
-        A2 = A2.contiguous()
+    A2 = _rows(A)
     if A2.shape[0] == 0:
         return A.new_empty((*lead, qw.shape[0]), dtype=torch.bfloat16)
     return mxfp4.mxfp4_linear_fused(A2, qw, sw, bias).reshape(*lead, qw.shape[0])

@@ -71,3 +71,27 @@ def test_compiled_mlp_has_no_graph_break_and_matches_the_oracle():
     torch.cuda.synchronize()
     assert torch.equal(y, mlp(static_x))
     assert w8.int8_sticky_status(clear=True) == 0
+
+
+def modules(device, n=24, k=64):
+    from paper_2606_14598_b200.torch_op import MXFP4Linear, W8A8Linear
+    g = torch.Generator(device).manual_seed(2)
+    bias = torch.randn(n, generator=g, device=device)
+    int8 = W8A8Linear(torch.randint(-127, 128, (n, k), generator=g, device=device, dtype=torch.int8), torch.rand(n, generator=g, device=device) + 0.1, bias.clone())
+    mx = MXFP4Linear(torch.randint(0, 256, (n, k // 2), generator=g, device=device, dtype=torch.uint8),
+                     torch.full(((n + 127) // 128, (k + 127) // 128, 512), 120, device=device, dtype=torch.uint8), bias.clone())
+    return int8, mx
+
+
+@pytest.mark.gpu
+def test_inputs_of_any_strides():
+    """Expanded rows, slices off 16-byte boundaries, odd row strides, other orders, single rows of them: as their dense copies."""
+    for module in modules("cuda"):
+        k = module.qw.shape[1] * (2 if module.qw.dtype == torch.uint8 else 1)
+        wide = torch.randn(12, 5, k + 7, device="cuda").bfloat16()
+        inputs = [wide[0, 0, :k].expand(9, k), wide[:, :1, :k].expand(12, 5, k), wide[..., 1:k + 1], wide[..., :k], wide[::2, 1, 3:k + 3], wide[0, 0, 5:k + 5],
+                  wide[:1, :1, 1:k + 1], wide[0, 0, :k].expand(1, k), wide[..., :k].transpose(0, 1), wide.permute(2, 0, 1)[:k].permute(1, 2, 0), wide[:0, :, :k]]
+        for x in inputs:
+            want = module(x.clone(memory_format=torch.contiguous_format))
+            got = module(x)
+            assert got.shape == (*x.shape[:-1], 24) and torch.equal(got, want)
