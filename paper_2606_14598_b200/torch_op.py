@@ -29,6 +29,19 @@ def _rows(A: torch.Tensor) -> torch.Tensor:
     return A2
 
 
+class _FloatsStay(torch.nn.Module):
+    """A module whose fp32 buffers (scales, bias) move with it but keep their type in .bfloat16(), .half() and .to(dtype): the
+    kernels take fp32, and rounding the scales would change the weights."""
+
+    def _apply(self, fn, recurse=True):
+        kept = {name: b for name, b in self._buffers.items() if b is not None and b.dtype == torch.float32}
+        super()._apply(fn, recurse)
+        for name, b in kept.items():
+            if self._buffers[name].dtype != torch.float32:
+                self._buffers[name] = b.to(self._buffers[name].device)
+        return self
+
+
 @torch.library.custom_op("w8a8_b200::linear_fused", mutates_args=())
 def linear_fused(A: torch.Tensor, qw: torch.Tensor, s_ch: torch.Tensor, bias: torch.Tensor | None) -> torch.Tensor:
     """bf16 [..., K] activations x int8 [N, K] per-channel weights -> bf16 [..., N] (quantize, int8 GEMM, dequantize)."""
@@ -51,7 +64,7 @@ def _linear_fused_fake(A, qw, s_ch, bias):
     return A.new_empty((*A.shape[:-1], qw.shape[0]), dtype=torch.bfloat16)
 
 
-class W8A8Linear(torch.nn.Module):
+class W8A8Linear(_FloatsStay):
     """Drop-in replacement of an ``nn.Linear`` forward: weights are quantized once per output channel (on the
     device, by the library), activations per token on every call."""
 
@@ -89,7 +102,7 @@ def _mxfp4_linear_fake(A, qw, sw, bias):
     return A.new_empty((*A.shape[:-1], qw.shape[0]), dtype=torch.bfloat16)
 
 
-class MXFP4Linear(torch.nn.Module):
+class MXFP4Linear(_FloatsStay):
     """The 4-bit counterpart of W8A8Linear: weights are quantized to MXFP4 once, activations on every call."""
 
     def __init__(self, qw: torch.Tensor, sw: torch.Tensor, bias: torch.Tensor | None = None):

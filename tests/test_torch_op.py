@@ -83,6 +83,16 @@ def modules(device, n=24, k=64):
     return int8, mx
 
 
+@pytest.mark.parametrize("cast", [lambda m: m.bfloat16(), lambda m: m.half(), lambda m: m.to(torch.bfloat16), lambda m: m.double(), lambda m: m.cpu(),
+                                  lambda m: torch.nn.Sequential(m).bfloat16()[0]])
+def test_casting_a_model_leaves_scales_and_bias_as_they_are(cast):
+    for module in modules("cpu"):
+        before = {name: b.clone() for name, b in module.named_buffers()}
+        after = dict(cast(module).named_buffers())
+        assert after.keys() == before.keys()
+        assert all(after[name].dtype == b.dtype and torch.equal(after[name], b) for name, b in before.items())
+
+
 @pytest.mark.gpu
 def test_inputs_of_any_strides():
     """Expanded rows, slices off 16-byte boundaries, odd row strides, other orders, single rows of them: as their dense copies."""
@@ -95,3 +105,11 @@ def test_inputs_of_any_strides():
             want = module(x.clone(memory_format=torch.contiguous_format))
             got = module(x)
             assert got.shape == (*x.shape[:-1], 24) and torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_forward_after_a_cast():
+    x = torch.randn(10, 64, device="cuda").bfloat16()
+    for module in modules("cuda"):
+        want = module(x)
+        assert torch.equal(module.bfloat16()(x), want) and torch.equal(module.cpu().half().cuda()(x), want)
