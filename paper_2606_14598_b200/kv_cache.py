@@ -77,9 +77,11 @@ class QuantKVCache:
 
     @classmethod
     def empty(cls, num_pages: int, page_size: int, heads: int, dim: int, fmt: str = "int8", device="cuda", values: bool = True) -> "QuantKVCache":
-        """A cache of zeros."""
+        """A cache of zeros. dim: a multiple of 8 up to 256."""
         if fmt not in ("int8", "mxfp4"):
             raise ValueError(f"fmt: 'int8' or 'mxfp4' expected, got {fmt!r}")
+        if dim <= 0 or dim % 8 or dim > KV_CACHE_MAX_DIM:
+            raise ValueError(f"dim: a multiple of 8 up to {KV_CACHE_MAX_DIM} expected, got {dim}")
         lead = (num_pages, page_size, heads)
 
         def side():

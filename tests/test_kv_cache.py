@@ -82,6 +82,16 @@ def test_python_refusals():
         w8.kv_cache_read(c, table, cu, 3, k_out=torch.zeros(2, 3, 16, dtype=torch.bfloat16))
 
 
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+def test_head_sizes_that_the_kernels_do_not_take(fmt):
+    """Refused when the cache is made (an odd size in 4 bits would have made a cache of one element less a head)."""
+    for dim in (0, -8, 4, 35, 63, 264):
+        with pytest.raises(ValueError):
+            w8.QuantKVCache.empty(2, 4, 3, dim, fmt, device="cpu")
+    for dim in (8, 72, 256):
+        assert w8.QuantKVCache.empty(2, 4, 3, dim, fmt, device="cpu").dim == dim
+
+
 def test_calls_on_nothing_are_not_refused():
     """No tokens, no slots, no rows, no pages: whatever has no elements may be NULL (a tensor without elements has no address). None of
     these calls launches anything; without a GPU they end at the check of the device."""
