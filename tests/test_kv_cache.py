@@ -372,6 +372,57 @@ def test_cache_without_pages(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("heads,dim,tokens", [(1, 8, 200003), (40, 64, 40007)])
+def test_write_of_more_tokens_than_the_grid_holds(fmt, heads, dim, tokens):
+    """A launch covers 75776 tokens of up to 256 lanes at a time (half of that where a token takes two CTAs): more go round its loop. The same
+    contents as writes of pieces that do not."""
+    page, piece = 64, 4096
+    pages = tokens // page + 2
+    slots = torch.randperm(pages * page, device="cuda")[:tokens]
+    slots[::1001] = -1
+    x = torch.randn(tokens, 2, heads, dim, device="cuda").bfloat16()
+    whole, parts = (w8.QuantKVCache.empty(pages, page, heads, dim, fmt) for _ in range(2))
+    w8.kv_cache_write(whole, x[:, 0], x[:, 1], slots)
+    for t in range(0, tokens, piece):
+        w8.kv_cache_write(parts, x[t:t + piece, 0], x[t:t + piece, 1], slots[t:t + piece])
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        assert torch.equal(getattr(whole, name), getattr(parts, name)), name
+    last = slots[tokens - 1]                                          # (its slot was written at all)
+    assert whole.k_scales.flatten(0, 1)[last].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("heads,dim,seqs,most", [(1, 8, 1500, 300), (1, 24, 3, 90000), (40, 64, 300, 400)])
+def test_read_of_more_tokens_than_the_grid_holds(fmt, heads, dim, seqs, most):
+    """The loop over the grid again, with hundreds of sequences to search (more than a CTA has threads) and with a few long ones."""
+    g = torch.Generator("cuda").manual_seed(seqs)
+    page = 16
+    lens = torch.randint(0, most + 1, (seqs,), generator=g, device="cuda")
+    lens[0], lens[seqs // 2], lens[-1] = 0, most, most
+    starts = torch.randint(0, 40, (seqs,), generator=g, device="cuda")
+    width = int((lens + starts).max()) // page + 1
+    pages = 997
+    c = random_cache(fmt, pages, page, heads, dim)
+    table = torch.randint(0, pages, (seqs, width), generator=g, device="cuda")
+    table[torch.rand(seqs, width, generator=g, device="cuda") < 0.01] = -1
+    cu = torch.cat([lens.new_zeros(1), lens.cumsum(0)])
+    total = int(cu[-1])
+    assert total > 2 * 75776 or (heads * dim > 2048 and total > 37888)
+    k, v = w8.kv_cache_read(c, table.int(), cu.int(), total, starts=starts.int())
+    seq = torch.repeat_interleave(torch.arange(seqs, device="cuda"), lens)
+    at = torch.arange(total, device="cuda") - cu[seq] + starts[seq]
+    id = table[seq, at // page]
+    row = (id * page + at % page).clamp(min=0)
+    for out, codes, scales in ((k, c.k_codes.flatten(0, 1), c.k_scales.flatten(0, 1)), (v, c.v_codes.flatten(0, 1), c.v_scales.flatten(0, 1))):
+        for t in range(0, total, 20000):
+            r, there = row[t:t + 20000], (id[t:t + 20000] >= 0)[:, None, None]
+            want = (codes[r].float() * scales[r][..., None]).double() if fmt == "int8" else ref.mx_values(ref.unpack(codes[r]), scales[r].long())
+            assert ref.same_values(out[t:t + 20000], torch.where(there, want, torch.zeros_like(want))), t
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
 def test_offsets_past_32_bits(fmt):
     heads, dim, page = 64, 256, 64
     pages = ((1 << 32) // (heads * dim * page // (1 if fmt == "int8" else 2))) + 3        # the codes pass 2^32 bytes

@@ -180,6 +180,13 @@ def test_quantizer(m, k, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantizer_of_more_rows_than_the_grid_holds(dtype):
+    """A launch holds 75776 warps of two rows (fp32 to codes: one): more rows go round its loop."""
+    check_quantized(torch.randn(160001, 64, generator=torch.Generator("cuda").manual_seed(9), device="cuda").to(dtype))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_quantizer_strides(dtype):
     x = torch.randn(70, 3, 352, device="cuda").to(dtype)
     check_quantized(x[:, 1])                                         # a slice of a fused buffer
