@@ -173,7 +173,7 @@ constexpr int kMxGemmConfigs = 3;
 
 // ---- mxfp4_skinny.cu : few tokens. Either bf16 activations, quantized in the kernel (lda in elements; the activations' fields of g are
 // not used), or their codes. Return a w8a8_status.
-constexpr int kMxSkinnyMost = 64;         // tokens the kernel takes (up to 16 if it is to quantize them)
+constexpr int kMxSkinnyMost = 64;         // tokens the kernel takes (up to 8 if it is to quantize them)
 bool mx_skinny_fits(int M);                  // what the kernel can run
 bool mx_skinny_preferred(int M, int K);     // where it is chosen when nothing is forced
 int launch_mx_skinny_bf16(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream_t st);

@@ -4,12 +4,15 @@
 //   MXFP4  per block of 32 along the head (a head's last block may be shorter): see mxfp4_math.cuh
 //
 // Both directions move bytes: a write reads 2 and stores 1 (or 0.53) bytes an element, a read loads 1 (0.53) and stores
-// 2. A lane handles 8 elements. All offsets into the cache are 64-bit.
+// 2. A lane takes 8 elements of a read, 16 of a write where sizes, strides and addresses allow it, else 8. All offsets into the
+// cache are 64-bit.
 //
-// What bounds them, keys and values of 8 x 128 a token: HBM, at 6.5 TB/s of copy bandwidth. Reads: 120000 int8 tokens 121 us =
-// 6.2 TB/s, 230000 MXFP4 tokens 202 us = 5.9 TB/s (16 elements a lane and 32-byte stores: 120 and 201 us, not kept); small ones
-// the chain sequence - page - codes (512 tokens of 36 x 128 5.5 us). Writes: 230000 MXFP4 tokens 184 us = 6.5 TB/s; int8 the
-// instructions of the exact quotient, 120000 tokens 137 us = 5.4 TB/s (189 us with 8 elements a lane).
+// What bounds them, keys and values of 8 x 128 a token: HBM, at 6.5 TB/s of copy bandwidth. Reads: 120000 int8 tokens 120 us =
+// 6.2 TB/s, 230000 MXFP4 tokens 200 us = 5.9 TB/s (16 elements a lane and 32-byte stores: no faster, not kept); small ones
+// the chain sequence - page - codes (512 tokens of 36 x 128 5.5 us). Writes: 230000 MXFP4 tokens 183 us = 6.5 TB/s; int8 the
+// instructions of the exact quotient, 120000 tokens 137 us = 5.4 TB/s (189 us with 8 elements a lane). Writes of heads that do not
+// fill their lanes (int8: the next power of two; MXFP4: whole blocks of 32) pay for the idle ones: 8220 tokens of 16 x 72 take
+// 35.0 us in int8 and 15.6 in MXFP4, for 9 and 7 us worth of bytes.
 #include "../../include/kv_cache.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"

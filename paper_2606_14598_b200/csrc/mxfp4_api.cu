@@ -13,8 +13,9 @@ using namespace w8a8;
 
 constexpr size_t kStatusBlock = 256;
 std::atomic<int> g_forced_config{-1};
-// Tokens up to which the few-token kernel quantizes them itself. GPU time of 8 x 4608 -> 4608 8.2 us that way, of 14 tokens with a
-// quantizer ahead 7.7 us, which costs the host a second launch (3 us); 12 x 4608 -> 13824 14.6 us, 16 tokens with a quantizer 11.7 us.
+// Tokens up to which the few-token kernel quantizes them itself. GPU time of 8 x 4608 -> 4608 8.5 us that way, of 14 tokens with a
+// quantizer ahead 8.4 us, which costs the host a second launch (3 us); 8 x 4608 -> 13824 12.3 us, 16 tokens with a quantizer 12.1 us
+// (12 tokens quantized inside 14.6, ahead 12.1 us).
 constexpr int kQuantizeInside = 8;
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 

@@ -18,10 +18,11 @@
 // swizzled staging; TMA store of 32 x 32 boxes, which clips ragged edges), 6 copies scales into tensor memory, 7 loads them.
 //
 // What bounds it: the tensor queue and the way operands take to it, not HBM (the operands of a 4110 x 4608 -> 13824 product come
-// out of L2). There 120 us = 4.35 PFLOP/s, 0.66 of four times the measured bf16 rate (8192 cubed 5.1 PFLOP/s, 0.78). With parts
-// left out: MMAs alone 86 us (162 cycles an MMA of 256 x 256 x 64 where 128 would be the pipe's), with scale copies 94 (a copy or
-// commit holds the queue 35-45 cycles; in the MMA thread they made it 159), with operand loads 110, with the hand-over of the
-// shared columns 120 (0.5 us a tile from the accumulator's completion to the peer's answer). Tried without gain: bands in the
+// out of L2). There 121-125 us = 4.2-4.3 PFLOP/s in a short run, 0.64-0.66 of four times the measured bf16 rate (8192 cubed 213-217 us,
+// 5.1 PFLOP/s, 0.77); over seconds the power limit takes the SM clock to 1.65 GHz and it is 138 us. With parts left out: MMAs alone
+// 86 us (162 cycles an MMA of 256 x 256 x 64 where 128 would be the pipe's), with scale copies 94 (a copy or commit holds the queue
+// 35-45 cycles; in the MMA thread they made it 159), with operand loads 110, with the hand-over of the shared columns 120 (0.5 us
+// a tile from the accumulator's completion to the peer's answer). Tried without gain: bands in the
 // tile order, L2 hints, one commit for both CTAs, stages of one k-block (258 against 217 us on 8192 cubed), stores straight from registers.
 //
 // Every wait is bounded as in the int8 GEMM: on expiry the status word is set, all roles unwind, TMEM is freed.
@@ -526,9 +527,9 @@ int launch_cfg(const MxLinearArgs& a, cudaStream_t st) {
 
 // The configuration with the lowest estimated time. Fitted on 20 shapes from (128, 256, 256) to (8192, 8192, 8192): launch,
 // fill and last epilogue, then for every wave of tiles its k-blocks and what the hand-over between tiles leaves exposed
-// (microseconds). Measured, 256 x 256 pairs / 256 x 192 pairs / 128 x 128: 8192 cubed 214 / 228 / 327 us, 4110 x 4608 -> 4608
-// 50.0 / 46.3 / 57.9, 2048 x 4608 -> 12288 57.4 / 54.0 / 75.8, 1024 x 4608 -> 4608 14.5 / 18.0 / 15.5, 512 x 12288 -> 4608
-// 25.7 / 22.3 / 18.8.
+// (microseconds). Measured on codes, 256 x 256 pairs / 256 x 192 pairs / 128 x 128: 8192 cubed 213 / 231 / 295 us, 4110 x 4608 -> 4608
+// 52.9 / 49.9 / 61.9, 2048 x 4608 -> 12288 63.8 / 59.7 / 76.4, 1024 x 4608 -> 4608 17.5 / 20.9 / 17.9, 512 x 12288 -> 4608
+// 29.5 / 25.8 / 21.8.
 int choose_mx_config(int M, int N, int K) {
     struct { int cg, bn; double fixed, per_kb, per_tile; } const c[] = {{2, 256, 4.5, 0.455, 0.8}, {2, 192, 4.0, 0.39, 0.1}, {1, 128, 2.8, 0.345, 0.0}};
     int best = 0;

@@ -7,7 +7,8 @@
 //
 // Everything but the rounding to E2M1 is exact in binary32: multiplying by 2^-e only moves the exponent (results
 // below 2^-126 are far under the smallest rounding boundary 0.25, so what subnormal rounding does to them cannot
-// show), and value * 2^e fits bf16 for every code and byte (the smallest, 2^-128, is a bf16 subnormal).
+// show), and value * 2^e fits bf16 for every code and every byte that the quantizer writes (0 to 252: the smallest, 2^-128, is a
+// bf16 subnormal). Under the bytes 253 and 254 the largest codes stand for more than fp32 holds: they read as infinities.
 #pragma once
 
 #include <cstdint>

@@ -7,9 +7,9 @@
 // words (one for each tile of four blocks that the segment crosses). Where the rows allow it a lane moves 32 bytes at
 // a time, so that every memory sector is touched by one instruction.
 //
-// Measured: 13824 x 4608 fp32 42.2 us to codes and 44.2 us back (6.8 and 6.5 TB/s, the copy bandwidth is 6.5); 4110 x 12288 bf16
-// 21.1 and 21.3 us (6.1 and 6.0 TB/s; 24.1 and 21.9 us when every segment worked out its own addresses, 12 instructions an element);
-// 77 x 4608 1.7 and 1.6 us, launch.
+// Measured: 13824 x 4608 fp32 42.3 us to codes and 44.4 us back (6.8 and 6.5 TB/s; the copy that gives 6.5 TB/s writes half of its bytes,
+// the quantizer a ninth, and what it wrote last is still in L2 when it ends); 4110 x 12288 bf16 21.7 and 21.7 us (5.9 TB/s;
+// 24.1 and 21.9 us when every segment worked out its own addresses, 12 instructions an element); 77 x 4608 1.9 and 1.9 us, launch.
 #include "internal.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"

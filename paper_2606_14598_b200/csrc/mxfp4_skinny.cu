@@ -10,11 +10,12 @@
 // k-blocks straight into the swizzled operand tile of the same ring stage. Accumulators are transposed (lane = output channel, column = token): they
 // go through shared memory, so that a warp stores 256 contiguous bytes a token.
 //
-// What bounds it: HBM where there is enough to stream (2 x 4608 -> 27648, 67.9 MB: 14.3 us, 4.75 TB/s, 0.73 of the copy
-// bandwidth), else the chain launch - first bytes - MMAs - cluster barrier - stores (1 x 4608 -> 4608, 11.3 MB: 6.2 us, of which a
-// call on a 256 x 512 weight takes 3.8). Measured against it: scale copies in the MMA thread and four accumulators instead of
-// one, no difference (the stream sets the pace); tokens of all k-blocks quantized up front, 54 KB of shared memory less for the
-// ring, 15.7 against 14.5 us; partial sums sent to one CTA, 8.2 against 6.2 us.
+// What bounds it: HBM where there is enough to stream (2 x 4608 -> 27648, 67.9 MB: 13.8-14.5 us, 4.7-4.9 TB/s, 0.72-0.75 of the copy
+// bandwidth), else the chain launch - first bytes - MMAs - cluster barrier - stores (1 x 4608 -> 4608, 11.3 MB: 6.5 us, of which a
+// call on a 256 x 512 weight takes 3.9). The first tiles reach shared memory after the kernel ahead, out of L2: 0.3 us at one token,
+// 1.0 us at 64 (10.4 us for 64 x 4608 -> 4608) more than loads ahead of it would take. Measured when those were loaded ahead: scale copies
+// in the MMA thread and four accumulators instead of one, no difference (the stream sets the pace); tokens of all k-blocks quantized up
+// front, 54 KB of shared memory less for the ring, 15.7 against 14.5 us; partial sums sent to one CTA, 8.2 against 6.2 us.
 #include "../../include/mxfp4_linear.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"
@@ -398,7 +399,9 @@ int launch_variant(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream
 } // namespace
 
 bool mx_skinny_fits(int M) { return M <= kMxSkinnyMost; }
-// (64 x 4608 -> 4608: 9.7 us against 13.2 in the tiled GEMM, 48 x 1056 -> 2048 7.3 against 7.9, 64 x 512 -> 512 7.7 against 6.2)
+// (This kernel against the tiled GEMM, quantizer included: 17 x 4608 -> 4608 8.9 / 12.2 us, 32 x 4608 -> 13824 13.5 / 15.5, 64 x 12288 -> 4608
+// 15.3 / 21.9, 64 x 4608 -> 4608 10.7 / 12.2, 64 x 768 -> 512 9.5 / 6.9. By M and K alone: about even on 48 x 1056 -> 2048, 8.4 / 8.0, and
+// 64 x 4608 -> 27648, 22.3 / 21.6; beyond that the tiled kernel's reuse of the tokens wins, 64 x 2048 -> 60000 30.7 / 22.1.)
 bool mx_skinny_preferred(int M, int K) { return M <= 16 || (M <= kMxSkinnyMost && K > 2 * BK); }
 
 // Up to 4 tokens 5 warps quantize and three CTAs fit an SM; more tokens need 10 warps.
