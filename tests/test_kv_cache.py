@@ -149,6 +149,15 @@ def test_storage_moved_after_the_cache_was_made(monkeypatch, fmt):
         places()
 
 
+def test_copy_of_a_cache_has_memory_of_its_own():
+    import copy
+    import pickle
+    c = w8.QuantKVCache.empty(2, 4, 3, 16, "int8", device="cpu")
+    for other in (copy.deepcopy(c), pickle.loads(pickle.dumps(c))):
+        assert other.places() == tuple(t.data_ptr() for t in (other.k_codes, other.k_scales, other.v_codes, other.v_scales))
+        assert not set(other.places()) & set(c.places())
+
+
 # ------------------------------------------------------------------------------------------ on the GPU
 
 def random_cache(fmt, pages, page, heads, dim, values=True):
