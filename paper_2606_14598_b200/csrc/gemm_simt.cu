@@ -24,7 +24,7 @@ __device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
 template <int MB, int NPW, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32)
 gemm_simt_kernel(const int8_t* qa, int64_t lda_q, const float* s_tok,
-                 const int8_t* __restrict__ qw, const float* __restrict__ s_ch, const float* __restrict__ bias,
+                 const int8_t* qw, const float* s_ch, const float* bias,
                  void* __restrict__ out, int64_t ldo, int M, int N, int K, int raw_i32, int after_quantizer, int* status,
                  float* rowmax) {
     grid_dep_launch_dependents();      // a following kernel launched to allow it may set itself up early
@@ -55,9 +55,9 @@ gemm_simt_kernel(const int8_t* qa, int64_t lda_q, const float* s_tok,
     for (int k = lane * 16; k < K; k += 32 * 16) {      // unrolled: several 512-byte slices of each weight row in flight
         uint4 w[NPW], a[MB];
 #pragma unroll
-        for (int j = 0; j < NPW; ++j) w[j] = __ldg(reinterpret_cast<const uint4*>(wrow[j] + k));
+        for (int j = 0; j < NPW; ++j) w[j] = __ldcg(reinterpret_cast<const uint4*>(wrow[j] + k));
 #pragma unroll
-        // Coherent loads (the quantizer ahead may have written these rows while this kernel was already resident).
+        // Coherent loads, of weights and rows (work ahead may have written them while this kernel was already resident).
         // One or two rows: plain, L1-cached ones, since every warp of the CTA re-reads them and nothing of them was
         // touched before the wait above, so no line in this SM's L1 can predate the quantizer's writes (12.1 against
         // 14.3-18.7 us at M = 1-2 with L2-only loads); more rows: L2-only loads, which leave L1 to the weight
@@ -90,9 +90,9 @@ gemm_simt_kernel(const int8_t* qa, int64_t lda_q, const float* s_tok,
                 static_cast<int32_t*>(out)[static_cast<int64_t>(m) * ldo + n] = mine;
             } else {
                 float t = __int2float_rn(mine);
-                t = __fmul_rn(t, __ldcg(s_tok + m));      // plain loads for what the quantizer ahead of this kernel wrote
-                t = __fmul_rn(t, s_ch[n]);
-                if (bias != nullptr) t = __fadd_rn(t, bias[n]);
+                t = __fmul_rn(t, __ldcg(s_tok + m));      // coherent loads again
+                t = __fmul_rn(t, __ldcg(s_ch + n));
+                if (bias != nullptr) t = __fadd_rn(t, __ldcg(bias + n));
                 const __nv_bfloat16 o = __float2bfloat16_rn(t);
                 static_cast<__nv_bfloat16*>(out)[static_cast<int64_t>(m) * ldo + n] = o;
                 if (rowmax != nullptr) {      // side output: largest magnitude written to row m (non-negative floats order like their bits)

@@ -116,7 +116,7 @@ template <int CG, int BNS, int NSUB, int STAGES, int KBS, bool RAW_I32>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                const __grid_constant__ CUtensorMap tm_out,
-               const float* s_tok, const float* __restrict__ s_ch, const float* __restrict__ bias,
+               const float* s_tok, const float* s_ch, const float* bias,
                int32_t* __restrict__ raw_out, int M, int N, int K, const RunCtl rc,
                int split_tiles, int split_s, int32_t* split_slabs, int* split_counters, int wide_per_row, int band,
                float* rowmax) {
@@ -450,8 +450,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
                 // the slot's buffer was last read two sub-tiles ago, which every warp has left behind
                 for (int j = ep_tid; j < BNS; j += EPI_THREADS) {
                     const int n = n0 + j;
-                    sm_sch[buf * BNS + j] = n < N ? __ldg(s_ch + n) : 0.f;
-                    sm_bias[buf * BNS + j] = (has_bias && n < N) ? __ldg(bias + n) : 0.f;
+                    sm_sch[buf * BNS + j] = n < N ? __ldcg(s_ch + n) : 0.f;
+                    sm_bias[buf * BNS + j] = (has_bias && n < N) ? __ldcg(bias + n) : 0.f;
                 }
                 asm volatile("bar.sync 1, 128;" ::: "memory");
             }

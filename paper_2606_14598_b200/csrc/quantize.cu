@@ -25,12 +25,15 @@
 namespace w8a8 {
 namespace {
 
+// Loads of what a call is given are plain, coherent ones: the kernel may be resident while the work ahead of it writes them, which
+// rules out the read-only path. (Past L1, a lane's neighbouring 16 bytes come twice: 13824 x 4608 fp32 82.8 us.)
+
 // ------------------------------------------------------------------------------------------- arithmetic
 
 // SmoothQuant hook: x'[k] = RN(float(x[k]) * mult[k]) before everything else. 8 smoothed values of a unit.
-__device__ __forceinline__ void smooth8(const uint4& v, const float* __restrict__ mult8, float (&f)[8]) {
-    const float4 m0 = __ldg(reinterpret_cast<const float4*>(mult8));
-    const float4 m1 = __ldg(reinterpret_cast<const float4*>(mult8) + 1);
+__device__ __forceinline__ void smooth8(const uint4& v, const float* mult8, float (&f)[8]) {
+    const float4 m0 = reinterpret_cast<const float4*>(mult8)[0];
+    const float4 m1 = reinterpret_cast<const float4*>(mult8)[1];
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
 #pragma unroll
@@ -88,9 +91,9 @@ __device__ __forceinline__ void bulk_load_row(uint32_t smem_dst, const void* gsr
 // kernel just ahead in the stream): the search pass and the exchange between the row's warps fall away.
 template <int WPR, bool SMOOTH, bool GIVEN>
 __global__ void __launch_bounds__(SG_THREADS, 2)
-quant_rows_staged_kernel(const __nv_bfloat16* __restrict__ x, int64_t ld, int rows, int K,
+quant_rows_staged_kernel(const __nv_bfloat16* x, int64_t ld, int rows, int K,
                          int8_t* __restrict__ q, float* __restrict__ s_out, const QuantCtl qc, int num_stages,
-                         const float* __restrict__ mult, const float* amax_in) {
+                         const float* mult, const float* amax_in) {
     int* const status = qc.status;
     // a dependent kernel (the GEMM) may set itself up while this one runs; it waits for this grid before reading
     grid_dep_launch_dependents();
@@ -261,8 +264,8 @@ template <> struct Chunk<__nv_bfloat16> {
     uint4 lo, hi;                          // 8 + 8 bf16
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
         const uint4* q = reinterpret_cast<const uint4*>(p);
-        lo = __ldg(q);
-        hi = __ldg(q + 1);
+        lo = q[0];
+        hi = q[1];
     }
     __device__ __forceinline__ void zero() { lo = make_uint4(0, 0, 0, 0); hi = lo; }
     __device__ __forceinline__ float absmax() const {
@@ -280,12 +283,12 @@ template <> struct Chunk<float> {
     __device__ __forceinline__ void load(const float* p) {
         const float4* q = reinterpret_cast<const float4*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __ldg(q + i);
+        for (int i = 0; i < 4; ++i) v[i] = q[i];
     }
     // 16 bf16 values widened to fp32 (exact)
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
         const uint4* q = reinterpret_cast<const uint4*>(p);
-        const uint4 lo = __ldg(q), hi = __ldg(q + 1);
+        const uint4 lo = q[0], hi = q[1];
         const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -293,11 +296,11 @@ template <> struct Chunk<float> {
                                __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xffff0000u));
     }
     // SmoothQuant hook: one rounded multiply per element by its input channel's factor
-    __device__ __forceinline__ void scale(const float* __restrict__ mult16) {
+    __device__ __forceinline__ void scale(const float* mult16) {
         const float4* m = reinterpret_cast<const float4*>(mult16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 f = __ldg(m + i);
+            const float4 f = m[i];
             v[i] = make_float4(__fmul_rn(v[i].x, f.x), __fmul_rn(v[i].y, f.y), __fmul_rn(v[i].z, f.z), __fmul_rn(v[i].w, f.w));
         }
     }
@@ -322,8 +325,8 @@ template <> struct Chunk<float> {
 // SMOOTH (SmoothQuant hook): elements are widened to fp32 and multiplied by mult[k] as they are loaded.
 template <typename T, int WPR, bool SMOOTH, bool GIVEN>
 __global__ void __launch_bounds__(WARPS * 32, 1)
-quant_rows_kernel(const T* __restrict__ x, int64_t ld, int rows, int K,
-                  int8_t* __restrict__ q, float* __restrict__ s_out, int* status, const float* __restrict__ mult,
+quant_rows_kernel(const T* x, int64_t ld, int rows, int K,
+                  int8_t* __restrict__ q, float* __restrict__ s_out, int* status, const float* mult,
                   const float* amax_in) {
     using C = Chunk<typename std::conditional<SMOOTH, float, T>::type>;
     auto fetch = [&](C& c, const T* row, int chunk) {

@@ -57,3 +57,33 @@ def test_weights_written_just_ahead(m, n, k, last):
         graph.replay()
         assert all(torch.equal(out, want[i % 2]) for i, out in enumerate(outs))
     assert w8.int8_check_status(ws) == 0 and w8.int8_check_status(ws_codes) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [256, 4608, 66560])
+def test_quantizer_inputs_written_just_ahead(k):
+    """Activations, weights and SmoothQuant factors written by the kernel directly ahead of their quantizers, for rows of every kind (the longest
+    go through the kernel without a ring)."""
+    rows = 40
+    g = torch.Generator("cuda").manual_seed(k)
+    both = [torch.randn(rows, k, generator=g, device="cuda") * (i + 1) for i in range(2)]
+    mults = [torch.rand(k, generator=g, device="cuda") + 0.5 + i for i in range(2)]
+    acts = [x.bfloat16() for x in both]
+    quantizers = {"act": lambda a, w, m: w8.int8_quantize_act_per_token(a), "weight": lambda a, w, m: w8.int8_quantize_weight_per_channel(w),
+                  "act_smooth": lambda a, w, m: w8.int8_quantize_act_per_token_smooth(a, m),
+                  "weight_smooth": lambda a, w, m: w8.int8_quantize_weight_per_channel_smooth(w, m)}
+    a, w, m = torch.zeros_like(acts[0]), torch.zeros_like(both[0]), torch.zeros_like(mults[0])
+    for name, quantize in quantizers.items():
+        want = [quantize(acts[i], both[i], mults[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        got = []
+        for i in range(20):
+            for last in (False, True):
+                if name.endswith("smooth") == last:
+                    torch.mul(mults[i % 2], 1.0, out=m)
+                else:
+                    torch.mul(acts[i % 2], 1.0, out=a)
+                    torch.mul(both[i % 2], 1.0, out=w)
+            got.append(quantize(a, w, m))
+        for i, (q, s) in enumerate(got):
+            assert torch.equal(q, want[i % 2][0]) and torch.equal(s, want[i % 2][1]), (name, i)
