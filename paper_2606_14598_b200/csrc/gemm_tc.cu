@@ -161,14 +161,22 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         prefetch_tensormap(&tm_b);
         if (!RAW_I32) prefetch_tensormap(&tm_out);
     }
+    // Tensor memory of a pair. A barrier of the cluster before the allocation: it concerns both CTAs, and only the barrier says that the peer
+    // has begun (without it a pair whose peer started late, beside CTAs of a kernel ahead, waited in its allocation for good). One after
+    // it, before the permit, which is the pair's too, goes back.
+    if (CG == 2) {
+        __syncwarp();
+        cluster_sync_all();
+    }
     if (warp == 1) {
-        if (CG == 2) { tmem_alloc_pair(base + L::OFF_TMEM, TMEM_COLS); tmem_relinquish_pair(); }
-        else { tmem_alloc(base + L::OFF_TMEM, TMEM_COLS); tmem_relinquish(); }
+        if (CG == 2) tmem_alloc_pair(base + L::OFF_TMEM, TMEM_COLS);
+        else tmem_alloc(base + L::OFF_TMEM, TMEM_COLS);
     }
     tc_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync_all();            // the peer's barriers exist before anything signals them
     tc_fence_after();
+    if (warp == 1) { if (CG == 2) tmem_relinquish_pair(); else tmem_relinquish(); }
     const uint32_t tmem_base = *tmem_holder;
 
     constexpr int TILE_M = BM * CG;
@@ -632,6 +640,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     if (warp == 1) {
         if (CG == 2) tmem_dealloc_pair(tmem_base, TMEM_COLS);
         else tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+    if (CG == 2) {
+        __syncwarp();
+        cluster_sync_all();                     // neither is gone while the other frees its half
     }
 }
 

@@ -144,14 +144,22 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         prefetch_tensormap(&tm_sb);
         prefetch_tensormap(&tm_out);
     }
+    // Tensor memory of a pair. A barrier of the cluster before the allocation: it concerns both CTAs, and only the barrier says that the peer
+    // has begun (without it a pair whose peer started late, beside CTAs of a kernel ahead, waited in its allocation for good). One after
+    // it, before the permit, which is the pair's too, goes back.
+    if (CG == 2) {
+        __syncwarp();
+        cluster_sync_all();
+    }
     if (warp == 1) {
-        if (CG == 2) { tmem_alloc_pair(base + L::OFF_TMEM, L::TMEM_COLS); tmem_relinquish_pair(); }
-        else { tmem_alloc(base + L::OFF_TMEM, L::TMEM_COLS); tmem_relinquish(); }
+        if (CG == 2) tmem_alloc_pair(base + L::OFF_TMEM, L::TMEM_COLS);
+        else tmem_alloc(base + L::OFF_TMEM, L::TMEM_COLS);
     }
     tc_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync_all();
     tc_fence_after();
+    if (warp == 1) { if (CG == 2) tmem_relinquish_pair(); else tmem_relinquish(); }
     const uint32_t tmem_base = *tmem_holder;
     // Only now: a kernel behind this one that allocates tensor memory and then waits for this one must not get there first.
     grid_dep_launch_dependents();
@@ -472,6 +480,10 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     if (warp == 1) {
         if (CG == 2) tmem_dealloc_pair(tmem_base, L::TMEM_COLS);
         else tmem_dealloc(tmem_base, L::TMEM_COLS);
+    }
+    if (CG == 2) {
+        __syncwarp();
+        cluster_sync_all();                     // neither is gone while the other frees its half
     }
 }
 
