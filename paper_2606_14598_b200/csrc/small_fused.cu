@@ -8,8 +8,8 @@
 //   1. a CTA prefetches its 32 x K slice of the int8 weights into L2 and, after the dependency wait, requests it (plain
 //      16-byte loads) and its share of the rows of A (row r belongs to the CTA of rank r mod cluster size): both fetches
 //      are in flight together;
-//   2. the weights go to shared memory in the 128-byte-swizzled K-major layout tcgen05.mma reads; every row of A is
-//      quantized by one warp, which writes the codes in the same layout into the operand tile of EVERY CTA of the
+//   2. the weights go to shared memory in the 128-byte-swizzled K-major layout tcgen05.mma reads; once every CTA of the
+//      cluster is known to have begun (a barrier that they arrived at first of all), every row of A is quantized by one warp, which writes the codes in the same layout into the operand tile of EVERY CTA of the
 //      cluster (st.shared::cluster), and the row's scale likewise; the first cluster also writes codes and scales
 //      to the workspace, where the two-kernel path leaves them for the caller;
 //   3. after a cluster barrier one thread issues the MMAs (M = 128, N = 32, K = 32 each) into 32 TMEM columns;
@@ -94,6 +94,7 @@ small_fused_kernel(const SmallArgs p) {
     const int n0 = blockIdx.x * SF_BN;
     const bool active = n0 < N;        // the grid is padded to whole clusters: a CTA past N only quantizes its share
     const uint32_t rank = CS > 1 ? cluster_ctarank() : 0u;
+    if (CS > 1) cluster_arrive();      // this CTA has begun: waited for before the first store into another one's shared memory
 
     if (warp == 0 && active) {
         tmem_alloc(smem_u32(tmem_slot), SF_BN);
@@ -179,6 +180,10 @@ small_fused_kernel(const SmallArgs p) {
                 if (threadIdx.x < SF_BN) {
                     s_ch_s[threadIdx.x] = my_sch;
                     bias_s[threadIdx.x] = my_bias;
+                }
+                if (CS > 1) {
+                    __syncwarp();
+                    cluster_wait();        // every CTA of the cluster has begun
                 }
             }
 #pragma unroll

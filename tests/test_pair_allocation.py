@@ -27,6 +27,14 @@ def test_barriers_around_what_concerns_the_pair(name):
                                                 "tmem_dealloc_pair", "cluster_sync_all"]
 
 
+def test_no_store_into_a_cta_that_may_not_have_begun():
+    """The one-kernel path of the int8 linear writes into the other CTAs' shared memory: behind a barrier of the cluster."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "small_fused.cu")).read())
+    body = text[text.index("small_fused_kernel(const SmallArgs p)"):]
+    arrive, wait = body.index("cluster_arrive()"), body.index("cluster_wait()")
+    assert arrive < wait < min(body.index("st_cluster_f32(s_remote"), body.index("st_cluster_v2(a_remote"))
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(5125, 10592, 1504), (4110, 4608, 1056), (2100, 13824, 512), (8192, 2048, 288)])
 def test_many_calls_back_to_back(m, n, k):
