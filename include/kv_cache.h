@@ -27,6 +27,7 @@ enum { KV_CACHE_INT8 = 0, KV_CACHE_MXFP4 = 1 };
 enum { KV_CACHE_ZERO_REST = 0x100 }; /* or'd into the fmt of a read */
 #define KV_CACHE_MAX_DIM 256
 #define KV_CACHE_MAX_WIDTH 65536 /* heads * dim */
+#define KV_CACHE_MAX_AXES 8
 
 /*
  * Quantizes `tokens` tokens into their slots. slots: int64 [tokens], device; one outside [0, num_slots) is skipped (-1 for
@@ -52,6 +53,61 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
                   int64_t heads, int64_t dim, const int32_t* table, int64_t table_stride, int64_t max_pages, const int32_t* cu_seqlens,
                   const int32_t* starts, int64_t seqs, int64_t total, void* k_out, int64_t k_token_stride, int64_t k_head_stride, void* v_out,
                   int64_t v_token_stride, int64_t v_head_stride, void* stream);
+
+/*
+ * Appends new tokens: rotates queries and keys by their positions, quantizes keys and values into the cache's slots, in one launch.
+ * Pairs of elements of a head turn by an angle that the token's position on the pair's axis gives (one axis for text; time, height and width
+ * for images and video):
+ *     p = positions[axis of pair i][token],  c = cos_sin[p][i],  s = cos_sin[p][rot / 2 + i]
+ *     a' = a * c - b * s,  b' = b * c + a * s           fp32: two products and a sum, each rounded once
+ * of the elements (a, b) = (2i, 2i + 1) if interleaved, else (i, i + rot / 2); elements from rot on stay as they are.
+ *   q_out = bf16(q'), the cache gets k' (not rounded to bf16 in between) and v as kv_cache_write would store them.
+ *   q, q_out    bf16 [tokens, q_heads, dim] with their strides; both NULL for none; q_out may be q itself
+ *   cos_sin     fp32 [num_positions, rot] dense, 16-byte aligned, or NULL: nothing is rotated (positions and axes are not read)
+ *   rot         a multiple of 8, at most dim
+ *   positions   int64 [axes, tokens], rows position_stride apart; a position outside the table makes its pairs NaN
+ *   axis_of     uint8 [rot / 2]: the axis of each pair, or NULL with one axis; one that is not below `axes` makes its pair NaN
+ * Everything else as for kv_cache_write; a token whose slot is outside the cache still gets its queries.
+ */
+int kv_cache_append(int fmt, const void* q, int64_t q_token_stride, int64_t q_head_stride, int64_t q_heads, void* q_out, int64_t q_out_token_stride,
+                    int64_t q_out_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                    int64_t v_head_stride, const float* cos_sin, int64_t num_positions, int64_t rot, int interleaved, const int64_t* positions,
+                    int64_t position_stride, int64_t axes, const uint8_t* axis_of, const int64_t* slots, int64_t tokens, int64_t heads, int64_t dim,
+                    void* k_codes, void* k_scales, void* v_codes, void* v_scales, int64_t num_slots, void* stream);
+
+/*
+ * The table that kv_cache_append reads: cos and sin of (first + p) * inv_freq[i], times `scale`, worked out in 64 bits and rounded once.
+ *   inv_freq  fp64 [pairs], device;  cos_sin  fp32 [num_positions, 2 * pairs]
+ */
+int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, int64_t num_positions, double scale, float* cos_sin, void* stream);
+
+/*
+ * Attention of new tokens over the cache, on the codes: nothing is expanded in memory.
+ *     o = sum_p softmax_p(scale * q . k_p) v_p             over the tokens p that the query sees; k, v: what the codes stand for, unrounded
+ * Sequence b holds lens[b] tokens in its pages. The last n_b = cu_q[b + 1] - cu_q[b] of them are its new ones, appended before the call;
+ * query i of them (row cu_q[b] + i of q) sees the tokens from starts[b] on that come before the new ones, and of the new ones
+ *   tree == NULL  those up to and with itself (one token a sequence, or a chain)
+ *   else          token j where bit j % 64 of tree[(cu_q[b] + i) * tree_words + j / 64] is set: a tree of drafted tokens, each of which sees its
+ *                 ancestors (and itself, where its own bit is set); new tokens from 64 * tree_words on are not seen
+ * Query head h reads the keys and values of head h / (q_heads / heads). A query that sees nothing gets zeros and a logarithm of -inf. A token whose page
+ * is outside the cache or past the table is not seen. NaN keys and values (their scale is NaN) reach the queries that see them, and no others.
+ *   q, out      bf16 [total_q, q_heads, dim] with their strides; rows of no sequence as for kv_cache_read (KV_CACHE_ZERO_REST)
+ *   lse         fp32 [total_q, q_heads]: log(sum_p exp(scale * q . k_p)), or NULL
+ *   table       int32 [seqs, max_pages];  lens, starts int32 [seqs] (starts may be NULL: from the first);  cu_q int32 [seqs + 1], not decreasing
+ *   tree        int64 [total_q, tree_words] or NULL
+ *   workspace   device scratch of kv_cache_attention_workspace_bytes(), 256-byte aligned; its first kv_cache_attention_zeroed_bytes() bytes must be zero
+ *               before the first call that uses it, and each call leaves them zero. Two calls that may overlap on the device need distinct workspaces.
+ * The cache must have both sides; num_pages * page_size <= 2^31 - 1; q_heads a multiple of heads. Scores, softmax and sums are fp32; probabilities are rounded
+ * to bf16 for the product with the values. Repeated calls give the same bits. What lies far below its neighbours may count as zero: elements of a query 2^-38 below its
+ * largest, MXFP4 blocks 2^-24 (keys) or 2^-126 (values) below the largest of their head and token, tokens whose probability is 2^-118 of the largest.
+ */
+size_t kv_cache_attention_workspace_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);
+size_t kv_cache_attention_zeroed_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);
+int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int64_t num_pages, int64_t page_size,
+                       int64_t heads, int64_t dim, const int32_t* table, int64_t table_stride, int64_t max_pages, const int32_t* lens, const int32_t* starts,
+                       const int32_t* cu_q, int64_t seqs, const void* q, int64_t q_token_stride, int64_t q_head_stride, int64_t q_heads, int64_t total_q,
+                       const int64_t* tree, int64_t tree_words, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                       void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }
