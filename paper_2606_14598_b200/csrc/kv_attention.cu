@@ -13,6 +13,7 @@
 #include "internal.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"
+#include "tensor_map.h"
 
 #include <cmath>
 #include <cuda_fp16.h>
@@ -21,8 +22,8 @@ namespace w8a8 {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kStep = 16;                       // tokens that a warp takes at a time
-constexpr int kTile = kStep * kWarps;           // tokens of a unit
+constexpr int kWaitAttention = 40;              // which wait gave up, for the status word
+constexpr float kNone = -3e38f;                 // reference of a row that has seen nothing (finite, so that differences are numbers)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttentionArgs {
@@ -37,9 +38,12 @@ struct AttentionArgs {
     float* parts;
     int64_t q_st, q_sh, o_st, o_sh, table_stride, tree_words;
     int num_pages, page, max_pages, heads, group, dim, seqs, total_q;
-    int copy;                                   // bytes of an asynchronous copy: 16, 8 or 4, by the alignment of the heads in the cache
+    int page_shift;                             // log2 of the page, or -1
+    int box, box_step;                          // tokens of a box of codes, elements from a box to the one beside it; 0: no boxes
     float scale;
     int zero_rest;
+    int *status, *sticky;
+    uint64_t limit_ns;
 };
 
 // ------------------------------------------------------------------------------------------------ the list of work
@@ -48,8 +52,10 @@ struct Sequence {
     int begin, n;                               // its rows of q
     int before;                                 // tokens ahead of the new ones (negative if the cache holds fewer than n)
     int start, stop;                            // tokens that may be seen
+    int base;                                   // where the units begin: start, rounded down to whole boxes
     int tiles, row_tiles;
 };
+template <int TILE>                             // tokens of a unit
 __device__ __forceinline__ Sequence read_sequence(const AttentionArgs& a, int b, int rows_of_tile) {
     Sequence s;
     const int begin = a.cu_q[b], end = a.cu_q[b + 1], len = a.lens[b];
@@ -59,7 +65,8 @@ __device__ __forceinline__ Sequence read_sequence(const AttentionArgs& a, int b,
     s.before = max(len, 0) - s.n;
     s.stop = static_cast<int>(min(static_cast<int64_t>(max(len, 0)), most));
     s.start = a.starts != nullptr ? max(0, min(a.starts[b], s.stop)) : 0;
-    s.tiles = max(1, (s.stop - s.start + kTile - 1) / kTile);
+    s.base = s.start & ~31;
+    s.tiles = max(1, (s.stop - s.base + TILE - 1) / TILE);
     s.row_tiles = static_cast<int>((static_cast<int64_t>(s.n) * a.group + rows_of_tile - 1) / rows_of_tile);
     return s;
 }
@@ -80,14 +87,14 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v) {
     }
     return v;
 }
-template <int THREADS>
+template <int THREADS, int TILE>
 __device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_tile) {
     __shared__ int64_t of_warp[THREADS / 32];
     __shared__ int64_t first_unit;
     __shared__ int found;
     const int per = (a.seqs + THREADS - 1) / THREADS, b0 = min(a.seqs, static_cast<int>(threadIdx.x) * per), b1 = min(a.seqs, b0 + per);
     int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += units_of(a, read_sequence(a, b, rows_of_tile));
+    for (int b = b0; b < b1; ++b) mine += units_of(a, read_sequence<TILE>(a, b, rows_of_tile));
     const int64_t scan = warp_scan(mine);
     if ((threadIdx.x & 31) == 31) of_warp[threadIdx.x >> 5] = scan;
     if (threadIdx.x == 0) found = a.seqs;
@@ -101,7 +108,7 @@ __device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_t
     const int64_t ctas = min(total, static_cast<int64_t>(gridDim.x)), u = blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
     if (u >= before && u < before + mine) {
         for (int b = b0; b < b1; ++b) {
-            const int64_t units = units_of(a, read_sequence(a, b, rows_of_tile));
+            const int64_t units = units_of(a, read_sequence<TILE>(a, b, rows_of_tile));
             if (u < before + units) {
                 found = b;
                 first_unit = before;
@@ -126,6 +133,10 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 p = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
@@ -154,21 +165,13 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid) : "memory");
 }
-// BYTES of a head's codes, of which those past `valid` are zeros, in pieces that the head's alignment allows
-template <int BYTES>
-__device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t* src, int valid, int piece) {
-    if (BYTES == 16 && piece == 16) {
-        cp_async<16>(dst, src, valid > 0 ? 16 : 0);
-    } else if (BYTES >= 8 && piece >= 8) {
-#pragma unroll
-        for (int i = 0; i < BYTES; i += 8) cp_async<8>(dst + i, src + (valid > i ? i : 0), valid > i ? 8 : 0);
-    } else {
-#pragma unroll
-        for (int i = 0; i < BYTES; i += 4) cp_async<4>(dst + i, src + (valid > i ? i : 0), valid > i ? 4 : 0);
-    }
-}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// a box of a head's codes (16-byte chunks swizzled), rows one token apart
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const void* tmap, uint32_t bar, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 
 // ------------------------------------------------------------------------------------------------ codes to matrix operands
 
@@ -180,145 +183,256 @@ __device__ __forceinline__ void int8_to_f16(uint32_t w, uint32_t (&r)[2]) {
 }
 // Codes in bytes 0 and 2 of x as bf16: the low seven bits in the fraction of 128, minus 128 or (sign bit) 256
 __device__ __forceinline__ uint32_t int8_to_bf16(uint32_t x) { return sub_bf16x2((x & 0x007f007fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u); }
-// Eight E2M1 codes as fp16 times 2^-14 (sign, two bits of exponent and one of fraction in their places): elements 0 2 | 1 3 | 4 6 | 5 7
-__device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t mul, uint32_t (&r)[4]) {
-    const uint32_t odd = (w & 0x80808080u) | ((w >> 3) & 0x0e0e0e0eu), even = ((w << 4) & 0x80808080u) | ((w << 1) & 0x0e0e0e0eu);
-    r[0] = mul_f16x2(__byte_perm(even, 0u, 0x1404), mul);
-    r[1] = mul_f16x2(__byte_perm(odd, 0u, 0x1404), mul);
-    r[2] = mul_f16x2(__byte_perm(even, 0u, 0x3424), mul);
-    r[3] = mul_f16x2(__byte_perm(odd, 0u, 0x3424), mul);
-}
-// E2M1 code i (0 to 3) of both halves of t as bf16 times 2^-126, times mul
-template <int I>
-__device__ __forceinline__ uint32_t e2m1_to_bf16(uint32_t t, uint32_t mul) {
-    const uint32_t sign = (I < 3 ? t << (12 - 4 * I) : t) & 0x80008000u;
-    const uint32_t mag = (I < 2 ? t << (6 - 4 * I) : t >> (4 * I - 6)) & 0x01c001c0u;
-    return mul_bf16x2(sign | mag, mul);
+// Eight E2M1 codes as fp16, in pairs
+__device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t (&r)[4]) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
 }
 
-template <int FMT, int DP> struct Layout {
+// Where things are. Lane (g, c) feeds column g of the products with a token's keys (dims of chunks that its c gives) and column g of the products with
+// values (its dims of four tokens); which dims those are is free as long as queries and outputs follow.
+template <int FMT, int DP, int NT> struct Layout {
+    static constexpr int TOK = 8 * NT;                                          // tokens of a step
     static constexpr int PER_BYTE = FMT == KV_CACHE_INT8 ? 1 : 2;
     static constexpr int ROW = DP / PER_BYTE;                                   // bytes of a head, padded
-    static constexpr int KB = ROW / 4 < 16 ? ROW / 4 : 16, KCH = ROW / 4 / KB;  // keys: chunk j of lane c at byte (j * 4 + c) * KB
-    static constexpr int VB = ROW / 8 < 16 ? ROW / 8 : 16, VCH = ROW / 8 / VB;  // values: chunk j of lane g at byte (j * 8 + g) * VB
-    static constexpr int KC = KB * PER_BYTE, VC = VB * PER_BYTE;                // codes of a chunk
+    static constexpr int BOX = ROW < 128 ? ROW : 128, BOXES = ROW / BOX;        // bytes of a row of a box, boxes side by side: a box is swizzled
+    static constexpr int KB = ROW / 4 < 16 ? ROW / 4 : 16, KCH = ROW / 4 / KB;  // keys: bytes of a chunk, chunks of a lane
+    static constexpr int VB = ROW / 8 < 16 ? ROW / 8 : 16, VCH = ROW / 8 / VB;  // values
+    static constexpr int VC = VB * PER_BYTE;                                    // codes of a chunk of values
     static constexpr int KS = DP / 16;                                          // products of 16 along a head
-    static constexpr int K_BYTES = kStep * ROW, SCALES = 2 * K_BYTES, FACTORS = SCALES + (FMT == KV_CACHE_INT8 ? 0 : 512), STAGE = FACTORS + 128 + 16;
-    static constexpr int STAGES = ROW <= 128 ? 3 : 2;                           // steps in a warp's ring
+    static constexpr int BLOCKS = DP / kMxBlock;
+    static constexpr int K_BYTES = TOK * ROW, CODES = 2 * K_BYTES;              // codes of a stage: a multiple of the swizzle's 1024 bytes
+    // and what goes with them: scales (4-bit: the words that hold a head's bytes), the shifts of these words, a bit for each token that may be seen
+    static constexpr int WORDS = FMT == KV_CACHE_INT8 ? 1 : BLOCKS > 4 ? 4 : 2;
+    static constexpr int META = 2 * TOK * 4 * WORDS, SEEN = META + (FMT == KV_CACHE_INT8 ? 0 : 4 * TOK), REST = SEEN + 16;
+    // per warp, not per stage (4-bit): multipliers [side][block][token] fp16, factors [side][token] fp32
+    static constexpr int MULS = FMT == KV_CACHE_INT8 ? 0 : 2 * BLOCKS * TOK * 2, PREP = FMT == KV_CACHE_INT8 ? 0 : MULS + 2 * TOK * 4;
+
+    __device__ static __forceinline__ int k_offset(int j, int c) {              // first byte of chunk j of lane c in a row
+        return KB == 16 && KCH > 1 ? (j / 2) * 128 + (2 * c + (j & 1)) * 16 : c * KB;
+    }
+    __device__ static __forceinline__ int v_offset(int j, int g) { return j * 128 + g * VB; }
+    // byte `off` of row r of one side of a stage: chunks of 16 bytes change places by the row
+    __device__ static __forceinline__ int place(int r, int off) {
+        const int box = off / BOX, in = off % BOX;
+        const int turn = BOX == 128 ? r & 7 : BOX == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+        return box * TOK * BOX + r * BOX + (in ^ (turn << 4));
+    }
     // element of q behind operand pair p, half e, of product s in lane c
     __device__ static __forceinline__ int element(int s, int c, int p, int e) {
-        if (FMT == KV_CACHE_INT8) return (s / 4 * 4 + c) * KC + s % 4 * 4 + 2 * p + e;
-        const int word = s / 2, words = KB / 4;
-        return (word / words * 4 + c) * KC + word % words * 8 + s % 2 * 4 + p + 2 * e;
+        constexpr int words = KB / 4, per_word = FMT == KV_CACHE_INT8 ? 1 : 2;
+        const int word = s / per_word;
+        return k_offset(word / words, c) * PER_BYTE + word % words * 4 * PER_BYTE + s % per_word * 4 + 2 * p + e;
     }
 };
 
+// ------------------------------------------------------------------------------------------------ results
+
+// Four elements of a row, on their way from parts to the output
+struct Row {
+    float o[4] = {0.f, 0.f, 0.f, 0.f}, m_o = kNone, m_l = kNone, l = 0.f;
+    __device__ __forceinline__ void add(const float4& x, float its_m_o, float its_m_l, float its_l) {
+        const float now_o = fmaxf(m_o, its_m_o), now_l = fmaxf(m_l, its_m_l), mine_o = ex2(m_o - now_o), its_o = ex2(its_m_o - now_o);
+        l = l * ex2(m_l - now_l) + its_l * ex2(its_m_l - now_l);
+        o[0] = o[0] * mine_o + x.x * its_o;
+        o[1] = o[1] * mine_o + x.y * its_o;
+        o[2] = o[2] * mine_o + x.z * its_o;
+        o[3] = o[3] * mine_o + x.w * its_o;
+        m_o = now_o;
+        m_l = now_l;
+    }
+    // r: row of the sequence's new tokens and the group's heads. (4-bit: o stands for o * 2^(m_o - m_l) / 2^12, which may be more than fp32 spans
+    // while o * 2^(m_o - m_l) / l is not: the power is applied in two halves.)
+    template <int FMT>
+    __device__ __forceinline__ void finish(const AttentionArgs& a, const Sequence& s, int head, int r, int d) const {
+        const int node = r / a.group, h = head * a.group + r - node * a.group;
+        float v[4];
+        const float inv = 1.f / l;
+        float by = 1.f;
+        if (FMT == KV_CACHE_MXFP4) by = ex2(fminf(fmaxf(0.5f * (m_o - m_l - 12.f), -126.f), 126.f));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : FMT == KV_CACHE_INT8 ? o[i] * inv : o[i] * inv * by * by;
+        *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(s.begin + node) * a.o_st + h * a.o_sh + d) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        if (d == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;
+    }
+};
+constexpr __host__ __device__ int part_floats(int rows, int dp) { return rows * (dp + 4); }
+
+// Rows of no sequence
+template <int THREADS>
+__device__ __forceinline__ void zero_rest(const AttentionArgs& a) {
+    if (a.zero_rest == 0) return;
+    const int lo = a.seqs > 0 ? max(0, min(a.cu_q[0], a.total_q)) : a.total_q, hi = a.seqs > 0 ? max(lo, min(a.cu_q[a.seqs], a.total_q)) : a.total_q;
+    const int q_heads = a.heads * a.group, eights = a.dim / 8;
+    const int64_t rest = lo + (a.total_q - hi), each = static_cast<int64_t>(q_heads) * eights;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; i < rest * each; i += static_cast<int64_t>(gridDim.x) * THREADS) {
+        int64_t t = i / each;
+        const int e = static_cast<int>(i - t * each), h = e / eights, d = (e - h * eights) * 8;
+        t = t < lo ? t : hi + (t - lo);
+        *reinterpret_cast<uint4*>(a.out + t * a.o_st + h * a.o_sh + d) = make_uint4(0, 0, 0, 0);
+        if (d == 0 && a.lse != nullptr) a.lse[t * q_heads + h] = -INFINITY;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ the kernel
 
-template <int FMT, int DP, int MT>
+// CTAs that are to share an SM: what the registers of the sums allow
+template <int DP, int MT> constexpr int resident() { return DP * MT <= 64 ? 4 : DP * MT <= 128 ? 3 : 2; }
+
+template <int FMT, int DP, int MT, int NT>
 struct Shared {
-    using L = Layout<FMT, DP>;
+    using L = Layout<FMT, DP, NT>;
     static constexpr int ROWS = 16 * MT;
-    static constexpr int RING = kWarps * L::STAGES * L::STAGE, MERGE = kWarps * ROWS * (DP + 4) * 4;      // the ring, and over it the warps' results
-    static constexpr int FRAGS = (RING > MERGE ? RING : MERGE), HALVES = FRAGS + MT * L::KS * 512, ROW_FACTOR = HALVES + ROWS * DP * 2;
-    static constexpr int STATE = ROW_FACTOR + ROWS * 4, BYTES = STATE + 2 * kWarps * ROWS * 4;
+    static constexpr int FRAGS_BYTES = MT * L::KS * 512, STATE_BYTES = 3 * kWarps * ROWS * 4 + ROWS * 4, MERGE = kWarps * ROWS * (DP + 4) * 4;
+    // as many steps in a warp's ring as let the CTAs meant to share an SM do so (227 KB, less what each is charged and wants besides)
+    static constexpr int EACH = 227 * 1024 / resident<DP, MT>() - 2 * 1024 - 512 - FRAGS_BYTES - STATE_BYTES - kWarps * L::PREP;
+    static constexpr int FIT = EACH / (kWarps * (L::CODES + L::REST + 8)), STAGES = FIT > 4 ? 4 : FIT;
+    static constexpr int RING = kWarps * STAGES * L::CODES;
+    // the ring (and over it, at the end, the warps' results); operands of the queries; the rest
+    static constexpr int FRAGS = (RING > MERGE ? RING : MERGE), REST = FRAGS + FRAGS_BYTES, PREP = REST + kWarps * STAGES * L::REST;
+    static constexpr int ROW_FACTOR = PREP + kWarps * L::PREP, STATE = ROW_FACTOR + ROWS * 4, BARS = STATE + 3 * kWarps * ROWS * 4;
+    static constexpr int BYTES = BARS + kWarps * STAGES * 8 + 1024;
+    static_assert(STAGES >= 2 && L::CODES % 1024 == 0 && BARS % 8 == 0, "");
 };
 
-template <int FMT, int DP, int MT>
-__global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ? 3 : 2) kv_attention_kernel(const AttentionArgs a) {
-    using L = Layout<FMT, DP>;
-    using S = Shared<FMT, DP, MT>;
-    constexpr int ROWS = S::ROWS;
-    extern __shared__ __align__(128) uint8_t smem[];
+template <int FMT, int DP, int MT, int NT>
+__global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                                                                                  const AttentionArgs a) {
+    using L = Layout<FMT, DP, NT>;
+    using S = Shared<FMT, DP, MT, NT>;
+    constexpr int ROWS = S::ROWS, TOK = L::TOK, STAGES = S::STAGES;
+    constexpr uint32_t kAllSeen = TOK == 32 ? 0xffffffffu : (1u << (TOK & 31)) - 1;
+    extern __shared__ uint8_t raw_smem[];
+    uint8_t* const smem = raw_smem + (1024 - (smem_u32(raw_smem) & 1023)) % 1024;
     __shared__ int last_one;
-    grid_dep_wait();
+    __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const Share share = share_out<kThreads>(a, ROWS);
+    const uint32_t bars = smem_u32(smem + S::BARS) + warp * STAGES * 8;
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) mbar_init(bars + 8 * i, 1);
+        fence_mbar_init();
+    }
+    const WaitCtl ctl{&abort_flag, a.status, a.sticky, a.limit_ns};
+    grid_dep_wait();
+    const Share share = share_out<kThreads, kWarps * TOK>(a, ROWS);             // (its barriers make the mbarriers known, too)
     int64_t u = share.begin;
     const int64_t u_begin = u, u_end = share.end;
     int b = share.b;
     int64_t first_of_b = share.first_of_b;
     const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
-    const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
-    uint8_t* const ring = smem + warp * L::STAGES * L::STAGE;
-    const uint32_t ring_u32 = smem_u32(ring);
+    uint8_t* const ring = smem + warp * STAGES * L::CODES;
+    uint8_t* const rest = smem + S::REST + warp * STAGES * L::REST;
+    const uint32_t ring_u32 = smem_u32(ring), rest_u32 = smem_u32(rest);
+    uint8_t* const prep = smem + S::PREP + warp * L::PREP;
+    uint32_t loads = 0;                                             // of this warp: stage and parity of a step go by it
+
+    // this lane's places in a stage
+    const int k_at = L::place(g, L::k_offset(0, c));
+    const int v_at[2] = {L::place(2 * c, L::v_offset(0, g)), L::place(2 * c + 1, L::v_offset(0, g))};
 
     while (u < u_end) {
-        Sequence s = read_sequence(a, b, ROWS);
-        while (b + 1 < a.seqs && u - first_of_b >= units_of(a, s)) {                  // (sequences without new tokens have no units)
+        Sequence s = read_sequence<kWarps * TOK>(a, b, ROWS);
+        while (b + 1 < a.seqs && u - first_of_b >= units_of(a, s)) {            // (sequences without new tokens have no units)
             first_of_b += units_of(a, s);
-            s = read_sequence(a, ++b, ROWS);
+            s = read_sequence<kWarps * TOK>(a, ++b, ROWS);
         }
         const int64_t of_b = u - first_of_b;
         const int item = static_cast<int>(of_b / s.tiles), tile0 = static_cast<int>(of_b - static_cast<int64_t>(item) * s.tiles);
         const int head = item / s.row_tiles, row0 = (item - head * s.row_tiles) * ROWS, rows = min(ROWS, s.n * a.group - row0);
         const int steps = static_cast<int>(min(static_cast<int64_t>(s.tiles - tile0), u_end - u));
         const int64_t item_begin = u - tile0, item_end = item_begin + s.tiles;
-        const int first_token = s.start + tile0 * kTile + warp * kStep;
+        const int first_token = s.base + (tile0 * kWarps + warp) * TOK;
 
-        // ---- the cache: a step's 16 tokens into a stage of the warp's ring, codes straight to the lane that will use them
-        auto find = [&](int step) {                                 // slot of token lane % 16 of a step, -1: not seen
-            const int t = first_token + step * kTile + (lane & 15);
+        // ---- the cache: a step's tokens into a stage of the warp's ring. A lane looks up the token of its number and copies its scales; codes come as
+        // boxes of as many tokens as lie side by side in any page, or (heads that are not whole 16-byte pieces) piece by piece.
+        auto find = [&](int step) {                                 // slot of a token, -1: no such page or behind the end
+            const int t = first_token + step * (kWarps * TOK) + (lane & (TOK - 1));
             if (step >= steps || t >= s.stop) return -1;
-            const uint32_t p = static_cast<uint32_t>(t) / static_cast<uint32_t>(a.page);
+            const int p = a.page_shift >= 0 ? t >> a.page_shift : t / a.page;
             const int id = a.table[b * a.table_stride + p];
-            return id >= 0 && id < a.num_pages ? id * a.page + (t - static_cast<int>(p) * a.page) : -1;
+            return id >= 0 && id < a.num_pages ? id * a.page + (t - p * a.page) : -1;
         };
-        auto issue = [&](int step, int slot) {
+        auto issue = [&](int step, int slot, uint32_t load) {
             if (step < steps) {
-                const uint32_t st = ring_u32 + step % L::STAGES * L::STAGE;
-                const uint32_t seen = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
+                const uint32_t stage = load % STAGES, st = ring_u32 + stage * L::CODES, more = rest_u32 + stage * L::REST, bar = bars + 8 * stage;
+                const uint32_t seen = __ballot_sync(0xffffffffu, slot >= 0 && first_token + step * (kWarps * TOK) + (lane & (TOK - 1)) >= s.start) & kAllSeen;
+                if (a.box > 0) {
+                    const bool mine = slot >= 0 && lane < TOK && lane % a.box == 0;
+                    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                    if (lane == 0) mbar_arrive_expect_tx(bar, boxes * 2 * L::BOXES * a.box * L::BOX);
+                    __syncwarp();
+                    if (mine) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int at = __shfl_sync(0xffffffffu, slot, i * 8 + g);
-                    const uint8_t* src = a.k_codes + max(at, 0) * token_bytes + head * row_bytes;
+                        for (int j = 0; j < L::BOXES; ++j) {
+                            tma_load_3d(st + j * TOK * L::BOX + lane * L::BOX, &k_map, bar, j * a.box_step, head, slot);
+                            tma_load_3d(st + L::K_BYTES + j * TOK * L::BOX + lane * L::BOX, &v_map, bar, j * a.box_step, head, slot);
+                        }
+                    }
+                } else {
+                    const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
+                    constexpr int kPieces = L::ROW / 4;                         // four bytes each; two at a time where the head allows it
+                    for (int e = lane; e < TOK * kPieces / 2; e += 32) {
+                        const int r = e / (kPieces / 2), off = (e - r * (kPieces / 2)) * 8;
+                        const int from = __shfl_sync(0xffffffffu, slot, r);
+                        const int64_t where = max(from, 0) * token_bytes + head * row_bytes + off;
+                        const uint32_t to = st + L::place(r, off);
+                        const int valid = from >= 0 ? row_bytes - off : 0;
+                        if (row_bytes % 8 == 0) {
+                            cp_async<8>(to, a.k_codes + (valid > 0 ? where : 0), valid > 0 ? 8 : 0);
+                            cp_async<8>(to + L::K_BYTES, a.v_codes + (valid > 0 ? where : 0), valid > 0 ? 8 : 0);
+                        } else {
 #pragma unroll
-                    for (int j = 0; j < L::KCH; ++j) {
-                        const int off = (j * 4 + c) * L::KB, valid = at >= 0 ? row_bytes - off : 0;
-                        copy_codes<L::KB>(st + ((i * L::KCH + j) * 32 + lane) * L::KB, src + (valid > 0 ? off : 0), valid, a.copy);
+                            for (int i = 0; i < 8; i += 4) {
+                                cp_async<4>(to + i, a.k_codes + (valid > i ? where + i : 0), valid > i ? 4 : 0);
+                                cp_async<4>(to + i + L::K_BYTES, a.v_codes + (valid > i ? where + i : 0), valid > i ? 4 : 0);
+                            }
+                        }
                     }
                 }
+                if (lane < TOK) {
+                    const int64_t entry = static_cast<int64_t>(max(slot, 0)) * a.heads + head;
+                    if (FMT == KV_CACHE_INT8) {
+                        cp_async<4>(more + lane * 4, static_cast<const float*>(a.k_scales) + entry, slot >= 0 ? 4 : 0);
+                        cp_async<4>(more + TOK * 4 + lane * 4, static_cast<const float*>(a.v_scales) + entry, slot >= 0 ? 4 : 0);
+                    } else {                                        // the aligned words that hold the head's bytes
+                        const int64_t first = entry * blocks;
+                        const int shift = static_cast<int>(first & 3);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = __shfl_sync(0xffffffffu, slot, (i >> 1) * 8 + 2 * c + (i & 1));
-                    const uint8_t* src = a.v_codes + max(at, 0) * token_bytes + head * row_bytes;
+                        for (int side = 0; side < 2; ++side) {
+                            const uint8_t* p = static_cast<const uint8_t*>(side == 0 ? a.k_scales : a.v_scales) + first - shift;
 #pragma unroll
-                    for (int j = 0; j < L::VCH; ++j) {
-                        const int off = (j * 8 + g) * L::VB, valid = at >= 0 ? row_bytes - off : 0;
-                        copy_codes<L::VB>(st + L::K_BYTES + ((i * L::VCH + j) * 32 + lane) * L::VB, src + (valid > 0 ? off : 0), valid, a.copy);
+                            for (int i = 0; i < (L::WORDS == 2 ? 2 : 3); ++i) {
+                                const bool there = slot >= 0 && shift + blocks > 4 * i;
+                                cp_async<4>(more + ((side * TOK + lane) * L::WORDS + i) * 4, p + (there ? 4 * i : 0), there ? 4 : 0);
+                            }
+                        }
+                        *reinterpret_cast<int*>(rest + stage * L::REST + L::META + lane * 4) = shift;
                     }
                 }
-                // scales: lanes 0 to 15 the keys', 16 to 31 the values'
-                const int at = __shfl_sync(0xffffffffu, slot, lane & 15);
-                const void* scales = lane < 16 ? a.k_scales : a.v_scales;
-                const int64_t entry = static_cast<int64_t>(max(at, 0)) * a.heads + head;
-                if (FMT == KV_CACHE_INT8) {
-                    cp_async<4>(st + L::FACTORS + lane * 4, static_cast<const float*>(scales) + entry, at >= 0 ? 4 : 0);
-                } else {                                            // the aligned words that hold the head's bytes, two at most
-                    const uint8_t* p = static_cast<const uint8_t*>(scales) + entry * blocks;
-                    const int shift = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 3);
-                    cp_async<4>(st + L::SCALES + lane * 16, p - shift, at >= 0 ? 4 : 0);
-                    const bool two = shift + blocks > 4;
-                    cp_async<4>(st + L::SCALES + lane * 16 + 4, p - shift + (two ? 4 : 0), at >= 0 && two ? 4 : 0);
-                    *reinterpret_cast<int*>(ring + step % L::STAGES * L::STAGE + L::SCALES + lane * 16 + 8) = shift;
-                }
-                if (lane == 0) *reinterpret_cast<uint32_t*>(ring + step % L::STAGES * L::STAGE + L::FACTORS + 128) = seen;
+                if (lane == 0) *reinterpret_cast<uint32_t*>(rest + stage * L::REST + L::SEEN) = seen;
             }
             cp_async_commit();
         };
         int slot;
         {
-            int slots[L::STAGES];
+            int slots[STAGES + 1];
 #pragma unroll
-            for (int i = 0; i < L::STAGES; ++i) slots[i] = find(i);
+            for (int i = 0; i <= STAGES; ++i) slots[i] = find(i);
 #pragma unroll
-            for (int i = 0; i < L::STAGES - 1; ++i) issue(i, slots[i]);
-            slot = slots[L::STAGES - 1];
+            for (int i = 0; i < STAGES; ++i) issue(i, slots[i], loads + i);
+            slot = slots[STAGES];
         }
 
         // ---- queries: rows of fp16 times a power of two, then as operands of the products
-        __half* const halves = reinterpret_cast<__half*>(smem + S::HALVES);
         float* const row_factor = reinterpret_cast<float*>(smem + S::ROW_FACTOR);
+        __half* const halves = reinterpret_cast<__half*>(smem + S::FRAGS);
         for (int r = warp; r < ROWS; r += kWarps) {
             uint4 x = make_uint4(0, 0, 0, 0);
             if (r < rows && lane * 8 < a.dim) {
@@ -326,8 +440,7 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                 x = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(s.begin + node) * a.q_st + h * a.q_sh + lane * 8);
             }
             uint32_t top = absmax_bits8(x);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = __reduce_max_sync(0xffffffffu, top);
             const int field = static_cast<int>(top >> 23);
             // the largest magnitude goes to [2^14, 2^15): elements down to 2^-28 of it stay exact
             const int up = field == 255 ? 0 : min(126, max(-126, 141 - max(field, 1)));
@@ -335,30 +448,35 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
             float f[8];
             unpack_bf16x8(x, f);
             if (lane * 8 < DP) {
-                __half2 h[4];
+                uint32_t h[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i] * mul, f[2 * i + 1] * mul);
-                *reinterpret_cast<uint4*>(halves + r * DP + lane * 8) = *reinterpret_cast<const uint4*>(h);
+                for (int i = 0; i < 4; ++i) h[i] = pack_f16(f[2 * i] * mul, f[2 * i + 1] * mul);
+                *reinterpret_cast<uint4*>(halves + r * DP + lane * 8) = make_uint4(h[0], h[1], h[2], h[3]);
             }
-            if (lane == 0) row_factor[r] = a.scale * kLog2e * __uint_as_float((127 - up) << 23);
+            if (lane == 0) row_factor[r] = a.scale * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f);
         }
         __syncthreads();
         uint4* const frags = reinterpret_cast<uint4*>(smem + S::FRAGS);
-        for (int e = threadIdx.x; e < MT * L::KS * 32; e += kThreads) {
-            const int ln = e & 31, ks = e / 32 % L::KS, r = e / 32 / L::KS * 16 + (ln >> 2);
+        constexpr int EACH = MT * L::KS * 32 / kThreads;            // (rearranged in place, by way of registers)
+        uint4 mine[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int e = threadIdx.x + i * kThreads, ln = e & 31, ks = e / 32 % L::KS, r = e / 32 / L::KS * 16 + (ln >> 2);
             uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __half* from = halves + (r + (i & 1) * 8) * DP;
-                const __half2 p = __halves2half2(from[L::element(ks, ln & 3, i >> 1, 0)], from[L::element(ks, ln & 3, i >> 1, 1)]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&p);
-            }
-            frags[e] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int j = 0; j < 4; ++j)                             // (elements of a pair lie side by side)
+                w[j] = *reinterpret_cast<const uint32_t*>(halves + (r + (j & 1) * 8) * DP + L::element(ks, ln & 3, j >> 1, 0));
+            mine[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) frags[threadIdx.x + i * kThreads] = mine[i];
+        __syncthreads();
 
-        // ---- the steps
-        float o[MT][DP / 8][4], m[MT][2], l[MT][2], factor[MT][2];
+        // ---- the steps. Kept per row: o and its reference m_o (int8: of the scores; 4-bit: of score + logarithm of the value's scale, so that what is
+        // rounded to fp16 is at most 2^8 whatever the scales), the sum l of the exponentials and its reference m_l (the scores').
+        float o[MT][DP / 8][4], m_l[MT][2], m_o[MT][2], factor[MT][2];
+        uint64_t l2[MT][2];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
@@ -367,84 +485,88 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                 for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                m[i][e] = -INFINITY;
-                l[i][e] = 0.f;
+                m_l[i][e] = m_o[i][e] = kNone;
+                l2[i][e] = 0;
                 factor[i][e] = row_factor[i * 16 + e * 8 + g];
             }
         }
-        for (int step = 0; step < steps; ++step) {
-            cp_async_wait<L::STAGES - 2>();
+        for (int step = 0; step < steps; ++step, ++loads) {
+            const int stage = static_cast<int>(loads % STAGES);
+            uint8_t* const st = ring + stage * L::CODES;
+            const uint8_t* const more = rest + stage * L::REST;
+            cp_async_wait<STAGES - 1>();
+            if (a.box > 0) mbar_wait(bars + 8 * stage, loads / STAGES & 1, ctl, kWaitAttention, kStatusTimeout);
             __syncwarp();
-            issue(step + L::STAGES - 1, slot);
-            slot = find(step + L::STAGES);
-            uint8_t* const st = ring + step % L::STAGES * L::STAGE;
-            const uint32_t seen16 = *reinterpret_cast<const uint32_t*>(st + L::FACTORS + 128);
-            float* const factors = reinterpret_cast<float*>(st + L::FACTORS);
-            uint32_t k_mul[2][L::KCH], v_mul[2][L::VCH];
+            const int slot_now = slot;
+            slot = find(step + STAGES + 1);
+            const uint32_t seen = *reinterpret_cast<const uint32_t*>(more + L::SEEN);
+            const int t0 = first_token + step * (kWarps * TOK);
+            const bool masked = seen != kAllSeen || t0 + TOK > s.before;
+            const float* const kf = reinterpret_cast<const float*>(FMT == KV_CACHE_INT8 ? more : prep + L::MULS);
+            const float* const vf = kf + TOK;                       // int8: the values' scales; 4-bit: logarithms of theirs
             bool poison = false;
             if (FMT == KV_CACHE_MXFP4) {
-                // a token's bytes and the largest of them, 2^(it - 127) being the token's factor: lane by lane, then for all to read
-                const uint4 raw = *reinterpret_cast<const uint4*>(st + L::SCALES + lane * 16);
-                uint64_t bytes = (static_cast<uint64_t>(raw.x) | static_cast<uint64_t>(raw.y) << 32) >> (8 * raw.z);
-                if (blocks < 8) bytes &= (uint64_t{1} << (8 * blocks)) - 1;
-                const uint32_t lo = static_cast<uint32_t>(bytes), hi = static_cast<uint32_t>(bytes >> 32);
-                const bool nan = (__vcmpeq4(lo, 0xffffffffu) | __vcmpeq4(hi, 0xffffffffu)) != 0;
-                // (values: a block that is NaN is so by itself, the token's other blocks are not)
-                uint32_t top = __vmaxu4(lo & ~__vcmpeq4(lo, 0xffffffffu), hi & ~__vcmpeq4(hi, 0xffffffffu));
-                top = __vmaxu4(top, top >> 16);
-                top = max(top & 0xffu, (top >> 8) & 0xffu);
-                poison = __any_sync(0xffffffffu, nan && lane >= 16);
-                *reinterpret_cast<uint2*>(st + L::SCALES + lane * 16) = make_uint2(lo, hi);
-                *reinterpret_cast<uint32_t*>(st + L::SCALES + lane * 16 + 8) = top;
-                factors[lane] = nan && lane < 16 ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
-                __syncwarp();
-                const uint8_t* const sb = st + L::SCALES;
+                // a token's bytes; the largest of them, t, makes 2^(t - 127) the token's factor and 2^12 * 2^(byte - t) its blocks' multipliers
+                constexpr int SIDES = TOK == 32 ? 2 : 1;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int largest = sb[(i * 8 + g) * 16 + 8];
+                for (int i = 0; i < SIDES; ++i) {
+                    const int side = TOK == 32 ? i : lane >> 4, tok = lane & (TOK - 1);
+                    const uint32_t* const words = reinterpret_cast<const uint32_t*>(more) + (side * TOK + tok) * L::WORDS;
+                    const int shift = 8 * *reinterpret_cast<const int*>(more + L::META + tok * 4);
+                    uint32_t lo = __funnelshift_r(words[0], words[1], shift), hi = L::BLOCKS > 4 ? __funnelshift_r(words[1], words[L::WORDS / 2], shift) : 0u;
+                    if (blocks < 4) lo &= (1u << (8 * blocks)) - 1;
+                    if (L::BLOCKS > 4 && blocks < 8) hi &= (1u << (8 * max(blocks - 4, 0))) - 1;
+                    const uint32_t nan_lo = __vcmpeq4(lo, 0xffffffffu), nan_hi = L::BLOCKS > 4 ? __vcmpeq4(hi, 0xffffffffu) : 0u;
+                    uint32_t top = __vmaxu4(lo & ~nan_lo, hi & ~nan_hi);
+                    top = __vmaxu4(top, top >> 16);
+                    top = max(top & 0xffu, (top >> 8) & 0xffu);
+                    const bool nan = (nan_lo | nan_hi) != 0;
+                    poison = poison || (nan && side == 1);
+                    __half* const muls = reinterpret_cast<__half*>(prep) + side * L::BLOCKS * TOK + tok;
 #pragma unroll
-                    for (int j = 0; j < L::KCH; ++j) {
-                        const int e = 29 + sb[(i * 8 + g) * 16 + (j * 4 + c) * L::KC / kMxBlock] - largest;        // 2^14 * 2^(byte - largest)
-                        k_mul[i][j] = e > 0 ? static_cast<uint32_t>(e) * 0x04000400u : 0u;
+                    for (int k = 0; k < L::BLOCKS; ++k) {
+                        const int byte = ((k < 4 ? lo : hi) >> (8 * (k & 3))) & 0xff, e = 27 + byte - static_cast<int>(top);
+                        const uint16_t bits = side == 1 && byte == 255 ? 0x7e00 : static_cast<uint16_t>(max(e, 0) << 10);
+                        *reinterpret_cast<uint16_t*>(muls + k * TOK) = bits;
                     }
-#pragma unroll
-                    for (int j = 0; j < L::VCH; ++j) {
-                        uint32_t two = 0;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint8_t* p = sb + (16 + i * 8 + 2 * c + h) * 16;
-                            const int byte = p[(j * 8 + g) * L::VC / kMxBlock], e = 253 + byte - p[8];              // 2^126 * 2^(byte - largest)
-                            two |= (byte == 255 ? 0x7fc0u : e > 0 ? static_cast<uint32_t>(e) << 7 : 0u) << (16 * h);
-                        }
-                        v_mul[i][j] = two;
-                    }
+                    reinterpret_cast<float*>(prep + L::MULS)[side * TOK + tok] =
+                        side == 1 ? static_cast<float>(static_cast<int>(top) - 127) : nan ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
                 }
+                poison = __any_sync(0xffffffffu, poison);
+                __syncwarp();
             }
             // scores
-            float sc[MT][2][4];
+            float sc[MT][NT][4];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sc[i][j][e] = 0.f;
 #pragma unroll
             for (int j = 0; j < L::KCH; ++j) {
-                uint32_t w[2][L::KB / 4];
+                uint32_t w[NT][L::KB / 4], mul[NT];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint8_t* p = st + ((i * L::KCH + j) * 32 + lane) * L::KB;
-                    if (L::KB == 16) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(p);
-                    else *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(p);
+                for (int n = 0; n < NT; ++n) {
+                    const uint8_t* p = st + (j / 2) * TOK * 128 + n * 8 * L::BOX + (k_at ^ ((j & 1) << 4));
+                    if constexpr (L::KB == 16) *reinterpret_cast<uint4*>(w[n]) = *reinterpret_cast<const uint4*>(p);
+                    else *reinterpret_cast<uint2*>(w[n]) = *reinterpret_cast<const uint2*>(p);
+                    if constexpr (FMT == KV_CACHE_MXFP4)
+                        mul[n] = 0x00010001u * *reinterpret_cast<const uint16_t*>(reinterpret_cast<const __half*>(prep) + L::k_offset(j, c) * 2 / kMxBlock * TOK + n * 8 + g);
                 }
 #pragma unroll
                 for (int x = 0; x < L::KB / 4; ++x) {
                     constexpr int PER = FMT == KV_CACHE_INT8 ? 1 : 2;           // products that a word feeds
-                    uint32_t r[2][2 * PER];
+                    uint32_t r[NT][2 * PER];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if constexpr (FMT == KV_CACHE_INT8) int8_to_f16(w[i][x], r[i]);
-                        else e2m1_to_f16(w[i][x], k_mul[i][j], r[i]);
+                    for (int n = 0; n < NT; ++n) {
+                        if constexpr (FMT == KV_CACHE_INT8) {
+                            int8_to_f16(w[n][x], r[n]);
+                        } else {
+                            e2m1_to_f16(w[n][x], r[n]);
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) r[n][y] = mul_f16x2(r[n][y], mul[n]);
+                        }
                     }
 #pragma unroll
                     for (int y = 0; y < PER; ++y) {
@@ -452,33 +574,33 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
 #pragma unroll
                         for (int i = 0; i < MT; ++i) {
                             const uint4 q = frags[(i * L::KS + ks) * 32 + lane];
-                            mma_f16(sc[i][0], q, r[0][2 * y], r[0][2 * y + 1]);
-                            mma_f16(sc[i][1], q, r[1][2 * y], r[1][2 * y + 1]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma_f16(sc[i][n], q, r[n][2 * y], r[n][2 * y + 1]);
                         }
                     }
                 }
             }
-            // softmax: this lane's tokens are 2c, 2c + 1, 8 + 2c and 9 + 2c of the step
-            const int t0 = first_token + step * kTile;
-            const bool masked = seen16 != 0xffffu || t0 + kStep > s.before;
-            float kf[4], vf[4];
-            *reinterpret_cast<float2*>(kf) = *reinterpret_cast<const float2*>(factors + 2 * c);
-            *reinterpret_cast<float2*>(kf + 2) = *reinterpret_cast<const float2*>(factors + 8 + 2 * c);
-            *reinterpret_cast<float2*>(vf) = *reinterpret_cast<const float2*>(factors + 16 + 2 * c);
-            *reinterpret_cast<float2*>(vf + 2) = *reinterpret_cast<const float2*>(factors + 24 + 2 * c);
-            uint4 p[MT];
+            // softmax: this lane's tokens are 8n + 2c and 8n + 2c + 1 of the step, its rows g and g + 8
+            uint64_t kf2[NT], vf2[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                kf2[n] = *reinterpret_cast<const uint64_t*>(kf + 8 * n + 2 * c);
+                vf2[n] = *reinterpret_cast<const uint64_t*>(vf + 8 * n + 2 * c);
+            }
+            uint4 p[MT][NT / 2];
+            bool clean = false;                                     // NaN blocks of values are taken out of the products
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                uint32_t sees[2] = {15u, 15u};
+                uint32_t sees[2] = {~0u, ~0u};
                 if (masked) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int node = min(row0 + i * 16 + e * 8 + g, s.n * a.group - 1) / a.group;
                         sees[e] = 0;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
+                        for (int x = 0; x < 2 * NT; ++x) {
                             const int at = (x >> 1) * 8 + 2 * c + (x & 1), j = t0 + at - s.before;
-                            bool see = (seen16 >> at & 1u) != 0;
+                            bool see = (seen >> at & 1u) != 0;
                             if (see && j >= 0) {
                                 if (a.tree == nullptr) see = j <= node;
                                 else see = (j >> 6) < a.tree_words && (a.tree[static_cast<int64_t>(s.begin + node) * a.tree_words + (j >> 6)] >> (j & 63) & 1) != 0;
@@ -487,14 +609,15 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                         }
                     }
                     if (FMT == KV_CACHE_MXFP4 && poison) {
-                        // NaN blocks of values, for the rows that see them only: taken out of the product, put into the sums
+                        // NaN blocks of values, for the rows that see them only: put into the sums here, kept out of the product below
+                        clean = true;
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             uint32_t bad = 0;
-                            for (int x = 0; x < 4; ++x) {
+                            for (int x = 0; x < 2 * NT; ++x) {
                                 if (!(sees[e] >> x & 1u)) continue;
-                                const uint8_t* bytes = st + L::SCALES + (16 + (x >> 1) * 8 + 2 * c + (x & 1)) * 16;
-                                for (int k = 0; k < blocks; ++k) bad |= static_cast<uint32_t>(bytes[k] == 255) << k;
+                                const uint16_t* its = reinterpret_cast<const uint16_t*>(prep) + L::BLOCKS * TOK + (x >> 1) * 8 + 2 * c + (x & 1);
+                                for (int k = 0; k < blocks; ++k) bad |= static_cast<uint32_t>(its[k * TOK] == 0x7e00) << k;
                             }
                             bad |= __shfl_xor_sync(0xffffffffu, bad, 1);
                             bad |= __shfl_xor_sync(0xffffffffu, bad, 2);
@@ -502,116 +625,159 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                             for (int j = 0; j < L::VCH; ++j)
 #pragma unroll
                                 for (int h = 0; h < 2; ++h)
-                                    if (bad >> ((j * 8 + 2 * c + h) * L::VC / kMxBlock) & 1u)
+                                    if (bad >> (L::v_offset(j, 2 * c + h) * L::PER_BYTE / kMxBlock) & 1u)
 #pragma unroll
                                         for (int x = 0; x < L::VC; ++x) o[i][j * L::VC + x][2 * e + h] = __uint_as_float(0x7fc00000u);
                         }
                     }
                 }
-                float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float v = sc[i][j][e] * kf[2 * j + (e & 1)] * factor[i][e >> 1];
-                        if (masked && !(sees[e >> 1] >> (2 * j + (e & 1)) & 1u)) v = -INFINITY;
-                        sc[i][j][e] = v;
-                        top[e >> 1] = fmaxf(top[e >> 1], v);
-                    }
+                // scores in powers of two; the largest of each row, without and (4-bit) with the values' scales
+                float top_l[2] = {kNone, kNone}, top_o[2] = {kNone, kNone};
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
-                    top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2));
+                    const uint64_t f = pack2(factor[i][e], factor[i][e]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float x, y;
+                        unpack2(mul2(mul2(pack2(sc[i][n][2 * e], sc[i][n][2 * e + 1]), kf2[n]), f), x, y);
+                        if (masked) {
+                            if (!(sees[e] >> (2 * n) & 1u)) x = -INFINITY;
+                            if (!(sees[e] >> (2 * n) & 2u)) y = -INFINITY;
+                        }
+                        sc[i][n][2 * e] = x;
+                        sc[i][n][2 * e + 1] = y;
+                        top_l[e] = fmaxf(top_l[e], fmaxf(x, y));
+                        if (FMT == KV_CACHE_MXFP4) {
+                            unpack2(add2(pack2(x, y), vf2[n]), x, y);
+                            top_o[e] = fmaxf(top_o[e], fmaxf(x, y));
+                        }
+                    }
                 }
-                // the running maximum may lag by 2^8: nothing is rescaled for less
-                if (__any_sync(0xffffffffu, top[0] > m[i][0] + 8.f || top[1] > m[i][1] + 8.f)) {
+                // the references may lag by 2^8: nothing is rescaled for less
+                bool move = top_l[0] > m_l[i][0] + 8.f || top_l[1] > m_l[i][1] + 8.f;
+                if (FMT == KV_CACHE_MXFP4) move = move || top_o[0] > m_o[i][0] + 8.f || top_o[1] > m_o[i][1] + 8.f;
+                if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float now = fmaxf(m[i][e], top[e]), scale = now == -INFINITY ? 1.f : ex2(m[i][e] - now);
-                        m[i][e] = now;
-                        l[i][e] *= scale;
+                        top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], 1));
+                        top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], 2));
+                        const float now_l = fmaxf(m_l[i][e], top_l[e]), by_l = ex2(m_l[i][e] - now_l);
+                        m_l[i][e] = now_l;
+                        l2[i][e] = mul2(l2[i][e], pack2(by_l, by_l));
+                        float by_o = by_l;
+                        if (FMT == KV_CACHE_MXFP4) {
+                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], 1));
+                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], 2));
+                            const float now_o = fmaxf(m_o[i][e], top_o[e]);
+                            by_o = ex2(m_o[i][e] - now_o);
+                            m_o[i][e] = now_o;
+                        }
 #pragma unroll
                         for (int j = 0; j < DP / 8; ++j) {
-                            o[i][j][2 * e] *= scale;
-                            o[i][j][2 * e + 1] *= scale;
+                            o[i][j][2 * e] *= by_o;
+                            o[i][j][2 * e + 1] *= by_o;
                         }
                     }
                 }
-                const float base[2] = {m[i][0] == -INFINITY ? 0.f : m[i][0], m[i][1] == -INFINITY ? 0.f : m[i][1]};
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t packed[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x = ex2(sc[i][j][e] - base[e >> 1]);
-                        l[i][e >> 1] += x;
-                        sc[i][j][e] = masked && !(sees[e >> 1] >> (2 * j + (e & 1)) & 1u) ? 0.f : x * vf[2 * j + (e & 1)];
+                    for (int e = 0; e < 2; ++e) {
+                        const uint64_t score = pack2(sc[i][n][2 * e], sc[i][n][2 * e + 1]);
+                        float x, y;
+                        unpack2(add2(score, pack2(-m_l[i][e], -m_l[i][e])), x, y);
+                        const uint64_t both = pack2(ex2(x), ex2(y));
+                        l2[i][e] = add2(l2[i][e], both);
+                        if (FMT == KV_CACHE_INT8) {
+                            unpack2(mul2(both, vf2[n]), x, y);
+                            if (masked) {                           // (the scale of a token that is not seen may be NaN)
+                                if (!(sees[e] >> (2 * n) & 1u)) x = 0.f;
+                                if (!(sees[e] >> (2 * n) & 2u)) y = 0.f;
+                            }
+                            packed[e] = pack_bf16(x, y);
+                        } else {
+                            unpack2(add2(score, add2(vf2[n], pack2(-m_o[i][e], -m_o[i][e]))), x, y);
+                            packed[e] = pack_f16(ex2(x), ex2(y));
+                        }
                     }
-                p[i] = make_uint4(pack_bf16(sc[i][0][0], sc[i][0][1]), pack_bf16(sc[i][0][2], sc[i][0][3]), pack_bf16(sc[i][1][0], sc[i][1][1]),
-                                  pack_bf16(sc[i][1][2], sc[i][1][3]));
-            }
-            if (FMT == KV_CACHE_MXFP4 && masked && poison) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < L::VCH; ++j) {
-                        if ((v_mul[i][j] & 0xffffu) == 0x7fc0u) v_mul[i][j] &= 0xffff0000u;
-                        if (v_mul[i][j] >> 16 == 0x7fc0u) v_mul[i][j] &= 0xffffu;
-                    }
-            }
-            // values
-#pragma unroll
-            for (int j = 0; j < L::VCH; ++j) {
-                uint32_t w[4][L::VB / 4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint8_t* from = st + L::K_BYTES + ((i * L::VCH + j) * 32 + lane) * L::VB;
-                    if constexpr (L::VB == 16) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(from);
-                    else if constexpr (L::VB == 8) *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(from);
-                    else w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+                    if (n & 1) { p[i][n / 2].z = packed[0]; p[i][n / 2].w = packed[1]; }
+                    else { p[i][n / 2].x = packed[0]; p[i][n / 2].y = packed[1]; }
                 }
+            }
+            // values, 16 tokens at a time
 #pragma unroll
-                for (int x = 0; x < L::VB / 4; ++x) {
+            for (int k = 0; k < NT / 2; ++k)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {                      // two bytes of each token's word, tokens side by side
-                        const uint32_t t0w = __byte_perm(w[0][x], w[1][x], half ? 0x7632 : 0x5410), t1w = __byte_perm(w[2][x], w[3][x], half ? 0x7632 : 0x5410);
+                for (int j = 0; j < L::VCH; ++j) {
+                    uint32_t w[4][L::VB / 4], mul[2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint8_t* from = st + L::K_BYTES + j * TOK * 128 + (16 * k + (i >> 1) * 8) * L::BOX + v_at[i & 1];
+                        if constexpr (L::VB == 16) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(from);
+                        else if constexpr (L::VB == 8) *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(from);
+                        else w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+                    }
+                    if constexpr (FMT == KV_CACHE_MXFP4) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            mul[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __half*>(prep) + (L::BLOCKS + L::v_offset(j, g) * 2 / kMxBlock) * TOK + 16 * k + 8 * i + 2 * c);
+                            if (clean) {
+                                if ((mul[i] & 0xffffu) == 0x7e00u) mul[i] &= 0xffff0000u;
+                                if (mul[i] >> 16 == 0x7e00u) mul[i] &= 0xffffu;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int x = 0; x < L::VB / 4; ++x) {
                         if constexpr (FMT == KV_CACHE_INT8) {
 #pragma unroll
-                            for (int y = 0; y < 2; ++y) {
-                                const uint32_t b0 = int8_to_bf16(y ? t0w >> 8 : t0w), b1 = int8_to_bf16(y ? t1w >> 8 : t1w);
+                            for (int half = 0; half < 2; ++half) {              // two bytes of each token's word, tokens side by side
+                                const uint32_t t0w = __byte_perm(w[0][x], w[1][x], half ? 0x7632 : 0x5410), t1w = __byte_perm(w[2][x], w[3][x], half ? 0x7632 : 0x5410);
 #pragma unroll
-                                for (int i = 0; i < MT; ++i) mma_bf16(o[i][j * L::VC + x * 4 + half * 2 + y], p[i], b0, b1);
+                                for (int y = 0; y < 2; ++y) {
+                                    const uint32_t b0 = int8_to_bf16(y ? t0w >> 8 : t0w), b1 = int8_to_bf16(y ? t1w >> 8 : t1w);
+#pragma unroll
+                                    for (int i = 0; i < MT; ++i) mma_bf16(o[i][j * L::VC + x * 4 + half * 2 + y], p[i][k], b0, b1);
+                                }
                             }
                         } else {
-                            const uint32_t b0[4] = {e2m1_to_bf16<0>(t0w, v_mul[0][j]), e2m1_to_bf16<1>(t0w, v_mul[0][j]), e2m1_to_bf16<2>(t0w, v_mul[0][j]),
-                                                    e2m1_to_bf16<3>(t0w, v_mul[0][j])};
-                            const uint32_t b1[4] = {e2m1_to_bf16<0>(t1w, v_mul[1][j]), e2m1_to_bf16<1>(t1w, v_mul[1][j]), e2m1_to_bf16<2>(t1w, v_mul[1][j]),
-                                                    e2m1_to_bf16<3>(t1w, v_mul[1][j])};
+                            uint32_t f[4][4];
 #pragma unroll
-                            for (int y = 0; y < 4; ++y)
+                            for (int i = 0; i < 4; ++i) e2m1_to_f16(w[i][x], f[i]);
 #pragma unroll
-                                for (int i = 0; i < MT; ++i) mma_bf16(o[i][j * L::VC + x * 8 + half * 4 + y], p[i], b0[y], b1[y]);
+                            for (int y = 0; y < 8; ++y) {
+                                const uint32_t pick = y & 1 ? 0x7632 : 0x5410;
+                                const uint32_t b0 = mul_f16x2(__byte_perm(f[0][y / 2], f[1][y / 2], pick), mul[0]), b1 = mul_f16x2(__byte_perm(f[2][y / 2], f[3][y / 2], pick), mul[1]);
+#pragma unroll
+                                for (int i = 0; i < MT; ++i) mma_f16(o[i][j * L::VC + x * 8 + y], p[i][k], b0, b1);
+                            }
                         }
                     }
                 }
-            }
+            __syncwarp();                                           // every lane is done with the stage
+            issue(step + STAGES, slot_now, loads + STAGES);
         }
         cp_async_wait<0>();
 
         // ---- the warps' results meet in shared memory
         __syncthreads();
         float* const merge = reinterpret_cast<float*>(smem);
-        float* const state = reinterpret_cast<float*>(smem + S::STATE);                       // [warp][row] maxima, then sums
+        float* const state = reinterpret_cast<float*>(smem + S::STATE);                       // [warp][row]: references of o, of the sums, the sums
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = i * 16 + e * 8 + g;
-                float sum = l[i][e];
+                float sum, other;
+                unpack2(l2[i][e], sum, other);
+                sum += other;
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                 if (c == 0) {
-                    state[warp * ROWS + r] = m[i][e];
-                    state[(kWarps + warp) * ROWS + r] = sum;
+                    state[warp * ROWS + r] = FMT == KV_CACHE_INT8 ? m_l[i][e] : m_o[i][e];
+                    state[(kWarps + warp) * ROWS + r] = m_l[i][e];
+                    state[(2 * kWarps + warp) * ROWS + r] = sum;
                 }
                 float* to = merge + (warp * ROWS + r) * (DP + 4);
 #pragma unroll
@@ -620,43 +786,25 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int x = 0; x < L::VC; x += 4)
-                            *reinterpret_cast<float4*>(to + (j * 8 + 2 * c + h) * L::VC + x) =
+                            *reinterpret_cast<float4*>(to + L::v_offset(j, 2 * c + h) * L::PER_BYTE + x) =
                                 make_float4(o[i][j * L::VC + x][2 * e + h], o[i][j * L::VC + x + 1][2 * e + h], o[i][j * L::VC + x + 2][2 * e + h], o[i][j * L::VC + x + 3][2 * e + h]);
             }
         __syncthreads();
         const bool whole = tile0 == 0 && steps == s.tiles;
-        constexpr int PART = ROWS * (DP + 2);
+        constexpr int PART = part_floats(ROWS, DP);
         float* const part = a.parts + (2 * static_cast<int64_t>(blockIdx.x) + (u_begin > item_begin ? 0 : 1)) * PART;
-        auto finish = [&](int r, int d, const float (&v)[4], float top, float sum) {          // four elements of a row
-            const int node = (row0 + r) / a.group, h = head * a.group + (row0 + r) - node * a.group;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const uint2 two = sum == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
-            *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(s.begin + node) * a.o_st + h * a.o_sh + d) = two;
-            if (d == 0 && a.lse != nullptr)
-                a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-        };
         const int quads = a.dim / 4;
         for (int e = threadIdx.x; e < rows * quads; e += kThreads) {
             const int r = e / quads, d = (e - r * quads) * 4;
-            float top = -INFINITY;
+            Row v;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, state[w * ROWS + r]);
-            float v[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float weight = top == -INFINITY ? 1.f : ex2(state[w * ROWS + r] - top);
-                const float4 x = *reinterpret_cast<const float4*>(merge + (w * ROWS + r) * (DP + 4) + d);
-                sum += weight * state[(kWarps + w) * ROWS + r];
-                v[0] += weight * x.x; v[1] += weight * x.y; v[2] += weight * x.z; v[3] += weight * x.w;
-            }
+            for (int w = 0; w < kWarps; ++w)
+                v.add(*reinterpret_cast<const float4*>(merge + (w * ROWS + r) * (DP + 4) + d), state[w * ROWS + r], state[(kWarps + w) * ROWS + r], state[(2 * kWarps + w) * ROWS + r]);
             if (whole) {
-                finish(r, d, v, top, sum);
+                v.finish<FMT>(a, s, head, row0 + r, d);
             } else {
-                *reinterpret_cast<float4*>(part + r * DP + d) = make_float4(v[0], v[1], v[2], v[3]);
-                if (d == 0) {
-                    part[ROWS * DP + r] = top;
-                    part[ROWS * DP + ROWS + r] = sum;
-                }
+                *reinterpret_cast<float4*>(part + r * DP + d) = make_float4(v.o[0], v.o[1], v.o[2], v.o[3]);
+                if (d == 0) *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(v.m_o, v.m_l, v.l, 0.f);
             }
         }
         if (!whole) {
@@ -672,36 +820,22 @@ __global__ void __launch_bounds__(kThreads, DP * MT <= 64 ? 4 : DP * MT <= 128 ?
                 __threadfence();
                 for (int e = threadIdx.x; e < rows * quads; e += kThreads) {
                     const int r = e / quads, d = (e - r * quads) * 4;
-                    float v[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f, top = -INFINITY;
+                    Row v;
+#pragma unroll 4
                     for (int x = first; x <= last; ++x) {
                         const float* from = a.parts + (2 * static_cast<int64_t>(x) + (x == first ? 1 : 0)) * PART;
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(from + r * DP + d));
-                        const float its_top = __ldcg(from + ROWS * DP + r), its_sum = __ldcg(from + ROWS * DP + ROWS + r);
-                        const float now = fmaxf(top, its_top);
-                        const float mine = now == -INFINITY ? 1.f : ex2(top - now), its = now == -INFINITY ? 1.f : ex2(its_top - now);
-                        top = now;
-                        sum = sum * mine + its_sum * its;
-                        v[0] = v[0] * mine + y.x * its; v[1] = v[1] * mine + y.y * its; v[2] = v[2] * mine + y.z * its; v[3] = v[3] * mine + y.w * its;
+                        const float4 its = __ldcg(reinterpret_cast<const float4*>(from + ROWS * DP + 4 * r));
+                        v.add(__ldcg(reinterpret_cast<const float4*>(from + r * DP + d)), its.x, its.y, its.z);
                     }
-                    finish(r, d, v, top, sum);
+                    v.finish<FMT>(a, s, head, row0 + r, d);
                 }
             }
         }
-        __syncthreads();                                            // shared memory is the next item's
+        fence_proxy_async_smem();                                   // what threads have written here is overwritten by boxes
+        __syncthreads();
         u += steps;
     }
-    if (a.zero_rest != 0) {                                         // rows of no sequence
-        const int lo = a.seqs > 0 ? max(0, min(a.cu_q[0], a.total_q)) : a.total_q, hi = a.seqs > 0 ? max(lo, min(a.cu_q[a.seqs], a.total_q)) : a.total_q;
-        const int q_heads = a.heads * a.group, eights = a.dim / 8;
-        const int64_t rest = lo + (a.total_q - hi), each = static_cast<int64_t>(q_heads) * eights;
-        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < rest * each; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-            int64_t t = i / each;
-            const int e = static_cast<int>(i - t * each), h = e / eights, d = (e - h * eights) * 8;
-            t = t < lo ? t : hi + (t - lo);
-            *reinterpret_cast<uint4*>(a.out + t * a.o_st + h * a.o_sh + d) = make_uint4(0, 0, 0, 0);
-            if (d == 0 && a.lse != nullptr) a.lse[t * q_heads + h] = -INFINITY;
-        }
-    }
+    zero_rest<kThreads>(a);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -714,21 +848,35 @@ constexpr size_t kAlign = 256;
 
 size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads) {
     const int64_t group = q_heads / heads;
-    return (static_cast<size_t>(seqs + total_q * group / kSmallestRows + 1) * heads * sizeof(uint32_t) + kAlign - 1) / kAlign * kAlign;
+    return kAlign + (static_cast<size_t>(seqs + total_q * group / kSmallestRows + 1) * heads * sizeof(uint32_t) + kAlign - 1) / kAlign * kAlign;
 }
 int padded(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-size_t parts_bytes(int64_t dim) { return static_cast<size_t>(sm_count()) * kMostCtas * 2 * 32 * (padded(dim) + 2) * sizeof(float); }
+size_t parts_bytes(int64_t dim) { return static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(32, padded(dim)) * sizeof(float); }
 bool sizes_fine(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
     return seqs >= 0 && seqs < INT32_MAX && total_q >= 0 && total_q <= INT32_MAX && heads > 0 && q_heads > 0 && q_heads <= KV_CACHE_MAX_WIDTH && q_heads % heads == 0 && dim > 0 &&
            dim <= KV_CACHE_MAX_DIM && q_heads * dim <= KV_CACHE_MAX_WIDTH && heads * dim <= KV_CACHE_MAX_WIDTH && total_q * q_heads <= INT32_MAX;
 }
 
-template <int FMT, int DP, int MT>
-cudaError_t launch(const AttentionArgs& a, cudaStream_t st) {
+// Codes of a side as [slots][heads][bytes of a head], in boxes of `box` tokens of one head. Rows of a box are padded with zeros.
+bool encode_codes(CUtensorMap* tm, const void* codes, int64_t slots, int64_t heads, int64_t row_bytes, int box, int box_bytes) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (enc == nullptr) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(slots)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(heads * row_bytes)};
+    const cuuint32_t boxes[3] = {static_cast<cuuint32_t>(box_bytes), 1, static_cast<cuuint32_t>(box)}, steps[3] = {1, 1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(codes), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+               box_bytes == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int FMT, int DP, int MT, int NT>
+cudaError_t launch(AttentionArgs a, cudaStream_t st) {
+    using S = Shared<FMT, DP, MT, NT>;
+    using L = Layout<FMT, DP, NT>;
     static PerDeviceOnce once;
     static int per_sm = 1;                          // (the same on every device that the library runs on)
-    constexpr int bytes = Shared<FMT, DP, MT>::BYTES;
-    const auto kern = kv_attention_kernel<FMT, DP, MT>;
+    constexpr int bytes = S::BYTES;
+    const auto kern = kv_attention_kernel<FMT, DP, MT, NT>;
     cudaError_t e = once.run([&] {
         const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (set != cudaSuccess) return set;
@@ -738,6 +886,17 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t st) {
         return asked;
     });
     if (e != cudaSuccess) return e;
+    CUtensorMap maps[2] = {};
+    const int64_t row_bytes = a.dim / L::PER_BYTE;
+    if (row_bytes % 16 == 0 && a.num_pages > 0) {
+        // tokens that lie side by side in any page, from any token that a box starts at
+        a.box = 16;
+        while (a.page % a.box != 0) a.box /= 2;
+        a.box_step = L::BOX;
+        if (a.box * L::BOX % 128 != 0) a.box = 0;   // (a box goes to a 128-byte boundary)
+        for (int side = 0; side < 2 && a.box > 0; ++side)
+            if (!encode_codes(&maps[side], side == 0 ? a.k_codes : a.v_codes, static_cast<int64_t>(a.num_pages) * a.page, a.heads, row_bytes, a.box, L::BOX)) return cudaErrorInvalidValue;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sm_count() * per_sm));
     cfg.blockDim = dim3(kThreads);
@@ -748,15 +907,15 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, a);
+    return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], a);
 }
 template <int FMT>
 cudaError_t launch_for(const AttentionArgs& a, int64_t most_rows, cudaStream_t st) {
     const int dp = padded(a.dim);
     const bool two = most_rows > 16;
-    if (dp == 64) return two ? launch<FMT, 64, 2>(a, st) : launch<FMT, 64, 1>(a, st);
-    if (dp == 128) return two ? launch<FMT, 128, 2>(a, st) : launch<FMT, 128, 1>(a, st);
-    return launch<FMT, 256, 1>(a, st);
+    if (dp == 64) return two ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 1, 4>(a, st);
+    if (dp == 128) return two ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 1, 4>(a, st);
+    return launch<FMT, 256, 1, 2>(a, st);
 }
 
 } // namespace
@@ -806,7 +965,7 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.out = static_cast<__nv_bfloat16*>(out);
     a.lse = lse;
-    a.counters = static_cast<uint32_t*>(workspace);
+    a.counters = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + kAlign);          // behind the status word
     a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + counters_bytes(seqs, total_q, q_heads, heads));
     a.q_st = q_token_stride;
     a.q_sh = q_head_stride;
@@ -822,9 +981,12 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.dim = static_cast<int>(dim);
     a.seqs = static_cast<int>(seqs);
     a.total_q = static_cast<int>(total_q);
-    const int64_t row_bytes = fmt == KV_CACHE_INT8 ? dim : dim / 2;
-    a.copy = row_bytes % 16 == 0 ? 16 : row_bytes % 8 == 0 ? 8 : 4;
+    a.page_shift = (page_size & (page_size - 1)) == 0 ? 0 : -1;
+    while (a.page_shift >= 0 && (int64_t{1} << a.page_shift) < page_size) ++a.page_shift;
     a.scale = scale;
+    a.status = static_cast<int*>(workspace);
+    a.sticky = sticky_status_word();
+    a.limit_ns = wait_limit_ns();
     a.zero_rest = zero_rest ? 1 : 0;
     const int64_t most_rows = total_q * a.group / (seqs > 0 ? seqs : 1);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -167,6 +167,11 @@ class Case:
                 unit = ref.two_to(torch.where(flat[3][slot] == 255, 0, flat[3][slot].long()).amax(-1) - 127)
                 bottom = torch.stack([torch.einsum("hgp,ph->hg", p[i][..., see[i]], unit[see[i]]) for i in range(n)])[..., None] * 2.0 ** -134
                 slack = slack + torch.where(dead, 0.0, bottom)
+                # p * unit is an fp16 number relative to the row's largest such product, with steps of 2^-24 at the bottom: half a step a token,
+                # times its value in units
+                worth = torch.where(see[:, None, None], p * unit.transpose(0, 1)[None, :, None], 0.0).amax(-1)
+                steps = torch.stack([torch.einsum("phd->hd", (v / unit[..., None]).abs()[see[i]]) for i in range(n)])[:, :, None]
+                slack = slack + torch.where(dead, 0.0, 2.0 ** -25 * worth[..., None] * steps)
             outs.append(o.reshape(n, -1, self.dim))
             slacks.append(slack.reshape(n, -1, self.dim))
             lse = torch.where(dead, -INF, torch.log(total) + torch.where(top == -INF, 0.0, top))
@@ -186,7 +191,7 @@ class Case:
         return got
 
 
-SHAPES = [(1, 1, 64), (2, 4, 128), (3, 5, 72), (8, 8, 128), (2, 1, 256), (1, 16, 80), (2, 3, 8), (5, 2, 96), (1, 40, 64), (2, 7, 136), (3, 2, 40)]
+SHAPES = [(1, 1, 64), (2, 4, 128), (3, 5, 72), (8, 8, 128), (2, 1, 256), (1, 16, 80), (2, 3, 8), (5, 2, 96), (1, 40, 64), (2, 7, 136), (3, 2, 40), (2, 2, 208), (1, 3, 224), (2, 1, 32)]
 
 
 @pytest.mark.gpu
@@ -223,9 +228,10 @@ def test_rows_that_see_nothing(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
-@pytest.mark.parametrize("page", [1, 3, 16, 64, 100])
-def test_pages_windows_and_empty_sequences(fmt, page):
-    c = Case(fmt, 2, 5, 80, [0, 130, 0, 57, 257, 1, 0], [0, 1, 0, 3, 0, 1, 0], page=page, seed=page)
+@pytest.mark.parametrize("page", [1, 2, 3, 4, 8, 16, 64, 100])
+@pytest.mark.parametrize("dim", [64, 80, 128])
+def test_pages_windows_and_empty_sequences(fmt, page, dim):
+    c = Case(fmt, 2, 5, dim, [0, 130, 0, 57, 257, 1, 0], [0, 1, 0, 3, 0, 1, 0], page=page, seed=page)
     c.check()
     c.starts = torch.tensor([0, 100, 0, 13, 0, 0, 0], dtype=torch.int32, device="cuda")
     c.check()
