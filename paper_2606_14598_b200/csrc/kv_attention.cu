@@ -139,9 +139,10 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 p = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&p);
 }
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&r);
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
@@ -152,13 +153,15 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 // D += A * B, 16 x 8 x 16: rows g and g + 8 of A and D (g = lane / 4), column g of B, column pairs 2c, 2c + 1 of D (c = lane % 4)
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+// 8 x 8 halves, lane (g, c) holding row g, columns 2c and 2c + 1: the transpose in the same places
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 template <int BYTES>
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t valid) {      // valid: BYTES, or 0 for zeros
@@ -175,14 +178,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const void* tmap,
 
 // ------------------------------------------------------------------------------------------------ codes to matrix operands
 
-// Four int8 codes as fp16: code + 128 in the low byte of 1024, minus 1152
-__device__ __forceinline__ void int8_to_f16(uint32_t w, uint32_t (&r)[2]) {
+// Four int8 codes, bytes 0 and 1 and bytes 2 and 3, as fp16: code + 128 in the low byte of 1024, minus 1152
+__device__ __forceinline__ void int8_to_f16(uint32_t w, uint32_t& r0, uint32_t& r1) {
     const uint32_t t = w ^ 0x80808080u;
-    r[0] = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4140), 0x64806480u);
-    r[1] = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4342), 0x64806480u);
+    r0 = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4140), 0x64806480u);
+    r1 = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4342), 0x64806480u);
 }
-// Codes in bytes 0 and 2 of x as bf16: the low seven bits in the fraction of 128, minus 128 or (sign bit) 256
-__device__ __forceinline__ uint32_t int8_to_bf16(uint32_t x) { return sub_bf16x2((x & 0x007f007fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u); }
 // Eight E2M1 codes as fp16, in pairs
 __device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t (&r)[4]) {
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
@@ -194,10 +195,11 @@ __device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t (&r)[4]) {
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
 }
 
-// Where things are. Lane (g, c) feeds column g of the products with a token's keys (dims of chunks that its c gives) and column g of the products with
-// values (its dims of four tokens); which dims those are is free as long as queries and outputs follow.
-template <int FMT, int DP, int NT> struct Layout {
-    static constexpr int TOK = 8 * NT;                                          // tokens of a step
+// Where things are. The codes are the first operand of both products: keys as 16 tokens by 16 elements, values as 16 elements by 16 tokens, so that eight
+// rows of queries are enough to fill the second. Lane (g, c) feeds the keys of tokens g and g + 8 (the elements of chunks that its c gives) and its own
+// elements (by g) of the values of tokens 2c, 2c + 1, 2c + 8 and 2c + 9; which elements those are is free as long as queries and outputs follow.
+template <int FMT, int DP, int TT> struct Layout {
+    static constexpr int TOK = 16 * TT;                                         // tokens of a step
     static constexpr int PER_BYTE = FMT == KV_CACHE_INT8 ? 1 : 2;
     static constexpr int ROW = DP / PER_BYTE;                                   // bytes of a head, padded
     static constexpr int BOX = ROW < 128 ? ROW : 128, BOXES = ROW / BOX;        // bytes of a row of a box, boxes side by side: a box is swizzled
@@ -210,8 +212,8 @@ template <int FMT, int DP, int NT> struct Layout {
     // and what goes with them: scales (4-bit: the words that hold a head's bytes), the shifts of these words, a bit for each token that may be seen
     static constexpr int WORDS = FMT == KV_CACHE_INT8 ? 1 : BLOCKS > 4 ? 4 : 2;
     static constexpr int META = 2 * TOK * 4 * WORDS, SEEN = META + (FMT == KV_CACHE_INT8 ? 0 : 4 * TOK), REST = SEEN + 16;
-    // per warp, not per stage (4-bit): multipliers [side][block][token] fp16, factors [side][token] fp32
-    static constexpr int MULS = FMT == KV_CACHE_INT8 ? 0 : 2 * BLOCKS * TOK * 2, PREP = FMT == KV_CACHE_INT8 ? 0 : MULS + 2 * TOK * 4;
+    // per warp, not per stage: (4-bit) multipliers [side][block][token] fp16; factors of the keys (4-bit) and logarithms of the values' scales, fp32 [token]
+    static constexpr int MULS = FMT == KV_CACHE_INT8 ? 0 : 2 * BLOCKS * TOK * 2, PREP = MULS + 2 * TOK * 4;
 
     __device__ static __forceinline__ int k_offset(int j, int c) {              // first byte of chunk j of lane c in a row
         return KB == 16 && KCH > 1 ? (j / 2) * 128 + (2 * c + (j & 1)) * 16 : c * KB;
@@ -246,17 +248,16 @@ struct Row {
         m_o = now_o;
         m_l = now_l;
     }
-    // r: row of the sequence's new tokens and the group's heads. (4-bit: o stands for o * 2^(m_o - m_l) / 2^12, which may be more than fp32 spans
-    // while o * 2^(m_o - m_l) / l is not: the power is applied in two halves.)
+    // r: row of the sequence's new tokens and the group's heads. o stands for o * 2^(m_o - m_l), 4-bit: / 2^12. The power
+    // may be more than fp32 spans while the result is not: it is applied in two halves.
     template <int FMT>
     __device__ __forceinline__ void finish(const AttentionArgs& a, const Sequence& s, int head, int r, int d) const {
         const int node = r / a.group, h = head * a.group + r - node * a.group;
         float v[4];
         const float inv = 1.f / l;
-        float by = 1.f;
-        if (FMT == KV_CACHE_MXFP4) by = ex2(fminf(fmaxf(0.5f * (m_o - m_l - 12.f), -126.f), 126.f));
+        const float by = ex2(fminf(fmaxf(0.5f * (m_o - m_l - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : FMT == KV_CACHE_INT8 ? o[i] * inv : o[i] * inv * by * by;
+        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : o[i] * inv * by * by;
         *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(s.begin + node) * a.o_st + h * a.o_sh + d) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
         if (d == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;
     }
@@ -281,16 +282,16 @@ __device__ __forceinline__ void zero_rest(const AttentionArgs& a) {
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-// CTAs that are to share an SM: what the registers of the sums allow
-template <int DP, int MT> constexpr int resident() { return DP * MT <= 64 ? 4 : DP * MT <= 128 ? 3 : 2; }
+// CTAs that are to share an SM: what the registers of the sums allow, and 50 KB of codes in flight on it do with
+template <int FMT, int DP, int NR> constexpr int resident() { return DP * NR <= 64 ? 4 : DP * NR <= 128 ? (FMT == KV_CACHE_INT8 ? 3 : 4) : DP * NR <= 256 ? 3 : 2; }
 
-template <int FMT, int DP, int MT, int NT>
+template <int FMT, int DP, int NR, int TT>
 struct Shared {
-    using L = Layout<FMT, DP, NT>;
-    static constexpr int ROWS = 16 * MT;
-    static constexpr int FRAGS_BYTES = MT * L::KS * 512, STATE_BYTES = 3 * kWarps * ROWS * 4 + ROWS * 4, MERGE = kWarps * ROWS * (DP + 4) * 4;
+    using L = Layout<FMT, DP, TT>;
+    static constexpr int ROWS = 8 * NR;
+    static constexpr int FRAGS_BYTES = NR * L::KS * 256, STATE_BYTES = 3 * kWarps * ROWS * 4 + ROWS * 4, MERGE = kWarps * ROWS * (DP + 4) * 4;
     // as many steps in a warp's ring as let the CTAs meant to share an SM do so (227 KB, less what each is charged and wants besides)
-    static constexpr int EACH = 227 * 1024 / resident<DP, MT>() - 2 * 1024 - 512 - FRAGS_BYTES - STATE_BYTES - kWarps * L::PREP;
+    static constexpr int EACH = 227 * 1024 / resident<FMT, DP, NR>() - 2 * 1024 - 512 - FRAGS_BYTES - STATE_BYTES - kWarps * L::PREP;
     static constexpr int FIT = EACH / (kWarps * (L::CODES + L::REST + 8)), STAGES = FIT > 4 ? 4 : FIT;
     static constexpr int RING = kWarps * STAGES * L::CODES;
     // the ring (and over it, at the end, the warps' results); operands of the queries; the rest
@@ -300,11 +301,11 @@ struct Shared {
     static_assert(STAGES >= 2 && L::CODES % 1024 == 0 && BARS % 8 == 0, "");
 };
 
-template <int FMT, int DP, int MT, int NT>
-__global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+template <int FMT, int DP, int NR, int TT>
+__global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attention_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                                                                                   const AttentionArgs a) {
-    using L = Layout<FMT, DP, NT>;
-    using S = Shared<FMT, DP, MT, NT>;
+    using L = Layout<FMT, DP, TT>;
+    using S = Shared<FMT, DP, NR, TT>;
     constexpr int ROWS = S::ROWS, TOK = L::TOK, STAGES = S::STAGES;
     constexpr uint32_t kAllSeen = TOK == 32 ? 0xffffffffu : (1u << (TOK & 31)) - 1;
     extern __shared__ uint8_t raw_smem[];
@@ -456,39 +457,39 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
             if (lane == 0) row_factor[r] = a.scale * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f);
         }
         __syncthreads();
-        uint4* const frags = reinterpret_cast<uint4*>(smem + S::FRAGS);
-        constexpr int EACH = MT * L::KS * 32 / kThreads;            // (rearranged in place, by way of registers)
-        uint4 mine[EACH];
+        uint2* const frags = reinterpret_cast<uint2*>(smem + S::FRAGS);
+        constexpr int EACH = NR * L::KS * 32 / kThreads;            // (rearranged in place, by way of registers)
+        uint2 moved[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int e = threadIdx.x + i * kThreads, ln = e & 31, ks = e / 32 % L::KS, r = e / 32 / L::KS * 16 + (ln >> 2);
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)                             // (elements of a pair lie side by side)
-                w[j] = *reinterpret_cast<const uint32_t*>(halves + (r + (j & 1) * 8) * DP + L::element(ks, ln & 3, j >> 1, 0));
-            mine[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            const int e = threadIdx.x + i * kThreads, ln = e & 31, ks = e / 32 % L::KS, r = e / 32 / L::KS * 8 + (ln >> 2);
+            const __half* from = halves + r * DP;                   // (elements of a pair lie side by side)
+            moved[i] = make_uint2(*reinterpret_cast<const uint32_t*>(from + L::element(ks, ln & 3, 0, 0)), *reinterpret_cast<const uint32_t*>(from + L::element(ks, ln & 3, 1, 0)));
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) frags[threadIdx.x + i * kThreads] = mine[i];
+        for (int i = 0; i < EACH; ++i) frags[threadIdx.x + i * kThreads] = moved[i];
         __syncthreads();
 
-        // ---- the steps. Kept per row: o and its reference m_o (int8: of the scores; 4-bit: of score + logarithm of the value's scale, so that what is
-        // rounded to fp16 is at most 2^8 whatever the scales), the sum l of the exponentials and its reference m_l (the scores').
-        float o[MT][DP / 8][4], m_l[MT][2], m_o[MT][2], factor[MT][2];
-        uint64_t l2[MT][2];
+        // ---- the steps. Kept per row: o and its reference m_o, the sum l of the exponentials and its reference m_l. m_l is the scores'; m_o is that of score
+        // + logarithm of the value's scale, so that the weights that are rounded to fp16 are of the row's own size whatever the scales. This lane's rows: pairs
+        // 2c and 2c + 1 of every eight; its elements of o: those of its g.
+        float o[DP / 16][NR][4];
+        uint64_t l2[NR], m_l[NR], m_o[NR], factor[NR];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
+        for (int i = 0; i < NR; ++i) {
 #pragma unroll
-            for (int j = 0; j < DP / 8; ++j)
+            for (int j = 0; j < DP / 16; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
+                for (int e = 0; e < 4; ++e) o[j][i][e] = 0.f;
+            m_l[i] = m_o[i] = pack2(kNone, kNone);
+            l2[i] = 0;
+            factor[i] = *reinterpret_cast<const uint64_t*>(row_factor + i * 8 + 2 * c);
+        }
+        uint2 queries[NR == 1 ? L::KS : 1];
+        if (NR == 1) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m_l[i][e] = m_o[i][e] = kNone;
-                l2[i][e] = 0;
-                factor[i][e] = row_factor[i * 16 + e * 8 + g];
-            }
+            for (int k = 0; k < (NR == 1 ? L::KS : 1); ++k) queries[k] = frags[k * 32 + lane];
         }
         for (int step = 0; step < steps; ++step, ++loads) {
             const int stage = static_cast<int>(loads % STAGES);
@@ -502,8 +503,12 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
             const uint32_t seen = *reinterpret_cast<const uint32_t*>(more + L::SEEN);
             const int t0 = first_token + step * (kWarps * TOK);
             const bool masked = seen != kAllSeen || t0 + TOK > s.before;
-            const float* const kf = reinterpret_cast<const float*>(FMT == KV_CACHE_INT8 ? more : prep + L::MULS);
-            const float* const vf = kf + TOK;                       // int8: the values' scales; 4-bit: logarithms of theirs
+            float* const logs = reinterpret_cast<float*>(prep + L::MULS) + TOK;                 // of the values' scales
+            const float* const kf = FMT == KV_CACHE_INT8 ? reinterpret_cast<const float*>(more) : logs - TOK;
+            if (FMT == KV_CACHE_INT8) {
+                if (lane < TOK) logs[lane] = lg2(reinterpret_cast<const float*>(more)[TOK + lane]);
+                __syncwarp();
+            }
             bool poison = false;
             if (FMT == KV_CACHE_MXFP4) {
                 // a token's bytes; the largest of them, t, makes 2^(t - 127) the token's factor and 2^12 * 2^(byte - t) its blocks' multipliers
@@ -535,19 +540,19 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
                 poison = __any_sync(0xffffffffu, poison);
                 __syncwarp();
             }
-            // scores
-            float sc[MT][NT][4];
+            // scores: tokens 16t + g ([0], [1]) and 16t + 8 + g ([2], [3]) for rows 2c and 2c + 1
+            float sc[TT][NR][4];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int t = 0; t < TT; ++t)
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+                for (int i = 0; i < NR; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[i][j][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) sc[t][i][e] = 0.f;
 #pragma unroll
             for (int j = 0; j < L::KCH; ++j) {
-                uint32_t w[NT][L::KB / 4], mul[NT];
+                uint32_t w[2 * TT][L::KB / 4], mul[2 * TT];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+                for (int n = 0; n < 2 * TT; ++n) {
                     const uint8_t* p = st + (j / 2) * TOK * 128 + n * 8 * L::BOX + (k_at ^ ((j & 1) << 4));
                     if constexpr (L::KB == 16) *reinterpret_cast<uint4*>(w[n]) = *reinterpret_cast<const uint4*>(p);
                     else *reinterpret_cast<uint2*>(w[n]) = *reinterpret_cast<const uint2*>(p);
@@ -557,11 +562,11 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
 #pragma unroll
                 for (int x = 0; x < L::KB / 4; ++x) {
                     constexpr int PER = FMT == KV_CACHE_INT8 ? 1 : 2;           // products that a word feeds
-                    uint32_t r[NT][2 * PER];
+                    uint32_t r[2 * TT][2 * PER];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
+                    for (int n = 0; n < 2 * TT; ++n) {
                         if constexpr (FMT == KV_CACHE_INT8) {
-                            int8_to_f16(w[n][x], r[n]);
+                            int8_to_f16(w[n][x], r[n][0], r[n][1]);
                         } else {
                             e2m1_to_f16(w[n][x], r[n]);
 #pragma unroll
@@ -572,40 +577,40 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
                     for (int y = 0; y < PER; ++y) {
                         const int ks = (j * (L::KB / 4) + x) * PER + y;
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            const uint4 q = frags[(i * L::KS + ks) * 32 + lane];
+                        for (int i = 0; i < NR; ++i) {
+                            const uint2 q = NR == 1 ? queries[NR == 1 ? ks : 0] : frags[(i * L::KS + ks) * 32 + lane];
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) mma_f16(sc[i][n], q, r[n][2 * y], r[n][2 * y + 1]);
+                            for (int t = 0; t < TT; ++t) mma_f16(sc[t][i], r[2 * t][2 * y], r[2 * t + 1][2 * y], r[2 * t][2 * y + 1], r[2 * t + 1][2 * y + 1], q.x, q.y);
                         }
                     }
                 }
             }
-            // softmax: this lane's tokens are 8n + 2c and 8n + 2c + 1 of the step, its rows g and g + 8
-            uint64_t kf2[NT], vf2[NT];
+            // softmax: this lane's tokens are 8n + g
+            float kfs[2 * TT], lvs[2 * TT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                kf2[n] = *reinterpret_cast<const uint64_t*>(kf + 8 * n + 2 * c);
-                vf2[n] = *reinterpret_cast<const uint64_t*>(vf + 8 * n + 2 * c);
+            for (int n = 0; n < 2 * TT; ++n) {
+                kfs[n] = kf[8 * n + g];
+                lvs[n] = logs[8 * n + g];
             }
-            uint4 p[MT][NT / 2];
+            uint32_t p[NR][2 * TT];
             bool clean = false;                                     // NaN blocks of values are taken out of the products
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                uint32_t sees[2] = {~0u, ~0u};
+            for (int i = 0; i < NR; ++i) {
+                uint32_t sees[2] = {~0u, ~0u};                      // rows 2c and 2c + 1: a bit for each of the lane's tokens
                 if (masked) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const int node = min(row0 + i * 16 + e * 8 + g, s.n * a.group - 1) / a.group;
+                        const int node = min(row0 + i * 8 + 2 * c + e, s.n * a.group - 1) / a.group;
                         sees[e] = 0;
 #pragma unroll
-                        for (int x = 0; x < 2 * NT; ++x) {
-                            const int at = (x >> 1) * 8 + 2 * c + (x & 1), j = t0 + at - s.before;
+                        for (int n = 0; n < 2 * TT; ++n) {
+                            const int at = 8 * n + g, j = t0 + at - s.before;
                             bool see = (seen >> at & 1u) != 0;
                             if (see && j >= 0) {
                                 if (a.tree == nullptr) see = j <= node;
                                 else see = (j >> 6) < a.tree_words && (a.tree[static_cast<int64_t>(s.begin + node) * a.tree_words + (j >> 6)] >> (j & 63) & 1) != 0;
                             }
-                            sees[e] |= static_cast<uint32_t>(see) << x;
+                            sees[e] |= static_cast<uint32_t>(see) << n;
                         }
                     }
                     if (FMT == KV_CACHE_MXFP4 && poison) {
@@ -614,106 +619,91 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             uint32_t bad = 0;
-                            for (int x = 0; x < 2 * NT; ++x) {
-                                if (!(sees[e] >> x & 1u)) continue;
-                                const uint16_t* its = reinterpret_cast<const uint16_t*>(prep) + L::BLOCKS * TOK + (x >> 1) * 8 + 2 * c + (x & 1);
+                            for (int n = 0; n < 2 * TT; ++n) {
+                                if (!(sees[e] >> n & 1u)) continue;
+                                const uint16_t* its = reinterpret_cast<const uint16_t*>(prep) + L::BLOCKS * TOK + 8 * n + g;
                                 for (int k = 0; k < blocks; ++k) bad |= static_cast<uint32_t>(its[k * TOK] == 0x7e00) << k;
                             }
-                            bad |= __shfl_xor_sync(0xffffffffu, bad, 1);
-                            bad |= __shfl_xor_sync(0xffffffffu, bad, 2);
+                            __syncwarp();
+#pragma unroll
+                            for (int x = 4; x < 32; x <<= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, x);       // (the lanes that share its rows)
 #pragma unroll
                             for (int j = 0; j < L::VCH; ++j)
+                                if (bad >> (L::v_offset(j, g) * L::PER_BYTE / kMxBlock) & 1u)
 #pragma unroll
-                                for (int h = 0; h < 2; ++h)
-                                    if (bad >> (L::v_offset(j, 2 * c + h) * L::PER_BYTE / kMxBlock) & 1u)
-#pragma unroll
-                                        for (int x = 0; x < L::VC; ++x) o[i][j * L::VC + x][2 * e + h] = __uint_as_float(0x7fc00000u);
+                                    for (int x = 0; x < L::VC; ++x) o[(j * L::VC + x) / 2][i][(x & 1) * 2 + e] = __uint_as_float(0x7fc00000u);
                         }
                     }
                 }
-                // scores in powers of two; the largest of each row, without and (4-bit) with the values' scales
+                // scores in powers of two; the largest of each row, without and with the values' scales
                 float top_l[2] = {kNone, kNone}, top_o[2] = {kNone, kNone};
+                uint64_t score[2 * TT];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint64_t f = pack2(factor[i][e], factor[i][e]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float x, y;
-                        unpack2(mul2(mul2(pack2(sc[i][n][2 * e], sc[i][n][2 * e + 1]), kf2[n]), f), x, y);
-                        if (masked) {
-                            if (!(sees[e] >> (2 * n) & 1u)) x = -INFINITY;
-                            if (!(sees[e] >> (2 * n) & 2u)) y = -INFINITY;
-                        }
-                        sc[i][n][2 * e] = x;
-                        sc[i][n][2 * e + 1] = y;
-                        top_l[e] = fmaxf(top_l[e], fmaxf(x, y));
-                        if (FMT == KV_CACHE_MXFP4) {
-                            unpack2(add2(pack2(x, y), vf2[n]), x, y);
-                            top_o[e] = fmaxf(top_o[e], fmaxf(x, y));
-                        }
+                for (int n = 0; n < 2 * TT; ++n) {
+                    float x, y;
+                    unpack2(mul2(mul2(pack2(sc[n / 2][i][(n & 1) * 2], sc[n / 2][i][(n & 1) * 2 + 1]), pack2(kfs[n], kfs[n])), factor[i]), x, y);
+                    if (masked) {
+                        if (!(sees[0] >> n & 1u)) x = -INFINITY;
+                        if (!(sees[1] >> n & 1u)) y = -INFINITY;
                     }
+                    top_l[0] = fmaxf(top_l[0], x);
+                    top_l[1] = fmaxf(top_l[1], y);
+                    score[n] = pack2(x, y);
+                    unpack2(add2(score[n], pack2(lvs[n], lvs[n])), x, y);
+                    top_o[0] = fmaxf(top_o[0], x);
+                    top_o[1] = fmaxf(top_o[1], y);
                 }
-                // the references may lag by 2^8: nothing is rescaled for less
-                bool move = top_l[0] > m_l[i][0] + 8.f || top_l[1] > m_l[i][1] + 8.f;
-                if (FMT == KV_CACHE_MXFP4) move = move || top_o[0] > m_o[i][0] + 8.f || top_o[1] > m_o[i][1] + 8.f;
-                if (__any_sync(0xffffffffu, move)) {
+                // Sums and weights may outgrow their references before these move: weights stay below 2^15 and are 2^7 at most where they moved last
+                // (fp16 keeps all its bits down to 2^-21 of that)
+                float ml[2], mo[2];
+                unpack2(m_l[i], ml[0], ml[1]);
+                unpack2(m_o[i], mo[0], mo[1]);
+                if (__any_sync(0xffffffffu, top_l[0] > ml[0] + 16.f || top_l[1] > ml[1] + 16.f || top_o[0] > mo[0] + 15.f || top_o[1] > mo[1] + 15.f)) {
+                    float by_l[2], by_o[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], 1));
-                        top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], 2));
-                        const float now_l = fmaxf(m_l[i][e], top_l[e]), by_l = ex2(m_l[i][e] - now_l);
-                        m_l[i][e] = now_l;
-                        l2[i][e] = mul2(l2[i][e], pack2(by_l, by_l));
-                        float by_o = by_l;
-                        if (FMT == KV_CACHE_MXFP4) {
-                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], 1));
-                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], 2));
-                            const float now_o = fmaxf(m_o[i][e], top_o[e]);
-                            by_o = ex2(m_o[i][e] - now_o);
-                            m_o[i][e] = now_o;
-                        }
 #pragma unroll
-                        for (int j = 0; j < DP / 8; ++j) {
-                            o[i][j][2 * e] *= by_o;
-                            o[i][j][2 * e + 1] *= by_o;
+                        for (int x = 4; x < 32; x <<= 1) {
+                            top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], x));
+                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], x));
                         }
+                        const float now_l = fmaxf(ml[e], top_l[e]), now_o = fmaxf(mo[e], top_o[e] - 7.f);
+                        by_l[e] = ex2(ml[e] - now_l);
+                        by_o[e] = ex2(mo[e] - now_o);
+                        ml[e] = now_l;
+                        mo[e] = now_o;
                     }
+                    m_l[i] = pack2(ml[0], ml[1]);
+                    m_o[i] = pack2(mo[0], mo[1]);
+                    l2[i] = mul2(l2[i], pack2(by_l[0], by_l[1]));
+#pragma unroll
+                    for (int j = 0; j < DP / 16; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[j][i][e] *= by_o[e & 1];
                 }
+                const uint64_t minus_l = pack2(-ml[0], -ml[1]), minus_o = pack2(-mo[0], -mo[1]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t packed[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint64_t score = pack2(sc[i][n][2 * e], sc[i][n][2 * e + 1]);
-                        float x, y;
-                        unpack2(add2(score, pack2(-m_l[i][e], -m_l[i][e])), x, y);
-                        const uint64_t both = pack2(ex2(x), ex2(y));
-                        l2[i][e] = add2(l2[i][e], both);
-                        if (FMT == KV_CACHE_INT8) {
-                            unpack2(mul2(both, vf2[n]), x, y);
-                            if (masked) {                           // (the scale of a token that is not seen may be NaN)
-                                if (!(sees[e] >> (2 * n) & 1u)) x = 0.f;
-                                if (!(sees[e] >> (2 * n) & 2u)) y = 0.f;
-                            }
-                            packed[e] = pack_bf16(x, y);
-                        } else {
-                            unpack2(add2(score, add2(vf2[n], pack2(-m_o[i][e], -m_o[i][e]))), x, y);
-                            packed[e] = pack_f16(ex2(x), ex2(y));
-                        }
+                for (int n = 0; n < 2 * TT; ++n) {
+                    float x, y;
+                    unpack2(add2(score[n], minus_l), x, y);
+                    l2[i] = add2(l2[i], pack2(ex2(x), ex2(y)));
+                    unpack2(add2(score[n], add2(pack2(lvs[n], lvs[n]), minus_o)), x, y);
+                    if (FMT == KV_CACHE_INT8 && masked) {           // (the scale of a token that is not seen may be NaN)
+                        if (!(sees[0] >> n & 1u)) x = -INFINITY;
+                        if (!(sees[1] >> n & 1u)) y = -INFINITY;
                     }
-                    if (n & 1) { p[i][n / 2].z = packed[0]; p[i][n / 2].w = packed[1]; }
-                    else { p[i][n / 2].x = packed[0]; p[i][n / 2].y = packed[1]; }
+                    p[i][n] = transpose8(pack_f16(ex2(x), ex2(y)));
                 }
             }
             // values, 16 tokens at a time
 #pragma unroll
-            for (int k = 0; k < NT / 2; ++k)
+            for (int t = 0; t < TT; ++t)
 #pragma unroll
                 for (int j = 0; j < L::VCH; ++j) {
                     uint32_t w[4][L::VB / 4], mul[2];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint8_t* from = st + L::K_BYTES + j * TOK * 128 + (16 * k + (i >> 1) * 8) * L::BOX + v_at[i & 1];
+                        const uint8_t* from = st + L::K_BYTES + j * TOK * 128 + (16 * t + (i >> 1) * 8) * L::BOX + v_at[i & 1];
                         if constexpr (L::VB == 16) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(from);
                         else if constexpr (L::VB == 8) *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(from);
                         else w[i][0] = *reinterpret_cast<const uint32_t*>(from);
@@ -721,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
                     if constexpr (FMT == KV_CACHE_MXFP4) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            mul[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __half*>(prep) + (L::BLOCKS + L::v_offset(j, g) * 2 / kMxBlock) * TOK + 16 * k + 8 * i + 2 * c);
+                            mul[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __half*>(prep) + (L::BLOCKS + L::v_offset(j, g) * 2 / kMxBlock) * TOK + 16 * t + 8 * i + 2 * c);
                             if (clean) {
                                 if ((mul[i] & 0xffffu) == 0x7e00u) mul[i] &= 0xffff0000u;
                                 if (mul[i] >> 16 == 0x7e00u) mul[i] &= 0xffffu;
@@ -732,25 +722,23 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
                     for (int x = 0; x < L::VB / 4; ++x) {
                         if constexpr (FMT == KV_CACHE_INT8) {
 #pragma unroll
-                            for (int half = 0; half < 2; ++half) {              // two bytes of each token's word, tokens side by side
-                                const uint32_t t0w = __byte_perm(w[0][x], w[1][x], half ? 0x7632 : 0x5410), t1w = __byte_perm(w[2][x], w[3][x], half ? 0x7632 : 0x5410);
+                            for (int half = 0; half < 2; ++half) {              // two elements of each token: tokens side by side
+                                uint32_t a0, a1, a2, a3;
+                                int8_to_f16(__byte_perm(w[0][x], w[1][x], half ? 0x7362 : 0x5140), a0, a1);
+                                int8_to_f16(__byte_perm(w[2][x], w[3][x], half ? 0x7362 : 0x5140), a2, a3);
 #pragma unroll
-                                for (int y = 0; y < 2; ++y) {
-                                    const uint32_t b0 = int8_to_bf16(y ? t0w >> 8 : t0w), b1 = int8_to_bf16(y ? t1w >> 8 : t1w);
-#pragma unroll
-                                    for (int i = 0; i < MT; ++i) mma_bf16(o[i][j * L::VC + x * 4 + half * 2 + y], p[i][k], b0, b1);
-                                }
+                                for (int i = 0; i < NR; ++i) mma_f16(o[(j * L::VC + x * 4) / 2 + half][i], a0, a1, a2, a3, p[i][2 * t], p[i][2 * t + 1]);
                             }
                         } else {
                             uint32_t f[4][4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) e2m1_to_f16(w[i][x], f[i]);
 #pragma unroll
-                            for (int y = 0; y < 8; ++y) {
-                                const uint32_t pick = y & 1 ? 0x7632 : 0x5410;
-                                const uint32_t b0 = mul_f16x2(__byte_perm(f[0][y / 2], f[1][y / 2], pick), mul[0]), b1 = mul_f16x2(__byte_perm(f[2][y / 2], f[3][y / 2], pick), mul[1]);
+                            for (int y = 0; y < 4; ++y) {
+                                const uint32_t a0 = mul_f16x2(__byte_perm(f[0][y], f[1][y], 0x5410), mul[0]), a1 = mul_f16x2(__byte_perm(f[0][y], f[1][y], 0x7632), mul[0]);
+                                const uint32_t a2 = mul_f16x2(__byte_perm(f[2][y], f[3][y], 0x5410), mul[1]), a3 = mul_f16x2(__byte_perm(f[2][y], f[3][y], 0x7632), mul[1]);
 #pragma unroll
-                                for (int i = 0; i < MT; ++i) mma_f16(o[i][j * L::VC + x * 8 + y], p[i][k], b0, b1);
+                                for (int i = 0; i < NR; ++i) mma_f16(o[(j * L::VC + x * 8) / 2 + y][i], a0, a1, a2, a3, p[i][2 * t], p[i][2 * t + 1]);
                             }
                         }
                     }
@@ -765,30 +753,31 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
         float* const merge = reinterpret_cast<float*>(smem);
         float* const state = reinterpret_cast<float*>(smem + S::STATE);                       // [warp][row]: references of o, of the sums, the sums
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < NR; ++i) {
+            float sum[2], ml[2], mo[2];
+            unpack2(l2[i], sum[0], sum[1]);
+            unpack2(m_l[i], ml[0], ml[1]);
+            unpack2(m_o[i], mo[0], mo[1]);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int r = i * 16 + e * 8 + g;
-                float sum, other;
-                unpack2(l2[i][e], sum, other);
-                sum += other;
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                if (c == 0) {
-                    state[warp * ROWS + r] = FMT == KV_CACHE_INT8 ? m_l[i][e] : m_o[i][e];
-                    state[(kWarps + warp) * ROWS + r] = m_l[i][e];
-                    state[(2 * kWarps + warp) * ROWS + r] = sum;
+                const int r = i * 8 + 2 * c + e;
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], x);
+                if (g == 0) {
+                    state[warp * ROWS + r] = mo[e];
+                    state[(kWarps + warp) * ROWS + r] = ml[e];
+                    state[(2 * kWarps + warp) * ROWS + r] = sum[e];
                 }
                 float* to = merge + (warp * ROWS + r) * (DP + 4);
 #pragma unroll
                 for (int j = 0; j < L::VCH; ++j)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int x = 0; x < L::VC; x += 4)
-                            *reinterpret_cast<float4*>(to + L::v_offset(j, 2 * c + h) * L::PER_BYTE + x) =
-                                make_float4(o[i][j * L::VC + x][2 * e + h], o[i][j * L::VC + x + 1][2 * e + h], o[i][j * L::VC + x + 2][2 * e + h], o[i][j * L::VC + x + 3][2 * e + h]);
+                    for (int x = 0; x < L::VC; x += 4) {
+                        const int at = (j * L::VC + x) / 2;
+                        *reinterpret_cast<float4*>(to + L::v_offset(j, g) * L::PER_BYTE + x) = make_float4(o[at][i][e], o[at][i][2 + e], o[at + 1][i][e], o[at + 1][i][2 + e]);
+                    }
             }
+        }
         __syncthreads();
         const bool whole = tile0 == 0 && steps == s.tiles;
         constexpr int PART = part_floats(ROWS, DP);
@@ -842,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, resident<DP, MT>()) kv_attention_ker
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-constexpr int kSmallestRows = 16;                   // rows of the smallest item: the most items, so the most counters
+constexpr int kSmallestRows = 8;                    // rows of the smallest item: the most items, so the most counters
 constexpr int kMostCtas = 4;                        // CTAs on an SM
 constexpr size_t kAlign = 256;
 
@@ -869,14 +858,14 @@ bool encode_codes(CUtensorMap* tm, const void* codes, int64_t slots, int64_t hea
                box_bytes == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int FMT, int DP, int MT, int NT>
+template <int FMT, int DP, int NR, int TT>
 cudaError_t launch(AttentionArgs a, cudaStream_t st) {
-    using S = Shared<FMT, DP, MT, NT>;
-    using L = Layout<FMT, DP, NT>;
+    using S = Shared<FMT, DP, NR, TT>;
+    using L = Layout<FMT, DP, TT>;
     static PerDeviceOnce once;
     static int per_sm = 1;                          // (the same on every device that the library runs on)
     constexpr int bytes = S::BYTES;
-    const auto kern = kv_attention_kernel<FMT, DP, MT, NT>;
+    const auto kern = kv_attention_kernel<FMT, DP, NR, TT>;
     cudaError_t e = once.run([&] {
         const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (set != cudaSuccess) return set;
@@ -912,10 +901,9 @@ cudaError_t launch(AttentionArgs a, cudaStream_t st) {
 template <int FMT>
 cudaError_t launch_for(const AttentionArgs& a, int64_t most_rows, cudaStream_t st) {
     const int dp = padded(a.dim);
-    const bool two = most_rows > 16;
-    if (dp == 64) return two ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 1, 4>(a, st);
-    if (dp == 128) return two ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 1, 4>(a, st);
-    return launch<FMT, 256, 1, 2>(a, st);
+    if (dp == 64) return most_rows <= 8 ? launch<FMT, 64, 1, 2>(a, st) : most_rows <= 16 ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 4, 2>(a, st);
+    if (dp == 128) return most_rows <= 8 ? launch<FMT, 128, 1, 2>(a, st) : most_rows <= 16 ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 4, 1>(a, st);
+    return most_rows <= 8 ? launch<FMT, 256, 1, 1>(a, st) : launch<FMT, 256, 2, 1>(a, st);
 }
 
 } // namespace

@@ -140,8 +140,15 @@ class Case:
             k, v = values(flat[0][slot], flat[1][slot], self.fmt), values(flat[2][slot], flat[3][slot], self.fmt)
             q = self.q[int(self.cu[b]):int(self.cu[b]) + n].double().view(n, self.heads, self.group, self.dim)
             s = torch.einsum("nhgd,phd->nhgp", q, k) * scale
-            # the score's error: dim products added in fp32 (2^-23 each, truncating adders allowed for), three factors, and the exponential's argument
+            # a token's unit: its scale (4 bits: the largest of its blocks'), in which its codes meet the matrix instructions
+            units = []
+            for scales in (flat[1][slot], flat[3][slot]):
+                units.append(scales.double() if self.fmt == "int8" else ref.two_to(torch.where(scales == 255, 0, scales.long()).amax(-1) - 127))
+            # the score's error: dim products added in fp32 (2^-23 each, truncating adders allowed for), three factors, and the exponential's argument;
+            # 4 bits: a block 2^-27 below the unit counts as zero, and its largest element is 6
             off = (torch.einsum("nhgd,phd->nhgp", q.abs(), k.abs()) * abs(scale) * (self.dim + 8) * 2.0 ** -23)
+            if self.fmt == "mxfp4":
+                off = off + torch.einsum("nhgd,ph->nhgp", q.abs(), units[0]) * abs(scale) * 6 * 2.0 ** -27
             hidden = ~see[:, None, None]
             s = s.masked_fill(hidden, -INF)
             top = s.amax(-1, keepdim=True)
@@ -154,28 +161,26 @@ class Case:
             o = torch.stack([torch.einsum("hgp,phd->hgd", p[i][..., see[i]], v[see[i]]) for i in range(n)])
             size = torch.stack([torch.einsum("hgp,phd->hgd", p[i][..., see[i]], v[see[i]].abs()) for i in range(n)])
             o = torch.where(dead, 0.0, o)
-            # probabilities are rounded to bf16 (2^-8), sums and exponentials are fp32; numerator and denominator carry the score's error
-            slack = torch.where(dead, 0.0, size) * (2.0 ** -8 + 2 * off + (self.lengths[b] / 16 + 64) * 2.0 ** -23) + o.abs() * 2.0 ** -8
-            # fp32 has no exponentials below 2^-126: x = 2^(s - m) for a running maximum m of at least (the tokens' largest) - 8 and, where parts meet,
-            # 2^(m - M), are zero there, so a token of less than 2^-126 * 2^8 of the largest may count as nothing: its p |v|. The factor of the product,
-            # x * scale of v, is a bf16 number with steps of 2^-133 at the bottom: half a step times a code of at most 127 a token.
-            small = torch.where(e < 2.0 ** -118, p, 0.0)
+            # weights (probability times unit) are rounded to fp16 (2^-11), sums and exponentials are fp32 (the logarithm of the unit adds 2^-16 for the spacing of
+            # numbers of a few hundred); numerator and denominator carry the score's error; the output is rounded to bf16
+            slack = torch.where(dead, 0.0, size) * (2.0 ** -11 + 2 * off + 2.0 ** -15 + (self.lengths[b] / 16 + 64) * 2.0 ** -23) + o.abs() * 2.0 ** -8
+            # fp32 has no exponentials below 2^-126: x = 2^(s - m) for a running maximum m of at least (the tokens' largest) - 16 and, where parts meet,
+            # 2^(m - M), are zero there, so a token of less than 2^-126 * 2^16 of the largest may count as nothing: its p |v|.
+            small = torch.where(e < 2.0 ** -110, p, 0.0)
             lost = torch.stack([torch.einsum("hgp,phd->hgd", small[i][..., see[i]], v[see[i]].abs()) for i in range(n)])
-            slack = slack + torch.where(dead, 0.0, lost) + self.lengths[b] * 2.0 ** -134 * 127
-            if self.fmt == "mxfp4":
-                # a value is a bf16 number in units of the largest of its head's scales, with steps of 2^-133 at the bottom: half a step a token
-                unit = ref.two_to(torch.where(flat[3][slot] == 255, 0, flat[3][slot].long()).amax(-1) - 127)
-                bottom = torch.stack([torch.einsum("hgp,ph->hg", p[i][..., see[i]], unit[see[i]]) for i in range(n)])[..., None] * 2.0 ** -134
-                slack = slack + torch.where(dead, 0.0, bottom)
-                # p * unit is an fp16 number relative to the row's largest such product, with steps of 2^-24 at the bottom: half a step a token,
-                # times its value in units
-                worth = torch.where(see[:, None, None], p * unit.transpose(0, 1)[None, :, None], 0.0).amax(-1)
-                steps = torch.stack([torch.einsum("phd->hd", (v / unit[..., None]).abs()[see[i]]) for i in range(n)])[:, :, None]
-                slack = slack + torch.where(dead, 0.0, 2.0 ** -25 * worth[..., None] * steps)
+            # weights are fp16 numbers relative to a reference that puts the row's largest at 2^7 at least, with steps of 2^-24 at the bottom: half a step
+            # a token, times its value in units
+            unit = units[1]
+            worth = torch.where(see[:, None, None], p * unit.transpose(0, 1)[None, :, None], 0.0).nan_to_num().amax(-1)
+            steps = torch.stack([torch.einsum("phd->hd", (v / torch.where(unit == 0, 1.0, unit)[..., None]).abs()[see[i]]) for i in range(n)])[:, :, None]
+            slack = slack + torch.where(dead, 0.0, lost + 2.0 ** -32 * worth[..., None] * steps)
+            if self.fmt == "mxfp4":                              # values, too, lose blocks 2^-27 below their unit
+                bottom = torch.stack([torch.einsum("hgp,ph->hg", p[i][..., see[i]], unit[see[i]]) for i in range(n)])[..., None]
+                slack = slack + torch.where(dead, 0.0, bottom * 6 * 2.0 ** -27)
             outs.append(o.reshape(n, -1, self.dim))
             slacks.append(slack.reshape(n, -1, self.dim))
             lse = torch.where(dead, -INF, torch.log(total) + torch.where(top == -INF, 0.0, top))
-            lses.append(torch.cat([lse, off + (self.lengths[b] / 16 + 64) * 2.0 ** -23 * (1 + torch.where(dead, 0.0, lse.abs()))], -1).reshape(n, -1, 2))
+            lses.append(torch.cat([lse, off + 2.0 ** -20 + (self.lengths[b] / 16 + 64) * 2.0 ** -23 * (1 + torch.where(dead, 0.0, lse.abs()))], -1).reshape(n, -1, 2))
         return torch.cat(outs), torch.cat(slacks), torch.cat(lses)
 
     def check(self, scale=None, **kw):
