@@ -4,197 +4,25 @@
 //
 // A token's scale factors out of both products: scores are (q . code) * s_k, and the values' scale multiplies the probability, so what the
 // matrix instructions take are the codes themselves, converted in registers and exact: keys as fp16 beside queries that a power of two of their
-// row brings into fp16's range, values as bf16 beside probabilities rounded to bf16 (their range is that of s_v).
+// row brings into fp16's range, values as fp16 beside weights (probability times s_v) relative to the row's own size.
 //
 // One pass over the cache with a running maximum and sum. The work is cut into units of a few dozen tokens of one head of one sequence, in one
 // long list that the CTAs share out evenly whatever the sequences' lengths: a CTA's range holds ends of at most two items that others share,
 // whose parts meet in the workspace and are added up, in the order of the tokens, by the CTA that arrives last.
-#include "../../include/kv_cache.h"
 #include "internal.h"
-#include "mxfp4_math.cuh"
-#include "ptx.cuh"
+#include "kv_attention.cuh"
 #include "tensor_map.h"
 
 #include <cmath>
-#include <cuda_fp16.h>
 
 namespace w8a8 {
+
+using namespace attention;
+
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kWaitAttention = 40;              // which wait gave up, for the status word
-constexpr float kNone = -3e38f;                 // reference of a row that has seen nothing (finite, so that differences are numbers)
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-struct AttentionArgs {
-    const uint8_t *k_codes, *v_codes;
-    const void *k_scales, *v_scales;
-    const int32_t *table, *lens, *starts, *cu_q;
-    const int64_t* tree;
-    const __nv_bfloat16* q;
-    __nv_bfloat16* out;
-    float* lse;
-    uint32_t* counters;
-    float* parts;
-    int64_t q_st, q_sh, o_st, o_sh, table_stride, tree_words;
-    int num_pages, page, max_pages, heads, group, dim, seqs, total_q;
-    int page_shift;                             // log2 of the page, or -1
-    int box, box_step;                          // tokens of a box of codes, elements from a box to the one beside it; 0: no boxes
-    float scale;
-    int zero_rest;
-    int *status, *sticky;
-    uint64_t limit_ns;
-};
-
-// ------------------------------------------------------------------------------------------------ the list of work
-
-struct Sequence {
-    int begin, n;                               // its rows of q
-    int before;                                 // tokens ahead of the new ones (negative if the cache holds fewer than n)
-    int start, stop;                            // tokens that may be seen
-    int base;                                   // where the units begin: start, rounded down to whole boxes
-    int tiles, row_tiles;
-};
-template <int TILE>                             // tokens of a unit
-__device__ __forceinline__ Sequence read_sequence(const AttentionArgs& a, int b, int rows_of_tile) {
-    Sequence s;
-    const int begin = a.cu_q[b], end = a.cu_q[b + 1], len = a.lens[b];
-    const int64_t most = static_cast<int64_t>(a.max_pages) * a.page;
-    s.begin = max(0, min(begin, a.total_q));
-    s.n = max(s.begin, min(end, a.total_q)) - s.begin;
-    s.before = max(len, 0) - s.n;
-    s.stop = static_cast<int>(min(static_cast<int64_t>(max(len, 0)), most));
-    s.start = a.starts != nullptr ? max(0, min(a.starts[b], s.stop)) : 0;
-    s.base = s.start & ~31;
-    s.tiles = max(1, (s.stop - s.base + TILE - 1) / TILE);
-    s.row_tiles = static_cast<int>((static_cast<int64_t>(s.n) * a.group + rows_of_tile - 1) / rows_of_tile);
-    return s;
-}
-__device__ __forceinline__ int64_t units_of(const AttentionArgs& a, const Sequence& s) { return static_cast<int64_t>(a.heads) * s.row_tiles * s.tiles; }
-
-struct Share {
-    int64_t total, first_of_b;                  // units of all sequences; of those before b
-    int64_t ctas;                               // CTAs that work: none without a unit
-    int64_t begin, end;                         // this CTA's units
-    int b;
-};
-// The sequence that unit `u` (of this CTA's range) belongs to, found by all threads at once; u < 0: only the total
-__device__ __forceinline__ int64_t warp_scan(int64_t v) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t w = __shfl_up_sync(0xffffffffu, v, o);
-        if ((threadIdx.x & 31) >= o) v += w;
-    }
-    return v;
-}
-template <int THREADS, int TILE>
-__device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_tile) {
-    __shared__ int64_t of_warp[THREADS / 32];
-    __shared__ int64_t first_unit;
-    __shared__ int found;
-    const int per = (a.seqs + THREADS - 1) / THREADS, b0 = min(a.seqs, static_cast<int>(threadIdx.x) * per), b1 = min(a.seqs, b0 + per);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += units_of(a, read_sequence<TILE>(a, b, rows_of_tile));
-    const int64_t scan = warp_scan(mine);
-    if ((threadIdx.x & 31) == 31) of_warp[threadIdx.x >> 5] = scan;
-    if (threadIdx.x == 0) found = a.seqs;
-    __syncthreads();
-    int64_t before = scan - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < static_cast<int>(threadIdx.x >> 5)) before += of_warp[w];
-        total += of_warp[w];
-    }
-    const int64_t ctas = min(total, static_cast<int64_t>(gridDim.x)), u = blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
-    if (u >= before && u < before + mine) {
-        for (int b = b0; b < b1; ++b) {
-            const int64_t units = units_of(a, read_sequence<TILE>(a, b, rows_of_tile));
-            if (u < before + units) {
-                found = b;
-                first_unit = before;
-                break;
-            }
-            before += units;
-        }
-    }
-    __syncthreads();
-    return Share{total, found < a.seqs ? first_unit : 0, ctas, u, blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : u, found};
-}
-
-// The CTA whose range holds unit u (CTA c takes units total * c / ctas up to total * (c + 1) / ctas)
-__device__ __forceinline__ int owner(int64_t u, const Share& s) { return static_cast<int>(((u + 1) * s.ctas - 1) / s.total); }
-
-// ------------------------------------------------------------------------------------------------ small pieces
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-    const __half2 p = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-}
-__device__ __forceinline__ float lg2(float x) {
-    float y;
-    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&r);
-}
-// D += A * B, 16 x 8 x 16: rows g and g + 8 of A and D (g = lane / 4), column g of B, column pairs 2c, 2c + 1 of D (c = lane % 4)
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// 8 x 8 halves, lane (g, c) holding row g, columns 2c and 2c + 1: the transpose in the same places
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-template <int BYTES>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t valid) {      // valid: BYTES, or 0 for zeros
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// a box of a head's codes (16-byte chunks swizzled), rows one token apart
-__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const void* tmap, uint32_t bar, int x, int y, int z) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                 ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
-}
-
-// ------------------------------------------------------------------------------------------------ codes to matrix operands
-
-// Four int8 codes, bytes 0 and 1 and bytes 2 and 3, as fp16: code + 128 in the low byte of 1024, minus 1152
-__device__ __forceinline__ void int8_to_f16(uint32_t w, uint32_t& r0, uint32_t& r1) {
-    const uint32_t t = w ^ 0x80808080u;
-    r0 = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4140), 0x64806480u);
-    r1 = sub_f16x2(__byte_perm(t, 0x64646464u, 0x4342), 0x64806480u);
-}
-// Eight E2M1 codes as fp16, in pairs
-__device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t (&r)[4]) {
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
-}
-
 // Where things are. The codes are the first operand of both products: keys as 16 tokens by 16 elements, values as 16 elements by 16 tokens, so that eight
 // rows of queries are enough to fill the second. Lane (g, c) feeds the keys of tokens g and g + 8 (the elements of chunks that its c gives) and its own
 // elements (by g) of the values of tokens 2c, 2c + 1, 2c + 8 and 2c + 9; which elements those are is free as long as queries and outputs follow.
@@ -233,53 +61,6 @@ template <int FMT, int DP, int TT> struct Layout {
     }
 };
 
-// ------------------------------------------------------------------------------------------------ results
-
-// Four elements of a row, on their way from parts to the output
-struct Row {
-    float o[4] = {0.f, 0.f, 0.f, 0.f}, m_o = kNone, m_l = kNone, l = 0.f;
-    __device__ __forceinline__ void add(const float4& x, float its_m_o, float its_m_l, float its_l) {
-        const float now_o = fmaxf(m_o, its_m_o), now_l = fmaxf(m_l, its_m_l), mine_o = ex2(m_o - now_o), its_o = ex2(its_m_o - now_o);
-        l = l * ex2(m_l - now_l) + its_l * ex2(its_m_l - now_l);
-        o[0] = o[0] * mine_o + x.x * its_o;
-        o[1] = o[1] * mine_o + x.y * its_o;
-        o[2] = o[2] * mine_o + x.z * its_o;
-        o[3] = o[3] * mine_o + x.w * its_o;
-        m_o = now_o;
-        m_l = now_l;
-    }
-    // r: row of the sequence's new tokens and the group's heads. o stands for o * 2^(m_o - m_l), 4-bit: / 2^12. The power
-    // may be more than fp32 spans while the result is not: it is applied in two halves.
-    template <int FMT>
-    __device__ __forceinline__ void finish(const AttentionArgs& a, const Sequence& s, int head, int r, int d) const {
-        const int node = r / a.group, h = head * a.group + r - node * a.group;
-        float v[4];
-        const float inv = 1.f / l;
-        const float by = ex2(fminf(fmaxf(0.5f * (m_o - m_l - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : o[i] * inv * by * by;
-        *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(s.begin + node) * a.o_st + h * a.o_sh + d) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-        if (d == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;
-    }
-};
-constexpr __host__ __device__ int part_floats(int rows, int dp) { return rows * (dp + 4); }
-
-// Rows of no sequence
-template <int THREADS>
-__device__ __forceinline__ void zero_rest(const AttentionArgs& a) {
-    if (a.zero_rest == 0) return;
-    const int lo = a.seqs > 0 ? max(0, min(a.cu_q[0], a.total_q)) : a.total_q, hi = a.seqs > 0 ? max(lo, min(a.cu_q[a.seqs], a.total_q)) : a.total_q;
-    const int q_heads = a.heads * a.group, eights = a.dim / 8;
-    const int64_t rest = lo + (a.total_q - hi), each = static_cast<int64_t>(q_heads) * eights;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; i < rest * each; i += static_cast<int64_t>(gridDim.x) * THREADS) {
-        int64_t t = i / each;
-        const int e = static_cast<int>(i - t * each), h = e / eights, d = (e - h * eights) * 8;
-        t = t < lo ? t : hi + (t - lo);
-        *reinterpret_cast<uint4*>(a.out + t * a.o_st + h * a.o_sh + d) = make_uint4(0, 0, 0, 0);
-        if (d == 0 && a.lse != nullptr) a.lse[t * q_heads + h] = -INFINITY;
-    }
-}
-
 // ------------------------------------------------------------------------------------------------ the kernel
 
 // CTAs that are to share an SM: what the registers of the sums allow, and 50 KB of codes in flight on it do with
@@ -311,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
     extern __shared__ uint8_t raw_smem[];
     uint8_t* const smem = raw_smem + (1024 - (smem_u32(raw_smem) & 1023)) % 1024;
     __shared__ int last_one;
-    __shared__ int abort_flag;
+    __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const uint32_t bars = smem_u32(smem + S::BARS) + warp * STAGES * 8;
     if (threadIdx.x == 0) abort_flag = 0;
@@ -747,6 +528,11 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
             issue(step + STAGES, slot_now, loads + STAGES);
         }
         cp_async_wait<0>();
+        if (abort_flag != 0 && a.box > 0) {                         // a wait gave up: the boxes on their way come first
+#pragma unroll
+            for (int i = 1; i <= STAGES; ++i)
+                if (loads >= static_cast<uint32_t>(i)) mbar_drain(bars + 8 * ((loads - i) % STAGES), (loads - i) / STAGES & 1, a.limit_ns);
+        }
 
         // ---- the warps' results meet in shared memory
         __syncthreads();
@@ -796,30 +582,8 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
                 if (d == 0) *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(v.m_o, v.m_l, v.l, 0.f);
             }
         }
-        if (!whole) {
-            const int first = owner(item_begin, share), last = owner(item_end - 1, share);
-            // (place of the item's counter: sequences' row tiles one after another, a place more for each that ends in the middle of one)
-            uint32_t* const counter = a.counters + (static_cast<int64_t>(b) + static_cast<int64_t>(s.begin) * a.group / ROWS + row0 / ROWS) * a.heads + head;
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) last_one = atomicAdd(counter, 1u) == static_cast<uint32_t>(last - first);
-            __syncthreads();
-            if (last_one) {
-                if (threadIdx.x == 0) *counter = 0;
-                __threadfence();
-                for (int e = threadIdx.x; e < rows * quads; e += kThreads) {
-                    const int r = e / quads, d = (e - r * quads) * 4;
-                    Row v;
-#pragma unroll 4
-                    for (int x = first; x <= last; ++x) {
-                        const float* from = a.parts + (2 * static_cast<int64_t>(x) + (x == first ? 1 : 0)) * PART;
-                        const float4 its = __ldcg(reinterpret_cast<const float4*>(from + ROWS * DP + 4 * r));
-                        v.add(__ldcg(reinterpret_cast<const float4*>(from + r * DP + d)), its.x, its.y, its.z);
-                    }
-                    v.finish<FMT>(a, s, head, row0 + r, d);
-                }
-            }
-        }
+        if (!whole)
+            merge_parts<FMT, ROWS, DP, kThreads>(a, s, b, head, row0, rows, owner(item_begin, share), owner(item_end - 1, share), threadIdx.x, &last_one, [] { __syncthreads(); });
         fence_proxy_async_smem();                                   // what threads have written here is overwritten by boxes
         __syncthreads();
         u += steps;
@@ -833,6 +597,7 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 constexpr int kSmallestRows = 8;                    // rows of the smallest item: the most items, so the most counters
 constexpr int kMostCtas = 4;                        // CTAs on an SM
+constexpr int kFewRows = 16;                        // rows of a sequence and head up to which the kernel of this file is chosen
 constexpr size_t kAlign = 256;
 
 size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads) {
@@ -840,7 +605,12 @@ size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t he
     return kAlign + (static_cast<size_t>(seqs + total_q * group / kSmallestRows + 1) * heads * sizeof(uint32_t) + kAlign - 1) / kAlign * kAlign;
 }
 int padded(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-size_t parts_bytes(int64_t dim) { return static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(32, padded(dim)) * sizeof(float); }
+// (most_rows: of any sequence and head; more of them need more)
+size_t parts_bytes(int64_t most_rows, int64_t dim) {
+    const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(32, padded(dim)) * sizeof(float);
+    const size_t many = most_rows > kFewRows ? many_rows_part_bytes(most_rows, dim) : 0;
+    return few > many ? few : many;
+}
 bool sizes_fine(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
     return seqs >= 0 && seqs < INT32_MAX && total_q >= 0 && total_q <= INT32_MAX && heads > 0 && q_heads > 0 && q_heads <= KV_CACHE_MAX_WIDTH && q_heads % heads == 0 && dim > 0 &&
            dim <= KV_CACHE_MAX_DIM && q_heads * dim <= KV_CACHE_MAX_WIDTH && heads * dim <= KV_CACHE_MAX_WIDTH && total_q * q_heads <= INT32_MAX;
@@ -899,11 +669,11 @@ cudaError_t launch(AttentionArgs a, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], a);
 }
 template <int FMT>
-cudaError_t launch_for(const AttentionArgs& a, int64_t most_rows, cudaStream_t st) {
+cudaError_t launch_for(const AttentionArgs& a, int64_t rows, cudaStream_t st) {
     const int dp = padded(a.dim);
-    if (dp == 64) return most_rows <= 8 ? launch<FMT, 64, 1, 2>(a, st) : most_rows <= 16 ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 4, 2>(a, st);
-    if (dp == 128) return most_rows <= 8 ? launch<FMT, 128, 1, 2>(a, st) : most_rows <= 16 ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 4, 1>(a, st);
-    return most_rows <= 8 ? launch<FMT, 256, 1, 1>(a, st) : launch<FMT, 256, 2, 1>(a, st);
+    if (dp == 64) return rows <= 8 ? launch<FMT, 64, 1, 2>(a, st) : rows <= 16 ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 4, 2>(a, st);
+    if (dp == 128) return rows <= 8 ? launch<FMT, 128, 1, 2>(a, st) : rows <= 16 ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 4, 1>(a, st);
+    return rows <= 8 ? launch<FMT, 256, 1, 1>(a, st) : launch<FMT, 256, 2, 1>(a, st);
 }
 
 } // namespace
@@ -917,7 +687,7 @@ size_t kv_cache_attention_zeroed_bytes(int64_t seqs, int64_t total_q, int64_t q_
     return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) : 0;
 }
 size_t kv_cache_attention_workspace_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
-    return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) + parts_bytes(dim) : 0;
+    return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) + parts_bytes(total_q * (q_heads / heads), dim) : 0;
 }
 
 int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int64_t num_pages, int64_t page_size,
@@ -976,9 +746,11 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.sticky = sticky_status_word();
     a.limit_ns = wait_limit_ns();
     a.zero_rest = zero_rest ? 1 : 0;
-    const int64_t most_rows = total_q * a.group / (seqs > 0 ? seqs : 1);
+    const int64_t rows = (total_q * a.group + seqs - 1) / (seqs > 0 ? seqs : 1);       // of a sequence and head, on average
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = fmt == KV_CACHE_INT8 ? launch_for<KV_CACHE_INT8>(a, most_rows, st) : launch_for<KV_CACHE_MXFP4>(a, most_rows, st);
+    const cudaError_t e = rows > kFewRows && many_rows_fits(a.dim) ? launch_many_rows(fmt, a, rows, st)
+                          : fmt == KV_CACHE_INT8                   ? launch_for<KV_CACHE_INT8>(a, rows, st)
+                                                                   : launch_for<KV_CACHE_MXFP4>(a, rows, st);
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }
 

@@ -161,9 +161,9 @@ class Case:
             o = torch.stack([torch.einsum("hgp,phd->hgd", p[i][..., see[i]], v[see[i]]) for i in range(n)])
             size = torch.stack([torch.einsum("hgp,phd->hgd", p[i][..., see[i]], v[see[i]].abs()) for i in range(n)])
             o = torch.where(dead, 0.0, o)
-            # weights (probability times unit) are rounded to fp16 (2^-11), sums and exponentials are fp32 (the logarithm of the unit adds 2^-16 for the spacing of
+            # weights (probability, or probability times unit) are rounded to fp16 (2^-11), and so may be unit and unit times code (many rows); sums and exponentials are fp32 (the logarithm of the unit adds 2^-16 for the spacing of
             # numbers of a few hundred); numerator and denominator carry the score's error; the output is rounded to bf16
-            slack = torch.where(dead, 0.0, size) * (2.0 ** -11 + 2 * off + 2.0 ** -15 + (self.lengths[b] / 16 + 64) * 2.0 ** -23) + o.abs() * 2.0 ** -8
+            slack = torch.where(dead, 0.0, size) * (3 * 2.0 ** -11 + 2 * off + 2.0 ** -15 + (self.lengths[b] / 16 + 64) * 2.0 ** -23) + o.abs() * 2.0 ** -8
             # fp32 has no exponentials below 2^-126: x = 2^(s - m) for a running maximum m of at least (the tokens' largest) - 16 and, where parts meet,
             # 2^(m - M), are zero there, so a token of less than 2^-126 * 2^16 of the largest may count as nothing: its p |v|.
             small = torch.where(e < 2.0 ** -110, p, 0.0)
@@ -174,6 +174,10 @@ class Case:
             worth = torch.where(see[:, None, None], p * unit.transpose(0, 1)[None, :, None], 0.0).nan_to_num().amax(-1)
             steps = torch.stack([torch.einsum("phd->hd", (v / torch.where(unit == 0, 1.0, unit)[..., None]).abs()[see[i]]) for i in range(n)])[:, :, None]
             slack = slack + torch.where(dead, 0.0, lost + 2.0 ** -32 * worth[..., None] * steps)
+            # many rows: the weight is the probability alone; values are fp16 relative to 2^15 = a code of 128 or 8 times twice the sequence's largest unit
+            whole = torch.stack([torch.einsum("phd->hd", v.abs()[see[i]]) for i in range(n)])[:, :, None]
+            largest = unit.nan_to_num().amax(0)[None, :, None, None] if self.lengths[b] else 0.0
+            slack = slack + torch.where(dead, 0.0, 2.0 ** -32 * whole + 2.0 ** -32 * largest)
             if self.fmt == "mxfp4":                              # values, too, lose blocks 2^-27 below their unit
                 bottom = torch.stack([torch.einsum("hgp,ph->hg", p[i][..., see[i]], unit[see[i]]) for i in range(n)])[..., None]
                 slack = slack + torch.where(dead, 0.0, bottom * 6 * 2.0 ** -27)
@@ -215,6 +219,17 @@ def test_several_tokens(fmt, heads, group, dim, tree):
     """Chains and trees of any bits (rows that see no new token, nor themselves), new tokens that are all a sequence has among them."""
     Case(fmt, heads, group, dim, [200, 9, 64, 33], [5, 9, 1, 17], page=20, tree=tree, seed=1).check()
     Case(fmt, heads, group, dim, [150, 333], [64, 70], page=7, tree=tree, seed=2).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("heads,group,dim", [(1, 1, 64), (2, 4, 128), (3, 5, 72), (2, 8, 96), (1, 40, 64), (2, 3, 8), (1, 8, 104)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("news", [(20, 31, 64), (65, 3, 100), (1, 2, 130)])
+def test_many_rows(fmt, heads, group, dim, tree, news):
+    """From a few dozen to some hundred rows of queries a sequence and head, lengths around whole tiles of tokens."""
+    Case(fmt, heads, group, dim, [n + more for n, more in zip(news, (0, 128, 700))], list(news), page=16, tree=tree, seed=3).check()
+    Case(fmt, heads, group, dim, [n + more for n, more in zip(news, (127, 257, 1))], list(news), page=25, tree=tree, seed=4).check()
 
 
 @pytest.mark.gpu
