@@ -179,12 +179,4 @@ bool mx_skinny_preferred(int M, int K);     // where it is chosen when nothing i
 int launch_mx_skinny_bf16(const MxLinearArgs& g, const void* A, int64_t lda, cudaStream_t st);
 int launch_mx_skinny_codes(const MxLinearArgs& g, cudaStream_t st);
 
-// ---- kv_attention_tc.cu : attention over the cache for many rows of queries a head
-namespace attention {
-struct AttentionArgs;
-bool many_rows_fits(int dim);                       // what the kernel can run
-size_t many_rows_part_bytes(int64_t most_rows, int64_t dim);       // scratch for the parts, for at most this many rows of a sequence and head
-cudaError_t launch_many_rows(int fmt, const AttentionArgs& a, int64_t rows, cudaStream_t st);
-} // namespace attention
-
 } // namespace w8a8

@@ -628,10 +628,23 @@ bool encode_codes(CUtensorMap* tm, const void* codes, int64_t slots, int64_t hea
                box_bytes == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The maps of both sides, and a.box: tokens that lie side by side in any page, from any token that a box starts at; 0 where heads are not whole 16-byte pieces
+bool encode_sides(CUtensorMap (&maps)[2], AttentionArgs& a, int fmt) {
+    const int per_byte = fmt == KV_CACHE_INT8 ? 1 : 2, row = padded(a.dim) / per_byte, row_bytes = a.dim / per_byte, box_bytes = row < 128 ? row : 128;
+    a.box = 0;
+    a.box_step = box_bytes;
+    if (row_bytes % 16 != 0 || a.num_pages == 0) return true;
+    a.box = 16;
+    while (a.page % a.box != 0) a.box /= 2;
+    if (a.box * box_bytes % 128 != 0) a.box = 0;                // (a box goes to a 128-byte boundary)
+    if (a.box == 0) return true;
+    const int64_t slots = static_cast<int64_t>(a.num_pages) * a.page;
+    return encode_codes(&maps[0], a.k_codes, slots, a.heads, row_bytes, a.box, box_bytes) && encode_codes(&maps[1], a.v_codes, slots, a.heads, row_bytes, a.box, box_bytes);
+}
+
 template <int FMT, int DP, int NR, int TT>
-cudaError_t launch(AttentionArgs a, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap (&maps)[2], const AttentionArgs& a, cudaStream_t st) {
     using S = Shared<FMT, DP, NR, TT>;
-    using L = Layout<FMT, DP, TT>;
     static PerDeviceOnce once;
     static int per_sm = 1;                          // (the same on every device that the library runs on)
     constexpr int bytes = S::BYTES;
@@ -645,17 +658,6 @@ cudaError_t launch(AttentionArgs a, cudaStream_t st) {
         return asked;
     });
     if (e != cudaSuccess) return e;
-    CUtensorMap maps[2] = {};
-    const int64_t row_bytes = a.dim / L::PER_BYTE;
-    if (row_bytes % 16 == 0 && a.num_pages > 0) {
-        // tokens that lie side by side in any page, from any token that a box starts at
-        a.box = 16;
-        while (a.page % a.box != 0) a.box /= 2;
-        a.box_step = L::BOX;
-        if (a.box * L::BOX % 128 != 0) a.box = 0;   // (a box goes to a 128-byte boundary)
-        for (int side = 0; side < 2 && a.box > 0; ++side)
-            if (!encode_codes(&maps[side], side == 0 ? a.k_codes : a.v_codes, static_cast<int64_t>(a.num_pages) * a.page, a.heads, row_bytes, a.box, L::BOX)) return cudaErrorInvalidValue;
-    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sm_count() * per_sm));
     cfg.blockDim = dim3(kThreads);
@@ -669,11 +671,11 @@ cudaError_t launch(AttentionArgs a, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], a);
 }
 template <int FMT>
-cudaError_t launch_for(const AttentionArgs& a, int64_t rows, cudaStream_t st) {
+cudaError_t launch_for(const CUtensorMap (&maps)[2], const AttentionArgs& a, int64_t rows, cudaStream_t st) {
     const int dp = padded(a.dim);
-    if (dp == 64) return rows <= 8 ? launch<FMT, 64, 1, 2>(a, st) : rows <= 16 ? launch<FMT, 64, 2, 2>(a, st) : launch<FMT, 64, 4, 2>(a, st);
-    if (dp == 128) return rows <= 8 ? launch<FMT, 128, 1, 2>(a, st) : rows <= 16 ? launch<FMT, 128, 2, 2>(a, st) : launch<FMT, 128, 4, 1>(a, st);
-    return rows <= 8 ? launch<FMT, 256, 1, 1>(a, st) : launch<FMT, 256, 2, 1>(a, st);
+    if (dp == 64) return rows <= 8 ? launch<FMT, 64, 1, 2>(maps, a, st) : rows <= 16 ? launch<FMT, 64, 2, 2>(maps, a, st) : launch<FMT, 64, 4, 2>(maps, a, st);
+    if (dp == 128) return rows <= 8 ? launch<FMT, 128, 1, 2>(maps, a, st) : rows <= 16 ? launch<FMT, 128, 2, 2>(maps, a, st) : launch<FMT, 128, 4, 1>(maps, a, st);
+    return rows <= 8 ? launch<FMT, 256, 1, 1>(maps, a, st) : launch<FMT, 256, 2, 1>(maps, a, st);
 }
 
 } // namespace
@@ -748,9 +750,11 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.zero_rest = zero_rest ? 1 : 0;
     const int64_t rows = (total_q * a.group + seqs - 1) / (seqs > 0 ? seqs : 1);       // of a sequence and head, on average
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = rows > kFewRows && many_rows_fits(a.dim) ? launch_many_rows(fmt, a, rows, st)
-                          : fmt == KV_CACHE_INT8                   ? launch_for<KV_CACHE_INT8>(a, rows, st)
-                                                                   : launch_for<KV_CACHE_MXFP4>(a, rows, st);
+    CUtensorMap maps[2] = {};
+    if (!encode_sides(maps, a, fmt)) return W8A8_ERR_CUDA;
+    const cudaError_t e = rows > kFewRows && many_rows_fits(a.dim) ? launch_many_rows(fmt, maps[0], maps[1], a, rows, st)
+                          : fmt == KV_CACHE_INT8                   ? launch_for<KV_CACHE_INT8>(maps, a, rows, st)
+                                                                   : launch_for<KV_CACHE_MXFP4>(maps, a, rows, st);
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }
 

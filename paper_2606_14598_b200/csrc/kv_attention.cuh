@@ -156,6 +156,8 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, uint32_t
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid) : "memory");
 }
+// one arrival on `bar` (not counted as pending by it) once the copies that this thread has asked for are there
+__device__ __forceinline__ void cp_async_mbar_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // a box of a head's codes (16-byte chunks swizzled), rows one token apart
@@ -201,15 +203,21 @@ struct Row {
     // r: row of the sequence's new tokens and the group's heads. o stands for o * 2^(m_o - m_l), 4-bit: / 2^12. The power
     // may be more than fp32 spans while the result is not: it is applied in two halves.
     template <int FMT>
+    __device__ __forceinline__ float2 scale() const {           // o times x, times y, times y is the result (l == 0: it is 0)
+        return make_float2(1.f / l, ex2(fminf(fmaxf(0.5f * (m_o - m_l - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f)));
+    }
+    __device__ __forceinline__ void write_lse(const AttentionArgs& a, const Sequence& s, int node, int h) const {
+        if (a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;
+    }
+    template <int FMT>
     __device__ __forceinline__ void finish(const AttentionArgs& a, const Sequence& s, int head, int r, int d) const {
         const int node = r / a.group, h = head * a.group + r - node * a.group;
         float v[4];
-        const float inv = 1.f / l;
-        const float by = ex2(fminf(fmaxf(0.5f * (m_o - m_l - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f));
+        const float2 by = scale<FMT>();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : o[i] * inv * by * by;
+        for (int i = 0; i < 4; ++i) v[i] = l == 0.f ? 0.f : o[i] * by.x * by.y * by.y;
         *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(s.begin + node) * a.o_st + h * a.o_sh + d) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-        if (d == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;
+        if (d == 0) write_lse(a, s, node, h);
     }
 };
 constexpr __host__ __device__ int part_floats(int rows, int dp) { return rows * (dp + 4); }
@@ -245,19 +253,35 @@ __device__ __forceinline__ void merge_parts(const AttentionArgs& a, const Sequen
         if (me == 0) *counter = 0;
         __threadfence();
         const int quads = a.dim / 4;
-        for (int e = me; e < rows * quads; e += THREADS) {
-            const int r = e / quads, d = (e - r * quads) * 4;
-            Row v;
-#pragma unroll 4
+        constexpr int AT_ONCE = ROWS >= 64 ? 4 : 1;             // (elements of a thread whose parts are on their way together)
+        for (int e0 = me; e0 < rows * quads; e0 += AT_ONCE * THREADS) {
+            Row v[AT_ONCE];
+#pragma unroll (4 / AT_ONCE)
             for (int x = first; x <= last; ++x) {
                 const float* from = a.parts + (2 * static_cast<int64_t>(x) + (x == first ? 1 : 0)) * PART;
-                const float4 its = __ldcg(reinterpret_cast<const float4*>(from + ROWS * DP + 4 * r));
-                v.add(__ldcg(reinterpret_cast<const float4*>(from + r * DP + d)), its.x, its.y, its.z);
+                float4 o[AT_ONCE], its[AT_ONCE];
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const int e = min(e0 + i * THREADS, rows * quads - 1), r = e / quads, d = (e - r * quads) * 4;
+                    its[i] = __ldcg(reinterpret_cast<const float4*>(from + ROWS * DP + 4 * r));
+                    o[i] = __ldcg(reinterpret_cast<const float4*>(from + r * DP + d));
+                }
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) v[i].add(o[i], its[i].x, its[i].y, its[i].z);
             }
-            v.finish<FMT>(a, s, head, row0 + r, d);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int e = e0 + i * THREADS, r = e / quads, d = (e - r * quads) * 4;
+                if (e < rows * quads) v[i].template finish<FMT>(a, s, head, row0 + r, d);
+            }
         }
     }
 }
+
+// ---- kv_attention_tc.cu : the attention for many rows of queries a head (the maps: codes of keys and of values in boxes of a.box tokens of a head)
+bool many_rows_fits(int dim);                                              // what the kernel can run
+size_t many_rows_part_bytes(int64_t most_rows, int64_t dim);               // scratch for the parts, for at most this many rows of a sequence and head
+cudaError_t launch_many_rows(int fmt, const CUtensorMap& k_map, const CUtensorMap& v_map, const AttentionArgs& a, int64_t rows, cudaStream_t st);
 
 } // namespace attention
 } // namespace w8a8

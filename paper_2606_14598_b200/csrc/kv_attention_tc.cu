@@ -1,8 +1,9 @@
 // Attention over the quantized cache for many rows of queries a head: trees of drafted tokens with grouped heads, chains, prompts.
 //
 // Both products run on the tensor memory's matrix unit, 128 rows of queries at a time: S = Q K^T with Q and K in shared memory, O += P V with P in
-// tensor memory, where it lies over the scores it came from. Eight warps turn the cache's codes into fp16 tiles of 128 tokens (keys: the codes, whose scale goes
-// to the scores; values: codes times scale, relative to the largest scale so far), a thread a row does the softmax, one warp issues the products.
+// tensor memory, where it lies over the scores it came from. One warp brings the cache's codes into shared memory, eight turn them into fp16 tiles of 128 tokens
+// (keys: the codes, whose scale goes to the scores; values: codes times scale, relative to the largest scale so far), a thread a row does the softmax, one warp issues
+// the products.
 //
 // Two softmax warpgroups, each with scores and an O of its own: of the same 128 rows and every other tile of tokens, or (PAIR) of 128 rows each and all
 // tiles, which then are converted once for 256 rows. What bounds it: the exponentials (128 x 128 a tile at 16 a cycle: 1024 cycles, the two products' time) and the
@@ -18,25 +19,37 @@ namespace {
 
 constexpr int kTok = 128;                       // tokens of a tile
 constexpr int kRows = 128;                      // rows of a product
-constexpr int kConvertWarp = 8, kMmaWarp = 16, kThreads = 32 * 17, kConverters = 256, kSoftmax = 256;
-constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 8 after it
+constexpr int kConvertWarp = 8, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 18, kConverters = 256, kSoftmax = 256;
+constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 9 after it
 constexpr int kSlots = 4;                       // tiles whose factors are kept
+constexpr int kRaw = 3;                         // tiles of codes on their way
 
 template <int FMT, int DP, bool PAIR>
 struct Plan {
     static constexpr int ROWS = PAIR ? 2 * kRows : kRows;
-    static constexpr int PER_BYTE = FMT == KV_CACHE_INT8 ? 1 : 2;
+    static constexpr int PER_BYTE = FMT == KV_CACHE_INT8 ? 1 : 2, ROW = DP / PER_BYTE;     // bytes of a head, padded
     static constexpr int TILE = kTok * DP * 2, PANEL = kTok * 128;             // an fp16 tile of tokens or queries: panels of 64 elements (128 bytes) a row
-    static constexpr int K = 0, V = K + 2 * TILE, Q = V + 2 * TILE, FACTORS = Q + (PAIR ? 2 : 1) * TILE;
+    // tiles of keys and values take turns in one ring: K0 V0 K1 V1 ...
+    static constexpr int RING = PAIR && DP == 128 ? 3 : 4;
+    static constexpr int Q = RING * TILE, RAW = Q + (PAIR ? 2 : 1) * TILE, MORE = RAW + kRaw * kTok * ROW;
+    // with the codes of keys come the scales of keys and values (4-bit: the two words that hold a head's bytes) and a byte a token: 0x80 where it
+    // may be seen, and (4-bit) where in the words its bytes begin
+    static constexpr int WORDS = FMT == KV_CACHE_INT8 ? 1 : 2, V_SCALES = kTok * 4 * WORDS, FLAGS = 2 * V_SCALES, MORE_BYTES = FLAGS + kTok;
+    static constexpr int FACTORS = MORE + kRaw * MORE_BYTES;
     static constexpr int NANS = FACTORS + kSlots * kTok * 4;                   // NaN blocks of a token's values, a byte each
-    static constexpr int SIGMA = NANS + kSlots * kTok, ANY_NAN = SIGMA + kSlots * 4, OF_WARP = ANY_NAN + kSlots * 4, STATE = OF_WARP + 2 * 8 * 4;
-    static constexpr int BARS = STATE + 2 * kRows * 16, BYTES = BARS + 16 * 8 + 16 + 1024;
+    static constexpr int SIGMA = NANS + kSlots * kTok, ANY_NAN = SIGMA + kSlots * 4, OF_WARP = ANY_NAN + kSlots * 4, ROW_FACTOR = OF_WARP + 2 * 8 * 4;
+    static constexpr int STATE = ROW_FACTOR + ROWS * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 24 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
-    static_assert(O + 2 * DP <= 512 && BYTES <= 227 * 1024, "");
-    // codes: a thread takes a chunk of 16 bytes of every PASS-th token
-    static constexpr int CHUNKS = DP / PER_BYTE / 16, PASS = kConverters / CHUNKS, EACH = kTok / PASS, CODES = 16 * PER_BYTE;
+    static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
+    // codes: a thread converts a chunk of 16 bytes of every PASS-th token
+    static constexpr int CHUNKS = ROW / 16, PASS = kConverters / CHUNKS, EACH = kTok / PASS, CODES = 16 * PER_BYTE;
+    // byte `off` of row r of a tile of codes, as boxes arrive: chunks of 16 bytes change places by the row
+    __device__ static __forceinline__ int raw_place(int r, int off) {
+        const int turn = ROW == 128 ? r & 7 : ROW == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+        return r * ROW + (off ^ (turn << 4));
+    }
 };
-enum Bar { K_FULL = 0, V_FULL = 2, K_EMPTY = 4, V_EMPTY = 6, S_FULL = 8, P_FULL = 10, O_DONE = 12, Q_FULL = 14, DRAINED = 15 };
+enum Bar { TILE_FULL = 0, TILE_EMPTY = 4, RAW_FULL = 8, RAW_EMPTY = 11, S_FULL = 14, P_FULL = 16, O_DONE = 18, Q_FULL = 20, DRAINED = 21 };
 
 // A CTA's segments, one after another: (sequence, head, rows) and a run of its tiles. Every role walks them by itself.
 template <int ROWS>
@@ -74,23 +87,6 @@ struct Segments {
 
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// 16 bytes of codes, `valid` of them there (a multiple of 4; the rest zeros), in loads that the head's alignment allows
-__device__ __forceinline__ uint4 load_codes(const uint8_t* p, int valid, int align) {
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (valid <= 0) return x;
-    if (align == 16) return __ldcg(reinterpret_cast<const uint4*>(p));
-    if (align == 8) {
-        const uint2 lo = __ldcg(reinterpret_cast<const uint2*>(p)), hi = valid > 8 ? __ldcg(reinterpret_cast<const uint2*>(p) + 1) : make_uint2(0, 0);
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
-    }
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
-    x.x = __ldcg(q);
-    if (valid > 4) x.y = __ldcg(q + 1);
-    if (valid > 8) x.z = __ldcg(q + 2);
-    if (valid > 12) x.w = __ldcg(q + 3);
-    return x;
-}
-
 // Elements first to first + 7 of row r of a tile: where their 16 bytes are
 __device__ __forceinline__ uint32_t place(int r, int first) { return (first >> 6) * (kTok * 128) + r * 128 + ((((first >> 3) & 7) ^ (r & 7)) << 4); }
 
@@ -110,8 +106,20 @@ __device__ __forceinline__ uint32_t sees32(const AttentionArgs& a, int64_t row_o
     return bits | static_cast<uint32_t>(x) << (from - j0);
 }
 
+// A position in a ring of N: which slot, and how often it came round
+template <int N>
+struct Turn {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == N) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
 template <int FMT, int DP, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const AttentionArgs a) {
     using L = Plan<FMT, DP, PAIR>;
     constexpr int ROWS = L::ROWS;
     extern __shared__ uint8_t raw_smem[];
@@ -124,11 +132,15 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
     auto bar = [&](int which, int i) { return bars + 8 * (which + i); };
     if (threadIdx.x == 0) {
         abort_flag = 0;
+        for (int i = 0; i < L::RING; ++i) {
+            mbar_init(bar(TILE_FULL, i), 8);
+            mbar_init(bar(TILE_EMPTY, i), 1);
+        }
+        for (int i = 0; i < kRaw; ++i) {
+            mbar_init(bar(RAW_FULL, i), 64);
+            mbar_init(bar(RAW_EMPTY, i), 8);
+        }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(K_FULL, i), 8);
-            mbar_init(bar(V_FULL, i), 8);
-            mbar_init(bar(K_EMPTY, i), 1);
-            mbar_init(bar(V_EMPTY, i), 1);
             mbar_init(bar(S_FULL, i), 1);
             mbar_init(bar(P_FULL, i), 4);
             mbar_init(bar(O_DONE, i), 1);
@@ -154,322 +166,416 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
     volatile int* const sigmas = reinterpret_cast<volatile int*>(smem + L::SIGMA);        // [slot]: values are relative to 2^this
     volatile int* const any_nan = reinterpret_cast<volatile int*>(smem + L::ANY_NAN);     // [slot]: whether values of the tile are NaN
     uint8_t* const nans = smem + L::NANS;
+    const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
     Segments<ROWS> seg(a, share);
 
     if (warp == kMmaWarp) {
         // ---- products. A job is a tile of tokens for one of the two softmax warpgroups: every other tile, or (PAIR) each tile for both.
-        uint32_t tile_base = 0, jobs_of[2] = {0, 0}, segments = 0;
+        uint32_t segments = 0, jobs_of[2] = {0, 0};
         constexpr uint32_t kQk = make_f16_idesc(kRows, kTok, false), kPv = make_f16_idesc(kRows, DP, true);
+        Turn<L::RING> k_turn, v_turn;                                            // tiles 2t and 2t + 1 of the ring
+        v_turn.next();
         while (seg.next()) {
             const int jobs = PAIR ? 2 * seg.tiles : seg.tiles;
             mbar_wait(bar(Q_FULL, 0), segments & 1, ctl, kWaitMany, kStatusTimeout);
             auto scores = [&](int n) {
-                const uint32_t t = tile_base + (PAIR ? n >> 1 : n), buf = t & 1, w = n & 1;
-                if (!PAIR || w == 0) mbar_wait(bar(K_FULL, buf), t >> 1 & 1, ctl, kWaitMany + 1, kStatusTimeout);
+                const uint32_t w = n & 1;
+                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, k_turn.slot), k_turn.phase, ctl, kWaitMany + 1, kStatusTimeout);
                 tc_fence_after();
                 if (lane == 0) {
-                    const uint32_t q = base + L::Q + (PAIR ? w * L::TILE : 0), k = base + L::K + buf * L::TILE;
+                    const uint32_t q = base + L::Q + (PAIR ? w * L::TILE : 0), k = base + k_turn.slot * L::TILE;
 #pragma unroll
                     for (int i = 0; i < DP / 16; ++i) {
                         const uint32_t off = (i / 4) * L::PANEL + (i % 4) * 32;
                         mma_f16_ss(tmem + w * kTok, make_kmajor_sw128_desc(q + off), make_kmajor_sw128_desc(k + off), kQk, i > 0);
                     }
                     tc_commit(bar(S_FULL, w));
-                    if (!PAIR || w == 1) tc_commit(bar(K_EMPTY, buf));
+                    if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, k_turn.slot));
                 }
                 __syncwarp();
+                if (!PAIR || w == 1) {
+                    k_turn.next();
+                    k_turn.next();
+                }
             };
             for (int n = 0; n < min(2, jobs); ++n) scores(n);
             for (int n = 0; n < jobs; ++n) {
-                const uint32_t t = tile_base + (PAIR ? n >> 1 : n), buf = t & 1, w = n & 1;
-                if (!PAIR || w == 0) mbar_wait(bar(V_FULL, buf), t >> 1 & 1, ctl, kWaitMany + 2, kStatusTimeout);
+                const uint32_t w = n & 1;
+                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, v_turn.slot), v_turn.phase, ctl, kWaitMany + 2, kStatusTimeout);
                 mbar_wait(bar(P_FULL, w), jobs_of[w] & 1, ctl, kWaitMany + 3, kStatusTimeout);
                 ++jobs_of[w];
                 tc_fence_after();
                 if (lane == 0) {
-                    const uint32_t v = base + L::V + buf * L::TILE;
-                    const bool first = n < 2;
+                    const uint32_t v = base + v_turn.slot * L::TILE;
 #pragma unroll
                     for (int i = 0; i < kTok / 16; ++i)
-                        mma_f16_ts(tmem + L::O + w * DP, tmem + w * kTok + 8 * i, make_mnmajor_sw128_desc(v + i * 16 * 128, L::PANEL), kPv, !first || i > 0);
+                        mma_f16_ts(tmem + L::O + w * DP, tmem + w * kTok + 8 * i, make_mnmajor_sw128_desc(v + i * 16 * 128, L::PANEL), kPv, n >= 2 || i > 0);
                     tc_commit(bar(O_DONE, w));
-                    if (!PAIR || w == 1) tc_commit(bar(V_EMPTY, buf));
+                    if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, v_turn.slot));
                 }
                 __syncwarp();
+                if (!PAIR || w == 1) {
+                    v_turn.next();
+                    v_turn.next();
+                }
                 if (n + 2 < jobs) scores(n + 2);
             }
-            tile_base += seg.tiles;
             ++segments;
         }
         if (lane == 0) tc_commit(bar(DRAINED, 0));                               // (whatever became of the waits, no product is left when the CTA goes)
         mbar_drain(bar(DRAINED, 0), 0, a.limit_ns);
-    } else if (warp >= kConvertWarp) {
-        // ---- codes to fp16 tiles. The codes of the next tile are on their way while this one is converted.
-        constexpr int EACH = L::EACH;
-        const int me = threadIdx.x - 32 * kConvertWarp, chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
-        const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock, off = chunk * 16;
-        const int align = row_bytes % 16 == 0 ? 16 : row_bytes % 8 == 0 ? 8 : 4;
+    } else if (warp == kLoadWarp) {
+        // ---- codes and scales into shared memory. A lane has four tokens of a tile; codes come as boxes of tokens that lie side by side in any page, or
+        // (heads that are not whole 16-byte pieces) piece by piece.
+        Turn<kRaw> turn;
         const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
-        int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
-        bool more = seg.next();
-        int tile = 0;                           // of the segment: the next to look up
-        int slots[EACH];
-        bool seen[EACH];
-        int head = 0;
-        auto look_up = [&] {                    // where the tokens of that tile are; then on to the next one
-            const int t0 = seg.token(tile) + tok;
-            head = seg.head;
+        int next[4], next_head = 0;
+        bool next_in[4], more = seg.next();
+        int tile = 0;
+        auto look_up = [&] {                                                     // where the tokens of the tile are; then on to the one after it
+            const int t0 = more ? seg.token(tile) + 4 * lane : 0;
+            next_head = seg.head;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int t = t0 + i * L::PASS;
-                slots[i] = -1;
-                seen[i] = false;
-                if (more && t >= seg.s.start && t < seg.s.stop) {
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + i;
+                next[i] = -1;
+                next_in[i] = false;
+                if (more && t < seg.s.stop) {
                     const int p = a.page_shift >= 0 ? t >> a.page_shift : t / a.page, id = a.table[seg.b * a.table_stride + p];
-                    if (id >= 0 && id < a.num_pages) slots[i] = id * a.page + (t - p * a.page);
+                    if (id >= 0 && id < a.num_pages) next[i] = id * a.page + (t - p * a.page);
+                    next_in[i] = next[i] >= 0 && t >= seg.s.start;
                 }
-                seen[i] = slots[i] >= 0;
             }
             if (more && ++tile == seg.tiles) {
                 more = seg.next();
                 tile = 0;
             }
         };
-        uint4 kx[EACH], vx[EACH];               // codes
-        uint32_t ksc[EACH], vsc[EACH], next_vsc[EACH];     // int8: the scale; 4-bit: the byte of this chunk's block
-        int now[EACH], now_head = 0, sigma = -126;
-        bool now_seen[EACH];
-        auto fetch_codes = [&](const uint8_t* codes, uint4 (&x)[EACH], const int (&where)[EACH], int h) {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                x[i] = where[i] >= 0 ? load_codes(codes + where[i] * token_bytes + h * row_bytes + off, row_bytes - off, align) : make_uint4(0, 0, 0, 0);
-        };
-        auto fetch_scales = [&](const void* scales, uint32_t (&sc)[EACH]) {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int64_t entry = static_cast<int64_t>(max(slots[i], 0)) * a.heads + head;
-                sc[i] = 0;
-                if (slots[i] >= 0) {
-                    if (FMT == KV_CACHE_INT8) sc[i] = __ldcg(static_cast<const uint32_t*>(scales) + entry);
-                    else if (chunk < blocks) sc[i] = __ldcg(static_cast<const uint8_t*>(scales) + entry * blocks + chunk);
-                }
-            }
-        };
-        auto take_over = [&] {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                now[i] = slots[i];
-                now_seen[i] = seen[i];
-                vsc[i] = next_vsc[i];
-            }
-            now_head = head;
-            fetch_codes(a.v_codes, vx, now, now_head);
-        };
-        static_assert(FMT == KV_CACHE_INT8 || L::CODES == kMxBlock, "a chunk is a block");
         look_up();
-        fetch_codes(a.k_codes, kx, slots, head);
-        fetch_scales(a.k_scales, ksc);
-        fetch_scales(a.v_scales, next_vsc);
-        take_over();
-        const int64_t tiles_in_all = share.end - share.begin;
-        int64_t left_of_item = 0;               // tiles of the current segment still to come: the values' reference starts anew with each
-        Segments<ROWS> at(a, share);
-        for (int64_t t = 0; t < tiles_in_all; ++t) {
-            if (left_of_item == 0) {
-                at.next();
-                left_of_item = at.tiles;
-                sigma = -126;
+        for (int64_t left = share.end - share.begin; left > 0; --left) {
+            int slots[4];
+            uint32_t flags = 0;
+            const int head = next_head;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                slots[i] = next[i];
+                const uint32_t shift = FMT == KV_CACHE_INT8 ? 0u : static_cast<uint32_t>((static_cast<int64_t>(max(slots[i], 0)) * a.heads + head) * blocks & 3);
+                flags |= (next_in[i] ? 0x80u | shift : 0u) << (8 * i);
             }
-            --left_of_item;
-            const uint32_t buf = t & 1, slot = t & (kSlots - 1), phase = (static_cast<uint32_t>(t) >> 1 & 1) ^ 1;
-            look_up();                          // of the tile after this one
-            // keys
-            mbar_wait(bar(K_EMPTY, buf), phase, ctl, kWaitMany + 4, kStatusTimeout);
-            const uint32_t k_tile = base + L::K + buf * L::TILE, v_tile = base + L::V + buf * L::TILE;
-            int top_sigma = -126, nan_any = 0;
+            look_up();                                                           // (of the tile after this one: on its way meanwhile)
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int r = tok + i * L::PASS;
-                const uint32_t w[4] = {kx[i].x, kx[i].y, kx[i].z, kx[i].w};
-                if (FMT == KV_CACHE_INT8) {
-                    uint32_t f[8];
+            for (int side = 0; side < 2; ++side) {
+                mbar_wait(bar(RAW_EMPTY, turn.slot), turn.phase ^ 1, ctl, kWaitMany + 4, kStatusTimeout);
+                const uint32_t full = bar(RAW_FULL, turn.slot), to = base + L::RAW + turn.slot * kTok * L::ROW, rest = base + L::MORE + turn.slot * L::MORE_BYTES;
+                if (side == 0) {
+                    *reinterpret_cast<uint32_t*>(smem + L::MORE + turn.slot * L::MORE_BYTES + L::FLAGS + 4 * lane) = flags;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
-                    if (!now_seen[i])
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t entry = static_cast<int64_t>(max(slots[i], 0)) * a.heads + head;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[j] = 0;
-                    store_16(k_tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
-                    store_16(k_tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
-                    if (chunk == 0) {
-                        factors[slot * kTok + r] = now_seen[i] ? __uint_as_float(ksc[i]) : -1.f;
-                        nans[slot * kTok + r] = 0;
-                    }
-                    const uint32_t bits = vsc[i];
-                    if (now_seen[i] && (bits & 0x7f800000u) == 0x7f800000u) {
-                        nan_any = 1;
-                        if (chunk == 0) nans[slot * kTok + r] = 0xff;
-                    } else if (now_seen[i]) {
-                        top_sigma = max(top_sigma, static_cast<int>(bits >> 23) - 126);         // s < 2^this
-                    }
-                } else {
-                    // the token's largest byte: of the lanes that hold its chunks
-                    const bool nan = chunk < blocks && ksc[i] == 255u;
-                    uint32_t top = nan ? 0u : ksc[i], bad = nan ? 1u : 0u, vbad = chunk < blocks && vsc[i] == 255u && now_seen[i] ? 1u << chunk : 0u;
-#pragma unroll
-                    for (int o = 1; o < L::CHUNKS; o <<= 1) {
-                        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-                        vbad |= __shfl_xor_sync(0xffffffffu, vbad, o);
-                    }
-                    const int e = 27 + static_cast<int>(ksc[i]) - static_cast<int>(top);
-                    const uint32_t mul = nan || e <= 0 ? 0u : static_cast<uint32_t>(e) * 0x04000400u;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t f[4];
-                        e2m1_to_f16(w[j], f);
-                        store_16(k_tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
-                    }
-                    if (chunk == 0) {
-                        factors[slot * kTok + r] = !now_seen[i] ? -1.f : bad != 0 ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
-                        nans[slot * kTok + r] = static_cast<uint8_t>(vbad);
-                    }
-                    nan_any |= vbad != 0;
-                    if (now_seen[i] && chunk < blocks && vsc[i] != 255u) top_sigma = max(top_sigma, static_cast<int>(vsc[i]) - 127);
-                }
-            }
-            // the largest scale of values so far (fp32 exponents: all of them fit a byte)
-            const int warp_top = __reduce_max_sync(0xffffffffu, top_sigma), warp_nan = __any_sync(0xffffffffu, nan_any);
-            if (lane == 0) of_warp[buf * 8 + warp - kConvertWarp] = warp_top * 2 + (warp_nan ? 1 : 0);
-            named_sync(1, kConverters);
-            int nan_of_all = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int its = of_warp[buf * 8 + i];
-                sigma = max(sigma, its >> 1);
-                nan_of_all |= its & 1;
-            }
-            if (me == 0) {
-                sigmas[slot] = sigma;
-                any_nan[slot] = nan_of_all;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(K_FULL, buf));
-            const bool another = t + 1 < tiles_in_all;
-            if (another) {
-                fetch_codes(a.k_codes, kx, slots, head);
-                fetch_scales(a.k_scales, ksc);
-                fetch_scales(a.v_scales, next_vsc);
-            }
-            // values: times their scale over 2^sigma, brought to 2^15 at most
-            mbar_wait(bar(V_EMPTY, buf), phase, ctl, kWaitMany + 5, kStatusTimeout);
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int r = tok + i * L::PASS;
-                const uint32_t w[4] = {vx[i].x, vx[i].y, vx[i].z, vx[i].w};
-                if (FMT == KV_CACHE_INT8) {
-                    const float s = __uint_as_float(vsc[i]);
-                    const bool fine = now_seen[i] && (vsc[i] & 0x7f800000u) != 0x7f800000u;
-                    // (two factors: 2^(8 - sigma) alone may be more than fp32 holds)
-                    const float by = fine ? s * __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23) * __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23) : 0.f;
-                    const uint32_t mul = pack_f16(by, by);
-                    uint32_t f[8];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = fine ? mul_f16x2(f[j], mul) : 0u;
-                    store_16(v_tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
-                    store_16(v_tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
-                } else {
-                    const int e = 27 + static_cast<int>(vsc[i]) - 127 - sigma;       // (2^12 * 2^(byte - 127 - sigma), subnormal from 0 down)
-                    const uint32_t bits = e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31), mul = !now_seen[i] || vsc[i] == 255u ? 0u : bits * 0x00010001u;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t f[4];
-                        e2m1_to_f16(w[j], f);
-                        store_16(v_tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
+                        for (int kv = 0; kv < 2; ++kv) {
+                            const void* scales = kv == 0 ? a.k_scales : a.v_scales;
+                            const uint32_t at = rest + kv * L::V_SCALES + (4 * lane + i) * 4 * L::WORDS;
+                            if (FMT == KV_CACHE_INT8) {
+                                cp_async<4>(at, static_cast<const float*>(scales) + entry, slots[i] >= 0 ? 4 : 0);
+                            } else {
+                                const int64_t first = entry * blocks;
+                                const int shift = static_cast<int>(first & 3);
+                                const uint8_t* p = static_cast<const uint8_t*>(scales) + first - shift;
+                                const bool two = slots[i] >= 0 && shift + blocks > 4;
+                                cp_async<4>(at, p, slots[i] >= 0 ? 4 : 0);
+                                cp_async<4>(at + 4, p + (two ? 4 : 0), two ? 4 : 0);
+                            }
+                        }
                     }
                 }
+                if (a.box > 0) {
+                    // boxes that begin with this lane's tokens: one of 4 or more tokens, or several smaller ones
+                    uint32_t mine = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mine |= static_cast<uint32_t>(slots[i] >= 0 && (4 * lane + i) % a.box == 0) << i;
+                    const uint32_t boxes = __reduce_add_sync(0xffffffffu, __popc(mine));
+                    if (lane == 0) mbar_arrive_expect_tx(full, boxes * a.box * L::ROW);
+                    else mbar_arrive(full);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (mine >> i & 1u) tma_load_3d(to + (4 * lane + i) * L::ROW, side == 0 ? &k_map : &v_map, full, 0, head, slots[i]);
+                } else {
+                    const uint8_t* codes = side == 0 ? a.k_codes : a.v_codes;
+                    constexpr int kPieces = L::ROW / 8;
+                    for (int e = lane; e < kTok * kPieces; e += 32) {
+                        const int r = e / kPieces, off = (e - r * kPieces) * 8;
+                        int from = -1;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int its = __shfl_sync(0xffffffffu, slots[i], r >> 2);
+                            if ((r & 3) == i) from = its;
+                        }
+                        const int64_t where = max(from, 0) * token_bytes + head * row_bytes + off;
+                        const int valid = from >= 0 ? row_bytes - off : 0;
+                        if (row_bytes % 8 == 0) {
+                            cp_async<8>(to + L::raw_place(r, off), codes + (valid > 0 ? where : 0), valid > 0 ? 8 : 0);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; i += 4) cp_async<4>(to + L::raw_place(r, off) + i, codes + (valid > i ? where + i : 0), valid > i ? 4 : 0);
+                        }
+                    }
+                    mbar_arrive(full);
+                }
+                cp_async_mbar_arrive(full);                                      // once this lane's own copies are there
+                turn.next();
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(V_FULL, buf));
-            if (another) take_over();
+        }
+        // nothing is on its way when the CTA goes: what was asked for has been waited for by those who convert it, unless a wait gave up
+        if (abort_flag != 0) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            for (int i = 0; i < kRaw; ++i) {
+                turn.slot = turn.slot == 0 ? kRaw - 1 : turn.slot - 1;
+                if (turn.slot == kRaw - 1) turn.phase ^= 1;
+                if (2 * (share.end - share.begin) > i) mbar_drain(bar(RAW_FULL, turn.slot), turn.phase, a.limit_ns);
+            }
+        }
+    } else if (warp >= kConvertWarp) {
+        // ---- codes to fp16 tiles
+        constexpr int EACH = L::EACH;
+        const int me = threadIdx.x - 32 * kConvertWarp, chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
+        static_assert(FMT == KV_CACHE_INT8 || L::CODES == kMxBlock, "a chunk is a block");
+        int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
+        Turn<kRaw> raw;
+        Turn<L::RING> ring;
+        uint32_t t = 0;                                                          // tiles so far
+        while (seg.next()) {
+            int sigma = -126;                                                    // the values' reference starts anew with each segment
+            for (int left = seg.tiles; left > 0; --left, ++t) {
+                const uint32_t slot = t & (kSlots - 1);
+                uint32_t vsc[EACH], seen = 0;                                    // int8: the scale; 4-bit: the byte of this chunk's block
+                // keys
+                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                int top_sigma = -126, nan_any = 0;
+                {
+                    const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
+                    const uint8_t* const rest = smem + L::MORE + raw.slot * L::MORE_BYTES;
+                    const uint32_t tile = base + ring.slot * L::TILE;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) {
+                        const int r = tok + i * L::PASS;
+                        const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w}, flag = rest[L::FLAGS + r];
+                        const bool in = flag != 0;
+                        seen |= static_cast<uint32_t>(in) << i;
+                        if (FMT == KV_CACHE_INT8) {
+                            uint32_t f[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+                            store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
+                            store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
+                            vsc[i] = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[r];
+                            const bool nan = (vsc[i] & 0x7f800000u) == 0x7f800000u && in;
+                            if (chunk == 0) {
+                                factors[slot * kTok + r] = in ? reinterpret_cast<const float*>(rest)[r] : -1.f;
+                                nans[slot * kTok + r] = nan ? 0xff : 0;
+                            }
+                            nan_any |= nan;
+                            if (in && !nan) top_sigma = max(top_sigma, static_cast<int>(vsc[i] >> 23) - 126);     // s < 2^this
+                        } else {
+                            const uint8_t* const its = rest + r * 8 + (flag & 3) + chunk;
+                            const uint32_t ksc = in && chunk < blocks ? its[0] : 0u;
+                            vsc[i] = in && chunk < blocks ? its[L::V_SCALES] : 0u;
+                            // the token's largest byte: of the lanes that hold its chunks
+                            const bool nan = ksc == 255u;
+                            uint32_t top = nan ? 0u : ksc, bad = (nan ? 256u : 0u) | (vsc[i] == 255u ? 1u << chunk : 0u);
+#pragma unroll
+                            for (int o = 1; o < L::CHUNKS; o <<= 1) {
+                                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                                bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+                            }
+                            const int e = 27 + static_cast<int>(ksc) - static_cast<int>(top);
+                            const uint32_t mul = nan || e <= 0 ? 0u : static_cast<uint32_t>(e) * 0x04000400u;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t f[4];
+                                e2m1_to_f16(w[j], f);
+                                store_16(tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
+                            }
+                            if (chunk == 0) {
+                                factors[slot * kTok + r] = !in ? -1.f : bad >= 256u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
+                                nans[slot * kTok + r] = static_cast<uint8_t>(bad);
+                            }
+                            nan_any |= (bad & 255u) != 0;
+                            if (in && chunk < blocks && vsc[i] != 255u) top_sigma = max(top_sigma, static_cast<int>(vsc[i]) - 127);
+                        }
+                    }
+                }
+                // the largest scale of values so far (an exponent of fp32)
+                const int warp_top = __reduce_max_sync(0xffffffffu, top_sigma), warp_nan = __any_sync(0xffffffffu, nan_any);
+                if (lane == 0) of_warp[(t & 1) * 8 + warp - kConvertWarp] = warp_top * 2 + (warp_nan ? 1 : 0);
+                named_sync(1, kConverters);
+                int nan_of_all = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int its = of_warp[(t & 1) * 8 + i];
+                    sigma = max(sigma, its >> 1);
+                    nan_of_all |= its & 1;
+                }
+                if (me == 0) {
+                    sigmas[slot] = sigma;
+                    any_nan[slot] = nan_of_all;
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(TILE_FULL, ring.slot));
+                    mbar_arrive(bar(RAW_EMPTY, raw.slot));
+                }
+                raw.next();
+                ring.next();
+                // values: times their scale over 2^sigma, brought to 2^15 at most
+                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                {
+                    const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
+                    const uint32_t tile = base + ring.slot * L::TILE;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) {
+                        const int r = tok + i * L::PASS;
+                        const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        const bool in = (seen >> i & 1u) != 0;
+                        if (FMT == KV_CACHE_INT8) {
+                            const bool fine = in && (vsc[i] & 0x7f800000u) != 0x7f800000u;
+                            // (two factors: 2^(8 - sigma) alone may be more than fp32 holds)
+                            const float by = fine ? __uint_as_float(vsc[i]) * __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23) *
+                                                        __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23)
+                                                  : 0.f;
+                            const uint32_t mul = pack_f16(by, by);
+                            uint32_t f[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
+                            store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
+                            store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
+                        } else {
+                            const int e = 27 + static_cast<int>(vsc[i]) - 127 - sigma;       // (2^12 * 2^(byte - 127 - sigma), subnormal from 0 down)
+                            const uint32_t bits = e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31), mul = !in || vsc[i] == 255u ? 0u : bits * 0x00010001u;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t f[4];
+                                e2m1_to_f16(w[j], f);
+                                store_16(tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
+                            }
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(TILE_FULL, ring.slot));
+                    mbar_arrive(bar(RAW_EMPTY, raw.slot));
+                }
+                raw.next();
+                ring.next();
+            }
         }
     } else {
         // ---- softmax: a thread a row
         const int w = warp >> 2, row = threadIdx.x & (kRows - 1);
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16, s_tmem = tmem + lanes + w * kTok, o_tmem = tmem + lanes + L::O + w * DP;
         float* const state = reinterpret_cast<float*>(smem + L::STATE);          // [warpgroup][row]: references of o and of the sum, the sum, NaN blocks
+        float* const row_factor = reinterpret_cast<float*>(smem + L::ROW_FACTOR);
         uint32_t tile_base = 0, jobs = 0;                                        // jobs of this warpgroup so far
         while (seg.next()) {
             const int r = (PAIR ? w * kRows : 0) + row;                          // of the item's rows
             const bool live = r < seg.rows, warp_live = (PAIR ? w * kRows : 0) + 32 * (warp & 3) < seg.rows;
-            const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group, h = seg.head * a.group + (seg.row0 + min(r, seg.rows - 1)) - node * a.group;
-            // queries: a power of two brings the row's largest magnitude to [2^14, 2^15)
-            float factor;
+            const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group;
+            // queries: a power of two brings a row's largest magnitude to [2^14, 2^15). DP / 8 lanes a row, several rows on their way at once.
             {
-                const __nv_bfloat16* from = a.q + static_cast<int64_t>(seg.s.begin + node) * a.q_st + h * a.q_sh;
-                uint32_t top = 0;
-                for (int d = 0; d < a.dim; d += 8) top = max(top, absmax_bits8(*reinterpret_cast<const uint4*>(from + d)));
-                const int field = static_cast<int>(top >> 23), up = field == 255 ? 0 : min(126, max(-126, 141 - max(field, 1)));
-                const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
-                factor = fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f);
-                const uint32_t to = base + L::Q + (PAIR ? w * L::TILE : 0);
-                // (one tile of queries: each warpgroup writes every other eight elements)
-                for (int d = PAIR ? 0 : 8 * w; d < DP; d += PAIR ? 8 : 16) {
-                    float f[8];
-                    unpack_bf16x8(live && d < a.dim ? *reinterpret_cast<const uint4*>(from + d) : make_uint4(0, 0, 0, 0), f);
-                    store_16(to + place(row, d), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul), pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
+                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8, BATCH = 4;
+                const int d = lane % LANES * 8;
+#pragma unroll 1
+                for (int first = 0; first < PER_WARP; first += BATCH * AT_ONCE) {
+                    uint4 x[BATCH];
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int q_row = warp * PER_WARP + first + i * AT_ONCE + lane / LANES;
+                        x[i] = make_uint4(0, 0, 0, 0);
+                        if (q_row < seg.rows && d < a.dim) {
+                            const int its = (seg.row0 + q_row) / a.group, its_head = seg.head * a.group + (seg.row0 + q_row) - its * a.group;
+                            x[i] = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int q_row = warp * PER_WARP + first + i * AT_ONCE + lane / LANES;
+                        uint32_t top = absmax_bits8(x[i]);
+#pragma unroll
+                        for (int o = 1; o < LANES; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int field = static_cast<int>(top >> 23), up = field == 255 ? 0 : min(126, max(-126, 141 - max(field, 1)));
+                        const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
+                        float f[8];
+                        unpack_bf16x8(x[i], f);
+                        store_16(base + L::Q + (q_row / kRows) * L::TILE + place(q_row % kRows, d), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul),
+                                 pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
+                        if (d == 0) row_factor[q_row] = fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f);
+                    }
                 }
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(Q_FULL, 0));
+            named_sync(2, kSoftmax);
+            const float factor = row_factor[r];
             float m = kNone;
             uint64_t l2 = 0;
             int sigma = -126;
             uint32_t poison = 0;                                                 // blocks of this row's output that are NaN
             const uint64_t f2 = pack2(factor, factor);
             bool first = true;
+#pragma unroll 1
             for (int t = PAIR ? 0 : w; t < seg.tiles; t += PAIR ? 1 : 2, ++jobs) {
                 const uint32_t slot = (tile_base + t) & (kSlots - 1);
-                mbar_wait(bar(S_FULL, w), jobs & 1, ctl, kWaitMany + 6, kStatusTimeout);
+                mbar_wait(bar(S_FULL, w), jobs & 1, ctl, kWaitMany + 7, kStatusTimeout);
                 tc_fence_after();
                 if (warp_live) {
                     const float* const kf = factors + slot * kTok;
                     const int j0 = seg.token(t) - seg.s.before;
-                    uint32_t sees[4];
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        sees[ch] = __ballot_sync(0xffffffffu, kf[32 * ch + lane] != -1.f);
-                        if (j0 + 32 * ch + 31 >= 0) sees[ch] &= sees32(a, seg.s.begin + node, node, j0 + 32 * ch);
-                    }
+                    // which of 32 tokens this row sees: those that anybody does, and of the new ones its own
+                    auto sees32_of = [&](int ch) {
+                        uint32_t sees = __ballot_sync(0xffffffffu, kf[32 * ch + lane] != -1.f);
+                        if (j0 + 32 * ch + 31 >= 0) sees &= sees32(a, seg.s.begin + node, node, j0 + 32 * ch);
+                        return sees;
+                    };
                     if (any_nan[slot] != 0) {
-                        for (int x = 0; x < kTok; ++x)
-                            if (sees[x >> 5] >> (x & 31) & 1u) poison |= nans[slot * kTok + x];
+#pragma unroll 1
+                        for (int ch = 0; ch < 4; ++ch) {
+                            const uint32_t sees = sees32_of(ch);
+                            for (int x = 0; x < 32; ++x)
+                                if (sees >> x & 1u) poison |= nans[slot * kTok + 32 * ch + x];
+                        }
                     }
                     // the row's largest score
                     float top = -INFINITY;
-#pragma unroll
+#pragma unroll 1
                     for (int ch = 0; ch < 4; ++ch) {
                         uint32_t v[32];
                         tmem_ld_32x32b_x32(s_tmem + 32 * ch, v);
+                        const uint32_t sees = sees32_of(ch);
                         tmem_wait_ld();
-                        const bool all = sees[ch] == ~0u;
+                        if (__all_sync(0xffffffffu, sees == ~0u)) {
 #pragma unroll
-                        for (int x = 0; x < 32; x += 4) {
-                            const float4 k = *reinterpret_cast<const float4*>(kf + 32 * ch + x);
-                            float p, q, y, z;
-                            unpack2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), pack2(k.x, k.y)), p, q);
-                            unpack2(mul2(pack2(__uint_as_float(v[x + 2]), __uint_as_float(v[x + 3])), pack2(k.z, k.w)), y, z);
-                            if (!all) {
-                                if (!(sees[ch] >> x & 1u)) p = -INFINITY;
-                                if (!(sees[ch] >> x & 2u)) q = -INFINITY;
-                                if (!(sees[ch] >> x & 4u)) y = -INFINITY;
-                                if (!(sees[ch] >> x & 8u)) z = -INFINITY;
+                            for (int x = 0; x < 32; x += 4) {
+                                const float4 k = *reinterpret_cast<const float4*>(kf + 32 * ch + x);
+                                float p, q, y, z;
+                                unpack2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), pack2(k.x, k.y)), p, q);
+                                unpack2(mul2(pack2(__uint_as_float(v[x + 2]), __uint_as_float(v[x + 3])), pack2(k.z, k.w)), y, z);
+                                top = fmaxf(top, fmaxf(fmaxf(p, q), fmaxf(y, z)));
                             }
-                            top = fmaxf(top, fmaxf(fmaxf(p, q), fmaxf(y, z)));
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (sees >> x & 1u) top = fmaxf(top, __uint_as_float(v[x]) * kf[32 * ch + x]);
                         }
                     }
                     top = top == -INFINITY ? kNone : top * factor;
@@ -479,10 +585,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
                         const float now = top > m + 15.f ? top - 7.f : m, by_l = ex2(m - now);
                         l2 = mul2(l2, pack2(by_l, by_l));
                         if (!first) {
-                            const float by = by_l * ex2(static_cast<float>(max(sigma - its_sigma, -252)) * 0.5f) * ex2(static_cast<float>(max(sigma - its_sigma, -252)) * 0.5f);
-                            mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 7, kStatusTimeout);
+                            const float half = ex2(static_cast<float>(max(sigma - its_sigma, -252)) * 0.5f), by = by_l * half * half;
+                            mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 8, kStatusTimeout);
                             tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                             for (int ch = 0; ch < DP / 16; ++ch) {
                                 uint32_t v[16];
                                 tmem_ld_32x32b_x16(o_tmem + 16 * ch, v);
@@ -498,23 +604,29 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
                     first = false;
                     // weights, over the scores that they came from
                     const uint64_t m2 = pack2(-m, -m);
-#pragma unroll
+#pragma unroll 1
                     for (int ch = 0; ch < 4; ++ch) {
                         uint32_t v[32], p[16];
                         tmem_ld_32x32b_x32(s_tmem + 32 * ch, v);
+                        const uint32_t sees = sees32_of(ch);
                         tmem_wait_ld();
-                        const bool all = sees[ch] == ~0u;
 #pragma unroll
                         for (int x = 0; x < 32; x += 2) {
                             const uint64_t k = *reinterpret_cast<const uint64_t*>(kf + 32 * ch + x);
+                            const uint64_t arg = fma2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), k), f2, m2);
                             float y, z;
-                            unpack2(fma2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), k), f2, m2), y, z);
-                            if (!all) {
-                                if (!(sees[ch] >> x & 1u)) y = -INFINITY;
-                                if (!(sees[ch] >> x & 2u)) z = -INFINITY;
-                            }
-                            y = ex2(y);
-                            z = ex2(z);
+                            unpack2(arg, y, z);
+                            v[x] = __float_as_uint(y);
+                            v[x + 1] = __float_as_uint(z);
+                        }
+                        if (!__all_sync(0xffffffffu, sees == ~0u)) {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (!(sees >> x & 1u)) v[x] = 0xff800000u;
+                        }
+#pragma unroll
+                        for (int x = 0; x < 32; x += 2) {
+                            const float y = ex2(__uint_as_float(v[x])), z = ex2(__uint_as_float(v[x + 1]));
                             l2 = add2(l2, pack2(y, z));
                             p[x / 2] = pack_f16(y, z);
                         }
@@ -531,20 +643,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
             unpack2(l2, l, other);
             l += other;
             // (reference of o with the values' in it: int8 tiles are 2^8 too large, 4-bit ones 2^12, which the results take account of)
-            float m_o = m + static_cast<float>(sigma - (FMT == KV_CACHE_INT8 ? 8 : 0));
-            const bool had = PAIR || w < seg.tiles;
-            if (had) mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 8, kStatusTimeout);
-            if (!PAIR) {
-                *reinterpret_cast<float4*>(state + (w * kRows + row) * 4) = make_float4(m_o, m, l, __uint_as_float(poison));
-            }
+            float m_o = m + static_cast<float>(sigma - (FMT == KV_CACHE_INT8 ? 8 : 0)), m_l = m;
+            if (PAIR || w < seg.tiles) mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 9, kStatusTimeout);
+            if (!PAIR) *reinterpret_cast<float4*>(state + (w * kRows + row) * 4) = make_float4(m_o, m, l, __uint_as_float(poison));
             named_sync(2, kSoftmax);
             tc_fence_after();
             const bool whole = seg.whole();
             constexpr int PART = part_floats(ROWS, DP);
             float* const part = a.parts + (2 * static_cast<int64_t>(blockIdx.x) + (share.begin > seg.item_begin ? 0 : 1)) * PART;
             if (warp_live) {
-                const float nan = __uint_as_float(0x7fc00000u);
-                float by[2] = {1.f, 0.f}, m_l = m;
+                float by[2] = {1.f, 0.f};
                 const bool two = !PAIR && seg.tiles > 1;
                 if (!PAIR) {
                     const float4 s0 = *reinterpret_cast<const float4*>(state + row * 4), s1 = *reinterpret_cast<const float4*>(state + (kRows + row) * 4);
@@ -562,37 +670,44 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
                 // (one item's rows: each warpgroup takes half of the elements)
                 constexpr int WIDTH = PAIR ? DP : DP / 2;
                 const int d0 = PAIR ? 0 : w * WIDTH;
-#pragma unroll
-                for (int ch = 0; ch < WIDTH / 16; ++ch) {
-                    uint32_t v[16];
-                    float o[16];
-                    tmem_ld_32x32b_x16(tmem + lanes + L::O + (PAIR ? w * DP : 0) + d0 + 16 * ch, v);
+                Row out;
+                out.m_o = m_o;
+                out.m_l = m_l;
+                out.l = l;
+                const int h = seg.head * a.group + seg.row0 + r - node * a.group;
+                __nv_bfloat16* const to = a.out + static_cast<int64_t>(seg.s.begin + node) * a.o_st + h * a.o_sh;
+                const float2 scale = out.scale<FMT>();
+#pragma unroll 1
+                for (int d = d0; d < d0 + WIDTH; d += 16) {
+                    uint32_t v[16], u[16];
+                    tmem_ld_32x32b_x16(tmem + lanes + L::O + (PAIR ? w * DP : 0) + d, v);
+                    if (two) tmem_ld_32x32b_x16(tmem + lanes + L::O + DP + d, u);
                     tmem_wait_ld();
+                    float o[16];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) o[x] = __uint_as_float(v[x]) * by[0];
-                    if (two) {
-                        tmem_ld_32x32b_x16(tmem + lanes + L::O + DP + d0 + 16 * ch, v);
-                        tmem_wait_ld();
+                    for (int x = 0; x < 16; ++x) o[x] = two ? __uint_as_float(v[x]) * by[0] + __uint_as_float(u[x]) * by[1] : __uint_as_float(v[x]);
+                    if ((FMT == KV_CACHE_INT8 ? poison : poison >> (d / kMxBlock) & 1u) != 0)
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) o[x] += __uint_as_float(v[x]) * by[1];
-                    }
-                    const int d = d0 + 16 * ch;
-                    const uint32_t bad = FMT == KV_CACHE_INT8 ? poison : poison >> (d / kMxBlock) & 1u;
-                    if (live) {
+                        for (int x = 0; x < 16; ++x) o[x] = __uint_as_float(0x7fc00000u);
+                    if (!live) continue;
 #pragma unroll
-                        for (int x = 0; x < 16; x += 4) {
-                            if (d + x >= a.dim) break;
-                            Row out;
-                            out.m_o = m_o;
-                            out.m_l = m_l;
-                            out.l = l;
+                    for (int x = 0; x < 16; x += 8) {
+                        if (d + x >= a.dim) break;
+                        if (whole) {
+                            uint32_t packed[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) out.o[e] = bad != 0 ? nan : o[x + e];
-                            if (whole) out.finish<FMT>(a, seg.s, seg.head, seg.row0 + r, d + x);
-                            else *reinterpret_cast<float4*>(part + r * DP + d + x) = make_float4(out.o[0], out.o[1], out.o[2], out.o[3]);
+                            for (int e = 0; e < 4; ++e) packed[e] = out.l == 0.f ? 0u : pack_bf16(o[x + 2 * e] * scale.x * scale.y * scale.y, o[x + 2 * e + 1] * scale.x * scale.y * scale.y);
+                            *reinterpret_cast<uint4*>(to + d + x) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+                        } else {
+                            float* const q = part + r * DP + d + x;
+                            *reinterpret_cast<float4*>(q) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+                            *reinterpret_cast<float4*>(q + 4) = make_float4(o[x + 4], o[x + 5], o[x + 6], o[x + 7]);
                         }
-                        if (!whole && d == 0) *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(m_o, m_l, l, 0.f);
                     }
+                }
+                if (live && d0 == 0) {
+                    if (whole) out.write_lse(a, seg.s, node, h);
+                    else *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(m_o, m_l, l, 0.f);
                 }
             }
             tc_fence_before();
@@ -611,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const AttentionA
 }
 
 template <int FMT, int DP, bool PAIR>
-cudaError_t launch(const AttentionArgs& a, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& k_map, const CUtensorMap& v_map, const AttentionArgs& a, cudaStream_t st) {
     static PerDeviceOnce once;
     constexpr int bytes = Plan<FMT, DP, PAIR>::BYTES;
     const auto kern = many_rows_kernel<FMT, DP, PAIR>;
@@ -627,12 +742,12 @@ cudaError_t launch(const AttentionArgs& a, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, a);
+    return cudaLaunchKernelEx(&cfg, kern, k_map, v_map, a);
 }
 template <int FMT>
-cudaError_t launch_for(const AttentionArgs& a, int64_t rows, cudaStream_t st) {
-    if (a.dim <= 64) return rows > kRows ? launch<FMT, 64, true>(a, st) : launch<FMT, 64, false>(a, st);
-    return rows > kRows ? launch<FMT, 128, true>(a, st) : launch<FMT, 128, false>(a, st);
+cudaError_t launch_for(const CUtensorMap& k, const CUtensorMap& v, const AttentionArgs& a, int64_t rows, cudaStream_t st) {
+    if (a.dim <= 64) return rows > kRows ? launch<FMT, 64, true>(k, v, a, st) : launch<FMT, 64, false>(k, v, a, st);
+    return rows > kRows ? launch<FMT, 128, true>(k, v, a, st) : launch<FMT, 128, false>(k, v, a, st);
 }
 
 } // namespace
@@ -642,8 +757,8 @@ size_t many_rows_part_bytes(int64_t most_rows, int64_t dim) {
     if (dim > 128) return 0;
     return static_cast<size_t>(sm_count()) * 2 * part_floats(most_rows > kRows ? 2 * kRows : kRows, dim <= 64 ? 64 : 128) * sizeof(float);
 }
-cudaError_t launch_many_rows(int fmt, const AttentionArgs& a, int64_t rows, cudaStream_t st) {
-    return fmt == KV_CACHE_INT8 ? launch_for<KV_CACHE_INT8>(a, rows, st) : launch_for<KV_CACHE_MXFP4>(a, rows, st);
+cudaError_t launch_many_rows(int fmt, const CUtensorMap& k_map, const CUtensorMap& v_map, const AttentionArgs& a, int64_t rows, cudaStream_t st) {
+    return fmt == KV_CACHE_INT8 ? launch_for<KV_CACHE_INT8>(k_map, v_map, a, rows, st) : launch_for<KV_CACHE_MXFP4>(k_map, v_map, a, rows, st);
 }
 
 } // namespace attention
