@@ -582,8 +582,20 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
                 if (d == 0) *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(v.m_o, v.m_l, v.l, 0.f);
             }
         }
-        if (!whole)
-            merge_parts<FMT, ROWS, DP, kThreads>(a, s, b, head, row0, rows, owner(item_begin, share), owner(item_end - 1, share), threadIdx.x, &last_one, [] { __syncthreads(); });
+        const int from = owner(item_begin, share), until = owner(item_end - 1, share);
+        if (!whole && last_to_arrive<ROWS>(a, s, b, head, row0, from, until, threadIdx.x, &last_one, [] { __syncthreads(); })) {
+            for (int e = threadIdx.x; e < rows * quads; e += kThreads) {         // the parts, added up in the order of the tokens
+                const int r = e / quads, d = (e - r * quads) * 4;
+                Row v;
+#pragma unroll 4
+                for (int x = from; x <= until; ++x) {
+                    const float* p = a.parts + (2 * static_cast<int64_t>(x) + (x == from ? 1 : 0)) * PART;
+                    const float4 its = __ldcg(reinterpret_cast<const float4*>(p + ROWS * DP + 4 * r));
+                    v.add(__ldcg(reinterpret_cast<const float4*>(p + r * DP + d)), its.x, its.y, its.z);
+                }
+                v.finish<FMT>(a, s, head, row0 + r, d);
+            }
+        }
         fence_proxy_async_smem();                                   // what threads have written here is overwritten by boxes
         __syncthreads();
         u += steps;

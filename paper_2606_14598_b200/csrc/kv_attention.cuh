@@ -119,6 +119,11 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&p);
@@ -238,44 +243,20 @@ __device__ __forceinline__ void zero_rest(const AttentionArgs& a) {
     }
 }
 
-// The last segment of an item to arrive, of those that CTAs `first` to `last` work on, adds the parts up in the order of the tokens. Called by THREADS threads that
-// `sync` brings together, `me` of them; `part` holds this CTA's.
-template <int FMT, int ROWS, int DP, int THREADS, typename Sync>
-__device__ __forceinline__ void merge_parts(const AttentionArgs& a, const Sequence& s, int b, int head, int row0, int rows, int first, int last, int me, int* last_one, Sync sync) {
-    constexpr int PART = part_floats(ROWS, DP);
+// Whether this segment of an item is the last to arrive, of those that CTAs `first` to `last` work on: its threads (which `sync` brings together, `me` of
+// them) find all parts written.
+template <int ROWS, typename Sync>
+__device__ __forceinline__ bool last_to_arrive(const AttentionArgs& a, const Sequence& s, int b, int head, int row0, int first, int last, int me, int* last_one, Sync sync) {
     // (place of the item's counter: sequences' row tiles one after another, a place more for each that ends in the middle of one)
     uint32_t* const counter = a.counters + (static_cast<int64_t>(b) + static_cast<int64_t>(s.begin) * a.group / ROWS + row0 / ROWS) * a.heads + head;
     __threadfence();
     sync();
     if (me == 0) *last_one = atomicAdd(counter, 1u) == static_cast<uint32_t>(last - first);
     sync();
-    if (*last_one) {
-        if (me == 0) *counter = 0;
-        __threadfence();
-        const int quads = a.dim / 4;
-        constexpr int AT_ONCE = ROWS >= 64 ? 4 : 1;             // (elements of a thread whose parts are on their way together)
-        for (int e0 = me; e0 < rows * quads; e0 += AT_ONCE * THREADS) {
-            Row v[AT_ONCE];
-#pragma unroll (4 / AT_ONCE)
-            for (int x = first; x <= last; ++x) {
-                const float* from = a.parts + (2 * static_cast<int64_t>(x) + (x == first ? 1 : 0)) * PART;
-                float4 o[AT_ONCE], its[AT_ONCE];
-#pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) {
-                    const int e = min(e0 + i * THREADS, rows * quads - 1), r = e / quads, d = (e - r * quads) * 4;
-                    its[i] = __ldcg(reinterpret_cast<const float4*>(from + ROWS * DP + 4 * r));
-                    o[i] = __ldcg(reinterpret_cast<const float4*>(from + r * DP + d));
-                }
-#pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) v[i].add(o[i], its[i].x, its[i].y, its[i].z);
-            }
-#pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) {
-                const int e = e0 + i * THREADS, r = e / quads, d = (e - r * quads) * 4;
-                if (e < rows * quads) v[i].template finish<FMT>(a, s, head, row0 + r, d);
-            }
-        }
-    }
+    if (!*last_one) return false;
+    if (me == 0) *counter = 0;
+    __threadfence();
+    return true;
 }
 
 // ---- kv_attention_tc.cu : the attention for many rows of queries a head (the maps: codes of keys and of values in boxes of a.box tokens of a head)

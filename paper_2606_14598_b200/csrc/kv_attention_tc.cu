@@ -19,10 +19,10 @@ namespace {
 
 constexpr int kTok = 128;                       // tokens of a tile
 constexpr int kRows = 128;                      // rows of a product
-constexpr int kConvertWarp = 8, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 18, kConverters = 256, kSoftmax = 256;
+constexpr int kConvertWarp = 8, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 20, kConverters = 256, kSoftmax = 256;
 constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 9 after it
 constexpr int kSlots = 4;                       // tiles whose factors are kept
-constexpr int kRaw = 3;                         // tiles of codes on their way
+constexpr int kRaw = 3;                         // tiles of codes on their way: a warp each, which loads every third one
 
 template <int FMT, int DP, bool PAIR>
 struct Plan {
@@ -36,13 +36,14 @@ struct Plan {
     // may be seen, and (4-bit) where in the words its bytes begin
     static constexpr int WORDS = FMT == KV_CACHE_INT8 ? 1 : 2, V_SCALES = kTok * 4 * WORDS, FLAGS = 2 * V_SCALES, MORE_BYTES = FLAGS + kTok;
     static constexpr int FACTORS = MORE + kRaw * MORE_BYTES;
-    static constexpr int NANS = FACTORS + kSlots * kTok * 4;                   // NaN blocks of a token's values, a byte each
-    static constexpr int SIGMA = NANS + kSlots * kTok, ANY_NAN = SIGMA + kSlots * 4, OF_WARP = ANY_NAN + kSlots * 4, ROW_FACTOR = OF_WARP + 2 * 8 * 4;
+    static constexpr int ONES = FACTORS + kSlots * kTok * 4;                   // factors of scores that have theirs already
+    static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
+    static constexpr int SIGMA = NANS + kSlots * kTok, ANY_NAN = SIGMA + kSlots * 4, OF_WARP = ANY_NAN + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, ROW_FACTOR = OF_V + 2 * kTok * 4;
     static constexpr int STATE = ROW_FACTOR + ROWS * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 24 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
     // codes: a thread converts a chunk of 16 bytes of every PASS-th token
-    static constexpr int CHUNKS = ROW / 16, PASS = kConverters / CHUNKS, EACH = kTok / PASS, CODES = 16 * PER_BYTE;
+    static constexpr int CHUNKS = ROW / 16, PASS = kConverters / CHUNKS, CODES = 16 * PER_BYTE;
     // byte `off` of row r of a tile of codes, as boxes arrive: chunks of 16 bytes change places by the row
     __device__ static __forceinline__ int raw_place(int r, int off) {
         const int turn = ROW == 128 ? r & 7 : ROW == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
@@ -130,6 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t bars = base + L::BARS;
     auto bar = [&](int which, int i) { return bars + 8 * (which + i); };
+    if (threadIdx.x < kTok) reinterpret_cast<float*>(smem + L::ONES)[threadIdx.x] = 1.f;
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int i = 0; i < L::RING; ++i) {
@@ -224,79 +226,60 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         }
         if (lane == 0) tc_commit(bar(DRAINED, 0));                               // (whatever became of the waits, no product is left when the CTA goes)
         mbar_drain(bar(DRAINED, 0), 0, a.limit_ns);
-    } else if (warp == kLoadWarp) {
-        // ---- codes and scales into shared memory. A lane has four tokens of a tile; codes come as boxes of tokens that lie side by side in any page, or
-        // (heads that are not whole 16-byte pieces) piece by piece.
-        Turn<kRaw> turn;
+    } else if (warp >= kLoadWarp) {
+        // ---- codes and scales into shared memory: each warp fills one slot, again and again, with every third tile of K0 V0 K1 V1 ... (and so waits for every use of
+        // it: a parity would not tell a use from the one after the next). A lane has four tokens of a tile; codes come as boxes of tokens that lie side by side in
+        // any page, or (heads that are not whole 16-byte pieces) piece by piece.
         const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
+        const bool runs = a.page % 4 == 0;                                       // a lane's tokens lie side by side
+        const uint32_t slot = warp - kLoadWarp, units = 2 * static_cast<uint32_t>(share.end - share.begin);
         int next[4], next_head = 0;
+        uint32_t first_of_seg = 0;                                               // tiles before the segment
         bool next_in[4], more = seg.next();
-        int tile = 0;
-        auto look_up = [&] {                                                     // where the tokens of the tile are; then on to the one after it
-            const int t0 = more ? seg.token(tile) + 4 * lane : 0;
+        auto look_up = [&](uint32_t tile) {                                      // where the tokens of a tile are (tiles are asked for in their order)
+            while (more && tile - first_of_seg >= static_cast<uint32_t>(seg.tiles)) {
+                first_of_seg += seg.tiles;
+                more = seg.next();
+            }
+            const int t0 = more ? seg.token(static_cast<int>(tile - first_of_seg)) + 4 * lane : 0;
             next_head = seg.head;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = t0 + i;
-                next[i] = -1;
-                next_in[i] = false;
-                if (more && t < seg.s.stop) {
-                    const int p = a.page_shift >= 0 ? t >> a.page_shift : t / a.page, id = a.table[seg.b * a.table_stride + p];
-                    if (id >= 0 && id < a.num_pages) next[i] = id * a.page + (t - p * a.page);
-                    next_in[i] = next[i] >= 0 && t >= seg.s.start;
+                if (i == 0 || !runs) {
+                    next[i] = -1;
+                    if (more && t < seg.s.stop) {
+                        const int p = a.page_shift >= 0 ? t >> a.page_shift : t / a.page, id = a.table[seg.b * a.table_stride + p];
+                        if (id >= 0 && id < a.num_pages) next[i] = id * a.page + (t - p * a.page);
+                    }
+                } else {
+                    next[i] = next[0] >= 0 && t < seg.s.stop ? next[0] + i : -1;
                 }
-            }
-            if (more && ++tile == seg.tiles) {
-                more = seg.next();
-                tile = 0;
+                next_in[i] = next[i] >= 0 && t >= seg.s.start;
             }
         };
-        look_up();
-        for (int64_t left = share.end - share.begin; left > 0; --left) {
+        look_up(slot >> 1);
+        uint32_t phase = 1;
+        for (uint32_t unit = slot; unit < units; unit += kRaw, phase ^= 1) {
             int slots[4];
             uint32_t flags = 0;
-            const int head = next_head;
+            const int head = next_head, side = unit & 1;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 slots[i] = next[i];
-                const uint32_t shift = FMT == KV_CACHE_INT8 ? 0u : static_cast<uint32_t>((static_cast<int64_t>(max(slots[i], 0)) * a.heads + head) * blocks & 3);
-                flags |= (next_in[i] ? 0x80u | shift : 0u) << (8 * i);
+                flags |= (next_in[i] ? 0x80u : 0u) << (8 * i);
             }
-            look_up();                                                           // (of the tile after this one: on its way meanwhile)
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                mbar_wait(bar(RAW_EMPTY, turn.slot), turn.phase ^ 1, ctl, kWaitMany + 4, kStatusTimeout);
-                const uint32_t full = bar(RAW_FULL, turn.slot), to = base + L::RAW + turn.slot * kTok * L::ROW, rest = base + L::MORE + turn.slot * L::MORE_BYTES;
-                if (side == 0) {
-                    *reinterpret_cast<uint32_t*>(smem + L::MORE + turn.slot * L::MORE_BYTES + L::FLAGS + 4 * lane) = flags;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t entry = static_cast<int64_t>(max(slots[i], 0)) * a.heads + head;
-#pragma unroll
-                        for (int kv = 0; kv < 2; ++kv) {
-                            const void* scales = kv == 0 ? a.k_scales : a.v_scales;
-                            const uint32_t at = rest + kv * L::V_SCALES + (4 * lane + i) * 4 * L::WORDS;
-                            if (FMT == KV_CACHE_INT8) {
-                                cp_async<4>(at, static_cast<const float*>(scales) + entry, slots[i] >= 0 ? 4 : 0);
-                            } else {
-                                const int64_t first = entry * blocks;
-                                const int shift = static_cast<int>(first & 3);
-                                const uint8_t* p = static_cast<const uint8_t*>(scales) + first - shift;
-                                const bool two = slots[i] >= 0 && shift + blocks > 4;
-                                cp_async<4>(at, p, slots[i] >= 0 ? 4 : 0);
-                                cp_async<4>(at + 4, p + (two ? 4 : 0), two ? 4 : 0);
-                            }
-                        }
-                    }
-                }
+            if (unit + kRaw < units) look_up((unit + kRaw) >> 1);                // (on its way meanwhile)
+            {
+                mbar_wait(bar(RAW_EMPTY, slot), phase, ctl, kWaitMany + 4, kStatusTimeout);
+                const uint32_t full = bar(RAW_FULL, slot), to = base + L::RAW + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
                 if (a.box > 0) {
                     // boxes that begin with this lane's tokens: one of 4 or more tokens, or several smaller ones
                     uint32_t mine = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mine |= static_cast<uint32_t>(slots[i] >= 0 && (4 * lane + i) % a.box == 0) << i;
                     const uint32_t boxes = __reduce_add_sync(0xffffffffu, __popc(mine));
-                    if (lane == 0) mbar_arrive_expect_tx(full, boxes * a.box * L::ROW);
-                    else mbar_arrive(full);
+                    if (lane == 0) mbar_expect_tx(full, boxes * a.box * L::ROW);
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -321,27 +304,45 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             for (int i = 0; i < 8; i += 4) cp_async<4>(to + L::raw_place(r, off) + i, codes + (valid > i ? where + i : 0), valid > i ? 4 : 0);
                         }
                     }
-                    mbar_arrive(full);
                 }
+                if (side == 0) {                                                 // with the keys, all scales
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t entry = static_cast<int64_t>(max(slots[i], 0)) * a.heads + head;
+                        const uint32_t at = rest + (4 * lane + i) * 4 * L::WORDS, there = slots[i] >= 0 ? 4 : 0;
+                        if (FMT == KV_CACHE_INT8) {
+                            cp_async<4>(at, static_cast<const float*>(a.k_scales) + entry, there);
+                            cp_async<4>(at + L::V_SCALES, static_cast<const float*>(a.v_scales) + entry, there);
+                        } else {
+                            const int64_t first = entry * blocks;
+                            const uint32_t shift = static_cast<uint32_t>(first) & 3u;
+                            flags |= (flags >> (8 * i) & 0x80u ? shift : 0u) << (8 * i);
+                            cp_async<4>(at, static_cast<const uint8_t*>(a.k_scales) + (first - shift), there);
+                            cp_async<4>(at + L::V_SCALES, static_cast<const uint8_t*>(a.v_scales) + (first - shift), there);
+                            if (blocks != 4 && blocks != 2) {                    // (bytes of a token may lie across two words)
+                                const uint32_t two = shift + blocks > 4 ? there : 0;
+                                cp_async<4>(at + 4, static_cast<const uint8_t*>(a.k_scales) + (first - shift) + two, two);
+                                cp_async<4>(at + L::V_SCALES + 4, static_cast<const uint8_t*>(a.v_scales) + (first - shift) + two, two);
+                            }
+                        }
+                    }
+                    *reinterpret_cast<uint32_t*>(smem + L::MORE + slot * L::MORE_BYTES + L::FLAGS + 4 * lane) = flags;
+                }
+                mbar_arrive(full);
                 cp_async_mbar_arrive(full);                                      // once this lane's own copies are there
-                turn.next();
             }
         }
         // nothing is on its way when the CTA goes: what was asked for has been waited for by those who convert it, unless a wait gave up
         if (abort_flag != 0) {
             asm volatile("cp.async.wait_all;" ::: "memory");
-            for (int i = 0; i < kRaw; ++i) {
-                turn.slot = turn.slot == 0 ? kRaw - 1 : turn.slot - 1;
-                if (turn.slot == kRaw - 1) turn.phase ^= 1;
-                if (2 * (share.end - share.begin) > i) mbar_drain(bar(RAW_FULL, turn.slot), turn.phase, a.limit_ns);
-            }
+            for (uint32_t last = units > kRaw ? units - kRaw : 0; last < units; ++last) mbar_drain(bar(RAW_FULL, last % kRaw), last / kRaw & 1, a.limit_ns);
         }
     } else if (warp >= kConvertWarp) {
         // ---- codes to fp16 tiles
-        constexpr int EACH = L::EACH;
         const int me = threadIdx.x - 32 * kConvertWarp, chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
         static_assert(FMT == KV_CACHE_INT8 || L::CODES == kMxBlock, "a chunk is a block");
         int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
+        uint8_t* const v_scales = smem + L::OF_V;                                // [tile % 2]
         Turn<kRaw> raw;
         Turn<L::RING> ring;
         uint32_t t = 0;                                                          // tiles so far
@@ -349,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             int sigma = -126;                                                    // the values' reference starts anew with each segment
             for (int left = seg.tiles; left > 0; --left, ++t) {
                 const uint32_t slot = t & (kSlots - 1);
-                uint32_t vsc[EACH], seen = 0;                                    // int8: the scale; 4-bit: the byte of this chunk's block
                 // keys
                 mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
                 mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
@@ -358,34 +358,33 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
                     const uint8_t* const rest = smem + L::MORE + raw.slot * L::MORE_BYTES;
                     const uint32_t tile = base + ring.slot * L::TILE;
-#pragma unroll
-                    for (int i = 0; i < EACH; ++i) {
-                        const int r = tok + i * L::PASS;
+#pragma unroll 2
+                    for (int r = tok; r < kTok; r += L::PASS) {
                         const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
                         const uint32_t w[4] = {x.x, x.y, x.z, x.w}, flag = rest[L::FLAGS + r];
                         const bool in = flag != 0;
-                        seen |= static_cast<uint32_t>(in) << i;
+                        // v_scales keeps for the values' turn: int8: the scale, 4-bit: the byte of this chunk's block; NaN and unseen ones as 0 (finite is what matters)
                         if (FMT == KV_CACHE_INT8) {
                             uint32_t f[8];
 #pragma unroll
                             for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
                             store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
                             store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
-                            vsc[i] = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[r];
-                            const bool nan = (vsc[i] & 0x7f800000u) == 0x7f800000u && in;
+                            const uint32_t vs = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[r];
+                            const bool nan = (vs & 0x7f800000u) == 0x7f800000u && in;
                             if (chunk == 0) {
                                 factors[slot * kTok + r] = in ? reinterpret_cast<const float*>(rest)[r] : -1.f;
                                 nans[slot * kTok + r] = nan ? 0xff : 0;
+                                reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + r] = in && !nan ? vs : 0u;
                             }
                             nan_any |= nan;
-                            if (in && !nan) top_sigma = max(top_sigma, static_cast<int>(vsc[i] >> 23) - 126);     // s < 2^this
+                            if (in && !nan) top_sigma = max(top_sigma, static_cast<int>(vs >> 23) - 126);         // s < 2^this
                         } else {
                             const uint8_t* const its = rest + r * 8 + (flag & 3) + chunk;
-                            const uint32_t ksc = in && chunk < blocks ? its[0] : 0u;
-                            vsc[i] = in && chunk < blocks ? its[L::V_SCALES] : 0u;
+                            const uint32_t ksc = in && chunk < blocks ? its[0] : 0u, vs = in && chunk < blocks ? its[L::V_SCALES] : 0u;
                             // the token's largest byte: of the lanes that hold its chunks
                             const bool nan = ksc == 255u;
-                            uint32_t top = nan ? 0u : ksc, bad = (nan ? 256u : 0u) | (vsc[i] == 255u ? 1u << chunk : 0u);
+                            uint32_t top = nan ? 0u : ksc, bad = (nan ? 256u : 0u) | (vs == 255u ? 1u << chunk : 0u);
 #pragma unroll
                             for (int o = 1; o < L::CHUNKS; o <<= 1) {
                                 top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -403,8 +402,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 factors[slot * kTok + r] = !in ? -1.f : bad >= 256u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
                                 nans[slot * kTok + r] = static_cast<uint8_t>(bad);
                             }
+                            v_scales[(t & 1) * kTok * 4 + r * 4 + chunk] = vs == 255u ? 0 : static_cast<uint8_t>(vs);
                             nan_any |= (bad & 255u) != 0;
-                            if (in && chunk < blocks && vsc[i] != 255u) top_sigma = max(top_sigma, static_cast<int>(vsc[i]) - 127);
+                            if (in && chunk < blocks && vs != 255u) top_sigma = max(top_sigma, static_cast<int>(vs) - 127);
                         }
                     }
                 }
@@ -437,18 +437,14 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 {
                     const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
                     const uint32_t tile = base + ring.slot * L::TILE;
-#pragma unroll
-                    for (int i = 0; i < EACH; ++i) {
-                        const int r = tok + i * L::PASS;
+                    // (int8: two factors, as 2^(8 - sigma) alone may be more than fp32 holds)
+                    const float by0 = __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23), by1 = __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23);
+#pragma unroll 2
+                    for (int r = tok; r < kTok; r += L::PASS) {
                         const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
                         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                        const bool in = (seen >> i & 1u) != 0;
                         if (FMT == KV_CACHE_INT8) {
-                            const bool fine = in && (vsc[i] & 0x7f800000u) != 0x7f800000u;
-                            // (two factors: 2^(8 - sigma) alone may be more than fp32 holds)
-                            const float by = fine ? __uint_as_float(vsc[i]) * __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23) *
-                                                        __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23)
-                                                  : 0.f;
+                            const float by = reinterpret_cast<const float*>(v_scales)[(t & 1) * kTok + r] * by0 * by1;
                             const uint32_t mul = pack_f16(by, by);
                             uint32_t f[8];
 #pragma unroll
@@ -458,8 +454,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
                             store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
                         } else {
-                            const int e = 27 + static_cast<int>(vsc[i]) - 127 - sigma;       // (2^12 * 2^(byte - 127 - sigma), subnormal from 0 down)
-                            const uint32_t bits = e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31), mul = !in || vsc[i] == 255u ? 0u : bits * 0x00010001u;
+                            // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
+                            const int byte = v_scales[(t & 1) * kTok * 4 + r * 4 + chunk], e = 27 + byte - 127 - sigma;
+                            const uint32_t bits = e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31), mul = bits * 0x00010001u;
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 uint32_t f[4];
@@ -526,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(Q_FULL, 0));
             named_sync(2, kSoftmax);
-            const float factor = row_factor[r];
+            const float factor = fmaxf(row_factor[r], 1e-38f);                   // (not 0: -inf times it is -inf)
             float m = kNone;
             uint64_t l2 = 0;
             int sigma = -126;
@@ -539,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 mbar_wait(bar(S_FULL, w), jobs & 1, ctl, kWaitMany + 7, kStatusTimeout);
                 tc_fence_after();
                 if (warp_live) {
-                    const float* const kf = factors + slot * kTok;
+                    const float* kf = factors + slot * kTok;
                     const int j0 = seg.token(t) - seg.s.before;
                     // which of 32 tokens this row sees: those that anybody does, and of the new ones its own
                     auto sees32_of = [&](int ch) {
@@ -551,32 +548,50 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
 #pragma unroll 1
                         for (int ch = 0; ch < 4; ++ch) {
                             const uint32_t sees = sees32_of(ch);
+#pragma unroll 1
                             for (int x = 0; x < 32; ++x)
-                                if (sees >> x & 1u) poison |= nans[slot * kTok + 32 * ch + x];
+                                if (sees >> x & 1u) poison |= nans[slot * kTok + x + 32 * ch];
                         }
                     }
-                    // the row's largest score
-                    float top = -INFINITY;
+                    // tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places
+                    const float4 flags = *reinterpret_cast<const float4*>(kf + 4 * lane);
+                    if (j0 + kTok > 0 || __any_sync(0xffffffffu, flags.x == -1.f || flags.y == -1.f || flags.z == -1.f || flags.w == -1.f)) {
 #pragma unroll 1
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t v[32];
-                        tmem_ld_32x32b_x32(s_tmem + 32 * ch, v);
-                        const uint32_t sees = sees32_of(ch);
-                        tmem_wait_ld();
-                        if (__all_sync(0xffffffffu, sees == ~0u)) {
+                        for (int ch = 0; ch < 8; ++ch) {
+                            uint32_t v[16];
+                            tmem_ld_32x32b_x16(s_tmem + 16 * ch, v);
+                            const uint32_t sees = sees32_of(ch / 2) >> (16 * (ch & 1));
+                            tmem_wait_ld();
 #pragma unroll
-                            for (int x = 0; x < 32; x += 4) {
-                                const float4 k = *reinterpret_cast<const float4*>(kf + 32 * ch + x);
-                                float p, q, y, z;
-                                unpack2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), pack2(k.x, k.y)), p, q);
-                                unpack2(mul2(pack2(__uint_as_float(v[x + 2]), __uint_as_float(v[x + 3])), pack2(k.z, k.w)), y, z);
-                                top = fmaxf(top, fmaxf(fmaxf(p, q), fmaxf(y, z)));
-                            }
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (sees >> x & 1u) top = fmaxf(top, __uint_as_float(v[x]) * kf[32 * ch + x]);
+                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? __float_as_uint(__uint_as_float(v[i]) * kf[16 * ch + i]) : 0xff800000u;
+                            tmem_st_32x32b_x16(s_tmem + 16 * ch, v);
                         }
+                        tmem_wait_st();
+                        kf = reinterpret_cast<const float*>(smem + L::ONES);
+                    }
+                    // the row's largest score: 16 columns at a time, the next ones on their way
+                    float top = -INFINITY;
+                    {
+                        uint32_t v[2][16];
+                        tmem_ld_32x32b_x16(s_tmem, v[0]);
+#pragma unroll 1
+                        for (int ch = 0; ch < 8; ch += 2) {
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                tmem_wait_ld();
+                                tmem_ld_32x32b_x16(s_tmem + 16 * ((ch + half + 1) & 7), v[half ^ 1]);
+                                const uint32_t (&x)[16] = v[half];
+#pragma unroll
+                                for (int i = 0; i < 16; i += 4) {
+                                    const float4 k = *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
+                                    float p, q, y, z;
+                                    unpack2(mul2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y)), p, q);
+                                    unpack2(mul2(pack2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), pack2(k.z, k.w)), y, z);
+                                    top = max3(max3(top, p, q), y, z);
+                                }
+                            }
+                        }
+                        tmem_wait_ld();
                     }
                     top = top == -INFINITY ? kNone : top * factor;
                     // references move when a weight would pass 2^15, to put it at 2^7, or when the values' does
@@ -604,33 +619,37 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     first = false;
                     // weights, over the scores that they came from
                     const uint64_t m2 = pack2(-m, -m);
+                    {
+                        uint32_t v[2][16];
+                        uint64_t sum[2] = {0, 0};
+                        tmem_ld_32x32b_x16(s_tmem, v[0]);
 #pragma unroll 1
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t v[32], p[16];
-                        tmem_ld_32x32b_x32(s_tmem + 32 * ch, v);
-                        const uint32_t sees = sees32_of(ch);
-                        tmem_wait_ld();
+                        for (int ch = 0; ch < 8; ch += 2) {
 #pragma unroll
-                        for (int x = 0; x < 32; x += 2) {
-                            const uint64_t k = *reinterpret_cast<const uint64_t*>(kf + 32 * ch + x);
-                            const uint64_t arg = fma2(mul2(pack2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), k), f2, m2);
-                            float y, z;
-                            unpack2(arg, y, z);
-                            v[x] = __float_as_uint(y);
-                            v[x + 1] = __float_as_uint(z);
-                        }
-                        if (!__all_sync(0xffffffffu, sees == ~0u)) {
+                            for (int half = 0; half < 2; ++half) {
+                                tmem_wait_ld();
+                                if (half == 0 || ch < 6) tmem_ld_32x32b_x16(s_tmem + 16 * (ch + half + 1), v[half ^ 1]);
+                                const uint32_t (&x)[16] = v[half];
+                                uint32_t p[8];
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (!(sees >> x & 1u)) v[x] = 0xff800000u;
+                                for (int i = 0; i < 16; i += 4) {
+                                    const float4 k = *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
+                                    float y, z;
+                                    unpack2(fma2(mul2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y)), f2, m2), y, z);
+                                    y = ex2(y);
+                                    z = ex2(z);
+                                    sum[0] = add2(sum[0], pack2(y, z));
+                                    p[i / 2] = pack_f16(y, z);
+                                    unpack2(fma2(mul2(pack2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), pack2(k.z, k.w)), f2, m2), y, z);
+                                    y = ex2(y);
+                                    z = ex2(z);
+                                    sum[1] = add2(sum[1], pack2(y, z));
+                                    p[i / 2 + 1] = pack_f16(y, z);
+                                }
+                                tmem_st_32x32b_x8(s_tmem + 8 * (ch + half), p);
+                            }
                         }
-#pragma unroll
-                        for (int x = 0; x < 32; x += 2) {
-                            const float y = ex2(__uint_as_float(v[x])), z = ex2(__uint_as_float(v[x + 1]));
-                            l2 = add2(l2, pack2(y, z));
-                            p[x / 2] = pack_f16(y, z);
-                        }
-                        tmem_st_32x32b_x16(s_tmem + 16 * ch, p);
+                        l2 = add2(l2, add2(sum[0], sum[1]));
                     }
                     tmem_wait_st();
                 }
@@ -649,8 +668,20 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             named_sync(2, kSoftmax);
             tc_fence_after();
             const bool whole = seg.whole();
+            // a part: elements 4q to 4q + 3 of row r at float4 q * ROWS + r (so that the threads of a warp, a row each, write and read side by side), then the states
             constexpr int PART = part_floats(ROWS, DP);
-            float* const part = a.parts + (2 * static_cast<int64_t>(blockIdx.x) + (share.begin > seg.item_begin ? 0 : 1)) * PART;
+            float4* const part = reinterpret_cast<float4*>(a.parts + (2 * static_cast<int64_t>(blockIdx.x) + (share.begin > seg.item_begin ? 0 : 1)) * PART);
+            // (one tile of rows: each warpgroup takes half of the elements)
+            constexpr int WIDTH = PAIR ? DP : DP / 2;
+            const int d0 = PAIR ? 0 : w * WIDTH, h = seg.head * a.group + seg.row0 + r - node * a.group;
+            __nv_bfloat16* const to = a.out + static_cast<int64_t>(seg.s.begin + node) * a.o_st + h * a.o_sh;
+            auto write8 = [&](const Row& state_of, float2 scale, const float* o, int d) {        // eight elements of this thread's row
+                uint32_t packed[4];
+                const float both = scale.x * scale.y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) packed[e] = state_of.l == 0.f ? 0u : pack_bf16(o[2 * e] * both * scale.y, o[2 * e + 1] * both * scale.y);
+                *reinterpret_cast<uint4*>(to + d) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+            };
             if (warp_live) {
                 float by[2] = {1.f, 0.f};
                 const bool two = !PAIR && seg.tiles > 1;
@@ -667,15 +698,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         poison |= __float_as_uint(s1.w);
                     }
                 }
-                // (one item's rows: each warpgroup takes half of the elements)
-                constexpr int WIDTH = PAIR ? DP : DP / 2;
-                const int d0 = PAIR ? 0 : w * WIDTH;
                 Row out;
                 out.m_o = m_o;
                 out.m_l = m_l;
                 out.l = l;
-                const int h = seg.head * a.group + seg.row0 + r - node * a.group;
-                __nv_bfloat16* const to = a.out + static_cast<int64_t>(seg.s.begin + node) * a.o_st + h * a.o_sh;
                 const float2 scale = out.scale<FMT>();
 #pragma unroll 1
                 for (int d = d0; d < d0 + WIDTH; d += 16) {
@@ -690,31 +716,60 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
 #pragma unroll
                         for (int x = 0; x < 16; ++x) o[x] = __uint_as_float(0x7fc00000u);
                     if (!live) continue;
+                    if (whole) {
 #pragma unroll
-                    for (int x = 0; x < 16; x += 8) {
-                        if (d + x >= a.dim) break;
-                        if (whole) {
-                            uint32_t packed[4];
+                        for (int x = 0; x < 16; x += 8)
+                            if (d + x < a.dim) write8(out, scale, o + x, d + x);
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) packed[e] = out.l == 0.f ? 0u : pack_bf16(o[x + 2 * e] * scale.x * scale.y * scale.y, o[x + 2 * e + 1] * scale.x * scale.y * scale.y);
-                            *reinterpret_cast<uint4*>(to + d + x) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-                        } else {
-                            float* const q = part + r * DP + d + x;
-                            *reinterpret_cast<float4*>(q) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-                            *reinterpret_cast<float4*>(q + 4) = make_float4(o[x + 4], o[x + 5], o[x + 6], o[x + 7]);
-                        }
+                        for (int x = 0; x < 16; x += 4) part[(d + x) / 4 * ROWS + r] = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
                     }
                 }
                 if (live && d0 == 0) {
                     if (whole) out.write_lse(a, seg.s, node, h);
-                    else *reinterpret_cast<float4*>(part + ROWS * DP + 4 * r) = make_float4(m_o, m_l, l, 0.f);
+                    else part[DP / 4 * ROWS + r] = make_float4(m_o, m_l, l, 0.f);
                 }
             }
             tc_fence_before();
             named_sync(2, kSoftmax);                                             // o and the states may be written over
-            if (!whole)
-                merge_parts<FMT, ROWS, DP, kSoftmax>(a, seg.s, seg.b, seg.head, seg.row0, seg.rows, owner(seg.item_begin, share), owner(seg.item_end - 1, share),
-                                                     threadIdx.x, &last_one, [] { named_sync(2, kSoftmax); });
+            if (!whole) {
+                const int from = owner(seg.item_begin, share), until = owner(seg.item_end - 1, share);
+                if (last_to_arrive<ROWS>(a, seg.s, seg.b, seg.head, seg.row0, from, until, threadIdx.x, &last_one, [] { named_sync(2, kSoftmax); }) && live) {
+                    // the parts of this thread's row and elements, in the order of the tokens: 16 elements at a time, their loads on their way together
+                    auto part_of = [&](int x) { return reinterpret_cast<const float4*>(a.parts + (2 * static_cast<int64_t>(x) + (x == from ? 1 : 0)) * PART); };
+#pragma unroll 1
+                    for (int d = d0; d < min(d0 + WIDTH, a.dim); d += 32) {
+                        float o[32];
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) o[x] = 0.f;
+                        Row sum;
+#pragma unroll 1
+                        for (int x = from; x <= until; ++x) {
+                            const float4* const p = part_of(x);
+                            const float4 its = __ldcg(p + DP / 4 * ROWS + r);
+                            float4 v[8];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) v[q] = __ldcg(p + (d / 4 + q) * ROWS + r);
+                            const float now_o = fmaxf(sum.m_o, its.x), now_l = fmaxf(sum.m_l, its.y), mine = ex2(sum.m_o - now_o), other_one = ex2(its.x - now_o);
+                            sum.l = sum.l * ex2(sum.m_l - now_l) + its.z * ex2(its.y - now_l);
+                            sum.m_o = now_o;
+                            sum.m_l = now_l;
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                o[4 * q] = o[4 * q] * mine + v[q].x * other_one;
+                                o[4 * q + 1] = o[4 * q + 1] * mine + v[q].y * other_one;
+                                o[4 * q + 2] = o[4 * q + 2] * mine + v[q].z * other_one;
+                                o[4 * q + 3] = o[4 * q + 3] * mine + v[q].w * other_one;
+                            }
+                        }
+                        const float2 scale = sum.scale<FMT>();
+#pragma unroll
+                        for (int x = 0; x < 32; x += 8)
+                            if (d + x < a.dim) write8(sum, scale, o + x, d + x);
+                        if (d == 0) sum.write_lse(a, seg.s, node, h);
+                    }
+                }
+            }
             tile_base += seg.tiles;
         }
     }
