@@ -20,7 +20,7 @@ namespace {
 constexpr int kTok = 128;                       // tokens of a tile
 constexpr int kRows = 128;                      // rows of a product
 constexpr int kConvertWarp = 8, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 20, kConverters = 256, kSoftmax = 256;
-constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 9 after it
+constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 10 after it
 constexpr int kSlots = 4;                       // tiles whose factors are kept
 constexpr int kRaw = 3;                         // tiles of codes on their way: a warp each, which loads every third one
 
@@ -38,8 +38,9 @@ struct Plan {
     static constexpr int FACTORS = MORE + kRaw * MORE_BYTES;
     static constexpr int ONES = FACTORS + kSlots * kTok * 4;                   // factors of scores that have theirs already
     static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
-    static constexpr int SIGMA = NANS + kSlots * kTok, ANY_NAN = SIGMA + kSlots * 4, OF_WARP = ANY_NAN + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, ROW_FACTOR = OF_V + 2 * kTok * 4;
-    static constexpr int STATE = ROW_FACTOR + ROWS * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 24 * 8 + 1024;
+    static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, OF_K = OF_V + 2 * kTok * 4;
+    static constexpr int FACTOR = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 8);         // of the scores, and the queries' maxima of the warps
+    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 24 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
     // codes: a thread converts a chunk of 16 bytes of every PASS-th token
@@ -50,7 +51,7 @@ struct Plan {
         return r * ROW + (off ^ (turn << 4));
     }
 };
-enum Bar { TILE_FULL = 0, TILE_EMPTY = 4, RAW_FULL = 8, RAW_EMPTY = 11, S_FULL = 14, P_FULL = 16, O_DONE = 18, Q_FULL = 20, DRAINED = 21 };
+enum Bar { TILE_FULL = 0, TILE_EMPTY = 4, RAW_FULL = 8, RAW_EMPTY = 11, S_FULL = 14, P_FULL = 16, O_DONE = 18, Q_FULL = 20, FACTOR_FULL = 21, DRAINED = 22 };
 
 // A CTA's segments, one after another: (sequence, head, rows) and a run of its tiles. Every role walks them by itself.
 template <int ROWS>
@@ -148,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             mbar_init(bar(O_DONE, i), 1);
         }
         mbar_init(bar(Q_FULL, 0), 8);
+        mbar_init(bar(FACTOR_FULL, 0), 8);
         mbar_init(bar(DRAINED, 0), 1);
         fence_mbar_init();
     }
@@ -164,9 +166,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     tc_fence_after();
     grid_dep_launch_dependents();
     const uint32_t tmem = tmem_slot;
-    float* const factors = reinterpret_cast<float*>(smem + L::FACTORS);          // [slot][token]: of the keys; -1: not seen by anybody
+    float* const factors = reinterpret_cast<float*>(smem + L::FACTORS);          // [slot][token]: of the scores; -1: not seen by anybody
     volatile int* const sigmas = reinterpret_cast<volatile int*>(smem + L::SIGMA);        // [slot]: values are relative to 2^this
-    volatile int* const any_nan = reinterpret_cast<volatile int*>(smem + L::ANY_NAN);     // [slot]: whether values of the tile are NaN
+    volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2)
     uint8_t* const nans = smem + L::NANS;
     const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
     Segments<ROWS> seg(a, share);
@@ -175,6 +177,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         // ---- products. A job is a tile of tokens for one of the two softmax warpgroups: every other tile, or (PAIR) each tile for both.
         uint32_t segments = 0, jobs_of[2] = {0, 0};
         constexpr uint32_t kQk = make_f16_idesc(kRows, kTok, false), kPv = make_f16_idesc(kRows, DP, true);
+        const uint64_t k_desc = make_kmajor_sw128_desc(base), v_desc = make_mnmajor_sw128_desc(base, L::PANEL);
+        const uint32_t k_lo = static_cast<uint32_t>(k_desc), k_hi = static_cast<uint32_t>(k_desc >> 32), v_lo = static_cast<uint32_t>(v_desc), v_hi = static_cast<uint32_t>(v_desc >> 32);
         Turn<L::RING> k_turn, v_turn;                                            // tiles 2t and 2t + 1 of the ring
         v_turn.next();
         while (seg.next()) {
@@ -185,11 +189,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, k_turn.slot), k_turn.phase, ctl, kWaitMany + 1, kStatusTimeout);
                 tc_fence_after();
                 if (lane == 0) {
-                    const uint32_t q = base + L::Q + (PAIR ? w * L::TILE : 0), k = base + k_turn.slot * L::TILE;
+                    // (addresses in units of 16 bytes; the tiles end well below what the field holds)
+                    const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_turn.slot * (L::TILE / 16), s_at = tmem + w * kTok;
 #pragma unroll
                     for (int i = 0; i < DP / 16; ++i) {
-                        const uint32_t off = (i / 4) * L::PANEL + (i % 4) * 32;
-                        mma_f16_ss(tmem + w * kTok, make_kmajor_sw128_desc(q + off), make_kmajor_sw128_desc(k + off), kQk, i > 0);
+                        const uint32_t off = ((i / 4) * L::PANEL + (i % 4) * 32) / 16;
+                        mma_f16_ss(s_at, q + off, k_hi, k + off, k_hi, kQk, i > 0);
                     }
                     tc_commit(bar(S_FULL, w));
                     if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, k_turn.slot));
@@ -208,10 +213,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 ++jobs_of[w];
                 tc_fence_after();
                 if (lane == 0) {
-                    const uint32_t v = base + v_turn.slot * L::TILE;
+                    const uint32_t v = v_lo + v_turn.slot * (L::TILE / 16), o_at = tmem + L::O + w * DP, p_at = tmem + w * kTok;
 #pragma unroll
-                    for (int i = 0; i < kTok / 16; ++i)
-                        mma_f16_ts(tmem + L::O + w * DP, tmem + w * kTok + 8 * i, make_mnmajor_sw128_desc(v + i * 16 * 128, L::PANEL), kPv, n >= 2 || i > 0);
+                    for (int i = 0; i < kTok / 16; ++i) mma_f16_ts(o_at, p_at + 8 * i, v + i * 16 * 128 / 16, v_hi, kPv, n >= 2 || i > 0);
                     tc_commit(bar(O_DONE, w));
                     if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, v_turn.slot));
                 }
@@ -338,197 +342,210 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             for (uint32_t last = units > kRaw ? units - kRaw : 0; last < units; ++last) mbar_drain(bar(RAW_FULL, last % kRaw), last / kRaw & 1, a.limit_ns);
         }
     } else if (warp >= kConvertWarp) {
-        // ---- codes to fp16 tiles
+        // ---- codes to fp16 tiles: a thread has a chunk of 16 bytes of every PASS-th token (PASS is a multiple of 8, so that its chunks are swizzled alike)
         const int me = threadIdx.x - 32 * kConvertWarp, chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
         static_assert(FMT == KV_CACHE_INT8 || L::CODES == kMxBlock, "a chunk is a block");
+        static_assert(L::PASS % 8 == 0, "");
         int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
-        uint8_t* const v_scales = smem + L::OF_V;                                // [tile % 2]
+        uint8_t* const v_scales = smem + L::OF_V;                                // [tile % 2][token]: int8: the values' scales, 4-bit: their four bytes
+        uint16_t* const k_muls = reinterpret_cast<uint16_t*>(smem + L::OF_K);    // 4-bit: [tile % 2][token][block]
+        const uint32_t raw_from = base + L::RAW + L::raw_place(tok, chunk * 16);
+        uint32_t to[L::CODES / 8];
+#pragma unroll
+        for (int j = 0; j < L::CODES / 8; ++j) to[j] = base + place(tok, chunk * L::CODES + 8 * j);
         Turn<kRaw> raw;
         Turn<L::RING> ring;
-        uint32_t t = 0;                                                          // tiles so far
+        uint32_t t = 0, segments = 0;                                            // tiles and segments so far
         while (seg.next()) {
             int sigma = -126;                                                    // the values' reference starts anew with each segment
+            mbar_wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
+            ++segments;
+            const float factor = reinterpret_cast<const volatile float*>(smem + L::FACTOR)[0];
             for (int left = seg.tiles; left > 0; --left, ++t) {
                 const uint32_t slot = t & (kSlots - 1);
-                // keys
                 mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
-                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
-                int top_sigma = -126, nan_any = 0;
-                {
-                    const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
+                // scales: a thread a token
+                int word = -126 * 4;                                             // this warp's: the largest exponent of a value's scale, and what is special
+                if (me < kTok) {
                     const uint8_t* const rest = smem + L::MORE + raw.slot * L::MORE_BYTES;
-                    const uint32_t tile = base + ring.slot * L::TILE;
-#pragma unroll 2
-                    for (int r = tok; r < kTok; r += L::PASS) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w}, flag = rest[L::FLAGS + r];
-                        const bool in = flag != 0;
-                        // v_scales keeps for the values' turn: int8: the scale, 4-bit: the byte of this chunk's block; NaN and unseen ones as 0 (finite is what matters)
-                        if (FMT == KV_CACHE_INT8) {
-                            uint32_t f[8];
+                    const uint32_t flag = rest[L::FLAGS + me];
+                    const bool in = flag != 0;
+                    int top_sigma = -126;
+                    bool nan = false;
+                    float k_factor;
+                    if (FMT == KV_CACHE_INT8) {
+                        const uint32_t vs = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[me];
+                        k_factor = reinterpret_cast<const float*>(rest)[me];
+                        nan = in && (vs & 0x7f800000u) == 0x7f800000u;
+                        if (in && !nan) top_sigma = static_cast<int>(vs >> 23) - 126;               // s < 2^this
+                        nans[slot * kTok + me] = nan ? 0xff : 0;
+                        reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + me] = in && !nan ? vs : 0u;     // (finite is what matters)
+                    } else {
+                        const uint32_t* const its = reinterpret_cast<const uint32_t*>(rest) + 2 * me;
+                        const uint32_t shift = 8 * (flag & 3), there = blocks == 4 ? ~0u : (1u << (8 * blocks)) - 1;
+                        const uint32_t kb = __funnelshift_r(its[0], its[1], shift) & there, vb = __funnelshift_r(its[kTok * 2], its[kTok * 2 + 1], shift) & there;
+                        const uint32_t k_nan = __vcmpeq4(kb, ~0u), v_nan = __vcmpeq4(vb, ~0u);
+                        uint32_t top = __vmaxu4(kb, kb >> 16), v_top = vb & ~v_nan;
+                        top = k_nan != 0 ? 255u : max(top & 0xffu, top >> 8 & 0xffu);
+                        v_top = __vmaxu4(v_top, v_top >> 16);
+                        nan = in && v_nan != 0;
+                        if (in) top_sigma = max(-126, static_cast<int>(max(v_top & 0xffu, v_top >> 8 & 0xffu)) - 127);
+                        // 2^12 * 2^(byte - top): exact beside the codes, and the token's factor makes up for it
+                        uint32_t m[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
-                            store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
-                            store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
-                            const uint32_t vs = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[r];
-                            const bool nan = (vs & 0x7f800000u) == 0x7f800000u && in;
-                            if (chunk == 0) {
-                                factors[slot * kTok + r] = in ? reinterpret_cast<const float*>(rest)[r] : -1.f;
-                                nans[slot * kTok + r] = nan ? 0xff : 0;
-                                reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + r] = in && !nan ? vs : 0u;
-                            }
-                            nan_any |= nan;
-                            if (in && !nan) top_sigma = max(top_sigma, static_cast<int>(vs >> 23) - 126);         // s < 2^this
-                        } else {
-                            const uint8_t* const its = rest + r * 8 + (flag & 3) + chunk;
-                            const uint32_t ksc = in && chunk < blocks ? its[0] : 0u, vs = in && chunk < blocks ? its[L::V_SCALES] : 0u;
-                            // the token's largest byte: of the lanes that hold its chunks
-                            const bool nan = ksc == 255u;
-                            uint32_t top = nan ? 0u : ksc, bad = (nan ? 256u : 0u) | (vs == 255u ? 1u << chunk : 0u);
-#pragma unroll
-                            for (int o = 1; o < L::CHUNKS; o <<= 1) {
-                                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                                bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-                            }
-                            const int e = 27 + static_cast<int>(ksc) - static_cast<int>(top);
-                            const uint32_t mul = nan || e <= 0 ? 0u : static_cast<uint32_t>(e) * 0x04000400u;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t f[4];
-                                e2m1_to_f16(w[j], f);
-                                store_16(tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
-                            }
-                            if (chunk == 0) {
-                                factors[slot * kTok + r] = !in ? -1.f : bad >= 256u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
-                                nans[slot * kTok + r] = static_cast<uint8_t>(bad);
-                            }
-                            v_scales[(t & 1) * kTok * 4 + r * 4 + chunk] = vs == 255u ? 0 : static_cast<uint8_t>(vs);
-                            nan_any |= (bad & 255u) != 0;
-                            if (in && chunk < blocks && vs != 255u) top_sigma = max(top_sigma, static_cast<int>(vs) - 127);
-                        }
+                        for (int j = 0; j < 4; ++j) m[j] = static_cast<uint32_t>(max(27 + static_cast<int>(kb >> (8 * j) & 0xffu) - static_cast<int>(top), 0)) << 10;
+                        *reinterpret_cast<uint2*>(k_muls + ((t & 1) * kTok + me) * 4) = make_uint2(m[0] | m[1] << 16, m[2] | m[3] << 16);
+                        k_factor = top == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
+                        nans[slot * kTok + me] = static_cast<uint8_t>((v_nan & 1u) | (v_nan >> 7 & 2u) | (v_nan >> 14 & 4u) | (v_nan >> 21 & 8u));
+                        reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + me] = vb & ~v_nan;
                     }
+                    k_factor *= factor;
+                    factors[slot * kTok + me] = in ? k_factor : -1.f;
+                    word = __reduce_max_sync(0xffffffffu, top_sigma) * 4 + (__any_sync(0xffffffffu, nan) ? 1 : 0) + (__any_sync(0xffffffffu, !in) ? 2 : 0);
                 }
-                // the largest scale of values so far (an exponent of fp32)
-                const int warp_top = __reduce_max_sync(0xffffffffu, top_sigma), warp_nan = __any_sync(0xffffffffu, nan_any);
-                if (lane == 0) of_warp[(t & 1) * 8 + warp - kConvertWarp] = warp_top * 2 + (warp_nan ? 1 : 0);
+                if (lane == 0) of_warp[(t & 1) * 8 + warp - kConvertWarp] = word;
                 named_sync(1, kConverters);
-                int nan_of_all = 0;
+                int all = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int its = of_warp[(t & 1) * 8 + i];
-                    sigma = max(sigma, its >> 1);
-                    nan_of_all |= its & 1;
+                    sigma = max(sigma, its >> 2);                                // the largest scale of values so far (an exponent of fp32)
+                    all |= its & 3;
                 }
                 if (me == 0) {
                     sigmas[slot] = sigma;
-                    any_nan[slot] = nan_of_all;
+                    special[slot] = all;
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(TILE_FULL, ring.slot));
-                    mbar_arrive(bar(RAW_EMPTY, raw.slot));
-                }
-                raw.next();
-                ring.next();
-                // values: times their scale over 2^sigma, brought to 2^15 at most
-                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                // keys
                 mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
-                {
-                    const uint8_t* const from = smem + L::RAW + raw.slot * kTok * L::ROW;
-                    const uint32_t tile = base + ring.slot * L::TILE;
-                    // (int8: two factors, as 2^(8 - sigma) alone may be more than fp32 holds)
-                    const float by0 = __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23), by1 = __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23);
+                auto convert = [&](auto multiplier) {                            // of a token: two equal halves, or none (0)
+                    const uint32_t from = raw_from + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
 #pragma unroll 2
-                    for (int r = tok; r < kTok; r += L::PASS) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(from + L::raw_place(r, chunk * 16));
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    for (int i = 0; i < kTok / L::PASS; ++i) {
+                        uint32_t w[4];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from + i * L::PASS * L::ROW) : "memory");
+                        const uint32_t mul = multiplier(tok + i * L::PASS), at = tile + i * L::PASS * 128;
                         if (FMT == KV_CACHE_INT8) {
-                            const float by = reinterpret_cast<const float*>(v_scales)[(t & 1) * kTok + r] * by0 * by1;
-                            const uint32_t mul = pack_f16(by, by);
                             uint32_t f[8];
 #pragma unroll
                             for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+                            if (mul != 0x3c003c00u) {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
-                            store_16(tile + place(r, chunk * 16), f[0], f[1], f[2], f[3]);
-                            store_16(tile + place(r, chunk * 16 + 8), f[4], f[5], f[6], f[7]);
+                                for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
+                            }
+                            store_16(to[0] + at, f[0], f[1], f[2], f[3]);
+                            store_16(to[1] + at, f[4], f[5], f[6], f[7]);
                         } else {
-                            // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
-                            const int byte = v_scales[(t & 1) * kTok * 4 + r * 4 + chunk], e = 27 + byte - 127 - sigma;
-                            const uint32_t bits = e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31), mul = bits * 0x00010001u;
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 uint32_t f[4];
                                 e2m1_to_f16(w[j], f);
-                                store_16(tile + place(r, chunk * 32 + 8 * j), mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
+                                store_16(to[j] + at, mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
                             }
                         }
                     }
+                };
+                auto pass_on = [&] {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(TILE_FULL, ring.slot));
+                        mbar_arrive(bar(RAW_EMPTY, raw.slot));
+                    }
+                    raw.next();
+                    ring.next();
+                };
+                if constexpr (FMT == KV_CACHE_INT8) convert([](int) { return 0x3c003c00u; });
+                else convert([&](int r) { return k_muls[((t & 1) * kTok + r) * 4 + chunk] * 0x00010001u; });
+                pass_on();
+                // values: times their scale over 2^sigma, brought to 2^15 at most
+                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                if constexpr (FMT == KV_CACHE_INT8) {
+                    // (two factors, as 2^(8 - sigma) alone may be more than fp32 holds)
+                    const float by0 = __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23), by1 = __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23);
+                    convert([&](int r) {
+                        const float by = reinterpret_cast<const float*>(v_scales)[(t & 1) * kTok + r] * by0 * by1;
+                        return pack_f16(by, by);
+                    });
+                } else {
+                    convert([&](int r) {                                         // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
+                        const int e = 27 + static_cast<int>(v_scales[(t & 1) * kTok * 4 + r * 4 + chunk]) - 127 - sigma;
+                        return (e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31)) * 0x00010001u;
+                    });
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(TILE_FULL, ring.slot));
-                    mbar_arrive(bar(RAW_EMPTY, raw.slot));
-                }
-                raw.next();
-                ring.next();
+                pass_on();
             }
         }
     } else {
-        // ---- softmax: a thread a row
+        // ---- softmax: a thread a row. Scores times their tokens' factors are powers of two.
         const int w = warp >> 2, row = threadIdx.x & (kRows - 1);
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16, s_tmem = tmem + lanes + w * kTok, o_tmem = tmem + lanes + L::O + w * DP;
         float* const state = reinterpret_cast<float*>(smem + L::STATE);          // [warpgroup][row]: references of o and of the sum, the sum, NaN blocks
-        float* const row_factor = reinterpret_cast<float*>(smem + L::ROW_FACTOR);
+        volatile float* const of_segment = reinterpret_cast<volatile float*>(smem + L::FACTOR);         // the scores' factor, [8 + warp]: the queries' maxima
         uint32_t tile_base = 0, jobs = 0;                                        // jobs of this warpgroup so far
         while (seg.next()) {
             const int r = (PAIR ? w * kRows : 0) + row;                          // of the item's rows
             const bool live = r < seg.rows, warp_live = (PAIR ? w * kRows : 0) + 32 * (warp & 3) < seg.rows;
             const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group;
-            // queries: a power of two brings a row's largest magnitude to [2^14, 2^15). DP / 8 lanes a row, several rows on their way at once.
+            // queries: a power of two brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes a row, several rows on their way at once.
             {
-                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8, BATCH = 4;
+                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8, BATCH = 8;
                 const int d = lane % LANES * 8;
-#pragma unroll 1
-                for (int first = 0; first < PER_WARP; first += BATCH * AT_ONCE) {
-                    uint4 x[BATCH];
+                uint4 x[BATCH];
+                auto load = [&](int begin) {
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        const int q_row = warp * PER_WARP + first + i * AT_ONCE + lane / LANES;
+                        const int q_row = warp * PER_WARP + begin + i * AT_ONCE + lane / LANES;
                         x[i] = make_uint4(0, 0, 0, 0);
-                        if (q_row < seg.rows && d < a.dim) {
+                        if (begin + i * AT_ONCE < PER_WARP && q_row < seg.rows && d < a.dim) {
                             const int its = (seg.row0 + q_row) / a.group, its_head = seg.head * a.group + (seg.row0 + q_row) - its * a.group;
                             x[i] = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d);
                         }
                     }
+                };
+                uint32_t top = 0;
+#pragma unroll 1
+                for (int begin = 0; begin < PER_WARP; begin += BATCH * AT_ONCE) {
+                    load(begin);
+                    // (a row with an Inf or a NaN does not set the power of the others)
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        const int q_row = warp * PER_WARP + first + i * AT_ONCE + lane / LANES;
-                        uint32_t top = absmax_bits8(x[i]);
+                        const uint32_t its = absmax_bits8(x[i]);
+                        top = max(top, its < 0x7f800000u ? its : 0u);
+                    }
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) of_segment[8 + warp] = __uint_as_float(top);
+                named_sync(2, kSoftmax);
 #pragma unroll
-                        for (int o = 1; o < LANES; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const int field = static_cast<int>(top >> 23), up = field == 255 ? 0 : min(126, max(-126, 141 - max(field, 1)));
-                        const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
+                for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(of_segment[8 + i]));
+                const int field = static_cast<int>(top >> 23), up = min(126, max(-126, 141 - max(field, 1)));
+                const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
+                if (threadIdx.x == 0) of_segment[0] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f), 1e-38f);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(FACTOR_FULL, 0));
+#pragma unroll 1
+                for (int begin = 0; begin < PER_WARP; begin += BATCH * AT_ONCE) {
+                    if (PER_WARP > BATCH * AT_ONCE) load(begin);
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        if (begin + i * AT_ONCE >= PER_WARP) break;
+                        const int q_row = warp * PER_WARP + begin + i * AT_ONCE + lane / LANES;
                         float f[8];
                         unpack_bf16x8(x[i], f);
                         store_16(base + L::Q + (q_row / kRows) * L::TILE + place(q_row % kRows, d), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul),
                                  pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
-                        if (d == 0) row_factor[q_row] = fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f);
                     }
                 }
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(Q_FULL, 0));
-            named_sync(2, kSoftmax);
-            const float factor = fmaxf(row_factor[r], 1e-38f);                   // (not 0: -inf times it is -inf)
             float m = kNone;
             uint64_t l2 = 0;
             int sigma = -126;
             uint32_t poison = 0;                                                 // blocks of this row's output that are NaN
-            const uint64_t f2 = pack2(factor, factor);
             bool first = true;
 #pragma unroll 1
             for (int t = PAIR ? 0 : w; t < seg.tiles; t += PAIR ? 1 : 2, ++jobs) {
@@ -544,7 +561,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         if (j0 + 32 * ch + 31 >= 0) sees &= sees32(a, seg.s.begin + node, node, j0 + 32 * ch);
                         return sees;
                     };
-                    if (any_nan[slot] != 0) {
+                    const int its_special = special[slot];
+                    if ((its_special & 1) != 0) {
 #pragma unroll 1
                         for (int ch = 0; ch < 4; ++ch) {
                             const uint32_t sees = sees32_of(ch);
@@ -554,8 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         }
                     }
                     // tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places
-                    const float4 flags = *reinterpret_cast<const float4*>(kf + 4 * lane);
-                    if (j0 + kTok > 0 || __any_sync(0xffffffffu, flags.x == -1.f || flags.y == -1.f || flags.z == -1.f || flags.w == -1.f)) {
+                    if (j0 + kTok > 0 || (its_special & 2) != 0) {
 #pragma unroll 1
                         for (int ch = 0; ch < 8; ++ch) {
                             uint32_t v[16];
@@ -593,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         }
                         tmem_wait_ld();
                     }
-                    top = top == -INFINITY ? kNone : top * factor;
+                    top = fmaxf(top, kNone);
                     // references move when a weight would pass 2^15, to put it at 2^7, or when the values' does
                     const int its_sigma = sigmas[slot];
                     if (__any_sync(0xffffffffu, top > m + 15.f || its_sigma != sigma)) {
@@ -635,12 +652,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 for (int i = 0; i < 16; i += 4) {
                                     const float4 k = *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
                                     float y, z;
-                                    unpack2(fma2(mul2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y)), f2, m2), y, z);
+                                    unpack2(fma2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y), m2), y, z);
                                     y = ex2(y);
                                     z = ex2(z);
                                     sum[0] = add2(sum[0], pack2(y, z));
                                     p[i / 2] = pack_f16(y, z);
-                                    unpack2(fma2(mul2(pack2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), pack2(k.z, k.w)), f2, m2), y, z);
+                                    unpack2(fma2(pack2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), pack2(k.z, k.w), m2), y, z);
                                     y = ex2(y);
                                     z = ex2(z);
                                     sum[1] = add2(sum[1], pack2(y, z));
