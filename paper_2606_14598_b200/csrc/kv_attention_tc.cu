@@ -12,6 +12,7 @@
 #include "kv_attention.cuh"
 
 #include <cmath>
+#include <type_traits>
 
 namespace w8a8 {
 namespace attention {
@@ -174,60 +175,73 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     Segments<ROWS> seg(a, share);
 
     if (warp == kMmaWarp) {
-        // ---- products. A job is a tile of tokens for one of the two softmax warpgroups: every other tile, or (PAIR) each tile for both.
-        uint32_t segments = 0, jobs_of[2] = {0, 0};
-        constexpr uint32_t kQk = make_f16_idesc(kRows, kTok, false), kPv = make_f16_idesc(kRows, DP, true);
-        const uint64_t k_desc = make_kmajor_sw128_desc(base), v_desc = make_mnmajor_sw128_desc(base, L::PANEL);
-        const uint32_t k_lo = static_cast<uint32_t>(k_desc), k_hi = static_cast<uint32_t>(k_desc >> 32), v_lo = static_cast<uint32_t>(v_desc), v_hi = static_cast<uint32_t>(v_desc >> 32);
-        Turn<L::RING> k_turn, v_turn;                                            // tiles 2t and 2t + 1 of the ring
-        v_turn.next();
-        while (seg.next()) {
-            const int jobs = PAIR ? 2 * seg.tiles : seg.tiles;
-            mbar_wait(bar(Q_FULL, 0), segments & 1, ctl, kWaitMany, kStatusTimeout);
-            auto scores = [&](int n) {
-                const uint32_t w = n & 1;
-                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, k_turn.slot), k_turn.phase, ctl, kWaitMany + 1, kStatusTimeout);
-                tc_fence_after();
-                if (lane == 0) {
-                    // (addresses in units of 16 bytes; the tiles end well below what the field holds)
-                    const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_turn.slot * (L::TILE / 16), s_at = tmem + w * kTok;
-#pragma unroll
-                    for (int i = 0; i < DP / 16; ++i) {
-                        const uint32_t off = ((i / 4) * L::PANEL + (i % 4) * 32) / 16;
-                        mma_f16_ss(s_at, q + off, k_hi, k + off, k_hi, kQk, i > 0);
-                    }
-                    tc_commit(bar(S_FULL, w));
-                    if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, k_turn.slot));
-                }
-                __syncwarp();
-                if (!PAIR || w == 1) {
-                    k_turn.next();
-                    k_turn.next();
+        // ---- products. A job is a tile of tokens for one of the two softmax warpgroups: every other tile, or (PAIR) each tile for both. One thread, and as few
+        // instructions between products as can be: the queue in front of the matrix unit is short, so that it stands still meanwhile.
+        if (lane == 0) {
+            constexpr uint32_t kQk = make_f16_idesc(kRows, kTok, false), kPv = make_f16_idesc(kRows, DP, true);
+            const uint64_t k_desc = make_kmajor_sw128_desc(base), v_desc = make_mnmajor_sw128_desc(base, L::PANEL);
+            const uint32_t k_lo = static_cast<uint32_t>(k_desc), k_hi = static_cast<uint32_t>(k_desc >> 32), v_lo = static_cast<uint32_t>(v_desc), v_hi = static_cast<uint32_t>(v_desc >> 32);
+            uint32_t segments = 0, k_slot = 0, k_phase = 0, v_slot = 1, v_phase = 0, p_phase[2] = {0, 0};
+            auto two_on = [](uint32_t& slot, uint32_t& phase) {                  // to the next tile's keys, or values
+                slot += 2;
+                if (slot >= L::RING) {
+                    slot -= L::RING;
+                    phase ^= 1;
                 }
             };
-            for (int n = 0; n < min(2, jobs); ++n) scores(n);
-            for (int n = 0; n < jobs; ++n) {
-                const uint32_t w = n & 1;
-                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, v_turn.slot), v_turn.phase, ctl, kWaitMany + 2, kStatusTimeout);
-                mbar_wait(bar(P_FULL, w), jobs_of[w] & 1, ctl, kWaitMany + 3, kStatusTimeout);
-                ++jobs_of[w];
-                tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t v = v_lo + v_turn.slot * (L::TILE / 16), o_at = tmem + L::O + w * DP, p_at = tmem + w * kTok;
+            // (addresses in units of 16 bytes; the tiles end well below what the field holds)
+            auto scores = [&](auto which) {
+                constexpr uint32_t w = decltype(which)::value;
+                if (!PAIR || w == 0) {
+                    mbar_wait(bar(TILE_FULL, k_slot), k_phase, ctl, kWaitMany + 1, kStatusTimeout);
+                    tc_fence_after();
+                }
+                const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_slot * (L::TILE / 16);
 #pragma unroll
-                    for (int i = 0; i < kTok / 16; ++i) mma_f16_ts(o_at, p_at + 8 * i, v + i * 16 * 128 / 16, v_hi, kPv, n >= 2 || i > 0);
-                    tc_commit(bar(O_DONE, w));
-                    if (!PAIR || w == 1) tc_commit(bar(TILE_EMPTY, v_turn.slot));
+                for (int i = 0; i < DP / 16; ++i) {
+                    const uint32_t off = ((i / 4) * L::PANEL + (i % 4) * 32) / 16;
+                    mma_f16_ss(tmem + w * kTok, q + off, k_hi, k + off, k_hi, kQk, i > 0);
                 }
-                __syncwarp();
+                tc_commit(bar(S_FULL, w));
                 if (!PAIR || w == 1) {
-                    v_turn.next();
-                    v_turn.next();
+                    tc_commit(bar(TILE_EMPTY, k_slot));
+                    two_on(k_slot, k_phase);
                 }
-                if (n + 2 < jobs) scores(n + 2);
+            };
+            auto values = [&](auto which, bool first) {
+                constexpr uint32_t w = decltype(which)::value;
+                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, v_slot), v_phase, ctl, kWaitMany + 2, kStatusTimeout);
+                mbar_wait(bar(P_FULL, w), p_phase[w], ctl, kWaitMany + 3, kStatusTimeout);
+                p_phase[w] ^= 1;
+                tc_fence_after();
+                const uint32_t v = v_lo + v_slot * (L::TILE / 16);
+#pragma unroll
+                for (int i = 0; i < kTok / 16; ++i) mma_f16_ts(tmem + L::O + w * DP, tmem + w * kTok + 8 * i, v + i * 16 * 128 / 16, v_hi, kPv, !first || i > 0);
+                tc_commit(bar(O_DONE, w));
+                if (!PAIR || w == 1) {
+                    tc_commit(bar(TILE_EMPTY, v_slot));
+                    two_on(v_slot, v_phase);
+                }
+            };
+            const std::integral_constant<uint32_t, 0> zero{};
+            const std::integral_constant<uint32_t, 1> one{};
+            while (seg.next()) {
+                const int jobs = PAIR ? 2 * seg.tiles : seg.tiles;
+                mbar_wait(bar(Q_FULL, 0), segments & 1, ctl, kWaitMany, kStatusTimeout);
+                ++segments;
+                scores(zero);
+                if (jobs > 1) scores(one);
+#pragma unroll 1
+                for (int n = 0; n < jobs; n += 2) {
+                    values(zero, n == 0);
+                    if (n + 2 < jobs) scores(zero);
+                    if (n + 1 == jobs) break;
+                    values(one, n == 0);
+                    if (n + 3 < jobs) scores(one);
+                }
             }
-            ++segments;
         }
+        __syncwarp();
         if (lane == 0) tc_commit(bar(DRAINED, 0));                               // (whatever became of the waits, no product is left when the CTA goes)
         mbar_drain(bar(DRAINED, 0), 0, a.limit_ns);
     } else if (warp >= kLoadWarp) {
