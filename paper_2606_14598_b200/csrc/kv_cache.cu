@@ -48,23 +48,6 @@ Cover make_cover(int lanes) {
     return c;
 }
 
-// amax / 127 and its reciprocal without a division (Markstein's theorem, as in quant_math.cuh): 1 / 127 correctly rounded, a
-// faithful quotient and its exact remainder give the correctly rounded quotient. Scales near the ends of the range, where a
-// remainder could underflow, take the division.
-__device__ __forceinline__ RowScale head_scale(float amax) {
-    if (amax < 1e-25f || amax > 1e25f) return make_row_scale(amax);
-    const float inv127 = 1.0f / 127.0f;
-    const float q = __fmul_rn(amax, inv127);
-    const float s = __fmaf_rn(__fmaf_rn(-127.0f, q, amax), inv127, q);
-    return RowScale{s, __frcp_rn(s), true};
-}
-// What quant8 needs of a scale; the low part of the reciprocal to 2^-40 of it (by a multiplication: its own error is 2^-24 of 2^-16)
-__device__ __forceinline__ RowScale2 head_scale2(const RowScale& rs) {
-    const float inv_hi = __uint_as_float(__float_as_uint(rs.inv) & 0xffffff00u);
-    const float inv_lo = rs.fast ? __fmul_rn(__fmaf_rn(-rs.s, inv_hi, 1.0f), rs.inv) : 0.f;
-    return RowScale2{pack2(-rs.s, -rs.s), pack2(rs.inv, rs.inv), pack2(MAGIC, MAGIC), pack2(inv_hi, inv_hi), pack2(inv_lo, inv_lo)};
-}
-
 // A unit is what shares a scale: a head of a token (int8) or a block of 32 of it (MXFP4); 2^lane_shift lanes, E elements each. 16
 // elements a lane, loaded as 32 bytes, where sizes, strides and addresses allow it: what a unit costs beside its elements (its
 // maximum, scale and places) is then shared by twice as many; else 8. Keys and values of UNROLL tokens are in flight at once.

@@ -93,20 +93,22 @@ __device__ __forceinline__ void reduce_row(float& squares, uint32_t& top, float2
 
 struct RowNorm {
     RowScale c;          // what the codes are divided by
+    RowScale2 c2;
     float r, s;          // the norm's factor, the row's scale
     bool fine;           // finite
 };
 __device__ __forceinline__ RowNorm row_norm(float squares, uint32_t top, int K, float eps) {
     RowNorm n;
     n.fine = top < 0x7f800000u && squares < INFINITY;
-    n.c = make_row_scale(n.fine ? __uint_as_float(top) : 0.f);
+    n.c = head_scale(n.fine ? __uint_as_float(top) : 0.f);
+    n.c2 = head_scale2(n.c);
     n.r = n.fine ? __frsqrt_rn(__fadd_rn(__fdiv_rn(squares, static_cast<float>(K)), eps)) : __uint_as_float(0x7fc00000u);
     n.s = !n.fine ? n.r : top == 0u ? 1.f : __fmul_rn(n.c.s, n.r);
     return n;
 }
 __device__ __forceinline__ void write8(const NormArgs& a, int64_t row, int k, const float (&u)[8], const RowNorm& n) {
     if (a.qa != nullptr) {
-        const uint2 c = n.fine ? make_uint2(quant4(u[0], u[1], u[2], u[3], n.c), quant4(u[4], u[5], u[6], u[7], n.c)) : make_uint2(0, 0);
+        const uint2 c = n.fine ? make_uint2(quant4f(u[0], u[1], u[2], u[3], n.c, n.c2), quant4f(u[4], u[5], u[6], u[7], n.c, n.c2)) : make_uint2(0, 0);
         *reinterpret_cast<uint2*>(a.qa + row * a.K + k) = c;
     }
     if (a.y != nullptr)

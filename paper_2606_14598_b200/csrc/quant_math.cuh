@@ -88,10 +88,37 @@ __device__ __forceinline__ uint64_t quant2(uint32_t w, const RowScale2& r2) {
     const uint64_t q2 = fma2(r1, r2.inv, q1);
     return add2(q2, r2.magic);
 }
+// Codes of two fp32 values in byte 0 and byte 4: the sequence of quant1 on a pair.
+__device__ __forceinline__ uint64_t quant2f(uint64_t x, const RowScale2& r2) {
+    const uint64_t q0 = mul2(x, r2.inv);
+    const uint64_t q1 = fma2(fma2(r2.neg_s, q0, x), r2.inv, q0);
+    const uint64_t q2 = fma2(fma2(r2.neg_s, q1, x), r2.inv, q1);
+    return add2(q2, r2.magic);
+}
 __device__ __forceinline__ uint32_t gather4(uint64_t a, uint64_t b) {   // bytes 0 and 4 of a, then of b
     const uint32_t lo = __byte_perm(static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32), 0x0040);
     const uint32_t hi = __byte_perm(static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32), 0x0040);
     return __byte_perm(lo, hi, 0x5410);
+}
+// Four fp32 values -> four codes
+__device__ __forceinline__ uint32_t quant4f(float a, float b, float c, float d, const RowScale& rs, const RowScale2& r2) {
+    if (rs.fast) return gather4(quant2f(pack2(a, b), r2), quant2f(pack2(c, d), r2));
+    return quant4(a, b, c, d, rs);
+}
+// amax / 127 and its reciprocal without a division (Markstein's theorem, as above): 1 / 127 correctly rounded, a faithful quotient and its exact
+// remainder give the correctly rounded quotient. Scales near the ends of the range, where a remainder could underflow, take the division.
+__device__ __forceinline__ RowScale head_scale(float amax) {
+    if (amax < 1e-25f || amax > 1e25f) return make_row_scale(amax);
+    const float inv127 = 1.0f / 127.0f;
+    const float q = __fmul_rn(amax, inv127);
+    const float s = __fmaf_rn(__fmaf_rn(-127.0f, q, amax), inv127, q);
+    return RowScale{s, __frcp_rn(s), true};
+}
+// What quant8 needs of a scale; the low part of the reciprocal to 2^-40 of it (by a multiplication: its own error is 2^-24 of 2^-16)
+__device__ __forceinline__ RowScale2 head_scale2(const RowScale& rs) {
+    const float inv_hi = __uint_as_float(__float_as_uint(rs.inv) & 0xffffff00u);
+    const float inv_lo = rs.fast ? __fmul_rn(__fmaf_rn(-rs.s, inv_hi, 1.0f), rs.inv) : 0.f;
+    return RowScale2{pack2(-rs.s, -rs.s), pack2(rs.inv, rs.inv), pack2(MAGIC, MAGIC), pack2(inv_hi, inv_hi), pack2(inv_lo, inv_lo)};
 }
 // 8 packed bf16 -> 8 int8 codes (bf16 -> fp32 is exact: the 16 bits become the high half of the word)
 __device__ __forceinline__ uint2 quant8(const uint4& v, const RowScale& rs, const RowScale2& r2) {
