@@ -60,6 +60,11 @@ __device__ __forceinline__ Sequence read_sequence(const AttentionArgs& a, int b,
 }
 __device__ __forceinline__ int64_t units_of(const AttentionArgs& a, const Sequence& s) { return static_cast<int64_t>(a.heads) * s.row_tiles * s.tiles; }
 
+// a / b of what is not negative: in 32 bits where it fits (a division of 64 bits takes several times as long, and a CTA begins with a few)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
 struct Share {
     int64_t total, first_of_b;                  // units of all sequences; of those before b
     int64_t ctas;                               // CTAs that work: none without a unit
@@ -93,7 +98,7 @@ __device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_t
         if (w < static_cast<int>(threadIdx.x >> 5)) before += of_warp[w];
         total += of_warp[w];
     }
-    const int64_t ctas = min(total, static_cast<int64_t>(gridDim.x)), u = blockIdx.x < ctas ? total * blockIdx.x / ctas : total;
+    const int64_t ctas = min(total, static_cast<int64_t>(gridDim.x)), u = blockIdx.x < ctas ? quotient(total * blockIdx.x, ctas) : total;
     if (u >= before && u < before + mine) {
         for (int b = b0; b < b1; ++b) {
             const int64_t units = units_of(a, read_sequence<TILE>(a, b, rows_of_tile));
@@ -106,11 +111,11 @@ __device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_t
         }
     }
     __syncthreads();
-    return Share{total, found < a.seqs ? first_unit : 0, ctas, u, blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : u, found};
+    return Share{total, found < a.seqs ? first_unit : 0, ctas, u, blockIdx.x < ctas ? quotient(total * (blockIdx.x + 1), ctas) : u, found};
 }
 
 // The CTA whose range holds unit u (CTA c takes units total * c / ctas up to total * (c + 1) / ctas)
-__device__ __forceinline__ int owner(int64_t u, const Share& s) { return static_cast<int>(((u + 1) * s.ctas - 1) / s.total); }
+__device__ __forceinline__ int owner(int64_t u, const Share& s) { return static_cast<int>(quotient((u + 1) * s.ctas - 1, s.total)); }
 
 // ------------------------------------------------------------------------------------------------ small pieces
 

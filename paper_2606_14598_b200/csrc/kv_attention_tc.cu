@@ -20,28 +20,29 @@ namespace {
 
 constexpr int kTok = 128;                       // tokens of a tile
 constexpr int kRows = 128;                      // rows of a product
-constexpr int kConvertWarp = 8, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 20, kConverters = 256, kSoftmax = 256;
-constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 10 after it
+constexpr int kSoftmax = 256, kConverters = 128;            // threads that do the softmax; that turn keys, or values, to fp16
+constexpr int kKeyWarp = 8, kValueWarp = 12, kMmaWarp = 16, kLoadWarp = 17, kThreads = 32 * 19;
+constexpr int kWaitMany = 41;                   // which wait gave up, for the status word: this and the 11 after it
 constexpr int kSlots = 4;                       // tiles whose factors are kept
-constexpr int kRaw = 3;                         // tiles of codes on their way: a warp each, which loads every third one
 
 template <int FMT, int DP, bool PAIR>
 struct Plan {
     static constexpr int ROWS = PAIR ? 2 * kRows : kRows;
     static constexpr int PER_BYTE = FMT == KV_CACHE_INT8 ? 1 : 2, ROW = DP / PER_BYTE;     // bytes of a head, padded
     static constexpr int TILE = kTok * DP * 2, PANEL = kTok * 128;             // an fp16 tile of tokens or queries: panels of 64 elements (128 bytes) a row
-    // tiles of keys and values take turns in one ring: K0 V0 K1 V1 ...
-    static constexpr int RING = PAIR && DP == 128 ? 3 : 4;
-    static constexpr int Q = RING * TILE, RAW = Q + (PAIR ? 2 : 1) * TILE, MORE = RAW + kRaw * kTok * ROW;
+    // a ring of fp16 tiles of keys, one of values, and rings of their codes on their way
+    static constexpr int KEYS = 2, VALUES = DP == 128 ? 1 : 2, RAW_KEYS = FMT == KV_CACHE_INT8 ? 2 : 3, RAW_VALUES = RAW_KEYS - (PAIR && DP == 128 ? 1 : 0);
+    static constexpr int V_TILES = KEYS * TILE, Q = V_TILES + VALUES * TILE, RAW = Q + (PAIR ? 2 : 1) * TILE, RAW_V = RAW + RAW_KEYS * kTok * ROW;
+    static constexpr int MORE = RAW_V + RAW_VALUES * kTok * ROW;
     // with the codes of keys come the scales of keys and values (4-bit: the two words that hold a head's bytes) and a byte a token: 0x80 where it
     // may be seen, and (4-bit) where in the words its bytes begin
     static constexpr int WORDS = FMT == KV_CACHE_INT8 ? 1 : 2, V_SCALES = kTok * 4 * WORDS, FLAGS = 2 * V_SCALES, MORE_BYTES = FLAGS + kTok;
-    static constexpr int FACTORS = MORE + kRaw * MORE_BYTES;
+    static constexpr int FACTORS = MORE + RAW_KEYS * MORE_BYTES;
     static constexpr int ONES = FACTORS + kSlots * kTok * 4;                   // factors of scores that have theirs already
     static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
-    static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, OF_K = OF_V + 2 * kTok * 4;
+    static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 4 * 4, OF_K = OF_V + kSlots * kTok * 4;
     static constexpr int FACTOR = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 8);         // of the scores, and the queries' maxima of the warps
-    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 24 * 8 + 1024;
+    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 33 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
     // codes: a thread converts a chunk of 16 bytes of every PASS-th token
@@ -52,7 +53,10 @@ struct Plan {
         return r * ROW + (off ^ (turn << 4));
     }
 };
-enum Bar { TILE_FULL = 0, TILE_EMPTY = 4, RAW_FULL = 8, RAW_EMPTY = 11, S_FULL = 14, P_FULL = 16, O_DONE = 18, Q_FULL = 20, FACTOR_FULL = 21, DRAINED = 22 };
+enum Bar {
+    K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_EMPTY = 6, RAW_K_FULL = 8, RAW_K_EMPTY = 11, RAW_V_FULL = 14, RAW_V_EMPTY = 17,
+    S_FULL = 20, P_FULL = 22, O_DONE = 24, SCALES_FULL = 26, Q_FULL = 30, FACTOR_FULL = 31, DRAINED = 32
+};
 
 // A CTA's segments, one after another: (sequence, head, rows) and a run of its tiles. Every role walks them by itself.
 template <int ROWS>
@@ -74,7 +78,7 @@ struct Segments {
             s = read_sequence<kTok>(a, ++b, ROWS);
         }
         const int64_t of_b = u - first_of_b;
-        const int item = static_cast<int>(of_b / s.tiles);
+        const int item = static_cast<int>(quotient(of_b, s.tiles));
         tile0 = static_cast<int>(of_b - static_cast<int64_t>(item) * s.tiles);
         head = item / s.row_tiles;
         row0 = (item - head * s.row_tiles) * ROWS;
@@ -136,19 +140,22 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     if (threadIdx.x < kTok) reinterpret_cast<float*>(smem + L::ONES)[threadIdx.x] = 1.f;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int i = 0; i < L::RING; ++i) {
-            mbar_init(bar(TILE_FULL, i), 8);
-            mbar_init(bar(TILE_EMPTY, i), 1);
-        }
-        for (int i = 0; i < kRaw; ++i) {
-            mbar_init(bar(RAW_FULL, i), 64);
-            mbar_init(bar(RAW_EMPTY, i), 8);
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(bar(RAW_K_FULL, i), 64);
+            mbar_init(bar(RAW_K_EMPTY, i), 4);
+            mbar_init(bar(RAW_V_FULL, i), 64);
+            mbar_init(bar(RAW_V_EMPTY, i), 4);
         }
         for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(K_FULL, i), 4);
+            mbar_init(bar(K_EMPTY, i), 1);
+            mbar_init(bar(V_FULL, i), 4);
+            mbar_init(bar(V_EMPTY, i), 1);
             mbar_init(bar(S_FULL, i), 1);
             mbar_init(bar(P_FULL, i), 4);
             mbar_init(bar(O_DONE, i), 1);
         }
+        for (int i = 0; i < kSlots; ++i) mbar_init(bar(SCALES_FULL, i), 4);
         mbar_init(bar(Q_FULL, 0), 8);
         mbar_init(bar(FACTOR_FULL, 0), 8);
         mbar_init(bar(DRAINED, 0), 1);
@@ -156,12 +163,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     }
     const WaitCtl ctl{&abort_flag, a.status, a.sticky, a.limit_ns};
     grid_dep_wait();
-    const Share share = share_out<kThreads, kTok>(a, ROWS);
     // tensor memory is taken behind the wait for the kernel ahead (whose CTAs may still want theirs), and dependents are released behind that
     if (warp == kMmaWarp) {
         tmem_alloc(smem_u32(&tmem_slot), 512);
         tmem_relinquish();
     }
+    const Share share = share_out<kThreads, kTok>(a, ROWS);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -179,24 +186,19 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         // instructions between products as can be: the queue in front of the matrix unit is short, so that it stands still meanwhile.
         if (lane == 0) {
             constexpr uint32_t kQk = make_f16_idesc(kRows, kTok, false), kPv = make_f16_idesc(kRows, DP, true);
-            const uint64_t k_desc = make_kmajor_sw128_desc(base), v_desc = make_mnmajor_sw128_desc(base, L::PANEL);
+            const uint64_t k_desc = make_kmajor_sw128_desc(base), v_desc = make_mnmajor_sw128_desc(base + L::V_TILES, L::PANEL);
             const uint32_t k_lo = static_cast<uint32_t>(k_desc), k_hi = static_cast<uint32_t>(k_desc >> 32), v_lo = static_cast<uint32_t>(v_desc), v_hi = static_cast<uint32_t>(v_desc >> 32);
-            uint32_t segments = 0, k_slot = 0, k_phase = 0, v_slot = 1, v_phase = 0, p_phase[2] = {0, 0};
-            auto two_on = [](uint32_t& slot, uint32_t& phase) {                  // to the next tile's keys, or values
-                slot += 2;
-                if (slot >= L::RING) {
-                    slot -= L::RING;
-                    phase ^= 1;
-                }
-            };
+            uint32_t segments = 0, p_phase[2] = {0, 0};
+            Turn<L::KEYS> k_at;
+            Turn<L::VALUES> v_at;
             // (addresses in units of 16 bytes; the tiles end well below what the field holds)
             auto scores = [&](auto which) {
                 constexpr uint32_t w = decltype(which)::value;
                 if (!PAIR || w == 0) {
-                    mbar_wait(bar(TILE_FULL, k_slot), k_phase, ctl, kWaitMany + 1, kStatusTimeout);
+                    mbar_wait(bar(K_FULL, k_at.slot), k_at.phase, ctl, kWaitMany + 1, kStatusTimeout);
                     tc_fence_after();
                 }
-                const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_slot * (L::TILE / 16);
+                const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_at.slot * (L::TILE / 16);
 #pragma unroll
                 for (int i = 0; i < DP / 16; ++i) {
                     const uint32_t off = ((i / 4) * L::PANEL + (i % 4) * 32) / 16;
@@ -204,23 +206,23 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 }
                 tc_commit(bar(S_FULL, w));
                 if (!PAIR || w == 1) {
-                    tc_commit(bar(TILE_EMPTY, k_slot));
-                    two_on(k_slot, k_phase);
+                    tc_commit(bar(K_EMPTY, k_at.slot));
+                    k_at.next();
                 }
             };
             auto values = [&](auto which, bool first) {
                 constexpr uint32_t w = decltype(which)::value;
-                if (!PAIR || w == 0) mbar_wait(bar(TILE_FULL, v_slot), v_phase, ctl, kWaitMany + 2, kStatusTimeout);
+                if (!PAIR || w == 0) mbar_wait(bar(V_FULL, v_at.slot), v_at.phase, ctl, kWaitMany + 2, kStatusTimeout);
                 mbar_wait(bar(P_FULL, w), p_phase[w], ctl, kWaitMany + 3, kStatusTimeout);
                 p_phase[w] ^= 1;
                 tc_fence_after();
-                const uint32_t v = v_lo + v_slot * (L::TILE / 16);
+                const uint32_t v = v_lo + v_at.slot * (L::TILE / 16);
 #pragma unroll
                 for (int i = 0; i < kTok / 16; ++i) mma_f16_ts(tmem + L::O + w * DP, tmem + w * kTok + 8 * i, v + i * 16 * 128 / 16, v_hi, kPv, !first || i > 0);
                 tc_commit(bar(O_DONE, w));
                 if (!PAIR || w == 1) {
-                    tc_commit(bar(TILE_EMPTY, v_slot));
-                    two_on(v_slot, v_phase);
+                    tc_commit(bar(V_EMPTY, v_at.slot));
+                    v_at.next();
                 }
             };
             const std::integral_constant<uint32_t, 0> zero{};
@@ -245,12 +247,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         if (lane == 0) tc_commit(bar(DRAINED, 0));                               // (whatever became of the waits, no product is left when the CTA goes)
         mbar_drain(bar(DRAINED, 0), 0, a.limit_ns);
     } else if (warp >= kLoadWarp) {
-        // ---- codes and scales into shared memory: each warp fills one slot, again and again, with every third tile of K0 V0 K1 V1 ... (and so waits for every use of
-        // it: a parity would not tell a use from the one after the next). A lane has four tokens of a tile; codes come as boxes of tokens that lie side by side in
-        // any page, or (heads that are not whole 16-byte pieces) piece by piece.
+        // ---- codes and scales into shared memory: a warp for keys (and all scales), one for values. A lane has four tokens of a tile; codes come as boxes of tokens
+        // that lie side by side in any page, or (heads that are not whole 16-byte pieces) piece by piece.
         const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
         const bool runs = a.page % 4 == 0;                                       // a lane's tokens lie side by side
-        const uint32_t slot = warp - kLoadWarp, units = 2 * static_cast<uint32_t>(share.end - share.begin);
+        const int side = warp - kLoadWarp;
+        const uint32_t raws = side == 0 ? L::RAW_KEYS : L::RAW_VALUES, units = static_cast<uint32_t>(share.end - share.begin);
+        const uint32_t fulls = bar(side == 0 ? RAW_K_FULL : RAW_V_FULL, 0), empties = bar(side == 0 ? RAW_K_EMPTY : RAW_V_EMPTY, 0), raw_at = base + (side == 0 ? L::RAW : L::RAW_V);
         int next[4], next_head = 0;
         uint32_t first_of_seg = 0;                                               // tiles before the segment
         bool next_in[4], more = seg.next();
@@ -276,21 +279,21 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 next_in[i] = next[i] >= 0 && t >= seg.s.start;
             }
         };
-        look_up(slot >> 1);
-        uint32_t phase = 1;
-        for (uint32_t unit = slot; unit < units; unit += kRaw, phase ^= 1) {
+        look_up(0);
+        uint32_t slot = 0, phase = 1;
+        for (uint32_t unit = 0; unit < units; ++unit) {
             int slots[4];
             uint32_t flags = 0;
-            const int head = next_head, side = unit & 1;
+            const int head = next_head;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 slots[i] = next[i];
                 flags |= (next_in[i] ? 0x80u : 0u) << (8 * i);
             }
-            if (unit + kRaw < units) look_up((unit + kRaw) >> 1);                // (on its way meanwhile)
+            if (unit + 1 < units) look_up(unit + 1);                             // (on its way meanwhile)
             {
-                mbar_wait(bar(RAW_EMPTY, slot), phase, ctl, kWaitMany + 4, kStatusTimeout);
-                const uint32_t full = bar(RAW_FULL, slot), to = base + L::RAW + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
+                mbar_wait(empties + 8 * slot, phase, ctl, kWaitMany + 4, kStatusTimeout);
+                const uint32_t full = fulls + 8 * slot, to = raw_at + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
                 if (a.box > 0) {
                     // boxes that begin with this lane's tokens: one of 4 or more tokens, or several smaller ones
                     uint32_t mine = 0;
@@ -348,39 +351,75 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 }
                 mbar_arrive(full);
                 cp_async_mbar_arrive(full);                                      // once this lane's own copies are there
+                if (++slot == raws) {
+                    slot = 0;
+                    phase ^= 1;
+                }
             }
         }
         // nothing is on its way when the CTA goes: what was asked for has been waited for by those who convert it, unless a wait gave up
         if (abort_flag != 0) {
             asm volatile("cp.async.wait_all;" ::: "memory");
-            for (uint32_t last = units > kRaw ? units - kRaw : 0; last < units; ++last) mbar_drain(bar(RAW_FULL, last % kRaw), last / kRaw & 1, a.limit_ns);
+            for (uint32_t last = units > raws ? units - raws : 0; last < units; ++last) mbar_drain(fulls + 8 * (last % raws), last / raws & 1, a.limit_ns);
         }
-    } else if (warp >= kConvertWarp) {
-        // ---- codes to fp16 tiles: a thread has a chunk of 16 bytes of every PASS-th token (PASS is a multiple of 8, so that its chunks are swizzled alike)
-        const int me = threadIdx.x - 32 * kConvertWarp, chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
+    } else if (warp >= kKeyWarp) {
+        // ---- codes to fp16 tiles, keys by four warps and values by four: a thread has a chunk of 16 bytes of every PASS-th token (PASS is a multiple of 8, so that its
+        // chunks are swizzled alike). The keys' warps work out the scales of both.
+        const bool keys = warp < kValueWarp;
+        const int me = threadIdx.x & (kConverters - 1), chunk = me % L::CHUNKS, tok = me / L::CHUNKS;
         static_assert(FMT == KV_CACHE_INT8 || L::CODES == kMxBlock, "a chunk is a block");
-        static_assert(L::PASS % 8 == 0, "");
-        int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
-        uint8_t* const v_scales = smem + L::OF_V;                                // [tile % 2][token]: int8: the values' scales, 4-bit: their four bytes
-        uint16_t* const k_muls = reinterpret_cast<uint16_t*>(smem + L::OF_K);    // 4-bit: [tile % 2][token][block]
-        const uint32_t raw_from = base + L::RAW + L::raw_place(tok, chunk * 16);
+        static_assert(L::PASS % 8 == 0 && kConverters == kTok, "");
+        uint8_t* const v_scales = smem + L::OF_V;                                // [slot][token]: int8: the values' scales, 4-bit: their four bytes
+        const uint32_t raw_from = base + L::raw_place(tok, chunk * 16);
         uint32_t to[L::CODES / 8];
 #pragma unroll
         for (int j = 0; j < L::CODES / 8; ++j) to[j] = base + place(tok, chunk * L::CODES + 8 * j);
-        Turn<kRaw> raw;
-        Turn<L::RING> ring;
-        uint32_t t = 0, segments = 0;                                            // tiles and segments so far
-        while (seg.next()) {
-            int sigma = -126;                                                    // the values' reference starts anew with each segment
-            mbar_wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
-            ++segments;
-            const float factor = reinterpret_cast<const volatile float*>(smem + L::FACTOR)[0];
-            for (int left = seg.tiles; left > 0; --left, ++t) {
-                const uint32_t slot = t & (kSlots - 1);
-                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
-                // scales: a thread a token
-                int word = -126 * 4;                                             // this warp's: the largest exponent of a value's scale, and what is special
-                if (me < kTok) {
+        auto convert = [&](uint32_t raw, uint32_t tile, auto multiplier) {       // of a token: two equal halves
+            const uint32_t from = raw_from + raw;
+#pragma unroll 2
+            for (int i = 0; i < kTok / L::PASS; ++i) {
+                uint32_t w[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from + i * L::PASS * L::ROW) : "memory");
+                const uint32_t mul = multiplier(tok + i * L::PASS), at = tile + i * L::PASS * 128;
+                if (FMT == KV_CACHE_INT8) {
+                    uint32_t f[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
+                    if (mul != 0x3c003c00u) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
+                    }
+                    store_16(to[0] + at, f[0], f[1], f[2], f[3]);
+                    store_16(to[1] + at, f[4], f[5], f[6], f[7]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t f[4];
+                        e2m1_to_f16(w[j], f);
+                        store_16(to[j] + at, mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
+                    }
+                }
+            }
+        };
+        uint32_t t = 0;                                                          // tiles so far
+        if (keys) {
+            int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
+            uint16_t* const k_muls = reinterpret_cast<uint16_t*>(smem + L::OF_K);                 // 4-bit: [tile % 2][token][block]
+            Turn<L::RAW_KEYS> raw;
+            Turn<L::KEYS> ring;
+            uint32_t segments = 0;
+            while (seg.next()) {
+                int sigma = -126;                                                // the values' reference starts anew with each segment
+                mbar_wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
+                ++segments;
+                const float factor = reinterpret_cast<const volatile float*>(smem + L::FACTOR)[0];
+                for (int left = seg.tiles; left > 0; --left, ++t) {
+                    const uint32_t slot = t & (kSlots - 1);
+                    mbar_wait(bar(RAW_K_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                    // (the products of two tiles back are done, so those of four back with their values: nobody reads this slot of the factors)
+                    mbar_wait(bar(K_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                    // scales: a thread a token
+                    int word;                                                    // this warp's: the largest exponent of a value's scale, and what is special
                     const uint8_t* const rest = smem + L::MORE + raw.slot * L::MORE_BYTES;
                     const uint32_t flag = rest[L::FLAGS + me];
                     const bool in = flag != 0;
@@ -393,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         nan = in && (vs & 0x7f800000u) == 0x7f800000u;
                         if (in && !nan) top_sigma = static_cast<int>(vs >> 23) - 126;               // s < 2^this
                         nans[slot * kTok + me] = nan ? 0xff : 0;
-                        reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + me] = in && !nan ? vs : 0u;     // (finite is what matters)
+                        reinterpret_cast<uint32_t*>(v_scales)[slot * kTok + me] = in && !nan ? vs : 0u;     // (finite is what matters)
                     } else {
                         const uint32_t* const its = reinterpret_cast<const uint32_t*>(rest) + 2 * me;
                         const uint32_t shift = 8 * (flag & 3), there = blocks == 4 ? ~0u : (1u << (8 * blocks)) - 1;
@@ -411,84 +450,70 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         *reinterpret_cast<uint2*>(k_muls + ((t & 1) * kTok + me) * 4) = make_uint2(m[0] | m[1] << 16, m[2] | m[3] << 16);
                         k_factor = top == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
                         nans[slot * kTok + me] = static_cast<uint8_t>((v_nan & 1u) | (v_nan >> 7 & 2u) | (v_nan >> 14 & 4u) | (v_nan >> 21 & 8u));
-                        reinterpret_cast<uint32_t*>(v_scales)[(t & 1) * kTok + me] = vb & ~v_nan;
+                        reinterpret_cast<uint32_t*>(v_scales)[slot * kTok + me] = vb & ~v_nan;
                     }
                     k_factor *= factor;
                     factors[slot * kTok + me] = in ? k_factor : -1.f;
                     word = __reduce_max_sync(0xffffffffu, top_sigma) * 4 + (__any_sync(0xffffffffu, nan) ? 1 : 0) + (__any_sync(0xffffffffu, !in) ? 2 : 0);
-                }
-                if (lane == 0) of_warp[(t & 1) * 8 + warp - kConvertWarp] = word;
-                named_sync(1, kConverters);
-                int all = 0;
+                    if (lane == 0) of_warp[(t & 1) * 4 + warp - kKeyWarp] = word;
+                    named_sync(1, kConverters);
+                    int all = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int its = of_warp[(t & 1) * 8 + i];
-                    sigma = max(sigma, its >> 2);                                // the largest scale of values so far (an exponent of fp32)
-                    all |= its & 3;
-                }
-                if (me == 0) {
-                    sigmas[slot] = sigma;
-                    special[slot] = all;
-                }
-                // keys
-                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
-                auto convert = [&](auto multiplier) {                            // of a token: two equal halves, or none (0)
-                    const uint32_t from = raw_from + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
-#pragma unroll 2
-                    for (int i = 0; i < kTok / L::PASS; ++i) {
-                        uint32_t w[4];
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from + i * L::PASS * L::ROW) : "memory");
-                        const uint32_t mul = multiplier(tok + i * L::PASS), at = tile + i * L::PASS * 128;
-                        if (FMT == KV_CACHE_INT8) {
-                            uint32_t f[8];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) int8_to_f16(w[j], f[2 * j], f[2 * j + 1]);
-                            if (mul != 0x3c003c00u) {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
-                            }
-                            store_16(to[0] + at, f[0], f[1], f[2], f[3]);
-                            store_16(to[1] + at, f[4], f[5], f[6], f[7]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t f[4];
-                                e2m1_to_f16(w[j], f);
-                                store_16(to[j] + at, mul_f16x2(f[0], mul), mul_f16x2(f[1], mul), mul_f16x2(f[2], mul), mul_f16x2(f[3], mul));
-                            }
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const int its = of_warp[(t & 1) * 4 + i];
+                        sigma = max(sigma, its >> 2);                            // the largest scale of values so far (an exponent of fp32)
+                        all |= its & 3;
                     }
-                };
-                auto pass_on = [&] {
+                    if (me == 0) {
+                        sigmas[slot] = sigma;
+                        special[slot] = all;
+                    }
+                    if (lane == 0) mbar_arrive(bar(SCALES_FULL, slot));
+                    const uint32_t from = L::RAW + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
+                    if constexpr (FMT == KV_CACHE_INT8) convert(from, tile, [](int) { return 0x3c003c00u; });
+                    else convert(from, tile, [&](int r) { return k_muls[((t & 1) * kTok + r) * 4 + chunk] * 0x00010001u; });
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(bar(TILE_FULL, ring.slot));
-                        mbar_arrive(bar(RAW_EMPTY, raw.slot));
+                        mbar_arrive(bar(K_FULL, ring.slot));
+                        mbar_arrive(bar(RAW_K_EMPTY, raw.slot));
                     }
                     raw.next();
                     ring.next();
-                };
-                if constexpr (FMT == KV_CACHE_INT8) convert([](int) { return 0x3c003c00u; });
-                else convert([&](int r) { return k_muls[((t & 1) * kTok + r) * 4 + chunk] * 0x00010001u; });
-                pass_on();
+                }
+            }
+        } else {
+            Turn<L::RAW_VALUES> raw;
+            Turn<L::VALUES> ring;
+            for (const uint32_t units = static_cast<uint32_t>(share.end - share.begin); t < units; ++t) {
                 // values: times their scale over 2^sigma, brought to 2^15 at most
-                mbar_wait(bar(RAW_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
-                mbar_wait(bar(TILE_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                const uint32_t slot = t & (kSlots - 1);
+                mbar_wait(bar(SCALES_FULL, slot), t / kSlots & 1, ctl, kWaitMany + 11, kStatusTimeout);
+                const int sigma = sigmas[slot];
+                mbar_wait(bar(RAW_V_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                mbar_wait(bar(V_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                const uint32_t from = L::RAW_V + raw.slot * kTok * L::ROW, tile = L::V_TILES + ring.slot * L::TILE;
                 if constexpr (FMT == KV_CACHE_INT8) {
                     // (two factors, as 2^(8 - sigma) alone may be more than fp32 holds)
                     const float by0 = __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23), by1 = __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23);
-                    convert([&](int r) {
-                        const float by = reinterpret_cast<const float*>(v_scales)[(t & 1) * kTok + r] * by0 * by1;
+                    convert(from, tile, [&](int r) {
+                        const float by = reinterpret_cast<const float*>(v_scales)[slot * kTok + r] * by0 * by1;
                         return pack_f16(by, by);
                     });
                 } else {
-                    convert([&](int r) {                                         // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
-                        const int e = 27 + static_cast<int>(v_scales[(t & 1) * kTok * 4 + r * 4 + chunk]) - 127 - sigma;
+                    convert(from, tile, [&](int r) {                             // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
+                        const int e = 27 + static_cast<int>(v_scales[(slot * kTok + r) * 4 + chunk]) - 127 - sigma;
                         return (e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31)) * 0x00010001u;
                     });
                 }
-                pass_on();
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(V_FULL, ring.slot));
+                    mbar_arrive(bar(RAW_V_EMPTY, raw.slot));
+                }
+                raw.next();
+                ring.next();
             }
         }
     } else {
@@ -502,32 +527,31 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             const int r = (PAIR ? w * kRows : 0) + row;                          // of the item's rows
             const bool live = r < seg.rows, warp_live = (PAIR ? w * kRows : 0) + 32 * (warp & 3) < seg.rows;
             const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group;
-            // queries: a power of two brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes a row, several rows on their way at once.
+            // queries: all on their way into their places at once, then a power of two that brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes
+            // a row; a thread converts what it copied.
             {
-                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8, BATCH = 8;
+                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8;
                 const int d = lane % LANES * 8;
-                uint4 x[BATCH];
-                auto load = [&](int begin) {
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-                        const int q_row = warp * PER_WARP + begin + i * AT_ONCE + lane / LANES;
-                        x[i] = make_uint4(0, 0, 0, 0);
-                        if (begin + i * AT_ONCE < PER_WARP && q_row < seg.rows && d < a.dim) {
-                            const int its = (seg.row0 + q_row) / a.group, its_head = seg.head * a.group + (seg.row0 + q_row) - its * a.group;
-                            x[i] = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d);
-                        }
-                    }
+                auto row_of = [&](int i) { return warp * PER_WARP + i + lane / LANES; };
+                auto place_of = [&](int i) { return base + L::Q + (row_of(i) / kRows) * L::TILE + place(row_of(i) % kRows, d); };
+                auto read = [&](int i) {
+                    uint4 x;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(place_of(i)) : "memory");
+                    return x;
                 };
-                uint32_t top = 0;
 #pragma unroll 1
-                for (int begin = 0; begin < PER_WARP; begin += BATCH * AT_ONCE) {
-                    load(begin);
-                    // (a row with an Inf or a NaN does not set the power of the others)
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-                        const uint32_t its = absmax_bits8(x[i]);
-                        top = max(top, its < 0x7f800000u ? its : 0u);
-                    }
+                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+                    const int q_row = row_of(i), its = (seg.row0 + q_row) / a.group, its_head = seg.head * a.group + (seg.row0 + q_row) - its * a.group;
+                    const bool valid = q_row < seg.rows && d < a.dim;
+                    cp_async<16>(place_of(i), a.q + (valid ? static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d : 0), valid ? 16 : 0);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                uint32_t top = 0;
+                // (a row with an Inf or a NaN does not set the power of the others)
+#pragma unroll 4
+                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+                    const uint32_t its = absmax_bits8(read(i));
+                    top = max(top, its < 0x7f800000u ? its : 0u);
                 }
                 top = __reduce_max_sync(0xffffffffu, top);
                 if (lane == 0) of_segment[8 + warp] = __uint_as_float(top);
@@ -539,18 +563,11 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 if (threadIdx.x == 0) of_segment[0] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f), 1e-38f);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(FACTOR_FULL, 0));
-#pragma unroll 1
-                for (int begin = 0; begin < PER_WARP; begin += BATCH * AT_ONCE) {
-                    if (PER_WARP > BATCH * AT_ONCE) load(begin);
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-                        if (begin + i * AT_ONCE >= PER_WARP) break;
-                        const int q_row = warp * PER_WARP + begin + i * AT_ONCE + lane / LANES;
-                        float f[8];
-                        unpack_bf16x8(x[i], f);
-                        store_16(base + L::Q + (q_row / kRows) * L::TILE + place(q_row % kRows, d), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul),
-                                 pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
-                    }
+#pragma unroll 4
+                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+                    float f[8];
+                    unpack_bf16x8(read(i), f);
+                    store_16(place_of(i), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul), pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
                 }
             }
             fence_proxy_async_smem();
@@ -765,40 +782,73 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             named_sync(2, kSoftmax);                                             // o and the states may be written over
             if (!whole) {
                 const int from = owner(seg.item_begin, share), until = owner(seg.item_end - 1, share);
-                if (last_to_arrive<ROWS>(a, seg.s, seg.b, seg.head, seg.row0, from, until, threadIdx.x, &last_one, [] { named_sync(2, kSoftmax); }) && live) {
-                    // the parts of this thread's row and elements, in the order of the tokens: 16 elements at a time, their loads on their way together
+                if (last_to_arrive<ROWS>(a, seg.s, seg.b, seg.head, seg.row0, from, until, threadIdx.x, &last_one, [] { named_sync(2, kSoftmax); })) {
+                    if (live) {
+                    // the parts of this thread's row and elements, in the order of the tokens: their states, then 32 elements at a time, several parts' loads on their way
                     auto part_of = [&](int x) { return reinterpret_cast<const float4*>(a.parts + (2 * static_cast<int64_t>(x) + (x == from ? 1 : 0)) * PART); };
-#pragma unroll 1
-                    for (int d = d0; d < min(d0 + WIDTH, a.dim); d += 32) {
-                        float o[32];
+                    Row sum;
+#pragma unroll 2
+                    for (int x = from; x <= until; ++x) {
+                        const float4 its = __ldcg(part_of(x) + DP / 4 * ROWS + r);
+                        const float now_l = fmaxf(sum.m_l, its.y);
+                        sum.l = sum.l * ex2(sum.m_l - now_l) + its.z * ex2(its.y - now_l);
+                        sum.m_l = now_l;
+                        sum.m_o = fmaxf(sum.m_o, its.x);
+                    }
+                    const float2 scale = sum.scale<FMT>();
+                    // (through the queries' place: 16 KB or more on their way)
+                    constexpr int Q_BYTES = (PAIR ? 2 : 1) * L::TILE, EACH = Q_BYTES >= 65536 ? 4 : 2, GROUPS = Q_BYTES / (EACH * 16 * kSoftmax);
+                    static_assert(GROUPS >= 2 && GROUPS <= 4, "");
+                    const uint32_t stage = base + L::Q + threadIdx.x * 16, m_stage = base + L::STATE + threadIdx.x * 4;
+                    const int chunks = (max(0, min(WIDTH, a.dim - d0)) + 4 * EACH - 1) / (4 * EACH);
+                    int in_chunk = 0, in_part = from, in_slot = 0;
+                    auto ask = [&] {
+                        if (in_chunk < chunks) {
+                            const float4* const p = part_of(in_part);
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] = 0.f;
-                        Row sum;
-#pragma unroll 1
-                        for (int x = from; x <= until; ++x) {
-                            const float4* const p = part_of(x);
-                            const float4 its = __ldcg(p + DP / 4 * ROWS + r);
-                            float4 v[8];
-#pragma unroll
-                            for (int q = 0; q < 8; ++q) v[q] = __ldcg(p + (d / 4 + q) * ROWS + r);
-                            const float now_o = fmaxf(sum.m_o, its.x), now_l = fmaxf(sum.m_l, its.y), mine = ex2(sum.m_o - now_o), other_one = ex2(its.x - now_o);
-                            sum.l = sum.l * ex2(sum.m_l - now_l) + its.z * ex2(its.y - now_l);
-                            sum.m_o = now_o;
-                            sum.m_l = now_l;
-#pragma unroll
-                            for (int q = 0; q < 8; ++q) {
-                                o[4 * q] = o[4 * q] * mine + v[q].x * other_one;
-                                o[4 * q + 1] = o[4 * q + 1] * mine + v[q].y * other_one;
-                                o[4 * q + 2] = o[4 * q + 2] * mine + v[q].z * other_one;
-                                o[4 * q + 3] = o[4 * q + 3] * mine + v[q].w * other_one;
+                            for (int q = 0; q < EACH; ++q) cp_async<16>(stage + (in_slot * EACH + q) * kSoftmax * 16, p + (d0 / 4 + in_chunk * EACH + q) * ROWS + r, 16);
+                            cp_async<4>(m_stage + in_slot * kSoftmax * 4, p + DP / 4 * ROWS + r, 4);
+                            if (++in_part > until) {
+                                in_part = from;
+                                ++in_chunk;
                             }
                         }
-                        const float2 scale = sum.scale<FMT>();
+                        cp_async_commit();
+                        in_slot = in_slot + 1 == GROUPS ? 0 : in_slot + 1;
+                    };
 #pragma unroll
-                        for (int x = 0; x < 32; x += 8)
-                            if (d + x < a.dim) write8(sum, scale, o + x, d + x);
-                        if (d == 0) sum.write_lse(a, seg.s, node, h);
+                    for (int i = 0; i < GROUPS - 1; ++i) ask();
+                    int slot = 0;
+#pragma unroll 1
+                    for (int c = 0; c < chunks; ++c) {
+                        float o[4 * EACH];
+#pragma unroll
+                        for (int i = 0; i < 4 * EACH; ++i) o[i] = 0.f;
+#pragma unroll 1
+                        for (int x = from; x <= until; ++x) {
+                            ask();
+                            cp_async_wait<GROUPS - 1>();
+                            float its_m;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(its_m) : "r"(m_stage + slot * kSoftmax * 4) : "memory");
+                            const float by = ex2(its_m - sum.m_o);
+#pragma unroll
+                            for (int q = 0; q < EACH; ++q) {
+                                float4 v;
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(stage + (slot * EACH + q) * kSoftmax * 16) : "memory");
+                                o[4 * q] += v.x * by;
+                                o[4 * q + 1] += v.y * by;
+                                o[4 * q + 2] += v.z * by;
+                                o[4 * q + 3] += v.w * by;
+                            }
+                            slot = slot + 1 == GROUPS ? 0 : slot + 1;
+                        }
+#pragma unroll
+                        for (int x = 0; x < 4 * EACH; x += 8)
+                            if (d0 + c * 4 * EACH + x < a.dim) write8(sum, scale, o + x, d0 + c * 4 * EACH + x);
                     }
+                    if (d0 == 0) sum.write_lse(a, seg.s, node, h);
+                    }
+                    named_sync(2, kSoftmax);                                     // (the queries' place is free again)
                 }
             }
             tile_base += seg.tiles;
