@@ -40,8 +40,8 @@ struct Plan {
     static constexpr int FACTORS = MORE + RAW_KEYS * MORE_BYTES;
     static constexpr int ONES = FACTORS + kSlots * kTok * 4;                   // factors of scores that have theirs already
     static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
-    static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 4 * 4, OF_K = OF_V + kSlots * kTok * 4;
-    static constexpr int FACTOR = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 8);         // of the scores, and the queries' maxima of the warps
+    static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, OF_K = OF_V + kSlots * kTok * 4, OF_TILE = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 4);
+    static constexpr int FACTOR = OF_TILE + kSlots * 4;         // of the scores, and the queries' maxima of the warps
     static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 33 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     const uint32_t tmem = tmem_slot;
     float* const factors = reinterpret_cast<float*>(smem + L::FACTORS);          // [slot][token]: of the scores; -1: not seen by anybody
     volatile int* const sigmas = reinterpret_cast<volatile int*>(smem + L::SIGMA);        // [slot]: values are relative to 2^this
+    volatile float* const tile_factors = reinterpret_cast<volatile float*>(smem + L::OF_TILE);      // 4-bit: [slot]: of all scores of a tile
     volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2)
     uint8_t* const nans = smem + L::NANS;
     const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
@@ -254,29 +255,22 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         const int side = warp - kLoadWarp;
         const uint32_t raws = side == 0 ? L::RAW_KEYS : L::RAW_VALUES, units = static_cast<uint32_t>(share.end - share.begin);
         const uint32_t fulls = bar(side == 0 ? RAW_K_FULL : RAW_V_FULL, 0), empties = bar(side == 0 ? RAW_K_EMPTY : RAW_V_EMPTY, 0), raw_at = base + (side == 0 ? L::RAW : L::RAW_V);
-        int next[4], next_head = 0;
+        int ids[4], next_t0 = 0, next_start = 0, next_stop = 0, next_head = 0;   // of the next tile: page table entries of this lane's tokens, which they are
         uint32_t first_of_seg = 0;                                               // tiles before the segment
-        bool next_in[4], more = seg.next();
-        auto look_up = [&](uint32_t tile) {                                      // where the tokens of a tile are (tiles are asked for in their order)
+        bool more = seg.next();
+        auto look_up = [&](uint32_t tile) {                                      // (tiles are asked for in their order)
             while (more && tile - first_of_seg >= static_cast<uint32_t>(seg.tiles)) {
                 first_of_seg += seg.tiles;
                 more = seg.next();
             }
-            const int t0 = more ? seg.token(static_cast<int>(tile - first_of_seg)) + 4 * lane : 0;
+            next_t0 = more ? seg.token(static_cast<int>(tile - first_of_seg)) + 4 * lane : 0;
+            next_start = seg.s.start;
+            next_stop = more ? seg.s.stop : 0;
             next_head = seg.head;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = t0 + i;
-                if (i == 0 || !runs) {
-                    next[i] = -1;
-                    if (more && t < seg.s.stop) {
-                        const int p = a.page_shift >= 0 ? t >> a.page_shift : t / a.page, id = a.table[seg.b * a.table_stride + p];
-                        if (id >= 0 && id < a.num_pages) next[i] = id * a.page + (t - p * a.page);
-                    }
-                } else {
-                    next[i] = next[0] >= 0 && t < seg.s.stop ? next[0] + i : -1;
-                }
-                next_in[i] = next[i] >= 0 && t >= seg.s.start;
+                const int t = next_t0 + i;
+                if ((i == 0 || !runs) && t < next_stop) ids[i] = a.table[seg.b * a.table_stride + (a.page_shift >= 0 ? t >> a.page_shift : t / a.page)];
             }
         };
         look_up(0);
@@ -287,8 +281,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             const int head = next_head;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                slots[i] = next[i];
-                flags |= (next_in[i] ? 0x80u : 0u) << (8 * i);
+                const int t = next_t0 + i, id = ids[runs ? 0 : i];
+                slots[i] = t < next_stop && id >= 0 && id < a.num_pages ? id * a.page + (a.page_shift >= 0 ? t & (a.page - 1) : t % a.page) : -1;
+                flags |= (slots[i] >= 0 && t >= next_start ? 0x80u : 0u) << (8 * i);
             }
             if (unit + 1 < units) look_up(unit + 1);                             // (on its way meanwhile)
             {
@@ -404,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         uint32_t t = 0;                                                          // tiles so far
         if (keys) {
             int* const of_warp = reinterpret_cast<int*>(smem + L::OF_WARP);
-            uint16_t* const k_muls = reinterpret_cast<uint16_t*>(smem + L::OF_K);                 // 4-bit: [tile % 2][token][block]
+            uint8_t* const k_scales = smem + L::OF_K;                            // 4-bit: [tile % 2][token]: their four bytes
             Turn<L::RAW_KEYS> raw;
             Turn<L::KEYS> ring;
             uint32_t segments = 0;
@@ -425,7 +420,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     const bool in = flag != 0;
                     int top_sigma = -126;
                     bool nan = false;
-                    float k_factor;
+                    float k_factor = 0.f;
+                    uint32_t top_of_k = 0;
                     if (FMT == KV_CACHE_INT8) {
                         const uint32_t vs = reinterpret_cast<const uint32_t*>(rest + L::V_SCALES)[me];
                         k_factor = reinterpret_cast<const float*>(rest)[me];
@@ -438,40 +434,45 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         const uint32_t shift = 8 * (flag & 3), there = blocks == 4 ? ~0u : (1u << (8 * blocks)) - 1;
                         const uint32_t kb = __funnelshift_r(its[0], its[1], shift) & there, vb = __funnelshift_r(its[kTok * 2], its[kTok * 2 + 1], shift) & there;
                         const uint32_t k_nan = __vcmpeq4(kb, ~0u), v_nan = __vcmpeq4(vb, ~0u);
-                        uint32_t top = __vmaxu4(kb, kb >> 16), v_top = vb & ~v_nan;
-                        top = k_nan != 0 ? 255u : max(top & 0xffu, top >> 8 & 0xffu);
+                        uint32_t k_top = kb & ~k_nan, v_top = vb & ~v_nan;
+                        k_top = __vmaxu4(k_top, k_top >> 16);
+                        if (in) top_of_k = max(k_top & 0xffu, k_top >> 8 & 0xffu);
                         v_top = __vmaxu4(v_top, v_top >> 16);
                         nan = in && v_nan != 0;
                         if (in) top_sigma = max(-126, static_cast<int>(max(v_top & 0xffu, v_top >> 8 & 0xffu)) - 127);
-                        // 2^12 * 2^(byte - top): exact beside the codes, and the token's factor makes up for it
-                        uint32_t m[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) m[j] = static_cast<uint32_t>(max(27 + static_cast<int>(kb >> (8 * j) & 0xffu) - static_cast<int>(top), 0)) << 10;
-                        *reinterpret_cast<uint2*>(k_muls + ((t & 1) * kTok + me) * 4) = make_uint2(m[0] | m[1] << 16, m[2] | m[3] << 16);
-                        k_factor = top == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top == 0 ? 0x00400000u : top << 23);
+                        reinterpret_cast<uint32_t*>(k_scales)[(t & 1) * kTok + me] = in ? kb : 0u;
                         nans[slot * kTok + me] = static_cast<uint8_t>((v_nan & 1u) | (v_nan >> 7 & 2u) | (v_nan >> 14 & 4u) | (v_nan >> 21 & 8u));
                         reinterpret_cast<uint32_t*>(v_scales)[slot * kTok + me] = vb & ~v_nan;
                     }
                     k_factor *= factor;
                     factors[slot * kTok + me] = in ? k_factor : -1.f;
                     word = __reduce_max_sync(0xffffffffu, top_sigma) * 4 + (__any_sync(0xffffffffu, nan) ? 1 : 0) + (__any_sync(0xffffffffu, !in) ? 2 : 0);
-                    if (lane == 0) of_warp[(t & 1) * 4 + warp - kKeyWarp] = word;
+                    if (FMT == KV_CACHE_MXFP4) top_of_k = __reduce_max_sync(0xffffffffu, top_of_k);
+                    if (lane == 0) {
+                        of_warp[(t & 1) * 8 + warp - kKeyWarp] = word;
+                        of_warp[(t & 1) * 8 + 4 + warp - kKeyWarp] = static_cast<int>(top_of_k);
+                    }
                     named_sync(1, kConverters);
                     int all = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int its = of_warp[(t & 1) * 4 + i];
+                        const int its = of_warp[(t & 1) * 8 + i];
+                        if (FMT == KV_CACHE_MXFP4) top_of_k = max(top_of_k, static_cast<uint32_t>(of_warp[(t & 1) * 8 + 4 + i]));
                         sigma = max(sigma, its >> 2);                            // the largest scale of values so far (an exponent of fp32)
                         all |= its & 3;
                     }
                     if (me == 0) {
                         sigmas[slot] = sigma;
                         special[slot] = all;
+                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23), 1.2e-38f);
                     }
                     if (lane == 0) mbar_arrive(bar(SCALES_FULL, slot));
                     const uint32_t from = L::RAW + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
                     if constexpr (FMT == KV_CACHE_INT8) convert(from, tile, [](int) { return 0x3c003c00u; });
-                    else convert(from, tile, [&](int r) { return k_muls[((t & 1) * kTok + r) * 4 + chunk] * 0x00010001u; });
+                    else convert(from, tile, [&](int r) {                        // 2^12 * 2^(byte - top), subnormal from e = 0 down (2^-39 of the tile's largest keys)
+                        const int its = k_scales[((t & 1) * kTok + r) * 4 + chunk], e = 27 + its - static_cast<int>(top_of_k);
+                        return (its == 255 ? 0x7e00u : e > 0 ? static_cast<uint32_t>(e) << 10 : 512u >> min(-e, 31)) * 0x00010001u;
+                    });
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -611,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             const uint32_t sees = sees32_of(ch / 2) >> (16 * (ch & 1));
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? __float_as_uint(__uint_as_float(v[i]) * kf[16 * ch + i]) : 0xff800000u;
+                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? (FMT == KV_CACHE_INT8 ? __float_as_uint(__uint_as_float(v[i]) * kf[16 * ch + i]) : v[i]) : 0xff800000u;
                             tmem_st_32x32b_x16(s_tmem + 16 * ch, v);
                         }
                         tmem_wait_st();
@@ -631,6 +632,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 const uint32_t (&x)[16] = v[half];
 #pragma unroll
                                 for (int i = 0; i < 16; i += 4) {
+                                    if (FMT == KV_CACHE_MXFP4) {
+                                        top = max3(max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1])), __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+                                        continue;
+                                    }
                                     const float4 k = *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
                                     float p, q, y, z;
                                     unpack2(mul2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y)), p, q);
@@ -641,7 +646,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         }
                         tmem_wait_ld();
                     }
-                    top = fmaxf(top, kNone);
+                    const float tile_factor = FMT == KV_CACHE_MXFP4 ? tile_factors[slot] : 1.f;
+                    top = fmaxf(FMT == KV_CACHE_MXFP4 ? top * tile_factor : top, kNone);
                     // references move when a weight would pass 2^15, to put it at 2^7, or when the values' does
                     const int its_sigma = sigmas[slot];
                     if (__any_sync(0xffffffffu, top > m + 15.f || its_sigma != sigma)) {
@@ -681,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 uint32_t p[8];
 #pragma unroll
                                 for (int i = 0; i < 16; i += 4) {
-                                    const float4 k = *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
+                                    const float4 k = FMT == KV_CACHE_MXFP4 ? make_float4(tile_factor, tile_factor, tile_factor, tile_factor) : *reinterpret_cast<const float4*>(kf + 16 * (ch + half) + i);
                                     float y, z;
                                     unpack2(fma2(pack2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), pack2(k.x, k.y), m2), y, z);
                                     y = ex2(y);
