@@ -249,100 +249,74 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         mbar_drain(bar(DRAINED, 0), 0, a.limit_ns);
     } else if (warp >= kLoadWarp) {
         // ---- codes and scales into shared memory: a warp for keys (and all scales), one for values. A lane has four tokens of a tile; codes come as boxes of tokens
-        // that lie side by side in any page, or (heads that are not whole 16-byte pieces) piece by piece.
+        // that lie side by side in any page, or (heads that are not whole 16-byte pieces) piece by piece. (Loops are not unrolled: what bounds a warp that comes
+        // round once a tile, beside others that run other code, is the fetching of its instructions.)
         const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
         const bool runs = a.page % 4 == 0;                                       // a lane's tokens lie side by side
         const int side = warp - kLoadWarp;
         const uint32_t raws = side == 0 ? L::RAW_KEYS : L::RAW_VALUES, units = static_cast<uint32_t>(share.end - share.begin);
         const uint32_t fulls = bar(side == 0 ? RAW_K_FULL : RAW_V_FULL, 0), empties = bar(side == 0 ? RAW_K_EMPTY : RAW_V_EMPTY, 0), raw_at = base + (side == 0 ? L::RAW : L::RAW_V);
-        int ids[4], next_t0 = 0, next_start = 0, next_stop = 0, next_head = 0;   // of the next tile: page table entries of this lane's tokens, which they are
-        uint32_t first_of_seg = 0;                                               // tiles before the segment
-        bool more = seg.next();
-        auto look_up = [&](uint32_t tile) {                                      // (tiles are asked for in their order)
-            while (more && tile - first_of_seg >= static_cast<uint32_t>(seg.tiles)) {
-                first_of_seg += seg.tiles;
-                more = seg.next();
-            }
-            next_t0 = more ? seg.token(static_cast<int>(tile - first_of_seg)) + 4 * lane : 0;
-            next_start = seg.s.start;
-            next_stop = more ? seg.s.stop : 0;
-            next_head = seg.head;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = next_t0 + i;
-                if ((i == 0 || !runs) && t < next_stop) ids[i] = a.table[seg.b * a.table_stride + (a.page_shift >= 0 ? t >> a.page_shift : t / a.page)];
-            }
-        };
-        look_up(0);
-        uint32_t slot = 0, phase = 1;
-        for (uint32_t unit = 0; unit < units; ++unit) {
-            int slots[4];
-            uint32_t flags = 0;
-            const int head = next_head;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = next_t0 + i, id = ids[runs ? 0 : i];
-                slots[i] = t < next_stop && id >= 0 && id < a.num_pages ? id * a.page + (a.page_shift >= 0 ? t & (a.page - 1) : t % a.page) : -1;
-                flags |= (slots[i] >= 0 && t >= next_start ? 0x80u : 0u) << (8 * i);
-            }
-            if (unit + 1 < units) look_up(unit + 1);                             // (on its way meanwhile)
-            {
+        const void* const map = side == 0 ? &k_map : &v_map;
+        int64_t table_of = 0;
+        auto look_up = [&](int t, int stop) { return t < stop ? a.table[table_of + (a.page_shift >= 0 ? t >> a.page_shift : t / a.page)] : -1; };
+        auto slot_of = [&](int id, int t) { return id >= 0 && id < a.num_pages ? id * a.page + (a.page_shift >= 0 ? t & (a.page - 1) : t % a.page) : -1; };
+        uint32_t slot = 0, phase = 1, unit = 0;
+        while (seg.next()) {
+            table_of = seg.b * a.table_stride;
+            const int stop = seg.s.stop, head = seg.head;
+            int t0 = seg.token(0) + 4 * lane, id = look_up(t0, stop);            // (of the first of a lane's tokens, a tile ahead)
+#pragma unroll 1
+            for (int left = seg.tiles; left > 0; --left, ++unit) {
+                const int t = t0, first = slot_of(id, t);
+                t0 += kTok;
+                if (left > 1) id = look_up(t0, stop);
                 mbar_wait(empties + 8 * slot, phase, ctl, kWaitMany + 4, kStatusTimeout);
                 const uint32_t full = fulls + 8 * slot, to = raw_at + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
-                if (a.box > 0) {
-                    // boxes that begin with this lane's tokens: one of 4 or more tokens, or several smaller ones
-                    uint32_t mine = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mine |= static_cast<uint32_t>(slots[i] >= 0 && (4 * lane + i) % a.box == 0) << i;
-                    const uint32_t boxes = __reduce_add_sync(0xffffffffu, __popc(mine));
-                    if (lane == 0) mbar_expect_tx(full, boxes * a.box * L::ROW);
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (mine >> i & 1u) tma_load_3d(to + (4 * lane + i) * L::ROW, side == 0 ? &k_map : &v_map, full, 0, head, slots[i]);
-                } else {
-                    const uint8_t* codes = side == 0 ? a.k_codes : a.v_codes;
-                    constexpr int kPieces = L::ROW / 8;
-                    for (int e = lane; e < kTok * kPieces; e += 32) {
-                        const int r = e / kPieces, off = (e - r * kPieces) * 8;
-                        int from = -1;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int its = __shfl_sync(0xffffffffu, slots[i], r >> 2);
-                            if ((r & 3) == i) from = its;
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int from = i == 0 ? first : t + i >= stop ? -1 : !runs ? slot_of(look_up(t + i, stop), t + i) : first >= 0 ? first + i : -1;
+                    if (a.box > 0) {                                             // boxes that begin with this token
+                        if (from >= 0 && (4 * lane + i) % a.box == 0) {
+                            mbar_expect_tx(full, a.box * L::ROW);
+                            tma_load_3d(to + (4 * lane + i) * L::ROW, map, full, 0, head, from);
                         }
-                        const int64_t where = max(from, 0) * token_bytes + head * row_bytes + off;
-                        const int valid = from >= 0 ? row_bytes - off : 0;
-                        if (row_bytes % 8 == 0) {
-                            cp_async<8>(to + L::raw_place(r, off), codes + (valid > 0 ? where : 0), valid > 0 ? 8 : 0);
-                        } else {
+                    } else {
+                        const uint8_t* const codes = side == 0 ? a.k_codes : a.v_codes;
+                        constexpr int kPieces = L::ROW / 8;
+#pragma unroll 1
+                        for (int e = lane; e < 32 * kPieces; e += 32) {
+                            const int its_lane = e / kPieces, r = 4 * its_lane + i, off = (e - its_lane * kPieces) * 8, its = __shfl_sync(0xffffffffu, from, its_lane);
+                            const int64_t where = max(its, 0) * token_bytes + head * row_bytes + off;
+                            const int valid = its >= 0 ? row_bytes - off : 0;
+                            if (row_bytes % 8 == 0) {
+                                cp_async<8>(to + L::raw_place(r, off), codes + (valid > 0 ? where : 0), valid > 0 ? 8 : 0);
+                            } else {
 #pragma unroll
-                            for (int i = 0; i < 8; i += 4) cp_async<4>(to + L::raw_place(r, off) + i, codes + (valid > i ? where + i : 0), valid > i ? 4 : 0);
+                                for (int x = 0; x < 8; x += 4) cp_async<4>(to + L::raw_place(r, off) + x, codes + (valid > x ? where + x : 0), valid > x ? 4 : 0);
+                            }
                         }
                     }
-                }
-                if (side == 0) {                                                 // with the keys, all scales
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t entry = static_cast<int64_t>(max(slots[i], 0)) * a.heads + head;
-                        const uint32_t at = rest + (4 * lane + i) * 4 * L::WORDS, there = slots[i] >= 0 ? 4 : 0;
+                    if (side == 0) {                                             // with the keys, all scales
+                        const int64_t entry = static_cast<int64_t>(max(from, 0)) * a.heads + head;
+                        const uint32_t at = rest + (4 * lane + i) * 4 * L::WORDS, there = from >= 0 ? 4 : 0;
+                        uint32_t flag = from >= 0 && t + i >= seg.s.start ? 0x80u : 0u;
                         if (FMT == KV_CACHE_INT8) {
                             cp_async<4>(at, static_cast<const float*>(a.k_scales) + entry, there);
                             cp_async<4>(at + L::V_SCALES, static_cast<const float*>(a.v_scales) + entry, there);
                         } else {
-                            const int64_t first = entry * blocks;
-                            const uint32_t shift = static_cast<uint32_t>(first) & 3u;
-                            flags |= (flags >> (8 * i) & 0x80u ? shift : 0u) << (8 * i);
-                            cp_async<4>(at, static_cast<const uint8_t*>(a.k_scales) + (first - shift), there);
-                            cp_async<4>(at + L::V_SCALES, static_cast<const uint8_t*>(a.v_scales) + (first - shift), there);
+                            const int64_t its_first = entry * blocks;
+                            const uint32_t shift = static_cast<uint32_t>(its_first) & 3u;
+                            if (flag != 0) flag |= shift;
+                            cp_async<4>(at, static_cast<const uint8_t*>(a.k_scales) + (its_first - shift), there);
+                            cp_async<4>(at + L::V_SCALES, static_cast<const uint8_t*>(a.v_scales) + (its_first - shift), there);
                             if (blocks != 4 && blocks != 2) {                    // (bytes of a token may lie across two words)
                                 const uint32_t two = shift + blocks > 4 ? there : 0;
-                                cp_async<4>(at + 4, static_cast<const uint8_t*>(a.k_scales) + (first - shift) + two, two);
-                                cp_async<4>(at + L::V_SCALES + 4, static_cast<const uint8_t*>(a.v_scales) + (first - shift) + two, two);
+                                cp_async<4>(at + 4, static_cast<const uint8_t*>(a.k_scales) + (its_first - shift) + two, two);
+                                cp_async<4>(at + L::V_SCALES + 4, static_cast<const uint8_t*>(a.v_scales) + (its_first - shift) + two, two);
                             }
                         }
+                        smem[L::MORE + slot * L::MORE_BYTES + L::FLAGS + 4 * lane + i] = static_cast<uint8_t>(flag);
                     }
-                    *reinterpret_cast<uint32_t*>(smem + L::MORE + slot * L::MORE_BYTES + L::FLAGS + 4 * lane) = flags;
                 }
                 mbar_arrive(full);
                 cp_async_mbar_arrive(full);                                      // once this lane's own copies are there
