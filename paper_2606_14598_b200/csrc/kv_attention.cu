@@ -641,12 +641,12 @@ bool encode_codes(CUtensorMap* tm, const void* codes, int64_t slots, int64_t hea
 }
 
 // The maps of both sides, and a.box: tokens that lie side by side in any page, from any token that a box starts at; 0 where heads are not whole 16-byte pieces
-bool encode_sides(CUtensorMap (&maps)[2], AttentionArgs& a, int fmt) {
+bool encode_sides(CUtensorMap (&maps)[2], AttentionArgs& a, int fmt, int most) {
     const int per_byte = fmt == KV_CACHE_INT8 ? 1 : 2, row = padded(a.dim) / per_byte, row_bytes = a.dim / per_byte, box_bytes = row < 128 ? row : 128;
     a.box = 0;
     a.box_step = box_bytes;
     if (row_bytes % 16 != 0 || a.num_pages == 0) return true;
-    a.box = 16;
+    a.box = most;
     while (a.page % a.box != 0) a.box /= 2;
     if (a.box * box_bytes % 128 != 0) a.box = 0;                // (a box goes to a 128-byte boundary)
     if (a.box == 0) return true;
@@ -763,10 +763,11 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     const int64_t rows = (total_q * a.group + seqs - 1) / (seqs > 0 ? seqs : 1);       // of a sequence and head, on average
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     CUtensorMap maps[2] = {};
-    if (!encode_sides(maps, a, fmt)) return W8A8_ERR_CUDA;
-    const cudaError_t e = rows > kFewRows && many_rows_fits(a.dim) ? launch_many_rows(fmt, maps[0], maps[1], a, rows, st)
-                          : fmt == KV_CACHE_INT8                   ? launch_for<KV_CACHE_INT8>(maps, a, rows, st)
-                                                                   : launch_for<KV_CACHE_MXFP4>(maps, a, rows, st);
+    const bool many = rows > kFewRows && many_rows_fits(a.dim);
+    if (!encode_sides(maps, a, fmt, many ? kMostBox : padded(a.dim) == 256 ? 16 : 32)) return W8A8_ERR_CUDA;      // (few rows: a step's tokens)
+    const cudaError_t e = many                     ? launch_many_rows(fmt, maps[0], maps[1], a, rows, st)
+                          : fmt == KV_CACHE_INT8 ? launch_for<KV_CACHE_INT8>(maps, a, rows, st)
+                                                 : launch_for<KV_CACHE_MXFP4>(maps, a, rows, st);
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;
 }
 

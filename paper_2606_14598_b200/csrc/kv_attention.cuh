@@ -11,6 +11,7 @@
 namespace w8a8 {
 namespace attention {
 
+constexpr int kMostBox = 64;                    // tokens of a box of codes, at most
 constexpr float kNone = -3e38f;                 // reference of a row that has seen nothing (finite, so that differences are numbers)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -53,7 +54,7 @@ __device__ __forceinline__ Sequence read_sequence(const AttentionArgs& a, int b,
     s.before = max(len, 0) - s.n;
     s.stop = static_cast<int>(min(static_cast<int64_t>(max(len, 0)), most));
     s.start = a.starts != nullptr ? max(0, min(a.starts[b], s.stop)) : 0;
-    s.base = s.start & ~31;
+    s.base = s.start & ~(kMostBox - 1);
     s.tiles = max(1, (s.stop - s.base + TILE - 1) / TILE);
     s.row_tiles = static_cast<int>((static_cast<int64_t>(s.n) * a.group + rows_of_tile - 1) / rows_of_tile);
     return s;

@@ -272,11 +272,22 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 if (left > 1) id = look_up(t0, stop);
                 mbar_wait(empties + 8 * slot, phase, ctl, kWaitMany + 4, kStatusTimeout);
                 const uint32_t full = fulls + 8 * slot, to = raw_at + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
+                if (a.box >= 4) {                                                // boxes that begin with the first token of a lane
+#pragma unroll 1
+                    for (int l = 0; l < 32; l += a.box / 4) {
+                        const int from = __shfl_sync(0xffffffffu, first, l);
+                        if (lane == 0 && from >= 0) {
+                            mbar_expect_tx(full, a.box * L::ROW);
+                            tma_load_3d(to + 4 * l * L::ROW, map, full, 0, head, from);
+                        }
+                    }
+                }
 #pragma unroll 1
                 for (int i = 0; i < 4; ++i) {
+                    if (side == 1 && a.box >= 4) break;                          // (nothing else for values)
                     const int from = i == 0 ? first : t + i >= stop ? -1 : !runs ? slot_of(look_up(t + i, stop), t + i) : first >= 0 ? first + i : -1;
-                    if (a.box > 0) {                                             // boxes that begin with this token
-                        if (from >= 0 && (4 * lane + i) % a.box == 0) {
+                    if (a.box > 0) {
+                        if (a.box < 4 && from >= 0 && i % a.box == 0) {          // smaller boxes
                             mbar_expect_tx(full, a.box * L::ROW);
                             tma_load_3d(to + (4 * lane + i) * L::ROW, map, full, 0, head, from);
                         }
