@@ -609,7 +609,9 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 constexpr int kSmallestRows = 8;                    // rows of the smallest item: the most items, so the most counters
 constexpr int kMostCtas = 4;                        // CTAs on an SM
-constexpr int kFewRows = 16;                        // rows of a sequence and head up to which the kernel of this file is chosen
+// Rows of a sequence and head up to which the kernel of this file is chosen, which reads the cache once for 16 of them; the other's time does not depend on them. 16
+// sequences, 6000 tokens, 8 heads of 128: 32 rows take 73 us here and 85 there in int8, 75 and 77 in 4 bits; 64 rows 136 and 87, 144 and 80.
+constexpr int kFewRows = 32;
 constexpr size_t kAlign = 256;
 
 size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads) {
@@ -619,7 +621,7 @@ size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t he
 int padded(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 // (most_rows: of any sequence and head; more of them need more)
 size_t parts_bytes(int64_t most_rows, int64_t dim) {
-    const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(32, padded(dim)) * sizeof(float);
+    const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(16, padded(dim)) * sizeof(float);
     const size_t many = most_rows > kFewRows ? many_rows_part_bytes(most_rows, dim) : 0;
     return few > many ? few : many;
 }
@@ -685,8 +687,8 @@ cudaError_t launch(const CUtensorMap (&maps)[2], const AttentionArgs& a, cudaStr
 template <int FMT>
 cudaError_t launch_for(const CUtensorMap (&maps)[2], const AttentionArgs& a, int64_t rows, cudaStream_t st) {
     const int dp = padded(a.dim);
-    if (dp == 64) return rows <= 8 ? launch<FMT, 64, 1, 2>(maps, a, st) : rows <= 16 ? launch<FMT, 64, 2, 2>(maps, a, st) : launch<FMT, 64, 4, 2>(maps, a, st);
-    if (dp == 128) return rows <= 8 ? launch<FMT, 128, 1, 2>(maps, a, st) : rows <= 16 ? launch<FMT, 128, 2, 2>(maps, a, st) : launch<FMT, 128, 4, 1>(maps, a, st);
+    if (dp == 64) return rows <= 8 ? launch<FMT, 64, 1, 2>(maps, a, st) : launch<FMT, 64, 2, 2>(maps, a, st);
+    if (dp == 128) return rows <= 8 ? launch<FMT, 128, 1, 2>(maps, a, st) : launch<FMT, 128, 2, 2>(maps, a, st);
     return rows <= 8 ? launch<FMT, 256, 1, 1>(maps, a, st) : launch<FMT, 256, 2, 1>(maps, a, st);
 }
 
