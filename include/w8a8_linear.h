@@ -284,7 +284,7 @@ int int8_sticky_status(int clear, void* stream);
  *                                 (default 2 s; 0 restores the default). Returns the previous value.
  *   int8_debug_set_starve         0: off. 1: the GEMM's producer warp withholds the first pipeline stage of its
  *                                 first tile. 2: the staged activation quantizer's producer withholds its first
- *                                 group of rows. No invalid address is touched and nothing traps: the consumers'
+ *                                 group of rows. With 1 kv_cache_attention's first load (of a warp, of keys) is withheld, too. No invalid address is touched and nothing traps: the consumers'
  *                                 waits run out, the kernel frees what it holds and returns, and the status word
  *                                 reports W8A8_ERR_TIMEOUT. Outputs of such a launch are undefined.
  *                                 Returns the previous mode, -1 for an unknown one.

@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
     const int k_at = L::place(g, L::k_offset(0, c));
     const int v_at[2] = {L::place(2 * c, L::v_offset(0, g)), L::place(2 * c + 1, L::v_offset(0, g))};
 
+    bool gave_up = false;                                           // one of this warp's waits did
     while (u < u_end) {
         Sequence s = read_sequence<kWarps * TOK>(a, b, ROWS);
         while (b + 1 < a.seqs && u - first_of_b >= units_of(a, s)) {            // (sequences without new tokens have no units)
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
             return id >= 0 && id < a.num_pages ? id * a.page + (t - p * a.page) : -1;
         };
         auto issue = [&](int step, int slot, uint32_t load) {
-            if (step < steps) {
+            if (step < steps && !gave_up && !(a.starve != 0 && warp == 0 && load == 0)) {
                 const uint32_t stage = load % STAGES, st = ring_u32 + stage * L::CODES, more = rest_u32 + stage * L::REST, bar = bars + 8 * stage;
                 const uint32_t seen = __ballot_sync(0xffffffffu, slot >= 0 && first_token + step * (kWarps * TOK) + (lane & (TOK - 1)) >= s.start) & kAllSeen;
                 if (a.box > 0) {
@@ -272,12 +273,17 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
 #pragma unroll
             for (int k = 0; k < (NR == 1 ? L::KS : 1); ++k) queries[k] = frags[k * 32 + lane];
         }
-        for (int step = 0; step < steps; ++step, ++loads) {
+        for (int step = 0; step < steps && !gave_up; ++step, ++loads) {
             const int stage = static_cast<int>(loads % STAGES);
             uint8_t* const st = ring + stage * L::CODES;
             const uint8_t* const more = rest + stage * L::REST;
             cp_async_wait<STAGES - 1>();
-            if (a.box > 0) mbar_wait(bars + 8 * stage, loads / STAGES & 1, ctl, kWaitAttention, kStatusTimeout);
+            if (a.box > 0 && !__all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, loads / STAGES & 1, ctl, kWaitAttention, kStatusTimeout))) {
+                // boxes on their way come first, then this warp is done with loads (what it leaves is undefined)
+                for (int i = 0; i < min(STAGES, steps - step); ++i) mbar_drain(bars + 8 * ((loads + i) % STAGES), (loads + i) / STAGES & 1, a.limit_ns);
+                gave_up = true;
+                break;
+            }
             __syncwarp();
             const int slot_now = slot;
             slot = find(step + STAGES + 1);
@@ -528,11 +534,6 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
             issue(step + STAGES, slot_now, loads + STAGES);
         }
         cp_async_wait<0>();
-        if (abort_flag != 0 && a.box > 0) {                         // a wait gave up: the boxes on their way come first
-#pragma unroll
-            for (int i = 1; i <= STAGES; ++i)
-                if (loads >= static_cast<uint32_t>(i)) mbar_drain(bars + 8 * ((loads - i) % STAGES), (loads - i) / STAGES & 1, a.limit_ns);
-        }
 
         // ---- the warps' results meet in shared memory
         __syncthreads();
@@ -762,6 +763,7 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.sticky = sticky_status_word();
     a.limit_ns = wait_limit_ns();
     a.zero_rest = zero_rest ? 1 : 0;
+    a.starve = starve_mode() == kStarveGemm ? 1 : 0;
     const int64_t rows = (total_q * a.group + seqs - 1) / (seqs > 0 ? seqs : 1);       // of a sequence and head, on average
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     CUtensorMap maps[2] = {};

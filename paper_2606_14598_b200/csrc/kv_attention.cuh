@@ -33,6 +33,7 @@ struct AttentionArgs {
     int zero_rest;
     int *status, *sticky;
     uint64_t limit_ns;
+    int starve;                                 // test hook: the first load of every CTA never arrives
 };
 
 // ------------------------------------------------------------------------------------------------ the list of work

@@ -94,6 +94,15 @@ struct Segments {
 
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
+// mbar_wait for roles that walk on to their end when a wait of the CTA has given up: those after it do not wait
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, const WaitCtl& ctl, int where, int status_code) {
+    return *static_cast<volatile int*>(ctl.abort_flag) == 0 && mbar_wait_slow(bar, parity, ctl, where, status_code);
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const WaitCtl& ctl, int where, int status_code) {
+    if (mbar_try_wait(bar, parity)) return true;
+    return wait_slow(bar, parity, ctl, where, status_code);
+}
+
 // Elements first to first + 7 of row r of a tile: where their 16 bytes are
 __device__ __forceinline__ uint32_t place(int r, int first) { return (first >> 6) * (kTok * 128) + r * 128 + ((((first >> 3) & 7) ^ (r & 7)) << 4); }
 
@@ -196,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             auto scores = [&](auto which) {
                 constexpr uint32_t w = decltype(which)::value;
                 if (!PAIR || w == 0) {
-                    mbar_wait(bar(K_FULL, k_at.slot), k_at.phase, ctl, kWaitMany + 1, kStatusTimeout);
+                    wait(bar(K_FULL, k_at.slot), k_at.phase, ctl, kWaitMany + 1, kStatusTimeout);
                     tc_fence_after();
                 }
                 const uint32_t q = k_lo + (L::Q + (PAIR ? w * L::TILE : 0)) / 16, k = k_lo + k_at.slot * (L::TILE / 16);
@@ -213,8 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             };
             auto values = [&](auto which, bool first) {
                 constexpr uint32_t w = decltype(which)::value;
-                if (!PAIR || w == 0) mbar_wait(bar(V_FULL, v_at.slot), v_at.phase, ctl, kWaitMany + 2, kStatusTimeout);
-                mbar_wait(bar(P_FULL, w), p_phase[w], ctl, kWaitMany + 3, kStatusTimeout);
+                if (!PAIR || w == 0) wait(bar(V_FULL, v_at.slot), v_at.phase, ctl, kWaitMany + 2, kStatusTimeout);
+                wait(bar(P_FULL, w), p_phase[w], ctl, kWaitMany + 3, kStatusTimeout);
                 p_phase[w] ^= 1;
                 tc_fence_after();
                 const uint32_t v = v_lo + v_at.slot * (L::TILE / 16);
@@ -230,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             const std::integral_constant<uint32_t, 1> one{};
             while (seg.next()) {
                 const int jobs = PAIR ? 2 * seg.tiles : seg.tiles;
-                mbar_wait(bar(Q_FULL, 0), segments & 1, ctl, kWaitMany, kStatusTimeout);
+                wait(bar(Q_FULL, 0), segments & 1, ctl, kWaitMany, kStatusTimeout);
                 ++segments;
                 scores(zero);
                 if (jobs > 1) scores(one);
@@ -254,24 +263,36 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         const int64_t token_bytes = static_cast<int64_t>(a.heads) * row_bytes;
         const bool runs = a.page % 4 == 0;                                       // a lane's tokens lie side by side
         const int side = warp - kLoadWarp;
-        const uint32_t raws = side == 0 ? L::RAW_KEYS : L::RAW_VALUES, units = static_cast<uint32_t>(share.end - share.begin);
+        const uint32_t raws = side == 0 ? L::RAW_KEYS : L::RAW_VALUES;
         const uint32_t fulls = bar(side == 0 ? RAW_K_FULL : RAW_V_FULL, 0), empties = bar(side == 0 ? RAW_K_EMPTY : RAW_V_EMPTY, 0), raw_at = base + (side == 0 ? L::RAW : L::RAW_V);
         const void* const map = side == 0 ? &k_map : &v_map;
         int64_t table_of = 0;
         auto look_up = [&](int t, int stop) { return t < stop ? a.table[table_of + (a.page_shift >= 0 ? t >> a.page_shift : t / a.page)] : -1; };
         auto slot_of = [&](int id, int t) { return id >= 0 && id < a.num_pages ? id * a.page + (a.page_shift >= 0 ? t & (a.page - 1) : t % a.page) : -1; };
         uint32_t slot = 0, phase = 1, unit = 0;
-        while (seg.next()) {
+        bool going = true;
+        while (going && seg.next()) {
             table_of = seg.b * a.table_stride;
             const int stop = seg.s.stop, head = seg.head;
             int t0 = seg.token(0) + 4 * lane, id = look_up(t0, stop);            // (of the first of a lane's tokens, a tile ahead)
 #pragma unroll 1
-            for (int left = seg.tiles; left > 0; --left, ++unit) {
+            for (int left = seg.tiles; left > 0; --left) {
                 const int t = t0, first = slot_of(id, t);
                 t0 += kTok;
                 if (left > 1) id = look_up(t0, stop);
-                mbar_wait(empties + 8 * slot, phase, ctl, kWaitMany + 4, kStatusTimeout);
+                // (once a wait of the CTA has given up, slots are called empty that are not)
+                going = __all_sync(0xffffffffu, wait(empties + 8 * slot, phase, ctl, kWaitMany + 4, kStatusTimeout) && *static_cast<volatile int*>(&abort_flag) == 0);
+                if (!going) break;
                 const uint32_t full = fulls + 8 * slot, to = raw_at + slot * kTok * L::ROW, rest = base + L::MORE + slot * L::MORE_BYTES;
+                const uint32_t its_slot = slot;
+                if (++slot == raws) {
+                    slot = 0;
+                    phase ^= 1;
+                }
+                if (unit++ == 0 && a.starve != 0 && side == 0) {
+                    going = false;
+                    break;
+                }
                 if (a.box >= 4) {                                                // boxes that begin with the first token of a lane
 #pragma unroll 1
                     for (int l = 0; l < 32; l += a.box / 4) {
@@ -326,21 +347,17 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 cp_async<4>(at + L::V_SCALES + 4, static_cast<const uint8_t*>(a.v_scales) + (its_first - shift) + two, two);
                             }
                         }
-                        smem[L::MORE + slot * L::MORE_BYTES + L::FLAGS + 4 * lane + i] = static_cast<uint8_t>(flag);
+                        smem[L::MORE + its_slot * L::MORE_BYTES + L::FLAGS + 4 * lane + i] = static_cast<uint8_t>(flag);
                     }
                 }
                 mbar_arrive(full);
                 cp_async_mbar_arrive(full);                                      // once this lane's own copies are there
-                if (++slot == raws) {
-                    slot = 0;
-                    phase ^= 1;
-                }
             }
         }
         // nothing is on its way when the CTA goes: what was asked for has been waited for by those who convert it, unless a wait gave up
-        if (abort_flag != 0) {
+        if (!going || abort_flag != 0) {
             asm volatile("cp.async.wait_all;" ::: "memory");
-            for (uint32_t last = units > raws ? units - raws : 0; last < units; ++last) mbar_drain(fulls + 8 * (last % raws), last / raws & 1, a.limit_ns);
+            for (uint32_t last = unit > raws ? unit - raws : 0; last < unit; ++last) mbar_drain(fulls + 8 * (last % raws), last / raws & 1, a.limit_ns);
         }
     } else if (warp >= kKeyWarp) {
         // ---- codes to fp16 tiles, keys by four warps and values by four: a thread has a chunk of 16 bytes of every PASS-th token (PASS is a multiple of 8, so that its
@@ -368,6 +385,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     if (mul != 0x3c003c00u) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], mul);
+                        if (static_cast<int>(mul) < 0)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) f[j] = mul_f16x2(f[j], 0x84008400u);
                     }
                     store_16(to[0] + at, f[0], f[1], f[2], f[3]);
                     store_16(to[1] + at, f[4], f[5], f[6], f[7]);
@@ -390,14 +410,14 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             uint32_t segments = 0;
             while (seg.next()) {
                 int sigma = -126;                                                // the values' reference starts anew with each segment
-                mbar_wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
+                wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
                 ++segments;
                 const float factor = reinterpret_cast<const volatile float*>(smem + L::FACTOR)[0];
                 for (int left = seg.tiles; left > 0; --left, ++t) {
                     const uint32_t slot = t & (kSlots - 1);
-                    mbar_wait(bar(RAW_K_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                    wait(bar(RAW_K_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
                     // (the products of two tiles back are done, so those of four back with their values: nobody reads this slot of the factors)
-                    mbar_wait(bar(K_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                    wait(bar(K_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
                     // scales: a thread a token
                     int word;                                                    // this warp's: the largest exponent of a value's scale, and what is special
                     const uint8_t* const rest = smem + L::MORE + raw.slot * L::MORE_BYTES;
@@ -427,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         if (in) top_sigma = max(-126, static_cast<int>(max(v_top & 0xffu, v_top >> 8 & 0xffu)) - 127);
                         reinterpret_cast<uint32_t*>(k_scales)[(t & 1) * kTok + me] = in ? kb : 0u;
                         nans[slot * kTok + me] = static_cast<uint8_t>((v_nan & 1u) | (v_nan >> 7 & 2u) | (v_nan >> 14 & 4u) | (v_nan >> 21 & 8u));
-                        reinterpret_cast<uint32_t*>(v_scales)[slot * kTok + me] = vb & ~v_nan;
+                        reinterpret_cast<uint32_t*>(v_scales)[slot * kTok + me] = in ? vb & ~v_nan : 0u;        // (those not seen may be above what is seen: finite is what matters)
                     }
                     k_factor *= factor;
                     factors[slot * kTok + me] = in ? k_factor : -1.f;
@@ -449,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     if (me == 0) {
                         sigmas[slot] = sigma;
                         special[slot] = all;
-                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23), 1.2e-38f);
+                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fminf(fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23), 1.2e-38f), 3e38f);   // (0 and infinity are no factors of -infinity and 0)
                     }
                     if (lane == 0) mbar_arrive(bar(SCALES_FULL, slot));
                     const uint32_t from = L::RAW + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
@@ -474,17 +494,18 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             for (const uint32_t units = static_cast<uint32_t>(share.end - share.begin); t < units; ++t) {
                 // values: times their scale over 2^sigma, brought to 2^15 at most
                 const uint32_t slot = t & (kSlots - 1);
-                mbar_wait(bar(SCALES_FULL, slot), t / kSlots & 1, ctl, kWaitMany + 11, kStatusTimeout);
+                wait(bar(SCALES_FULL, slot), t / kSlots & 1, ctl, kWaitMany + 11, kStatusTimeout);
                 const int sigma = sigmas[slot];
-                mbar_wait(bar(RAW_V_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
-                mbar_wait(bar(V_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
+                wait(bar(RAW_V_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
+                wait(bar(V_EMPTY, ring.slot), ring.phase ^ 1, ctl, kWaitMany + 6, kStatusTimeout);
                 const uint32_t from = L::RAW_V + raw.slot * kTok * L::ROW, tile = L::V_TILES + ring.slot * L::TILE;
                 if constexpr (FMT == KV_CACHE_INT8) {
                     // (two factors, as 2^(8 - sigma) alone may be more than fp32 holds)
                     const float by0 = __uint_as_float(static_cast<uint32_t>(127 - sigma / 2) << 23), by1 = __uint_as_float(static_cast<uint32_t>(127 + 8 - (sigma - sigma / 2)) << 23);
                     convert(from, tile, [&](int r) {
                         const float by = reinterpret_cast<const float*>(v_scales)[slot * kTok + r] * by0 * by1;
-                        return pack_f16(by, by);
+                        // (where fp16 holds only part of it, in two steps: 2^14 times as much, negative, then times -2^-14)
+                        return by >= 0x1p-14f ? pack_f16(by, by) : pack_f16(by * -0x1p14f, by * -0x1p14f);
                     });
                 } else {
                     convert(from, tile, [&](int r) {                             // 2^12 * 2^(byte - 127 - sigma), subnormal from e = 0 down
@@ -567,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
 #pragma unroll 1
             for (int t = PAIR ? 0 : w; t < seg.tiles; t += PAIR ? 1 : 2, ++jobs) {
                 const uint32_t slot = (tile_base + t) & (kSlots - 1);
-                mbar_wait(bar(S_FULL, w), jobs & 1, ctl, kWaitMany + 7, kStatusTimeout);
+                wait(bar(S_FULL, w), jobs & 1, ctl, kWaitMany + 7, kStatusTimeout);
                 tc_fence_after();
                 if (warp_live) {
                     const float* kf = factors + slot * kTok;
@@ -640,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         l2 = mul2(l2, pack2(by_l, by_l));
                         if (!first) {
                             const float half = ex2(static_cast<float>(max(sigma - its_sigma, -252)) * 0.5f), by = by_l * half * half;
-                            mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 8, kStatusTimeout);
+                            wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 8, kStatusTimeout);
                             tc_fence_after();
 #pragma unroll 1
                             for (int ch = 0; ch < DP / 16; ++ch) {
@@ -702,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             l += other;
             // (reference of o with the values' in it: int8 tiles are 2^8 too large, 4-bit ones 2^12, which the results take account of)
             float m_o = m + static_cast<float>(sigma - (FMT == KV_CACHE_INT8 ? 8 : 0)), m_l = m;
-            if (PAIR || w < seg.tiles) mbar_wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 9, kStatusTimeout);
+            if (PAIR || w < seg.tiles) wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 9, kStatusTimeout);
             if (!PAIR) *reinterpret_cast<float4*>(state + (w * kRows + row) * 4) = make_float4(m_o, m, l, __uint_as_float(poison));
             named_sync(2, kSoftmax);
             tc_fence_after();

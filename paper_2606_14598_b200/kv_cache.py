@@ -320,7 +320,8 @@ def kv_cache_attention(cache: QuantKVCache, q: torch.Tensor, table: torch.Tensor
         workspace = kv_cache_attention_workspace(c, seqs, total, heads)
     elif not workspace.is_contiguous():
         raise TypeError("workspace: dense tensor expected")
-    if any(t is not None and t.get_device() != dev for t in (table, lens, cu_q, starts, tree, lse, workspace)):
+    if (table.get_device() != dev or lens.get_device() != dev or cu_q.get_device() != dev or workspace.get_device() != dev or (starts is not None and starts.get_device() != dev) or
+            (tree is not None and tree.get_device() != dev) or (lse is not None and lse.get_device() != dev)):
         raise different_devices("kv_cache_attention")
     if total > 0 and (seqs > 0 or fill):
         call(_lib.kv_cache_attention, "kv_cache_attention", dev, c.fmt | (KV_CACHE_ZERO_REST if fill else 0), kc, ks, vc, vs, c.num_pages, c.page_size, c.heads, c.dim,

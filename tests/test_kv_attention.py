@@ -149,6 +149,9 @@ class Case:
             off = (torch.einsum("nhgd,phd->nhgp", q.abs(), k.abs()) * abs(scale) * (self.dim + 8) * 2.0 ** -23)
             if self.fmt == "mxfp4":
                 off = off + torch.einsum("nhgd,ph->nhgp", q.abs(), units[0]) * abs(scale) * 6 * 2.0 ** -27
+                # many rows: the unit is the largest of 128 tokens, at 2^12 in fp16, where a block's factor of 2^-25, 2^-37 of it, counts as zero; an element is 6 at most
+                if self.lengths[b]:
+                    off = off + (q.abs().sum(-1) * units[0].amax(0)[None, :, None])[..., None] * abs(scale) * 6 * 2.0 ** -37
             hidden = ~see[:, None, None]
             s = s.masked_fill(hidden, -INF)
             top = s.amax(-1, keepdim=True)
@@ -259,6 +262,49 @@ def test_pages_windows_and_empty_sequences(fmt, page, dim):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("page", [1, 2, 3, 4, 8, 16, 32, 64, 100, 192])
+@pytest.mark.parametrize("heads,group,dim", [(2, 5, 128), (1, 9, 64), (2, 12, 80)])
+def test_pages_and_windows_of_many_rows(fmt, page, heads, group, dim):
+    """Rows beyond a few, and beyond one tile of rows, with pages of all sizes; windows that begin anywhere, empty sequences among them."""
+    c = Case(fmt, heads, group, dim, [330, 0, 64, 9, 515], [29, 0, 7, 9, 40], page=page, seed=page, tree=page % 3 == 0)
+    c.check()
+    c.starts = torch.tensor([31, 0, 63, 9, 190], dtype=torch.int32, device="cuda")
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 2), (2, 8), (4, 8), (3, 11), (4, 32), (4, 33), (8, 61), (1, 300)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_either_side_of_the_choices(fmt, group, new, dim):
+    """Rows around those at which another kernel, or another form of it, is chosen."""
+    Case(fmt, 2, group, dim, [new + 200, new, new + 1000], [new] * 3, page=64, seed=new, tree=True).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 1), (4, 4), (4, 20), (8, 40)])
+def test_wait_runs_out_and_the_kernel_returns(fmt, group, new):
+    c = Case(fmt, 2, group, 128, [900, 300], [new, new], page=64, seed=30)
+    ws = w8.kv_cache_attention_workspace(c.cache, 2, 2 * new, 2 * group)
+    run = lambda: w8.kv_cache_attention(c.cache, c.q, c.table, c.lens, c.cu, workspace=ws)
+    want = run()
+    assert w8.int8_check_status(ws) == 0
+    try:
+        w8.debug_set_wait_limit_ns(3_000_000)
+        w8.debug_set_starve(1)
+        run()
+        assert w8.int8_check_status(ws) == 7 and w8.int8_sticky_status() == 7
+    finally:
+        w8.debug_set_starve(0)
+        w8.debug_set_wait_limit_ns(0)
+        w8.int8_sticky_status(clear=True)
+    again = run()
+    assert w8.int8_check_status(ws) == 0 and torch.equal(again, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
 def test_pages_outside_the_cache(fmt):
     """Such tokens are not seen (and nothing is read for them): unset pages, ids past the cache, tokens past the table."""
     c = Case(fmt, 2, 2, 64, [160, 90], [2, 2])
@@ -272,10 +318,11 @@ def test_pages_outside_the_cache(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
-def test_nan_reaches_those_who_see_it(fmt):
+@pytest.mark.parametrize("group", [4, 16, 40])
+def test_nan_reaches_those_who_see_it(fmt, group):
     """NaN scales behind the end of a sequence, in other branches of a tree and outside a window reach nobody; those that are seen do, a block of
     a value its own elements only."""
-    c = Case(fmt, 2, 4, 128, [83, 64], [6, 3], tree=True, seed=5)
+    c = Case(fmt, 2, group, 128, [83, 64], [6, 3], tree=True, seed=5)
     bad = NAN if fmt == "int8" else 255
 
     def slot(b, t):
@@ -301,10 +348,10 @@ def test_nan_reaches_those_who_see_it(fmt):
             page, at = slot(0, t)
             c.cache.v_codes[page, at] = 0
     got = c.check()
-    assert bool(torch.isnan(got[2]).all()) and bool(torch.isnan(got[4, 4:]).all())
-    assert not bool(torch.isnan(got[[0, 1, 3]]).any()) and not bool(torch.isnan(got[4, :4]).any())
+    assert bool(torch.isnan(got[2]).all()) and bool(torch.isnan(got[4, group:]).all())
+    assert not bool(torch.isnan(got[[0, 1, 3]]).any()) and not bool(torch.isnan(got[4, :group]).any())
     if fmt == "mxfp4":
-        assert bool(torch.isnan(got[5, :4, 64:96]).all()) and bool(torch.isnan(got[6:, 4:, 96:]).all()) and not bool(torch.isnan(got[6:, :4]).any())
+        assert bool(torch.isnan(got[5, :group, 64:96]).all()) and bool(torch.isnan(got[6:, group:, 96:]).all()) and not bool(torch.isnan(got[6:, :group]).any())
     c.starts = torch.tensor([0, 21], dtype=torch.int32, device="cuda")
     got = c.check()
     assert not bool(torch.isnan(got[6:]).any())
@@ -312,10 +359,11 @@ def test_nan_reaches_those_who_see_it(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
-def test_scales_far_apart(fmt):
+@pytest.mark.parametrize("group", [4, 32, 130])
+def test_scales_far_apart(fmt, group):
     """Keys and values of very different sizes, from token to token and (4 bits) block to block; the softmax is nearly one token in one case, nearly flat in
     the other; tokens whose values are zero keep their weight."""
-    c = Case(fmt, 2, 4, 128, [500, 77], [3, 1], tree=False, seed=6)
+    c = Case(fmt, 2, group, 128, [500, 77], [3, 1], tree=False, seed=6)
     if fmt == "int8":
         c.cache.v_scales.mul_(torch.exp2(torch.randint(-90, 90, c.cache.v_scales.shape, generator=c.gen, device="cuda").float()))
         c.cache.v_codes[::3] = 0
@@ -334,8 +382,9 @@ def test_scales_far_apart(fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
-def test_queries_of_any_size(fmt):
-    c = Case(fmt, 1, 8, 128, [90], [4], seed=8)
+@pytest.mark.parametrize("group", [8, 16, 40])
+def test_queries_of_any_size(fmt, group):
+    c = Case(fmt, 1, group, 128, [90], [4], seed=8)
     c.q *= torch.exp2(torch.randint(-100, 3, c.q.shape[:2], generator=c.gen, device="cuda"))[..., None].to(torch.bfloat16)
     c.q[0, 0] = 0
     c.q[1, 3, 7] = NAN
