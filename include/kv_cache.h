@@ -97,12 +97,14 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  *   tree        int64 [total_q, tree_words] or NULL
  *   workspace   device scratch of kv_cache_attention_workspace_bytes(), 256-byte aligned; its first kv_cache_attention_zeroed_bytes() bytes must be zero
  *               before the first call that uses it, and each call leaves them zero. Two calls that may overlap on the device need distinct workspaces.
- * The cache must have both sides, scales that are not negative and 4-byte aligned; num_pages * page_size <= 2^31 - 1; q_heads a multiple of heads. Scores, softmax
+ *               A wait that runs out shows in its first word (int8_check_status) and in the sticky status.
+ * The cache must have both sides, scales that are not negative and 4-byte aligned; num_pages * page_size <= 2^31 - 1, max_pages * page_size <= 2^31 - 4096; q_heads a
+ * multiple of heads. Scores, softmax
  * and sums are fp32; for the product with the values, probability times the token's value scale (MXFP4: that of its largest block) is rounded to fp16, relative to the
- * row's own size; where a sequence and head have more than 16 rows of queries, it is the probability that is, and values are rounded to fp16 relative to the sequence's
- * largest scale. Repeated calls give the same bits. What lies far below its neighbours may count as zero: elements of a query 2^-38 below its largest, MXFP4 blocks
+ * row's own size; with many rows of queries (more than 32 a sequence and head on average, heads of at most 128 elements), it is the probability that is, and values are
+ * rounded to fp16 relative to the sequence's largest scale. Repeated calls give the same bits. What lies far below its neighbours may count as zero: elements of a query 2^-38 below its largest, MXFP4 blocks
  * 2^-27 below the largest of their head and token, tokens whose probability is 2^-110, or whose product with the value's scale is 2^-31, of the row's largest
- * (more than 16 rows: whose probability is 2^-31, or whose value's scale 2^-32 of the sequence's largest).
+ * (many rows: MXFP4 blocks of keys 2^-37 below the largest of 128 tokens, tokens whose probability is 2^-31, or whose value's scale 2^-32 of the sequence's largest).
  */
 size_t kv_cache_attention_workspace_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);
 size_t kv_cache_attention_zeroed_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);

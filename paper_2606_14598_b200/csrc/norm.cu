@@ -4,7 +4,8 @@
 //   int8: t = max |u|, c = t / 127, q = rne(u / c), s = c * r          bf16: y = bf16(u * r)
 //
 // The norm is one factor of the row, so it cancels out of the codes: the sum of squares and the largest |u| are found in one pass over
-// the row, which then sits in registers as u and is written from there. One trip through HBM: 4 bytes an element in, 3 or 4 out.
+// the row, which then sits in registers as u and is written from there. One trip through HBM: 4 bytes an element in, 3 or 4 out, which is what bounds it: 8221 rows
+// of 12288 in bf16 take 131 us (123 at the copy's rate), 4110 of 4608 in int8 28 us (20; one wave and a half of CTAs, whose ends show), one row of 4608 3.5 us.
 #include "../../include/int8_norm.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"
@@ -200,9 +201,11 @@ int run_norm(const NormArgs& a, bool w16, cudaStream_t st) {
         const auto kern = res ? (w16 ? norm_long_kernel<true, true> : norm_long_kernel<true, false>) : (w16 ? norm_long_kernel<false, true> : norm_long_kernel<false, false>);
         e = launch_pdl(kern, dim3(static_cast<unsigned>(a.M)), kMaxThreads, st, a);
     } else {
-        const int vpt = vecs <= 256 ? 1 : vecs <= 512 ? 2 : 3;
+        // three vectors a thread, all on their way at once, are the best of 1, 2, 3, 4 and 6 from 449 vectors a row up (4110 rows of 4608: 36, 30, 28, 29 and 31 us; of
+        // 12288: 99, 99, 69, 71 and 67), two up to 256 (of 2048: 16.6, 15.7, 16.1)
+        const int vpt = vecs <= 256 ? 2 : 3;
         const int per_row = ((vecs + vpt - 1) / vpt + 31) / 32 * 32, rows = per_row >= 256 ? 1 : 256 / per_row;
-        const auto kern = vpt == 1 ? norm_variant<1>(res, w16) : vpt == 2 ? norm_variant<2>(res, w16) : norm_variant<3>(res, w16);
+        const auto kern = vpt == 2 ? norm_variant<2>(res, w16) : norm_variant<3>(res, w16);
         e = launch_pdl(kern, dim3(static_cast<unsigned>((a.M + rows - 1) / rows)), rows * per_row, st, a, per_row);
     }
     return e == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA;

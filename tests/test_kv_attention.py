@@ -28,6 +28,7 @@ def test_refusals():
         assert status(**{name: None}) == INVALID, name
     assert status(fmt=2) == INVALID and status(heads=0) == INVALID and status(dim=264) == INVALID and status(page=0) == INVALID and status(num_pages=-1) == INVALID
     assert status(num_pages=1 << 28) == INVALID                                       # slots past 32 bits
+    assert status(max_pages=1 << 27, stride=1 << 27) == INVALID                       # tokens of a sequence past 32 bits
     assert status(stride=2) == INVALID and status(seqs=-1) == INVALID and status(total=-1) == INVALID and status(q_heads=7) == INVALID and status(q_heads=0) == INVALID
     assert status(words=0) == INVALID and status(scale=NAN) == INVALID and status(scale=INF) == INVALID
     assert status(dim=60) == ALIGNMENT
