@@ -1,14 +1,15 @@
 """B200-native fused W8A8 linear layer: per-token int8 activations x per-channel int8 weights,
 int32 accumulation on the tensor cores, dequantization and bias in the GEMM epilogue. Beside it the
-4-bit form of the same layer (MXFP4 weights and activations, ``mxfp4``) and a paged cache that keeps
-keys and values in int8 or MXFP4 (``kv_cache``).
+4-bit form of the same layer (MXFP4 weights and activations, ``mxfp4``), a norm that makes a linear's
+input (``norm``), and a paged cache that keeps keys and values in int8 or MXFP4, appends to it with a
+rotation by position, and attends over its codes (``kv_cache``).
 
 The compute lives in ``libw8a8_linear.so`` (CUDA, sm_100a; C ABI in ``include/w8a8_linear.h``);
 ``binding`` is the thin ctypes layer over it. The helper modules ``inputs`` (seeded synthetic
 tensors), ``roofline`` (work and byte model) and ``dist`` (multi-rank plumbing) hold none of the
 method's arithmetic and do not need the CUDA library: importing them, or this package, maps no
 native code. The library is loaded the first time a compute entry point (any name exported by
-``binding``, ``mxfp4`` or ``kv_cache``) is touched, and that raises if it has not been built: there is no CPU fallback.
+``binding``, ``mxfp4``, ``norm`` or ``kv_cache``) is touched, and that raises if it has not been built: there is no CPU fallback.
 """
 from __future__ import annotations
 
