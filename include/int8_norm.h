@@ -31,6 +31,7 @@ enum { INT8_NORM_FP32 = 0, INT8_NORM_BF16 = 1 }; /* type of the weight */
  *   sum_out    out  bf16 [M,K], row stride lds: h; may be x or residual itself (same address and stride); NULL if not wanted
  *   qa, s_tok  out  int8 [M,K] dense and fp32 [M], or both NULL
  *   y          out  bf16 [M,K], row stride ldy, or NULL; one of qa and y is needed, both are fine
+ * Outputs overlap neither one another nor, but for sum_out, an input.
  * Strides in elements, multiples of 8, at least K; K % 8 == 0 (the int8 linear wants K % 16 == 0), 0 < K <= INT8_NORM_K_MAX; x, residual,
  * weight, sum_out, qa and y 16-byte aligned; eps > 0 and finite. M == 0 is a valid call.
  */

@@ -62,7 +62,7 @@ int kv_cache_read(int fmt, const void* k_codes, const void* k_scales, const void
  *     a' = a * c - b * s,  b' = b * c + a * s           fp32: two products and a sum, each rounded once
  * of the elements (a, b) = (2i, 2i + 1) if interleaved, else (i, i + rot / 2); elements from rot on stay as they are.
  *   q_out = bf16(q'), the cache gets k' (not rounded to bf16 in between) and v as kv_cache_write would store them.
- *   q, q_out    bf16 [tokens, q_heads, dim] with their strides; both NULL for none; q_out may be q itself
+ *   q, q_out    bf16 [tokens, q_heads, dim] with their strides; both NULL for none; q_out may be q itself (with its strides)
  *   cos_sin     fp32 [num_positions, rot] dense, 16-byte aligned, or NULL: nothing is rotated (positions and axes are not read)
  *   rot         a multiple of 8, at most dim
  *   positions   int64 [axes, tokens], rows position_stride apart; a position outside the table makes its pairs NaN
@@ -91,12 +91,14 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  *                 ancestors (and itself, where its own bit is set); new tokens from 64 * tree_words on are not seen
  * Query head h reads the keys and values of head h / (q_heads / heads). A query that sees nothing gets zeros and a logarithm of -inf. A token whose page
  * is outside the cache or past the table is not seen. NaN keys and values (their scale is NaN) reach the queries that see them, and no others.
- *   q, out      bf16 [total_q, q_heads, dim] with their strides; rows of no sequence as for kv_cache_read (KV_CACHE_ZERO_REST)
+ *   q, out      bf16 [total_q, q_heads, dim] with their strides; rows of no sequence as for kv_cache_read (KV_CACHE_ZERO_REST); out and lse overlap no input (a
+ *               row of queries is read by several CTAs, at different times)
  *   lse         fp32 [total_q, q_heads]: log(sum_p exp(scale * q . k_p)), or NULL
  *   table       int32 [seqs, max_pages];  lens, starts int32 [seqs] (starts may be NULL: from the first);  cu_q int32 [seqs + 1], not decreasing
  *   tree        int64 [total_q, tree_words] or NULL
  *   workspace   device scratch of kv_cache_attention_workspace_bytes(), 256-byte aligned; its first kv_cache_attention_zeroed_bytes() bytes must be zero
- *               before the first call that uses it, and each call leaves them zero. Two calls that may overlap on the device need distinct workspaces.
+ *               before the first call that uses it, and each call leaves them zero. One workspace, given with its whole size, serves calls with fewer
+ *               sequences and rows too, in any order, if what the largest needs to be zero was. Two calls that may overlap on the device need distinct workspaces.
  *               A wait that runs out shows in its first word (int8_check_status) and in the sticky status.
  * The cache must have both sides, scales that are not negative and 4-byte aligned; num_pages * page_size <= 2^31 - 1, max_pages * page_size <= 2^31 - 4096; q_heads a
  * multiple of heads. Scores, softmax

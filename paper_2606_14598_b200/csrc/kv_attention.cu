@@ -628,7 +628,7 @@ int padded(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 size_t parts_bytes(int64_t most_rows, int64_t dim) {
     const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(16, padded(dim)) * sizeof(float);
     const size_t many = most_rows > kFewRows ? many_rows_part_bytes(most_rows, dim) : 0;
-    return few > many ? few : many;
+    return ((few > many ? few : many) + kAlign - 1) / kAlign * kAlign;
 }
 bool sizes_fine(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
     return seqs >= 0 && seqs < INT32_MAX && total_q >= 0 && total_q <= INT32_MAX && heads > 0 && q_heads > 0 && q_heads <= KV_CACHE_MAX_WIDTH && q_heads % heads == 0 && dim > 0 &&
@@ -745,7 +745,8 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.out = static_cast<__nv_bfloat16*>(out);
     a.lse = lse;
     a.counters = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + kAlign);          // behind the status word
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + counters_bytes(seqs, total_q, q_heads, heads));
+    // parts at the end of what is given, so that a call with fewer sequences leaves alone what must be zero for one with more
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + workspace_bytes / kAlign * kAlign - parts_bytes(total_q * (q_heads / heads), dim));
     a.q_st = q_token_stride;
     a.q_sh = q_head_stride;
     a.o_st = out_token_stride;

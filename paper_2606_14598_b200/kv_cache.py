@@ -314,6 +314,8 @@ def kv_cache_attention(cache: QuantKVCache, q: torch.Tensor, table: torch.Tensor
     if fill:
         out = torch.empty(total, heads, c.dim, dtype=torch.bfloat16, device=c.device)
     op, ot, oh = _vectors(c, out, "out", total, heads)
+    if op == qp and total > 0:
+        raise ValueError("out: must not be q (a row of queries is read by several CTAs, at different times)")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (total, heads) or not lse.is_contiguous()):
         raise TypeError(f"lse: dense fp32 [{total}, {heads}] expected")
     if workspace is None:

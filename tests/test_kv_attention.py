@@ -61,7 +61,7 @@ def test_python_refusals():
     for kw in ({"tree": tree.int()}, {"tree": tree[:, 0]}, {"starts": lens.long()}, {"lse": torch.zeros(3, 2)}):
         with pytest.raises(TypeError):
             call(c, q, table, lens, cu, **kw)
-    for kw in ({"tree": tree[:2]}, {"out": q[:2]}, {"tree": tree[:, :0]}):
+    for kw in ({"tree": tree[:2]}, {"out": q[:2]}, {"out": q}, {"tree": tree[:, :0]}):
         with pytest.raises(ValueError):
             call(c, q, table, lens, cu, **kw)
     with pytest.raises(ValueError):
@@ -280,6 +280,20 @@ def test_pages_and_windows_of_many_rows(fmt, page, heads, group, dim):
 def test_either_side_of_the_choices(fmt, group, new, dim):
     """Rows around those at which another kernel, or another form of it, is chosen."""
     Case(fmt, 2, group, dim, [new + 200, new, new + 1000], [new] * 3, page=64, seed=new, tree=True).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("heads,group,new", [(2, 4, 1), (2, 8, 9), (1, 8, 40)])
+def test_one_workspace_for_all_sizes(fmt, heads, group, new):
+    """Calls of few and of many sequences and rows take turns on a workspace made for the largest; parts of sequences that CTAs share lie in it."""
+    many = Case(fmt, heads, group, 128, [700 + 40 * i for i in range(60)], [new] * 60, page=16, seed=40)
+    few = Case(fmt, heads, group, 128, [9000, 5000], [1, new], page=16, seed=41)
+    ws = w8.kv_cache_attention_workspace(many.cache, 60, many.total, heads * group)
+    for c in (many, few, many, few, few, many):
+        c.check(workspace=ws)
+    zeroed = kv_cache._lib.kv_cache_attention_zeroed_bytes(60, many.total, heads * group, heads, 128)
+    assert not bool(ws[:zeroed].any()) and w8.int8_check_status(ws) == 0
 
 
 @pytest.mark.gpu
