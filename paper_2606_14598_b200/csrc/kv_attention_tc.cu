@@ -540,29 +540,44 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             const int r = (PAIR ? w * kRows : 0) + row;                          // of the item's rows
             const bool live = r < seg.rows, warp_live = (PAIR ? w * kRows : 0) + 32 * (warp & 3) < seg.rows;
             const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group;
-            // queries: all on their way into their places at once, then a power of two that brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes
-            // a row; a thread converts what it copied.
+            // queries: a power of two brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes a row; all rows are on their way at once, those of one tile of
+            // rows in registers, those of two by way of the places that they go to (twice through registers costs 10 us).
             {
-                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PER_WARP = ROWS / 8;
+                constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, STEPS = ROWS / 8 / AT_ONCE;
                 const int d = lane % LANES * 8;
-                auto row_of = [&](int i) { return warp * PER_WARP + i + lane / LANES; };
+                uint4 x[PAIR ? 1 : STEPS] = {};
+                auto row_of = [&](int i) { return (warp * STEPS + i) * AT_ONCE + lane / LANES; };
                 auto place_of = [&](int i) { return base + L::Q + (row_of(i) / kRows) * L::TILE + place(row_of(i) % kRows, d); };
-                auto read = [&](int i) {
-                    uint4 x;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(place_of(i)) : "memory");
-                    return x;
-                };
-#pragma unroll 1
-                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+                auto from = [&](int i, bool& valid) {
                     const int q_row = row_of(i), its = (seg.row0 + q_row) / a.group, its_head = seg.head * a.group + (seg.row0 + q_row) - its * a.group;
-                    const bool valid = q_row < seg.rows && d < a.dim;
-                    cp_async<16>(place_of(i), a.q + (valid ? static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d : 0), valid ? 16 : 0);
+                    valid = q_row < seg.rows && d < a.dim;
+                    return a.q + (valid ? static_cast<int64_t>(seg.s.begin + its) * a.q_st + its_head * a.q_sh + d : 0);
+                };
+                auto read = [&](int i) {
+                    if (!PAIR) return x[PAIR ? 0 : i];
+                    uint4 v;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(place_of(i)) : "memory");
+                    return v;
+                };
+                bool valid;
+                if (PAIR) {
+#pragma unroll 1
+                    for (int i = 0; i < STEPS; ++i) {
+                        const __nv_bfloat16* const p = from(i, valid);
+                        cp_async<16>(place_of(i), p, valid ? 16 : 0);
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                } else {
+#pragma unroll
+                    for (int i = 0; i < (PAIR ? 1 : STEPS); ++i) {
+                        const __nv_bfloat16* const p = from(i, valid);
+                        x[i] = valid ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+                    }
                 }
-                asm volatile("cp.async.wait_all;" ::: "memory");
                 uint32_t top = 0;
                 // (a row with an Inf or a NaN does not set the power of the others)
-#pragma unroll 4
-                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+#pragma unroll(PAIR ? 4 : STEPS)
+                for (int i = 0; i < STEPS; ++i) {
                     const uint32_t its = absmax_bits8(read(i));
                     top = max(top, its < 0x7f800000u ? its : 0u);
                 }
@@ -576,8 +591,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 if (threadIdx.x == 0) of_segment[0] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f), 1e-38f);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(FACTOR_FULL, 0));
-#pragma unroll 4
-                for (int i = 0; i < PER_WARP; i += AT_ONCE) {
+#pragma unroll(PAIR ? 4 : STEPS)
+                for (int i = 0; i < STEPS; ++i) {
                     float f[8];
                     unpack_bf16x8(read(i), f);
                     store_16(place_of(i), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul), pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
