@@ -12,8 +12,8 @@
 //
 // What bounds it: no one thing. A tile of 128 tokens and 128 rows in int8 takes some 3700 cycles, of which HBM's share is 1060, the products' 1024, the exponentials' 1024 and
 // the issue slots' (softmax, conversion) 1500: they meet in a chain (scores, softmax, products) two of which are under way, all that tensor memory has room for. 12 x 32
-// nodes behind 6000 tokens: 78 us (16 at the copy's rate), of which some 25 are beginnings and ends: queries, a first tile, parts. 4 bits, 3 x 61 nodes, 256 rows a tile, behind
-// 20000 tokens: 155 us (53, bound by the products, at cuBLAS's rate).
+// nodes behind 6000 tokens: 76 us (16 at the copy's rate), of which some 25 are beginnings and ends: queries, a first tile, parts. 4 bits, 3 x 61 nodes, 256 rows a tile, behind
+// 20000 tokens: 152 us (53, bound by the products, at cuBLAS's rate).
 #include "internal.h"
 #include "kv_attention.cuh"
 
@@ -829,10 +829,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         sum.m_o = fmaxf(sum.m_o, its.x);
                     }
                     const float2 scale = sum.scale<FMT>();
-                    // (through the queries' place: 16 KB or more on their way)
-                    constexpr int Q_BYTES = (PAIR ? 2 : 1) * L::TILE, EACH = Q_BYTES >= 65536 ? 4 : 2, GROUPS = Q_BYTES / (EACH * 16 * kSoftmax);
-                    static_assert(GROUPS >= 2 && GROUPS <= 4, "");
-                    const uint32_t stage = base + L::Q + threadIdx.x * 16, m_stage = base + L::STATE + threadIdx.x * 4;
+                    // by way of the queries' place or, where nothing follows in this CTA, of the tiles' too, so that several parts are on their way (46.6 to 44.3 us for 12 x 32
+                    // nodes behind 1500 tokens, against 8 elements at a time by way of the queries' place)
+                    constexpr int Q_BYTES = (PAIR ? 2 : 1) * L::TILE, EACH = DP == 128 ? 8 : 4, GROUP = EACH * 16 * kSoftmax, MOST = (L::Q + Q_BYTES) / GROUP;
+                    static_assert(Q_BYTES >= GROUP && WIDTH % (4 * EACH) == 0 && MOST >= 4, "");
+                    const bool at_end = seg.u + seg.tiles == share.end;
+                    const int groups = at_end ? 4 : Q_BYTES / GROUP >= 2 ? 2 : 1;
+                    const uint32_t stage = base + (at_end ? 0 : L::Q) + threadIdx.x * 16, m_stage = base + L::STATE + threadIdx.x * 4;
                     const int chunks = (max(0, min(WIDTH, a.dim - d0)) + 4 * EACH - 1) / (4 * EACH);
                     int in_chunk = 0, in_part = from, in_slot = 0;
                     auto ask = [&] {
@@ -847,10 +850,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             }
                         }
                         cp_async_commit();
-                        in_slot = in_slot + 1 == GROUPS ? 0 : in_slot + 1;
+                        in_slot = in_slot + 1 == groups ? 0 : in_slot + 1;
                     };
-#pragma unroll
-                    for (int i = 0; i < GROUPS - 1; ++i) ask();
+#pragma unroll 1
+                    for (int i = 0; i < groups; ++i) ask();
                     int slot = 0;
 #pragma unroll 1
                     for (int c = 0; c < chunks; ++c) {
@@ -859,21 +862,25 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         for (int i = 0; i < 4 * EACH; ++i) o[i] = 0.f;
 #pragma unroll 1
                         for (int x = from; x <= until; ++x) {
-                            ask();
-                            cp_async_wait<GROUPS - 1>();
+                            if (groups == 4) cp_async_wait<3>();
+                            else if (groups == 2) cp_async_wait<1>();
+                            else cp_async_wait<0>();
                             float its_m;
                             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(its_m) : "r"(m_stage + slot * kSoftmax * 4) : "memory");
+                            float4 v[EACH];
+#pragma unroll
+                            for (int q = 0; q < EACH; ++q)
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[q].x), "=f"(v[q].y), "=f"(v[q].z), "=f"(v[q].w) : "r"(stage + (slot * EACH + q) * kSoftmax * 16) : "memory");
                             const float by = ex2(its_m - sum.m_o);
 #pragma unroll
                             for (int q = 0; q < EACH; ++q) {
-                                float4 v;
-                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(stage + (slot * EACH + q) * kSoftmax * 16) : "memory");
-                                o[4 * q] += v.x * by;
-                                o[4 * q + 1] += v.y * by;
-                                o[4 * q + 2] += v.z * by;
-                                o[4 * q + 3] += v.w * by;
+                                o[4 * q] += v[q].x * by;
+                                o[4 * q + 1] += v[q].y * by;
+                                o[4 * q + 2] += v[q].z * by;
+                                o[4 * q + 3] += v[q].w * by;
                             }
-                            slot = slot + 1 == GROUPS ? 0 : slot + 1;
+                            ask();                                               // (into the place just read)
+                            slot = slot + 1 == groups ? 0 : slot + 1;
                         }
 #pragma unroll
                         for (int x = 0; x < 4 * EACH; x += 8)
