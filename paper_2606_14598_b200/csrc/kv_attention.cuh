@@ -73,7 +73,6 @@ struct Share {
     int64_t begin, end;                         // this CTA's units
     int b;
 };
-// The sequence that unit `u` (of this CTA's range) belongs to, found by all threads at once; u < 0: only the total
 __device__ __forceinline__ int64_t warp_scan(int64_t v) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -82,6 +81,7 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v) {
     }
     return v;
 }
+// This CTA's units, and the sequence that the first of them belongs to: found by all threads at once
 template <int THREADS, int TILE>
 __device__ __forceinline__ Share share_out(const AttentionArgs& a, int rows_of_tile) {
     __shared__ int64_t of_warp[THREADS / 32];
