@@ -257,8 +257,9 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
         for (int i = 0; i < EACH; ++i) frags[threadIdx.x + i * kThreads] = moved[i];
         __syncthreads();
 
-        // ---- the steps. Kept per row: o and its reference m_o, the sum l of the exponentials and its reference m_l. m_l is the scores'; m_o is that of score
-        // + logarithm of the value's scale, so that the weights that are rounded to fp16 are of the row's own size whatever the scales. This lane's rows: pairs
+        // ---- the steps. Kept per row: o and its reference m_l + m_o, the sum l of the exponentials and its reference m_l. m_l is the scores'; m_l + m_o is that of score
+        // + logarithm of the value's scale, so that the weights that are rounded to fp16 are of the row's own size whatever the scales. (A score meets m_l before anything else is
+        // added: that difference is small and exact where the score is large.) This lane's rows: pairs
         // 2c and 2c + 1 of every eight; its elements of o: those of its g.
         float o[DP / 16][NR][4];
         uint64_t l2[NR], m_l[NR], m_o[NR], factor[NR];
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
                         }
                     }
                 }
-                // scores in powers of two; the largest of each row, without and with the values' scales
+                // scores in powers of two; the largest of each row
                 float top_l[2] = {kNone, kNone}, top_o[2] = {kNone, kNone};
                 uint64_t score[2 * TT];
 #pragma unroll
@@ -440,45 +441,61 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
                     top_l[0] = fmaxf(top_l[0], x);
                     top_l[1] = fmaxf(top_l[1], y);
                     score[n] = pack2(x, y);
-                    unpack2(add2(score[n], pack2(lvs[n], lvs[n])), x, y);
-                    top_o[0] = fmaxf(top_o[0], x);
-                    top_o[1] = fmaxf(top_o[1], y);
                 }
                 // Sums and weights may outgrow their references before these move: weights stay below 2^15 and are 2^7 at most where they moved last
                 // (fp16 keeps all its bits down to 2^-21 of that)
                 float ml[2], mo[2];
                 unpack2(m_l[i], ml[0], ml[1]);
                 unpack2(m_o[i], mo[0], mo[1]);
-                if (__any_sync(0xffffffffu, top_l[0] > ml[0] + 16.f || top_l[1] > ml[1] + 16.f || top_o[0] > mo[0] + 15.f || top_o[1] > mo[1] + 15.f)) {
-                    float by_l[2], by_o[2];
+                if (__any_sync(0xffffffffu, top_l[0] - ml[0] > 16.f || top_l[1] - ml[1] > 16.f)) {
+                    float by_l[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) {
-                            top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], x));
-                            top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], x));
-                        }
-                        const float now_l = fmaxf(ml[e], top_l[e]), now_o = fmaxf(mo[e], top_o[e] - 7.f);
+                        for (int x = 4; x < 32; x <<= 1) top_l[e] = fmaxf(top_l[e], __shfl_xor_sync(0xffffffffu, top_l[e], x));
+                        const float now_l = fmaxf(ml[e], top_l[e]);
                         by_l[e] = ex2(ml[e] - now_l);
-                        by_o[e] = ex2(mo[e] - now_o);
+                        mo[e] = fmaxf(mo[e] + (ml[e] - now_l), kNone);
                         ml[e] = now_l;
-                        mo[e] = now_o;
                     }
                     m_l[i] = pack2(ml[0], ml[1]);
                     m_o[i] = pack2(mo[0], mo[1]);
                     l2[i] = mul2(l2[i], pack2(by_l[0], by_l[1]));
+                }
+                // relative to m_l, without and with the values' scales
+                const uint64_t minus_l = pack2(-ml[0], -ml[1]);
+#pragma unroll
+                for (int n = 0; n < 2 * TT; ++n) {
+                    float x, y;
+                    score[n] = add2(score[n], minus_l);
+                    unpack2(score[n], x, y);
+                    l2[i] = add2(l2[i], pack2(ex2(x), ex2(y)));
+                    score[n] = add2(score[n], pack2(lvs[n], lvs[n]));
+                    unpack2(score[n], x, y);
+                    top_o[0] = fmaxf(top_o[0], x);
+                    top_o[1] = fmaxf(top_o[1], y);
+                }
+                if (__any_sync(0xffffffffu, top_o[0] - mo[0] > 15.f || top_o[1] - mo[1] > 15.f)) {
+                    float by_o[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top_o[e] = fmaxf(top_o[e], __shfl_xor_sync(0xffffffffu, top_o[e], x));
+                        const float now_o = fmaxf(mo[e], top_o[e] - 7.f);
+                        by_o[e] = ex2(mo[e] - now_o);
+                        mo[e] = now_o;
+                    }
+                    m_o[i] = pack2(mo[0], mo[1]);
 #pragma unroll
                     for (int j = 0; j < DP / 16; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[j][i][e] *= by_o[e & 1];
                 }
-                const uint64_t minus_l = pack2(-ml[0], -ml[1]), minus_o = pack2(-mo[0], -mo[1]);
+                const uint64_t minus_o = pack2(-mo[0], -mo[1]);
 #pragma unroll
                 for (int n = 0; n < 2 * TT; ++n) {
                     float x, y;
-                    unpack2(add2(score[n], minus_l), x, y);
-                    l2[i] = add2(l2[i], pack2(ex2(x), ex2(y)));
-                    unpack2(add2(score[n], add2(pack2(lvs[n], lvs[n]), minus_o)), x, y);
+                    unpack2(add2(score[n], minus_o), x, y);
                     if (FMT == KV_CACHE_INT8 && masked) {           // (the scale of a token that is not seen may be NaN)
                         if (!(sees[0] >> n & 1u)) x = -INFINITY;
                         if (!(sees[1] >> n & 1u)) y = -INFINITY;

@@ -203,12 +203,14 @@ __device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t (&r)[4]) {
 
 // ------------------------------------------------------------------------------------------------ results
 
-// Four elements of a row, on their way from parts to the output
+// Four elements of a row, on their way from parts to the output: o stands for o * 2^(m_l + m_o), l for l * 2^m_l. (m_o is of the size of the values' scales; with m_l in it, which
+// may be any fp32 number, it would be rounded to that one's spacing, and the result with it.)
 struct Row {
     float o[4] = {0.f, 0.f, 0.f, 0.f}, m_o = kNone, m_l = kNone, l = 0.f;
     __device__ __forceinline__ void add(const float4& x, float its_m_o, float its_m_l, float its_l) {
-        const float now_o = fmaxf(m_o, its_m_o), now_l = fmaxf(m_l, its_m_l), mine_o = ex2(m_o - now_o), its_o = ex2(its_m_o - now_o);
-        l = l * ex2(m_l - now_l) + its_l * ex2(its_m_l - now_l);
+        const float now_l = fmaxf(m_l, its_m_l), down = m_l - now_l, its_down = its_m_l - now_l;
+        const float now_o = fmaxf(m_o + down, its_m_o + its_down), mine_o = ex2(m_o + down - now_o), its_o = ex2(its_m_o + its_down - now_o);
+        l = l * ex2(down) + its_l * ex2(its_down);
         o[0] = o[0] * mine_o + x.x * its_o;
         o[1] = o[1] * mine_o + x.y * its_o;
         o[2] = o[2] * mine_o + x.z * its_o;
@@ -216,11 +218,11 @@ struct Row {
         m_o = now_o;
         m_l = now_l;
     }
-    // r: row of the sequence's new tokens and the group's heads. o stands for o * 2^(m_o - m_l), 4-bit: / 2^12. The power
+    // r: row of the sequence's new tokens and the group's heads. The result is o * 2^m_o / l, 4-bit: / 2^12. The power
     // may be more than fp32 spans while the result is not: it is applied in two halves.
     template <int FMT>
     __device__ __forceinline__ float2 scale() const {           // o times x, times y, times y is the result (l == 0: it is 0)
-        return make_float2(1.f / l, ex2(fminf(fmaxf(0.5f * (m_o - m_l - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f)));
+        return make_float2(1.f / l, ex2(fminf(fmaxf(0.5f * (m_o - (FMT == KV_CACHE_INT8 ? 0.f : 12.f)), -126.f), 126.f)));
     }
     __device__ __forceinline__ void write_lse(const AttentionArgs& a, const Sequence& s, int node, int h) const {
         if (a.lse != nullptr) a.lse[static_cast<int64_t>(s.begin + node) * a.heads * a.group + h] = l == 0.f ? -INFINITY : (m_l + log2f(l)) * kLn2;

@@ -48,7 +48,7 @@ struct Plan {
     static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
     static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, OF_K = OF_V + kSlots * kTok * 4, OF_TILE = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 4);
     static constexpr int FACTOR = OF_TILE + kSlots * 4;         // of the scores, and the queries' maxima of the warps
-    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 2 * kRows * 16, BYTES = BARS + 33 * 8 + 1024;
+    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 4 * kSoftmax * 8, BYTES = BARS + 33 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
     // codes: a thread converts a chunk of 16 bytes of every PASS-th token
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     float* const factors = reinterpret_cast<float*>(smem + L::FACTORS);          // [slot][token]: of the scores; -1: not seen by anybody
     volatile int* const sigmas = reinterpret_cast<volatile int*>(smem + L::SIGMA);        // [slot]: values are relative to 2^this
     volatile float* const tile_factors = reinterpret_cast<volatile float*>(smem + L::OF_TILE);      // 4-bit: [slot]: of all scores of a tile
-    volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2)
+    volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2), scores large (4)
     uint8_t* const nans = smem + L::NANS;
     const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
     Segments<ROWS> seg(a, share);
@@ -457,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     }
                     k_factor *= factor;
                     factors[slot * kTok + me] = in ? k_factor : -1.f;
-                    word = __reduce_max_sync(0xffffffffu, top_sigma) * 4 + (__any_sync(0xffffffffu, nan) ? 1 : 0) + (__any_sync(0xffffffffu, !in) ? 2 : 0);
+                    word = __reduce_max_sync(0xffffffffu, top_sigma) * 8 + (__any_sync(0xffffffffu, nan) ? 1 : 0) + (__any_sync(0xffffffffu, !in) ? 2 : 0) +
+                           (FMT == KV_CACHE_INT8 && __any_sync(0xffffffffu, in && k_factor > 0x1p-9f) ? 4 : 0);
                     if (FMT == KV_CACHE_MXFP4) top_of_k = __reduce_max_sync(0xffffffffu, top_of_k);
                     if (lane == 0) {
                         of_warp[(t & 1) * 8 + warp - kKeyWarp] = word;
@@ -469,8 +470,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     for (int i = 0; i < 4; ++i) {
                         const int its = of_warp[(t & 1) * 8 + i];
                         if (FMT == KV_CACHE_MXFP4) top_of_k = max(top_of_k, static_cast<uint32_t>(of_warp[(t & 1) * 8 + 4 + i]));
-                        sigma = max(sigma, its >> 2);                            // the largest scale of values so far (an exponent of fp32)
-                        all |= its & 3;
+                        sigma = max(sigma, its >> 3);                            // the largest scale of values so far (an exponent of fp32)
+                        all |= its & 7;
                     }
                     if (me == 0) {
                         sigmas[slot] = sigma;
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         // ---- softmax: a thread a row. Scores times their tokens' factors are powers of two.
         const int w = warp >> 2, row = threadIdx.x & (kRows - 1);
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16, s_tmem = tmem + lanes + w * kTok, o_tmem = tmem + lanes + L::O + w * DP;
-        float* const state = reinterpret_cast<float*>(smem + L::STATE);          // [warpgroup][row]: references of o and of the sum, the sum, NaN blocks
+        float* const state = reinterpret_cast<float*>(smem + L::STATE);          // [warpgroup][row]: references of o (beside the sum's) and of the sum, the sum, NaN blocks
         volatile float* const of_segment = reinterpret_cast<volatile float*>(smem + L::FACTOR);         // the scores' factor, [8 + warp]: the queries' maxima
         uint32_t tile_base = 0, jobs = 0;                                        // jobs of this warpgroup so far
         while (seg.next()) {
@@ -630,8 +631,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                                 if (sees >> x & 1u) poison |= nans[slot * kTok + x + 32 * ch];
                         }
                     }
-                    // tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places
-                    if (j0 + kTok > 0 || (its_special & 2) != 0) {
+                    float tile_factor = FMT == KV_CACHE_MXFP4 ? tile_factors[slot] : 1.f;
+                    // Tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places. So are scores that may be beyond 2^20
+                    // (before their factors they are below 2^29 or 2^37): of a product that is not rounded before its reference is taken off, which was, more than 2^15 might be left.
+                    if (j0 + kTok > 0 || (its_special & 6) != 0 || (FMT == KV_CACHE_MXFP4 && __any_sync(0xffffffffu, tile_factor > 0x1p-17f))) {
 #pragma unroll 1
                         for (int ch = 0; ch < 8; ++ch) {
                             uint32_t v[16];
@@ -639,11 +642,12 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             const uint32_t sees = sees32_of(ch / 2) >> (16 * (ch & 1));
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? (FMT == KV_CACHE_INT8 ? __float_as_uint(__uint_as_float(v[i]) * kf[16 * ch + i]) : v[i]) : 0xff800000u;
+                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? __float_as_uint(__uint_as_float(v[i]) * (FMT == KV_CACHE_INT8 ? kf[16 * ch + i] : tile_factor)) : 0xff800000u;
                             tmem_st_32x32b_x16(s_tmem + 16 * ch, v);
                         }
                         tmem_wait_st();
                         kf = reinterpret_cast<const float*>(smem + L::ONES);
+                        tile_factor = 1.f;
                     }
                     // the row's largest score: 16 columns at a time, the next ones on their way
                     float top = -INFINITY;
@@ -673,12 +677,11 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         }
                         tmem_wait_ld();
                     }
-                    const float tile_factor = FMT == KV_CACHE_MXFP4 ? tile_factors[slot] : 1.f;
                     top = fmaxf(FMT == KV_CACHE_MXFP4 ? top * tile_factor : top, kNone);
                     // references move when a weight would pass 2^15, to put it at 2^7, or when the values' does
                     const int its_sigma = sigmas[slot];
-                    if (__any_sync(0xffffffffu, top > m + 15.f || its_sigma != sigma)) {
-                        const float now = top > m + 15.f ? top - 7.f : m, by_l = ex2(m - now);
+                    if (__any_sync(0xffffffffu, top - m > 15.f || its_sigma != sigma)) {
+                        const float now = top - m > 15.f ? top - 7.f : m, by_l = ex2(m - now);
                         l2 = mul2(l2, pack2(by_l, by_l));
                         if (!first) {
                             const float half = ex2(static_cast<float>(max(sigma - its_sigma, -252)) * 0.5f), by = by_l * half * half;
@@ -742,8 +745,8 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
             float l, other;
             unpack2(l2, l, other);
             l += other;
-            // (reference of o with the values' in it: int8 tiles are 2^8 too large, 4-bit ones 2^12, which the results take account of)
-            float m_o = m + static_cast<float>(sigma - (FMT == KV_CACHE_INT8 ? 8 : 0)), m_l = m;
+            // (reference of o beside the sum's: the values'; int8 tiles are 2^8 too large, 4-bit ones 2^12, which the results take account of)
+            float m_o = static_cast<float>(sigma - (FMT == KV_CACHE_INT8 ? 8 : 0)), m_l = m;
             if (PAIR || w < seg.tiles) wait(bar(O_DONE, w), (jobs - 1) & 1, ctl, kWaitMany + 9, kStatusTimeout);
             if (!PAIR) *reinterpret_cast<float4*>(state + (w * kRows + row) * 4) = make_float4(m_o, m, l, __uint_as_float(poison));
             named_sync(2, kSoftmax);
@@ -768,14 +771,17 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 const bool two = !PAIR && seg.tiles > 1;
                 if (!PAIR) {
                     const float4 s0 = *reinterpret_cast<const float4*>(state + row * 4), s1 = *reinterpret_cast<const float4*>(state + (kRows + row) * 4);
-                    m_o = two ? fmaxf(s0.x, s1.x) : s0.x;
-                    m_l = two ? fmaxf(s0.y, s1.y) : s0.y;
+                    m_o = s0.x;
+                    m_l = s0.y;
                     l = s0.z;
                     poison = __float_as_uint(s0.w);
                     if (two) {
-                        by[0] = ex2(s0.x - m_o);
-                        by[1] = ex2(s1.x - m_o);
-                        l = s0.z * ex2(s0.y - m_l) + s1.z * ex2(s1.y - m_l);
+                        m_l = fmaxf(s0.y, s1.y);
+                        const float down0 = s0.y - m_l, down1 = s1.y - m_l;
+                        m_o = fmaxf(s0.x + down0, s1.x + down1);
+                        by[0] = ex2(s0.x + down0 - m_o);
+                        by[1] = ex2(s1.x + down1 - m_o);
+                        l = s0.z * ex2(down0) + s1.z * ex2(down1);
                         poison |= __float_as_uint(s1.w);
                     }
                 }
@@ -823,10 +829,10 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
 #pragma unroll 2
                     for (int x = from; x <= until; ++x) {
                         const float4 its = __ldcg(part_of(x) + DP / 4 * ROWS + r);
-                        const float now_l = fmaxf(sum.m_l, its.y);
-                        sum.l = sum.l * ex2(sum.m_l - now_l) + its.z * ex2(its.y - now_l);
+                        const float now_l = fmaxf(sum.m_l, its.y), down = sum.m_l - now_l, its_down = its.y - now_l;
+                        sum.l = sum.l * ex2(down) + its.z * ex2(its_down);
                         sum.m_l = now_l;
-                        sum.m_o = fmaxf(sum.m_o, its.x);
+                        sum.m_o = fmaxf(sum.m_o + down, its.x + its_down);
                     }
                     const float2 scale = sum.scale<FMT>();
                     // by way of the queries' place or, where nothing follows in this CTA, of the tiles' too, so that several parts are on their way (46.6 to 44.3 us for 12 x 32
@@ -835,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     static_assert(Q_BYTES >= GROUP && WIDTH % (4 * EACH) == 0 && MOST >= 4, "");
                     const bool at_end = seg.u + seg.tiles == share.end;
                     const int groups = at_end ? 4 : Q_BYTES / GROUP >= 2 ? 2 : 1;
-                    const uint32_t stage = base + (at_end ? 0 : L::Q) + threadIdx.x * 16, m_stage = base + L::STATE + threadIdx.x * 4;
+                    const uint32_t stage = base + (at_end ? 0 : L::Q) + threadIdx.x * 16, m_stage = base + L::STATE + threadIdx.x * 8;
                     const int chunks = (max(0, min(WIDTH, a.dim - d0)) + 4 * EACH - 1) / (4 * EACH);
                     int in_chunk = 0, in_part = from, in_slot = 0;
                     auto ask = [&] {
@@ -843,7 +849,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             const float4* const p = part_of(in_part);
 #pragma unroll
                             for (int q = 0; q < EACH; ++q) cp_async<16>(stage + (in_slot * EACH + q) * kSoftmax * 16, p + (d0 / 4 + in_chunk * EACH + q) * ROWS + r, 16);
-                            cp_async<4>(m_stage + in_slot * kSoftmax * 4, p + DP / 4 * ROWS + r, 4);
+                            cp_async<8>(m_stage + in_slot * kSoftmax * 8, p + DP / 4 * ROWS + r, 8);
                             if (++in_part > until) {
                                 in_part = from;
                                 ++in_chunk;
@@ -865,13 +871,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             if (groups == 4) cp_async_wait<3>();
                             else if (groups == 2) cp_async_wait<1>();
                             else cp_async_wait<0>();
-                            float its_m;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(its_m) : "r"(m_stage + slot * kSoftmax * 4) : "memory");
+                            float its_m, its_l;
+                            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(its_m), "=f"(its_l) : "r"(m_stage + slot * kSoftmax * 8) : "memory");
                             float4 v[EACH];
 #pragma unroll
                             for (int q = 0; q < EACH; ++q)
                                 asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[q].x), "=f"(v[q].y), "=f"(v[q].z), "=f"(v[q].w) : "r"(stage + (slot * EACH + q) * kSoftmax * 16) : "memory");
-                            const float by = ex2(its_m - sum.m_o);
+                            const float by = ex2(its_m + (its_l - sum.m_l) - sum.m_o);
 #pragma unroll
                             for (int q = 0; q < EACH; ++q) {
                                 o[4 * q] += v[q].x * by;

@@ -514,3 +514,33 @@ def test_norm_append_attend(fmt):
     slots = c.table[torch.tensor([0, 0, 0, 1, 1], device="cuda"), where // page].long() * page + where % page
     c.q = w8.kv_cache_append(c.cache, qkv[:, 4:6], qkv[:, 6:], slots, where, table, q=qkv[:, :4])
     c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 1), (16, 2), (40, 3), (8, 30)])
+@pytest.mark.parametrize("power", [12, 16, 20, 22, 24, 25, 26, 27, 28, 29, 30, 32, 40, 100])
+def test_scores_of_any_size(fmt, group, new, power):
+    """Large queries: a row is its largest token's value, however far the spacing of numbers of its scores' size is above the logarithm of a scale."""
+    c = Case(fmt, 2, group, 128, [300, 5000, new + 40], [new] * 3, seed=52)
+    if fmt == "int8":
+        c.cache.v_scales.mul_(2.0 ** -9)
+    c.q *= 2.0 ** power
+    got = c.check().double().view(c.total, 2, group, 128)
+    flat, rows = [t.flatten(0, 1) for t in c.cache._tensors], 0
+    for b in range(3):
+        see, t = c.sees(b), torch.arange(c.lengths[b], device="cuda")
+        slot = c.table[b].long()[t // c.page] * c.page + t % c.page
+        k, v = values(flat[0][slot], flat[1][slot], fmt), values(flat[2][slot], flat[3][slot], fmt)
+        q = c.q[new * b:new * (b + 1)].double().view(new, 2, group, 128)
+        s = (torch.einsum("nhgd,phd->nhgp", q, k) * 128 ** -0.5).masked_fill(~see[:, None, None], -INF)
+        # error of a score: as in Case.want; all others together then weigh less than 5000 * 2^-60 of the largest
+        off = (torch.einsum("nhgd,phd->nhgp", q.abs(), k.abs()) * 128 ** -0.5 * (128 + 8) * 2.0 ** -23).amax(-1) + q.abs().amax(-1) * k.abs().amax() * 128 * 2.0 ** -27
+        first, second = s.topk(2, -1).values.unbind(-1)
+        alone = first - second > 2 * off + 42
+        want = v[s.argmax(-1), torch.arange(2, device="cuda")[None, :, None]]
+        # weight, unit and unit times code rounded to fp16, the output to bf16
+        wrong = (got[new * b:new * (b + 1)] - want).abs() > want.abs() * (2.0 ** -8 + 3 * 2.0 ** -11) + 2.0 ** -32 * v.abs().amax()
+        assert not bool((wrong.any(-1) & alone).any())
+        rows += int(alone.sum())
+    assert rows > c.total * group
