@@ -433,7 +433,8 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
 #pragma unroll
                 for (int n = 0; n < 2 * TT; ++n) {
                     float x, y;
-                    unpack2(mul2(mul2(pack2(sc[n / 2][i][(n & 1) * 2], sc[n / 2][i][(n & 1) * 2 + 1]), pack2(kfs[n], kfs[n])), factor[i]), x, y);
+                    // (factors first: the key's alone may take a product past fp32 that the row's brings back)
+                    unpack2(mul2(pack2(sc[n / 2][i][(n & 1) * 2], sc[n / 2][i][(n & 1) * 2 + 1]), mul2(pack2(kfs[n], kfs[n]), factor[i])), x, y);
                     if (masked) {
                         if (!(sees[0] >> n & 1u)) x = -INFINITY;
                         if (!(sees[1] >> n & 1u)) y = -INFINITY;

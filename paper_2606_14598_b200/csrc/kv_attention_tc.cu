@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     if (me == 0) {
                         sigmas[slot] = sigma;
                         special[slot] = all;
-                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fminf(fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23), 1.2e-38f), 3e38f);   // (0 and infinity are no factors of -infinity and 0)
+                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fminf(fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23) * 0x1p-12f, 1.2e-38f), 3e38f);   // (0 and infinity are no factors of -infinity and 0)
                     }
                     if (lane == 0) mbar_arrive(bar(SCALES_FULL, slot));
                     const uint32_t from = L::RAW + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(of_segment[8 + i]));
                 const int field = static_cast<int>(top >> 23), up = min(126, max(-126, 141 - max(field, 1)));
                 const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
-                if (threadIdx.x == 0) of_segment[0] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23) * (FMT == KV_CACHE_INT8 ? 1.f : 0x1p-12f), 1e-38f);
+                if (threadIdx.x == 0) of_segment[0] = fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(FACTOR_FULL, 0));
 #pragma unroll(PAIR ? 4 : STEPS)

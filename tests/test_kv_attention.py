@@ -544,3 +544,19 @@ def test_scores_of_any_size(fmt, group, new, power):
         assert not bool((wrong.any(-1) & alone).any())
         rows += int(alone.sum())
     assert rows > c.total * group
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 1), (16, 2), (40, 3), (8, 30)])
+def test_keys_of_any_size(fmt, group, new):
+    """Large keys, with ordinary queries (whose scores fp32 holds) and with small ones."""
+    for power in (60, 90, 105):
+        c = Case(fmt, 2, group, 128, [300, new + 40], [new] * 2, seed=53)
+        if fmt == "int8":
+            c.cache.k_scales.mul_(2.0 ** power)
+        else:
+            c.cache.k_scales.add_(power)
+        assert bool(torch.isfinite(c.check()).all())
+        c.q *= 2.0 ** -power
+        c.check()
