@@ -106,7 +106,7 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  * row's own size; with many rows of queries (more than 32 a sequence and head on average, heads of at most 128 elements), it is the probability that is, and values are
  * rounded to fp16 relative to the sequence's largest scale. Repeated calls give the same bits. What lies far below its neighbours may count as zero: elements of a query 2^-38 below its largest, MXFP4 blocks
  * 2^-27 below the largest of their head and token, tokens whose probability is 2^-110, or whose product with the value's scale is 2^-31, of the row's largest
- * (many rows: MXFP4 blocks of keys 2^-37 below the largest of 128 tokens, tokens whose probability is 2^-31, or whose value's scale 2^-32 of the sequence's largest).
+ * (many rows: elements of a query 2^-30 below its largest, MXFP4 blocks of keys 2^-37 below the largest of 128 tokens, tokens whose probability is 2^-31, or whose value's scale 2^-32 of the sequence's largest).
  */
 size_t kv_cache_attention_workspace_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);
 size_t kv_cache_attention_zeroed_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim);

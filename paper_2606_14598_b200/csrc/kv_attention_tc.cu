@@ -47,8 +47,8 @@ struct Plan {
     static constexpr int ONES = FACTORS + kSlots * kTok * 4;                   // factors of scores that have theirs already
     static constexpr int NANS = ONES + kTok * 4;                               // NaN blocks of a token's values, a byte each
     static constexpr int SIGMA = NANS + kSlots * kTok, SPECIAL = SIGMA + kSlots * 4, OF_WARP = SPECIAL + kSlots * 4, OF_V = OF_WARP + 2 * 8 * 4, OF_K = OF_V + kSlots * kTok * 4, OF_TILE = OF_K + (FMT == KV_CACHE_INT8 ? 0 : 2 * kTok * 4);
-    static constexpr int FACTOR = OF_TILE + kSlots * 4;         // of the scores, and the queries' maxima of the warps
-    static constexpr int STATE = FACTOR + 16 * 4, BARS = STATE + 4 * kSoftmax * 8, BYTES = BARS + 33 * 8 + 1024;
+    static constexpr int FACTOR = OF_TILE + kSlots * 4;         // of the scores; the queries' maxima and odd rows of the warps
+    static constexpr int POWERS = FACTOR + 24 * 4, STATE = POWERS + 2 * kRows * 4, BARS = STATE + 4 * kSoftmax * 8, BYTES = BARS + 33 * 8 + 1024;
     static constexpr int O = 2 * kTok;                                         // tensor memory: scores (and weights) of the two, then their O
     static_assert(O + 2 * DP <= 512 && BYTES <= 226 * 1024, "");
     // codes: a thread converts a chunk of 16 bytes of every PASS-th token
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
     float* const factors = reinterpret_cast<float*>(smem + L::FACTORS);          // [slot][token]: of the scores; -1: not seen by anybody
     volatile int* const sigmas = reinterpret_cast<volatile int*>(smem + L::SIGMA);        // [slot]: values are relative to 2^this
     volatile float* const tile_factors = reinterpret_cast<volatile float*>(smem + L::OF_TILE);      // 4-bit: [slot]: of all scores of a tile
-    volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2), scores large (4)
+    volatile int* const special = reinterpret_cast<volatile int*>(smem + L::SPECIAL);     // [slot]: whether values of the tile are NaN (1), tokens not to be seen (2), scores large (4), rows odd (8)
     uint8_t* const nans = smem + L::NANS;
     const int row_bytes = a.dim / L::PER_BYTE, blocks = (a.dim + kMxBlock - 1) / kMxBlock;
     Segments<ROWS> seg(a, share);
@@ -418,7 +418,9 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                 int sigma = -126;                                                // the values' reference starts anew with each segment
                 wait(bar(FACTOR_FULL, 0), segments & 1, ctl, kWaitMany + 10, kStatusTimeout);
                 ++segments;
-                const float factor = reinterpret_cast<const volatile float*>(smem + L::FACTOR)[0];
+                const volatile float* const of_segment = reinterpret_cast<const volatile float*>(smem + L::FACTOR);
+                const float factor = of_segment[0];
+                const int odd = __any_sync(0xffffffffu, of_segment[16 + (lane & 7)] != 0.f) ? 8 : 0;
                 for (int left = seg.tiles; left > 0; --left, ++t) {
                     const uint32_t slot = t & (kSlots - 1);
                     wait(bar(RAW_K_FULL, raw.slot), raw.phase, ctl, kWaitMany + 5, kStatusTimeout);
@@ -475,8 +477,13 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                     }
                     if (me == 0) {
                         sigmas[slot] = sigma;
+                        all |= odd;
+                        if (FMT == KV_CACHE_MXFP4) {                             // (0 and infinity are no factors of -infinity and 0)
+                            const float of_tile = fminf(fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23) * 0x1p-12f, 1.2e-38f), 3e38f);
+                            tile_factors[slot] = of_tile;
+                            if (of_tile > 0x1p-17f) all |= 4;
+                        }
                         special[slot] = all;
-                        if (FMT == KV_CACHE_MXFP4) tile_factors[slot] = fminf(fmaxf(factor * __uint_as_float(top_of_k == 0 ? 0x00400000u : top_of_k << 23) * 0x1p-12f, 1.2e-38f), 3e38f);   // (0 and infinity are no factors of -infinity and 0)
                     }
                     if (lane == 0) mbar_arrive(bar(SCALES_FULL, slot));
                     const uint32_t from = L::RAW + raw.slot * kTok * L::ROW, tile = ring.slot * L::TILE;
@@ -535,14 +542,19 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
         const int w = warp >> 2, row = threadIdx.x & (kRows - 1);
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16, s_tmem = tmem + lanes + w * kTok, o_tmem = tmem + lanes + L::O + w * DP;
         float* const state = reinterpret_cast<float*>(smem + L::STATE);          // [warpgroup][row]: references of o (beside the sum's) and of the sum, the sum, NaN blocks
-        volatile float* const of_segment = reinterpret_cast<volatile float*>(smem + L::FACTOR);         // the scores' factor, [8 + warp]: the queries' maxima
+        volatile float* const of_segment = reinterpret_cast<volatile float*>(smem + L::FACTOR);         // the scores' factor, [8 + warp]: the queries' maxima, [16 + warp]: 1 with odd rows
+        volatile uint32_t* const powers = reinterpret_cast<volatile uint32_t*>(smem + L::POWERS);       // [row]: what its queries are multiplied by
         uint32_t tile_base = 0, jobs = 0;                                        // jobs of this warpgroup so far
         while (seg.next()) {
             const int r = (PAIR ? w * kRows : 0) + row;                          // of the item's rows
             const bool live = r < seg.rows, warp_live = (PAIR ? w * kRows : 0) + 32 * (warp & 3) < seg.rows;
             const int node = (seg.row0 + min(r, seg.rows - 1)) / a.group;
-            // queries: a power of two brings the largest magnitude of all rows to [2^14, 2^15). DP / 8 lanes a row; all rows are on their way at once, those of one tile of
+            // queries: a power of two, which the tokens' factors take account of, brings the largest magnitude of all rows to [2^14, 2^15) (a larger one counts as 2^15: factors stay
+            // within fp32). It serves the rows whose own largest is 2^-8 of that or more, so 2^6 after it. Others are odd, and have their own: no row's result depends on how large its
+            // neighbours are. Their scores are brought to the common power in tensor memory (exact), which costs the segment a trip for each tile.
+            // DP / 8 lanes a row; all rows are on their way at once, those of one tile of
             // rows in registers, those of two by way of the places that they go to (twice through registers costs 10 us).
+            int common_up;
             {
                 constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, STEPS = ROWS / 8 / AT_ONCE;
                 const int d = lane % LANES * 8;
@@ -575,25 +587,55 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         x[i] = valid ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
                     }
                 }
+                // largest magnitudes, of N steps' rows at a time: lanes swap halves of what they hold, until each has one row's (what is Inf or NaN sets no power)
+                constexpr int N = PAIR ? 4 : STEPS;
                 uint32_t top = 0;
-                // (a row with an Inf or a NaN does not set the power of the others)
-#pragma unroll(PAIR ? 4 : STEPS)
-                for (int i = 0; i < STEPS; ++i) {
-                    const uint32_t its = absmax_bits8(read(i));
-                    top = max(top, its < 0x7f800000u ? its : 0u);
+                int my_row = 0;
+#pragma unroll 1
+                for (int i = 0; i < STEPS; i += N) {
+                    uint32_t its[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        its[j] = absmax_bits8(read(i + j));
+                        if (its[j] >= 0x7f800000u) its[j] = 0;
+                    }
+#pragma unroll
+                    for (int o = LANES / 2, n = N; o > 0; o /= 2, n = n > 1 ? n / 2 : 1) {
+                        if (n == 1) its[0] = max(its[0], __shfl_xor_sync(0xffffffffu, its[0], o));
+#pragma unroll
+                        for (int j = 0; j < n / 2; ++j) {
+                            const bool upper = (lane & o) != 0;
+                            its[j] = max(upper ? its[j + n / 2] : its[j], __shfl_xor_sync(0xffffffffu, upper ? its[j] : its[j + n / 2], o));
+                        }
+                    }
+                    top = its[0];
+                    my_row = row_of(i + lane % LANES / (LANES / N));
+                    if (PAIR) powers[my_row] = top;
                 }
-                top = __reduce_max_sync(0xffffffffu, top);
-                if (lane == 0) of_segment[8 + warp] = __uint_as_float(top);
+                if (PAIR) {                                                      // (32 rows a warp)
+                    __syncwarp();
+                    my_row = warp * 32 + lane;
+                    top = powers[my_row];
+                }
+                uint32_t largest = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) of_segment[8 + warp] = __uint_as_float(largest);
                 named_sync(2, kSoftmax);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(of_segment[8 + i]));
-                const int field = static_cast<int>(top >> 23), up = min(126, max(-126, 141 - max(field, 1)));
-                const float mul = a.scale < 0.f ? -__uint_as_float((127 + up) << 23) : __uint_as_float((127 + up) << 23);
-                if (threadIdx.x == 0) of_segment[0] = fabsf(a.scale) * kLog2e * __uint_as_float((127 - up) << 23);
-                __syncwarp();
+                for (int i = 0; i < 8; ++i) largest = max(largest, __float_as_uint(of_segment[8 + i]));
+                const int field = static_cast<int>(top >> 23), common = min(static_cast<int>(largest >> 23), 141);
+                common_up = min(126, 141 - max(common, 1));
+                const bool odd = top != 0 && (field > common || field + 8 < common);
+                const bool any_odd = __any_sync(0xffffffffu, odd);
+                if (lane == 0) of_segment[16 + warp] = any_odd ? 1.f : 0.f;
+                if (threadIdx.x == 0) of_segment[0] = fabsf(a.scale) * kLog2e * __uint_as_float((127 - common_up) << 23);
                 if (lane == 0) mbar_arrive(bar(FACTOR_FULL, 0));
+                const uint32_t my_power = static_cast<uint32_t>(127 + (odd ? min(126, 141 - max(field, 1)) : common_up)) << 23;
+                powers[my_row] = my_power;
+                if (PAIR) __syncwarp();
 #pragma unroll(PAIR ? 4 : STEPS)
                 for (int i = 0; i < STEPS; ++i) {
+                    const float power = __uint_as_float(PAIR ? powers[row_of(i)] : __shfl_sync(0xffffffffu, my_power, (lane & ~(LANES - 1)) + i * (LANES / N)));
+                    const float mul = a.scale < 0.f ? -power : power;
                     float f[8];
                     unpack_bf16x8(read(i), f);
                     store_16(place_of(i), pack_f16(f[0] * mul, f[1] * mul), pack_f16(f[2] * mul, f[3] * mul), pack_f16(f[4] * mul, f[5] * mul), pack_f16(f[6] * mul, f[7] * mul));
@@ -632,9 +674,11 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                         }
                     }
                     float tile_factor = FMT == KV_CACHE_MXFP4 ? tile_factors[slot] : 1.f;
-                    // Tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places. So are scores that may be beyond 2^20
-                    // (before their factors they are below 2^29 or 2^37): of a product that is not rounded before its reference is taken off, which was, more than 2^15 might be left.
-                    if (j0 + kTok > 0 || (its_special & 6) != 0 || (FMT == KV_CACHE_MXFP4 && __any_sync(0xffffffffu, tile_factor > 0x1p-17f))) {
+                    // Tiles with tokens that not all rows see (a sequence's last ones): scores with their factors, or -inf, put back in their places. So are those of rows with powers
+                    // of their own, and scores that may be beyond 2^20 (before their factors they are below 2^29 or 2^37): of a product that is not rounded before its reference is
+                    // taken off, which was, more than 2^15 might be left.
+                    if (j0 + kTok > 0 || its_special > 1) {
+                        if ((its_special & 8) != 0) tile_factor = fminf(tile_factor * __uint_as_float(((254u + common_up) << 23) - powers[r]), 3e38f);
 #pragma unroll 1
                         for (int ch = 0; ch < 8; ++ch) {
                             uint32_t v[16];
@@ -642,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             const uint32_t sees = sees32_of(ch / 2) >> (16 * (ch & 1));
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? __float_as_uint(__uint_as_float(v[i]) * (FMT == KV_CACHE_INT8 ? kf[16 * ch + i] : tile_factor)) : 0xff800000u;
+                            for (int i = 0; i < 16; ++i) v[i] = sees >> i & 1u ? __float_as_uint(__uint_as_float(v[i]) * (FMT == KV_CACHE_INT8 ? kf[16 * ch + i] * tile_factor : tile_factor)) : 0xff800000u;
                             tmem_st_32x32b_x16(s_tmem + 16 * ch, v);
                         }
                         tmem_wait_st();

@@ -560,3 +560,34 @@ def test_keys_of_any_size(fmt, group, new):
         assert bool(torch.isfinite(c.check()).all())
         c.q *= 2.0 ** -power
         c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 4), (40, 3), (8, 30)])
+@pytest.mark.parametrize("power", [12, 40, 100])
+@pytest.mark.parametrize("dim", [64, 72, 128])
+def test_a_large_query_leaves_the_others_alone(fmt, group, new, power, dim):
+    """A node, and a head of another, that are far larger than the rest; rows of few and of many to a tile."""
+    c = Case(fmt, 2, group, dim, [300, new + 40], [new, new], seed=50)
+    c.q[1] *= 2.0 ** power
+    c.q[new + 2, 3] *= 2.0 ** power
+    c.check()
+    c.check(scale=-0.05)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "mxfp4"])
+@pytest.mark.parametrize("group,new", [(4, 4), (40, 3), (8, 30)])
+@pytest.mark.parametrize("power", [7, 8, 9, 30])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_small_queries_beside_ordinary_ones(fmt, group, new, power, dim):
+    """Large keys: the small queries have scores of ordinary size, the others see one token each."""
+    c = Case(fmt, 2, group, dim, [300, new + 40], [new, new], seed=51)
+    if fmt == "int8":
+        c.cache.k_scales.mul_(2.0 ** power)
+    else:
+        c.cache.k_scales.add_(power)
+    c.q[::2] *= 2.0 ** -power
+    c.q[:, 1::3] *= 2.0 ** -power
+    c.check()
