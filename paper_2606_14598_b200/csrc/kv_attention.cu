@@ -188,19 +188,18 @@ __global__ void __launch_bounds__(kThreads, resident<FMT, DP, NR>()) kv_attentio
                     if (FMT == KV_CACHE_INT8) {
                         cp_async<4>(more + lane * 4, static_cast<const float*>(a.k_scales) + entry, slot >= 0 ? 4 : 0);
                         cp_async<4>(more + TOK * 4 + lane * 4, static_cast<const float*>(a.v_scales) + entry, slot >= 0 ? 4 : 0);
-                    } else {                                        // the aligned words that hold the head's bytes
-                        const int64_t first = entry * blocks;
-                        const int shift = static_cast<int>(first & 3);
+                    } else {                                        // the words that hold the head's bytes
+                        const ScaleWords its = scale_words(entry, blocks);
 #pragma unroll
                         for (int side = 0; side < 2; ++side) {
-                            const uint8_t* p = static_cast<const uint8_t*>(side == 0 ? a.k_scales : a.v_scales) + first - shift;
+                            const uint8_t* p = static_cast<const uint8_t*>(side == 0 ? a.k_scales : a.v_scales) + its.from;
 #pragma unroll
                             for (int i = 0; i < (L::WORDS == 2 ? 2 : 3); ++i) {
-                                const bool there = slot >= 0 && shift + blocks > 4 * i;
-                                cp_async<4>(more + ((side * TOK + lane) * L::WORDS + i) * 4, p + (there ? 4 * i : 0), there ? 4 : 0);
+                                const int there = slot >= 0 ? its.bytes(i) : 0;
+                                cp_async<4>(more + ((side * TOK + lane) * L::WORDS + i) * 4, p + (there > 0 ? 4 * i : 0), there);
                             }
                         }
-                        *reinterpret_cast<int*>(rest + stage * L::REST + L::META + lane * 4) = shift;
+                        *reinterpret_cast<int*>(rest + stage * L::REST + L::META + lane * 4) = its.shift;
                     }
                 }
                 if (lane == 0) *reinterpret_cast<uint32_t*>(rest + stage * L::REST + L::SEEN) = seen;

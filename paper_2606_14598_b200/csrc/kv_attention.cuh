@@ -4,6 +4,7 @@
 #include "../../include/kv_cache.h"
 #include "mxfp4_math.cuh"
 #include "ptx.cuh"
+#include "scale_words.h"
 
 #include <cuda.h>
 #include <cuda_fp16.h>

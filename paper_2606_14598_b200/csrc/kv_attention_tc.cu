@@ -342,15 +342,16 @@ __global__ void __launch_bounds__(kThreads, 1) many_rows_kernel(const __grid_con
                             cp_async<4>(at, static_cast<const float*>(a.k_scales) + entry, there);
                             cp_async<4>(at + L::V_SCALES, static_cast<const float*>(a.v_scales) + entry, there);
                         } else {
-                            const int64_t its_first = entry * blocks;
-                            const uint32_t shift = static_cast<uint32_t>(its_first) & 3u;
-                            if (flag != 0) flag |= shift;
-                            cp_async<4>(at, static_cast<const uint8_t*>(a.k_scales) + (its_first - shift), there);
-                            cp_async<4>(at + L::V_SCALES, static_cast<const uint8_t*>(a.v_scales) + (its_first - shift), there);
+                            const ScaleWords its = scale_words(entry, blocks);
+                            const uint8_t *const k_words = static_cast<const uint8_t*>(a.k_scales) + its.from, *const v_words = static_cast<const uint8_t*>(a.v_scales) + its.from;
+                            if (flag != 0) flag |= static_cast<uint32_t>(its.shift);
+                            const int one = from >= 0 ? its.bytes(0) : 0;
+                            cp_async<4>(at, k_words, one);
+                            cp_async<4>(at + L::V_SCALES, v_words, one);
                             if (blocks != 4 && blocks != 2) {                    // (bytes of a token may lie across two words)
-                                const uint32_t two = shift + blocks > 4 ? there : 0;
-                                cp_async<4>(at + 4, static_cast<const uint8_t*>(a.k_scales) + (its_first - shift) + two, two);
-                                cp_async<4>(at + L::V_SCALES + 4, static_cast<const uint8_t*>(a.v_scales) + (its_first - shift) + two, two);
+                                const int two = from >= 0 ? its.bytes(1) : 0;
+                                cp_async<4>(at + 4, k_words + (two > 0 ? 4 : 0), two);
+                                cp_async<4>(at + L::V_SCALES + 4, v_words + (two > 0 ? 4 : 0), two);
                             }
                         }
                         smem[L::MORE + its_slot * L::MORE_BYTES + L::FLAGS + 4 * lane + i] = static_cast<uint8_t>(flag);

@@ -1,6 +1,8 @@
 """Attention over the quantized cache: refusals without a GPU, results against a plain 64-bit form on one."""
 import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
@@ -591,3 +593,27 @@ def test_small_queries_beside_ordinary_ones(fmt, group, new, power, dim):
     c.q[::2] *= 2.0 ** -power
     c.q[:, 1::3] *= 2.0 ** -power
     c.check()
+
+
+def test_scales_are_fetched_within_their_buffer(tmp_path):
+    """MXFP4 scales come as 4-byte words: up to a head's last byte, and from no byte before the buffer, whatever the caches' sizes."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_14598_b200", "csrc")
+    source = tmp_path / "words.cpp"
+    source.write_text('''
+        #include "scale_words.h"
+        int main() {
+            for (int blocks = 1; blocks <= 8; ++blocks)
+                for (int64_t entries = 1; entries <= 70; ++entries)
+                    for (int64_t entry = 0; entry < entries; ++entry) {
+                        const w8a8::ScaleWords w = w8a8::scale_words(entry, blocks);
+                        int64_t end = w.from;
+                        for (int i = 0; i < (blocks <= 4 ? 2 : 3); ++i) {
+                            if (w.bytes(i) < 0 || w.bytes(i) > 4 || (w.bytes(i) > 0 && w.from + 4 * i != end)) return 1;     // without gaps
+                            end += w.bytes(i);
+                        }
+                        if (w.from < 0 || w.from % 4 || w.from + w.shift != entry * blocks || end != (entry + 1) * blocks || end > entries * blocks) return 2;
+                    }
+            return 0;
+        }''')
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-I", csrc, str(source), "-o", str(tmp_path / "words")], check=True)
+    assert subprocess.run([str(tmp_path / "words")]).returncode == 0
