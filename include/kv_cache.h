@@ -92,7 +92,7 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  * Query head h reads the keys and values of head h / (q_heads / heads). A query that sees nothing gets zeros and a logarithm of -inf. A token whose page
  * is outside the cache or past the table is not seen. NaN keys and values (their scale is NaN) reach the queries that see them, and no others.
  *   q, out      bf16 [total_q, q_heads, dim] with their strides; rows of no sequence as for kv_cache_read (KV_CACHE_ZERO_REST); out and lse overlap no input (a
- *               row of queries is read by several CTAs, at different times)
+ *               row of queries is read by several CTAs, at different times; out over q is refused, and so are two that reach into one another with different strides)
  *   lse         fp32 [total_q, q_heads]: log(sum_p exp(scale * q . k_p)), or NULL
  *   table       int32 [seqs, max_pages];  lens, starts int32 [seqs] (starts may be NULL: from the first);  cu_q int32 [seqs + 1], not decreasing
  *   tree        int64 [total_q, tree_words] or NULL

@@ -652,6 +652,31 @@ bool sizes_fine(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, i
            dim <= KV_CACHE_MAX_DIM && q_heads * dim <= KV_CACHE_MAX_WIDTH && heads * dim <= KV_CACHE_MAX_WIDTH && total_q * q_heads <= INT32_MAX;
 }
 
+// Whether two sets of [tokens][heads][dim] elements share any, given where the second begins. Exact where strides are equal (slices of one buffer); where they are not,
+// sets that reach into one another count as sharing.
+bool overlap(int64_t tokens, int64_t heads, int64_t dim, int64_t st, int64_t sh, int64_t to, int64_t to_st, int64_t to_sh) {
+    using Wide = __int128;
+    if (tokens == 1) st = to_st = 0;
+    if (heads == 1) sh = to_sh = 0;
+    auto first = [&](int64_t t, int64_t h) { return (t < 0 ? static_cast<Wide>(tokens - 1) * t : 0) + (h < 0 ? static_cast<Wide>(heads - 1) * h : 0); };
+    auto end = [&](int64_t t, int64_t h) { return (t > 0 ? static_cast<Wide>(tokens - 1) * t : 0) + (h > 0 ? static_cast<Wide>(heads - 1) * h : 0) + dim; };
+    if (to + first(to_st, to_sh) >= end(st, sh) || first(st, sh) >= to + end(to_st, to_sh)) return false;
+    if (st != to_st || sh != to_sh) return true;
+    const Wide each = end(0, sh), apart = st > 0 ? (to % st + st) % st : 0;
+    if (st > 0 && sh >= 0 && each <= apart && apart <= st - each) return false;           // tokens' heads lie side by side
+    // a head of the second lies `to` + h * sh + t * st from one of the first, for some differences h and t of heads and tokens: those t count that bring it nearest
+    for (int64_t h = 1 - heads; h < heads; ++h) {
+        const Wide at = to + static_cast<Wide>(h) * sh;
+        for (int more = -1; more <= 1; ++more) {
+            Wide t = st != 0 ? -at / st + more : 0;
+            t = t < 1 - tokens ? 1 - tokens : t > tokens - 1 ? tokens - 1 : t;
+            const Wide gap = at + t * st;
+            if (gap < dim && -gap < dim) return true;
+        }
+    }
+    return false;
+}
+
 // Codes of a side as [slots][heads][bytes of a head], in boxes of `box` tokens of one head. Rows of a box are padded with zeros.
 bool encode_codes(CUtensorMap* tm, const void* codes, int64_t slots, int64_t heads, int64_t row_bytes, int box, int box_bytes) {
     EncodeTiledFn enc = encode_tiled_fn();
@@ -748,6 +773,8 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < kv_cache_attention_workspace_bytes(seqs, total_q, q_heads, heads, dim)) return W8A8_ERR_WORKSPACE;
     if (int e = check_arch()) return e;
     if (total_q == 0 || (seqs == 0 && !zero_rest)) return W8A8_OK;
+    if (overlap(total_q, q_heads, dim, q_token_stride, q_head_stride, (reinterpret_cast<intptr_t>(out) - reinterpret_cast<intptr_t>(q)) / 2, out_token_stride, out_head_stride))
+        return W8A8_ERR_INVALID_ARG;
     AttentionArgs a{};
     a.k_codes = static_cast<const uint8_t*>(k_codes);
     a.v_codes = static_cast<const uint8_t*>(v_codes);

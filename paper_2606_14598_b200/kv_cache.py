@@ -265,6 +265,26 @@ def kv_cache_append(cache: QuantKVCache, k: torch.Tensor, v: torch.Tensor | None
     return q_out
 
 
+def _overlap(tokens: int, heads: int, dim: int, st: int, sh: int, to: int, to_st: int, to_sh: int) -> bool:
+    """Whether two sets of [tokens, heads, dim] elements share any, the second beginning `to` elements behind the first. Exact where strides are equal (slices of
+    one buffer); where they are not, sets that reach into one another count as sharing."""
+    ends, to_ends = (tokens - 1) * st + (heads - 1) * sh + dim, (tokens - 1) * to_st + (heads - 1) * to_sh + dim
+    if to >= ends or -to >= to_ends:
+        return False
+    if (st, sh) != (to_st, to_sh):
+        return True
+    each = (heads - 1) * sh + dim
+    if st and each <= to % st <= st - each:                      # tokens' heads lie side by side
+        return False
+    for h in range(1 - heads, heads):
+        at = to + h * sh
+        for more in (0, 1):
+            t = min(max(-at // st + more, 1 - tokens), tokens - 1) if st else 0
+            if abs(at + t * st) < dim:
+                return True
+    return False
+
+
 def kv_cache_attention_workspace(cache: QuantKVCache, seqs: int, total_q: int, q_heads: int) -> torch.Tensor:
     """Scratch for kv_cache_attention with up to this many sequences, rows and heads of queries: made once, zero where it has to be. The calls leave it
     ready for the next one; two that may overlap on the device need one each."""
@@ -314,8 +334,8 @@ def kv_cache_attention(cache: QuantKVCache, q: torch.Tensor, table: torch.Tensor
     if fill:
         out = torch.empty(total, heads, c.dim, dtype=torch.bfloat16, device=c.device)
     op, ot, oh = _vectors(c, out, "out", total, heads)
-    if op == qp and total > 0:
-        raise ValueError("out: must not be q (a row of queries is read by several CTAs, at different times)")
+    if not fill and total > 0 and abs(op - qp) < 2 * total * (qt + ot + heads * (qh + oh + c.dim)) and _overlap(total, heads, c.dim, qt, qh, (op - qp) // 2, ot, oh):
+        raise ValueError("out: must not overlap q (a row of queries is read by several CTAs, at different times)")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (total, heads) or not lse.is_contiguous()):
         raise TypeError(f"lse: dense fp32 [{total}, {heads}] expected")
     if workspace is None:

@@ -2,6 +2,7 @@
 import ctypes
 import math
 import os
+import random
 import subprocess
 
 import pytest
@@ -617,3 +618,60 @@ def test_scales_are_fetched_within_their_buffer(tmp_path):
         }''')
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-I", csrc, str(source), "-o", str(tmp_path / "words")], check=True)
     assert subprocess.run([str(tmp_path / "words")]).returncode == 0
+
+
+def test_outputs_over_queries_are_refused():
+    """Views of one buffer that share elements, wherever they begin; those that share none are fine."""
+    c = w8.QuantKVCache.empty(4, 4, 2, 16, "int8", device="cpu")
+    table, lens, cu = torch.zeros(2, 2, dtype=torch.int32), torch.ones(2, dtype=torch.int32), torch.tensor([0, 1, 3], dtype=torch.int32)
+    wide = torch.zeros(8, 12, 48, dtype=torch.bfloat16)
+
+    def refused(q, out):
+        with pytest.raises(ValueError) as e:
+            w8.kv_cache_attention(c, q, table, lens, cu, out=out)
+        return "overlap" in str(e.value)                         # (else: not on a CUDA device)
+
+    q = wide[2:5, 4:8, 16:32]
+    for over in (q, wide[3:6, 4:8, 16:32], wide[0:3, 4:8, 16:32], wide[2:5, 7:11, 16:32], wide[2:5, 4:8, 24:40], wide[2:5, 1:5, 8:24], wide[4:7, 2:6, 16:32]):
+        assert refused(q, over)
+    for beside in (wide[5:8, 4:8, 16:32], wide[2:5, 8:12, 16:32], wide[2:5, 0:4, 16:32], wide[2:5, 4:8, 32:48], wide[2:5, 4:8, 0:16], wide[3:6, 0:4, 24:40], torch.zeros(3, 4, 16, dtype=torch.bfloat16)):
+        assert not refused(q, beside)
+    dense = torch.zeros(3 * 4 * 16 + 64, dtype=torch.bfloat16)
+    assert refused(dense[:192].view(3, 4, 16), dense[8:200].view(3, 4, 16)) and not refused(dense[64:].view(3, 4, 16).expand(3, 4, 16), dense.new_zeros(3, 4, 16))
+    assert refused(dense[:192].view(3, 4, 16), dense[:64].view(1, 4, 16).expand(3, 4, 16))
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_what_overlaps(seed):
+    """Against all elements' places."""
+    rng = random.Random(seed)
+    for _ in range(400):
+        tokens, heads, dim = rng.randint(1, 5), rng.randint(1, 4), 8 * rng.randint(1, 3)
+        st, sh = 8 * rng.randint(0, 20), 8 * rng.randint(0, 6)
+        if tokens == 1:
+            st = 0
+        if heads == 1:
+            sh = 0
+        to = 8 * rng.randint(-60, 60)
+        mine = {t * st + h * sh + e for t in range(tokens) for h in range(heads) for e in range(dim)}
+        assert kv_cache._overlap(tokens, heads, dim, st, sh, to, st, sh) == any(x + to in mine for x in mine)
+
+
+@pytest.mark.gpu
+def test_outputs_over_queries_are_refused_by_the_library():
+    c = Case("int8", 2, 2, 64, [40, 30], [2, 2], seed=54)
+    wide = torch.zeros(8, 12, 64, dtype=torch.bfloat16, device="cuda")
+    ws = w8.kv_cache_attention_workspace(c.cache, 2, 4, 4)
+    kc, ks, vc, vs = c.cache.places()
+
+    def status(q, out):
+        return kv_cache._lib.kv_cache_attention(0, kc, ks, vc, vs, c.cache.num_pages, c.page, 2, 64, c.table.data_ptr(), c.table.stride(0), c.table.shape[1], c.lens.data_ptr(), None,
+                                                c.cu.data_ptr(), 2, q.data_ptr(), q.stride(0), q.stride(1), 4, 4, None, 0, 0.125, out.data_ptr(), out.stride(0), out.stride(1), None,
+                                                ws.data_ptr(), ws.nbytes, torch.cuda.current_stream().cuda_stream)
+
+    q = wide[2:6, 4:8]
+    for over in (q, wide[3:7, 4:8], wide[0:4, 6:10], wide[2:6, 1:5], wide[2:6, 4:8].transpose(0, 1)):
+        assert status(q, over) == INVALID
+    for beside in (wide[2:6, 0:4], wide[2:6, 8:12], wide[3:7, 0:4], torch.empty(4, 4, 64, dtype=torch.bfloat16, device="cuda")):
+        assert status(q, beside) == 0
+    torch.cuda.synchronize()
