@@ -98,7 +98,7 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  *   tree        int64 [total_q, tree_words] or NULL
  *   workspace   device scratch of kv_cache_attention_workspace_bytes(), 256-byte aligned; its first kv_cache_attention_zeroed_bytes() bytes must be zero
  *               before the first call that uses it, and each call leaves them zero. One workspace, given with its whole size, serves calls with fewer
- *               sequences and rows too, in any order, if what the largest needs to be zero was. Two calls that may overlap on the device need distinct workspaces.
+ *               sequences and rows too, in any order, if what the largest needs to be zero was; one that needs more counters than it has is refused. Two calls that may overlap on the device need distinct workspaces.
  *               A wait that runs out shows in its first word (int8_check_status) and in the sticky status.
  * The cache must have both sides, scales that are not negative and 4-byte aligned; num_pages * page_size <= 2^31 - 1, max_pages * page_size <= 2^31 - 4096; q_heads a
  * multiple of heads. Scores, softmax

@@ -641,10 +641,10 @@ size_t counters_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t he
     return kAlign + (static_cast<size_t>(seqs + total_q * group / kSmallestRows + 1) * heads * sizeof(uint32_t) + kAlign - 1) / kAlign * kAlign;
 }
 int padded(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-// (most_rows: of any sequence and head; more of them need more)
-size_t parts_bytes(int64_t most_rows, int64_t dim) {
-    const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(16, padded(dim)) * sizeof(float);
-    const size_t many = most_rows > kFewRows ? many_rows_part_bytes(most_rows, dim) : 0;
+// The same for every call, though most need less of it: what is left of a workspace is then what it has for counters, whatever calls it was made for, so that one with too few of
+// them is refused and never finds old parts where zeros should be.
+size_t parts_bytes() {
+    const size_t few = static_cast<size_t>(sm_count()) * kMostCtas * 2 * part_floats(16, KV_CACHE_MAX_DIM) * sizeof(float), many = many_rows_part_bytes();
     return ((few > many ? few : many) + kAlign - 1) / kAlign * kAlign;
 }
 bool sizes_fine(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
@@ -750,7 +750,7 @@ size_t kv_cache_attention_zeroed_bytes(int64_t seqs, int64_t total_q, int64_t q_
     return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) : 0;
 }
 size_t kv_cache_attention_workspace_bytes(int64_t seqs, int64_t total_q, int64_t q_heads, int64_t heads, int64_t dim) {
-    return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) + parts_bytes(total_q * (q_heads / heads), dim) : 0;
+    return sizes_fine(seqs, total_q, q_heads, heads, dim) ? counters_bytes(seqs, total_q, q_heads, heads) + parts_bytes() : 0;
 }
 
 int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, int64_t num_pages, int64_t page_size,
@@ -790,7 +790,7 @@ int kv_cache_attention(int fmt, const void* k_codes, const void* k_scales, const
     a.lse = lse;
     a.counters = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + kAlign);          // behind the status word
     // parts at the end of what is given, so that a call with fewer sequences leaves alone what must be zero for one with more
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + workspace_bytes / kAlign * kAlign - parts_bytes(total_q * (q_heads / heads), dim));
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + workspace_bytes / kAlign * kAlign - parts_bytes());
     a.q_st = q_token_stride;
     a.q_sh = q_head_stride;
     a.o_st = out_token_stride;

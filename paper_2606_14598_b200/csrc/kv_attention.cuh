@@ -275,7 +275,7 @@ __device__ __forceinline__ bool last_to_arrive(const AttentionArgs& a, const Seq
 
 // ---- kv_attention_tc.cu : the attention for many rows of queries a head (the maps: codes of keys and of values in boxes of a.box tokens of a head)
 bool many_rows_fits(int dim);                                              // what the kernel can run
-size_t many_rows_part_bytes(int64_t most_rows, int64_t dim);               // scratch for the parts, for at most this many rows of a sequence and head
+size_t many_rows_part_bytes();                                             // scratch for the parts of any call
 cudaError_t launch_many_rows(int fmt, const CUtensorMap& k_map, const CUtensorMap& v_map, const AttentionArgs& a, int64_t rows, cudaStream_t st);
 
 } // namespace attention

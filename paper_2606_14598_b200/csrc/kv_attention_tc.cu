@@ -980,10 +980,7 @@ cudaError_t launch_for(const CUtensorMap& k, const CUtensorMap& v, const Attenti
 } // namespace
 
 bool many_rows_fits(int dim) { return dim <= 128; }
-size_t many_rows_part_bytes(int64_t most_rows, int64_t dim) {
-    if (dim > 128) return 0;
-    return static_cast<size_t>(sm_count()) * 2 * part_floats(most_rows > kRows ? 2 * kRows : kRows, dim <= 64 ? 64 : 128) * sizeof(float);
-}
+size_t many_rows_part_bytes() { return static_cast<size_t>(sm_count()) * 2 * part_floats(2 * kRows, 128) * sizeof(float); }
 cudaError_t launch_many_rows(int fmt, const CUtensorMap& k_map, const CUtensorMap& v_map, const AttentionArgs& a, int64_t rows, cudaStream_t st) {
     return fmt == KV_CACHE_INT8 ? launch_for<KV_CACHE_INT8>(k_map, v_map, a, rows, st) : launch_for<KV_CACHE_MXFP4>(k_map, v_map, a, rows, st);
 }

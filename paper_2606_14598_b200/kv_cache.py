@@ -291,7 +291,9 @@ def kv_cache_attention_workspace(cache: QuantKVCache, seqs: int, total_q: int, q
     size = int(_lib.kv_cache_attention_workspace_bytes(seqs, total_q, q_heads, cache.heads, cache.dim))
     if size == 0:
         raise ValueError(f"kv_cache_attention_workspace: {seqs} sequences, {total_q} rows and {q_heads} heads of queries do not go with {cache.heads} heads of {cache.dim}")
-    return torch.zeros(size, dtype=torch.uint8, device=cache.device)
+    workspace = torch.empty(size, dtype=torch.uint8, device=cache.device)
+    workspace[:int(_lib.kv_cache_attention_zeroed_bytes(seqs, total_q, q_heads, cache.heads, cache.dim))].zero_()
+    return workspace
 
 
 def kv_cache_attention(cache: QuantKVCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor, scale: float | None = None,

@@ -675,3 +675,27 @@ def test_outputs_over_queries_are_refused_by_the_library():
     for beside in (wide[2:6, 0:4], wide[2:6, 8:12], wide[3:7, 0:4], torch.empty(4, 4, 64, dtype=torch.bfloat16, device="cuda")):
         assert status(q, beside) == 0
     torch.cuda.synchronize()
+
+
+def test_workspaces_with_too_few_counters_are_refused():
+    """A workspace made for many rows of few sequences, or for other heads, and a call with many sequences: its counters would lie where parts were."""
+    lib = kv_cache._lib
+    p, need = P(4096), lib.kv_cache_attention_workspace_bytes
+
+    def status(size, seqs, total, q_heads, heads, dim):
+        return lib.kv_cache_attention(0, p, p, p, p, 4, 16, heads, dim, p, 3, 3, p, None, p, seqs, p, q_heads * dim, dim, q_heads, total, None, 0, 0.125, p, q_heads * dim, dim,
+                                      None, p, size, None)
+
+    for made in ((2, 6000, 8, 2, 64), (1, 400, 64, 8, 128), (1, 300, 4, 2, 256), (1, 1, 4, 2, 128)):
+        size = need(*made)
+        for seqs, total, q_heads, heads, dim in ((9000, 1, 8, 2, 64), (9000, 10, 8, 2, 128), (7000, 7000, 4, 4, 256), (90000, 90000, 64, 8, 128)):
+            counters = lib.kv_cache_attention_zeroed_bytes(seqs, total, q_heads, heads, dim)
+            assert counters > lib.kv_cache_attention_zeroed_bytes(*made) and status(size, seqs, total, q_heads, heads, dim) == WORKSPACE
+
+
+def test_python_workspace_is_zero_where_it_has_to_be():
+    for fmt in ("int8", "mxfp4"):
+        c = w8.QuantKVCache.empty(4, 4, 2, 64, fmt, device="cpu")
+        ws = w8.kv_cache_attention_workspace(c, 500, 3000, 16)
+        zeroed = kv_cache._lib.kv_cache_attention_zeroed_bytes(500, 3000, 16, 2, 64)
+        assert ws.nbytes == kv_cache._lib.kv_cache_attention_workspace_bytes(500, 3000, 16, 2, 64) and 0 < zeroed < ws.nbytes and not bool(ws[:zeroed].any())
