@@ -85,10 +85,11 @@ int kv_cache_rope_table(const double* inv_freq, int64_t pairs, int64_t first, in
  * Attention of new tokens over the cache, on the codes: nothing is expanded in memory.
  *     o = sum_p softmax_p(scale * q . k_p) v_p             over the tokens p that the query sees; k, v: what the codes stand for, unrounded
  * Sequence b holds lens[b] tokens in its pages. The last n_b = cu_q[b + 1] - cu_q[b] of them are its new ones, appended before the call;
- * query i of them (row cu_q[b] + i of q) sees the tokens from starts[b] on that come before the new ones, and of the new ones
+ * query i of them (row cu_q[b] + i of q) sees, of the tokens from starts[b] on, those that come before the new ones, and of the new ones
  *   tree == NULL  those up to and with itself (one token a sequence, or a chain)
  *   else          token j where bit j % 64 of tree[(cu_q[b] + i) * tree_words + j / 64] is set: a tree of drafted tokens, each of which sees its
  *                 ancestors (and itself, where its own bit is set); new tokens from 64 * tree_words on are not seen
+ * starts[b] is one for all new tokens of a sequence, and hides those of them that come before it, too: a window that moves on with each of several new tokens is not one of its uses.
  * Query head h reads the keys and values of head h / (q_heads / heads). A query that sees nothing gets zeros and a logarithm of -inf. A token whose page
  * is outside the cache or past the table is not seen. NaN keys and values (their scale is NaN) reach the queries that see them, and no others.
  *   q, out      bf16 [total_q, q_heads, dim] with their strides; rows of no sequence as for kv_cache_read (KV_CACHE_ZERO_REST); out and lse overlap no input (a

@@ -210,7 +210,7 @@ def kv_cache_append(cache: QuantKVCache, k: torch.Tensor, v: torch.Tensor | None
                     q_out: torch.Tensor | None = None) -> torch.Tensor | None:
     """kv_cache_write of k rotated by the tokens' positions (and v as it is); returns q bf16 [T, q_heads, dim], rotated too (in q_out, which may be q).
     positions int64 [T], or [axes, T] with axes uint8 [rot / 2] telling each pair's axis; cos_sin fp32 [positions, rot] (kv_cache_rope_table); without
-    a table nothing is rotated. Pairs are (2i, 2i + 1) if interleaved, else (i, i + rot / 2)."""
+    a table nothing is rotated. Pairs are (2i, 2i + 1) if interleaved, else (i, i + rot / 2). For inference: autograd does not see the call."""
     c = cache
     kc, ks, vc, vs = c.places()
     dev = c.device_index
@@ -300,10 +300,10 @@ def kv_cache_attention(cache: QuantKVCache, q: torch.Tensor, table: torch.Tensor
                        tree: torch.Tensor | None = None, starts: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                        workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Attention of q bf16 [total, q_heads, dim] over the cache, bf16 [total, q_heads, dim]. Rows cu_q[b] to cu_q[b + 1] (int32 [B + 1]) are the newest tokens of
-    sequence b, which are in the cache already and counted in lens (int32 [B]); table int32 [B, max_pages]. Each sees what comes before them (from
-    starts int32 [B] on) and, of the new ones, those up to itself, or those whose bits are set in its row of tree int64 [total, words]. scale:
+    sequence b, which are in the cache already and counted in lens (int32 [B]); table int32 [B, max_pages]. Each sees what comes before them
+    and, of the new ones, those up to itself, or those whose bits are set in its row of tree int64 [total, words]; nothing ahead of starts int32 [B], new tokens included. scale:
     dim ** -0.5 by default. lse fp32 [total, q_heads] receives the logarithms of the softmax's sums. Rows of no sequence are zeros, in an out that is given
-    they are left as they are."""
+    they are left as they are. For inference: autograd does not see the call, and results carry no gradients."""
     c = cache
     if table.dtype is not torch.int32 or table.dim() != 2:
         raise TypeError("table: int32 [sequences, max_pages] expected")

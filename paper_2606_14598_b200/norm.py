@@ -2,6 +2,8 @@
 
     qa, s_tok, h = int8_rmsnorm(x, weight, residual=h)       # codes for int8_linear_fused(qa, qw, s_ch, s_tok=s_tok)
     y, h = rmsnorm(x, weight, residual=h)                    # bf16, for mxfp4_linear_fused
+
+For inference: autograd sees neither the calls nor what they write into sum_out, and results carry no gradients.
 """
 from __future__ import annotations
 
