@@ -10,9 +10,10 @@
 // long list that the CTAs share out evenly whatever the sequences' lengths: a CTA's range holds ends of at most two items that others share,
 // whose parts meet in the workspace and are added up, in the order of the tokens, by the CTA that arrives last.
 //
-// What bounds it: int8, HBM and the latency of loads (48 sequences of up to 4000 tokens, 8 heads of 128, 4 queries a head: 61 us, 39 at the copy's rate; loads alone, without
-// the products, 55). 4 bits: issue slots, some 1100 instructions for 32 tokens of a head, most of them conversions (12 sequences of up to 30000, 8 heads, 8 queries: 104 us, 39).
-// One sequence of 777 tokens: 9 us, launch, list, one step and the parts' meeting after one another.
+// What bounds it: int8, HBM and the latency of loads (48 sequences of up to 4000 tokens, 8 heads of 128, 4 queries a head: 62 us, 39 at the copy's rate; loads alone, without
+// the products, 55). 4 bits: issue slots, some 1100 instructions for 32 tokens of a head, most of them conversions (12 sequences of up to 30000, 8 heads, 8 queries: 106 us, 39;
+// its 128 registers, for four CTAs an SM, spill 128 bytes).
+// One sequence of 777 tokens: 9.5 us, launch, list, one step and the parts' meeting after one another. (SM clock 1965 MHz in all.)
 #include "internal.h"
 #include "kv_attention.cuh"
 #include "tensor_map.h"
@@ -632,7 +633,8 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 constexpr int kSmallestRows = 8;                    // rows of the smallest item: the most items, so the most counters
 constexpr int kMostCtas = 4;                        // CTAs on an SM
 // Rows of a sequence and head up to which the kernel of this file is chosen, which reads the cache once for 16 of them; the other's time does not depend on them. 16
-// sequences, 6000 tokens, 8 heads of 128: 32 rows take 73 us here and 85 there in int8, 75 and 77 in 4 bits; 64 rows 136 and 87, 144 and 80.
+// sequences of up to 6000 tokens, 8 heads of 128, trees, here and there: int8, 16 rows 55 and 86 us, 32 rows 82 and 87, 48 rows 113 and 88; 4 bits, 16 rows 58 and 79, 24 rows 80 and 79,
+// 32 rows 92 and 80, 48 rows 129 and 82. (One border for both; in 4 bits it lies higher than it need.)
 constexpr int kFewRows = 32;
 constexpr size_t kAlign = 256;
 

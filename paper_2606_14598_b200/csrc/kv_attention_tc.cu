@@ -5,15 +5,16 @@
 // of 128 tokens; a thread a row does the softmax; one thread issues the products. Tiles and codes of either side go round in rings of their own.
 //
 // Keys in int8 are the codes, exact, and a token's scale goes to its scores. Keys in 4 bits are codes times their block's scale relative to the tile's largest (powers of
-// two: exact down to 2^-36 of it), so that one factor stands for all scores of a tile. Values are codes times scale, relative to the largest scale so far.
+// two: exact down to 2^-35 of it), so that one factor stands for all scores of a tile. Values are codes times scale, relative to the largest scale so far.
 //
 // Two softmax warpgroups, each with scores and an O of its own: of the same 128 rows and every other tile of tokens, or (PAIR) of 128 rows each and all
-// tiles, which then are converted once for 256 rows (61 nodes, 8 queries a head, int8: 3 sequences of 20000 tokens 167 us against 184 without, one of 60000 210 against 237).
+// tiles, which then are converted once for 256 rows (61 nodes, 8 queries a head, int8: 3 sequences of 20000 tokens 204 us against 242 without, one of 60000 212 against 243).
 //
-// What bounds it: no one thing. A tile of 128 tokens and 128 rows in int8 takes some 3700 cycles, of which HBM's share is 1060, the products' 1024, the exponentials' 1024 and
+// What bounds it: no one thing. A tile of 128 tokens and 128 rows in int8 takes some 3700 cycles (at 1965 MHz), of which HBM's share is 1500, the products' 1024, the exponentials' 1024 and
 // the issue slots' (softmax, conversion) 1500: they meet in a chain (scores, softmax, products) two of which are under way, all that tensor memory has room for. 12 x 32
-// nodes behind 6000 tokens: 76 us (16 at the copy's rate), of which some 25 are beginnings and ends: queries, a first tile, parts. 4 bits, 3 x 61 nodes, 256 rows a tile, behind
-// 20000 tokens: 152 us (53, bound by the products, at cuBLAS's rate).
+// nodes behind up to 6000 tokens: 78 us (16 at the copy's rate), of which some 25 are beginnings and ends: queries, a first tile, parts. 4 bits, 3 x 61 nodes, 256 rows a tile, behind
+// up to 20000 tokens: 153 us (53, bound by the products, at cuBLAS's rate). A chain's tiles of rows all go over all tokens of their sequence, those that none of their rows sees, too: a
+// prompt of 8000 tokens from the first on, 32 / 8 heads of 128, takes 2500 us in int8 and 1830 in 4 bits (313 by its products).
 #include "internal.h"
 #include "kv_attention.cuh"
 

@@ -5,7 +5,8 @@
 //
 // The norm is one factor of the row, so it cancels out of the codes: the sum of squares and the largest |u| are found in one pass over
 // the row, which then sits in registers as u and is written from there. One trip through HBM: 4 bytes an element in, 3 or 4 out, which is what bounds it: 8221 rows
-// of 12288 in bf16 take 131 us (123 at the copy's rate), 4110 of 4608 in int8 28 us (20; one wave and a half of CTAs, whose ends show), one row of 4608 3.5 us.
+// of 12288 in bf16 take 131 to 141 us (123 at the copy's rate; the clock falls to 1740 MHz under the power limit where calls follow one another), 4110 of 4608 in int8 28 us (20, at
+// 1965 MHz; 4.6 waves of six CTAs an SM; what holds them at 4.7 TB/s is not known), one row of 4608 3.3 us.
 #include "../../include/int8_norm.h"
 #include "internal.h"
 #include "mxfp4_math.cuh"
@@ -201,8 +202,9 @@ int run_norm(const NormArgs& a, bool w16, cudaStream_t st) {
         const auto kern = res ? (w16 ? norm_long_kernel<true, true> : norm_long_kernel<true, false>) : (w16 ? norm_long_kernel<false, true> : norm_long_kernel<false, false>);
         e = launch_pdl(kern, dim3(static_cast<unsigned>(a.M)), kMaxThreads, st, a);
     } else {
-        // three vectors a thread, all on their way at once, are the best of 1, 2, 3, 4 and 6 from 449 vectors a row up (4110 rows of 4608: 36, 30, 28, 29 and 31 us; of
-        // 12288: 99, 99, 69, 71 and 67), two up to 256 (of 2048: 16.6, 15.7, 16.1)
+        // three vectors a thread, all on their way at once, are the best of 1, 2, 3, 4 and 6 in long rows (4110 rows of 4608: 36, 30, 28, 29 and 31 us; of
+        // 12288: 99, 99, 69, 71 and 67), two up to 256 vectors (of 2048: 16.6, 15.7, 16.1). Between them, three and two, 20000 rows: of 2064 elements 56 and 62 us, of 2304 57 and 63,
+        // of 2560 71 and 67 (a sixth of three vectors' places idle), of 2816 74 and 81, of 3328 84 and 96, of 3584 90 and 100. (One row: 3.3 and 2.9.)
         const int vpt = vecs <= 256 ? 2 : 3;
         const int per_row = ((vecs + vpt - 1) / vpt + 31) / 32 * 32, rows = per_row >= 256 ? 1 : 256 / per_row;
         const auto kern = vpt == 2 ? norm_variant<2>(res, w16) : norm_variant<3>(res, w16);
